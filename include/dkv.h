@@ -60,6 +60,8 @@ typedef enum {
 #define DKV_DEV_APPEND_OVERFLOW 0x1 /* n_appended reached the slab's reserve: token not appended */
 #define DKV_DEV_TMA_TIMEOUT 0x2     /* a bulk copy did not complete within the wait bound */
 #define DKV_DEV_MERGE_TIMEOUT 0x4   /* a fused merge's partials were not all written within the wait bound: outputs of the plan's calls are not to be used until the word is cleared */
+#define DKV_DEV_PAGES_EXHAUSTED 0x10 /* dkv_page_tables: fewer free pages than the call needs; it changed nothing */
+#define DKV_DEV_PAGE_RANGE 0x20     /* paged cache: a length, token count, slot or page number on the device was out of its range; a table call changed nothing, another call skipped what it could not place */
 #define DKV_DEV_BOUNDS 0x8          /* bounds-checked build only: an index or offset a kernel read was out of its range; the access was skipped */
 
 /* Pattern and model geometry (Sec. 3.2, Sec. 3.4). */
@@ -391,6 +393,148 @@ int64_t dkv_budget(double rho, int32_t L, int32_t H, int32_t D);
 int64_t dkv_topk_workspace_bytes(void);
 dkv_status dkv_topk_mask(const float* P, int64_t n, int64_t K, uint8_t* M, void* workspace,
                          int64_t workspace_bytes, cudaStream_t stream);
+
+/*
+ * Paged cache: compressed sequences that grow, come and go. The packed cache above
+ * gives every slab a fixed reserve; here a slab's rows lie in pages of a pool,
+ * so a pruned sequence can take a new turn of any length, tokens of its answer, and
+ * give its pages back when it ends.
+ *
+ * The geometry names B sequence slots. A slab is one (layer l, slot b, KV head g),
+ * h = (l*B + b)*H_kv + g, as in a plan of B sequences; NH = L*B*H_kv. The caller owns
+ * all memory (device, 4-byte aligned unless stated):
+ *   Kp, Vp      16-bit [num_pages * page_rows][128] each: the page pools, 16-byte aligned
+ *   table       int32 [NH][max_pages]: row r of slab h is row
+ *               table[h][r / page_rows] * page_rows + r % page_rows of Kp and Vp
+ *   len         int32 [NH]: rows of each slab (0 for a free slot). Slabs of one
+ *               sequence differ, as pruning leaves them
+ *   free_pages  int32 [num_pages], free_count int32 [1]: the pages of no slab are
+ *               free_pages[0 .. free_count)
+ * At the start: len all 0, free_pages 0 .. num_pages - 1, free_count num_pages.
+ * Table entries behind a slab's ceil(len / page_rows) pages are not read.
+ *
+ * One step of a serving loop:
+ *   dkv_page_release   sequences that ended give their pages back
+ *   dkv_page_tables    pages for the step's new tokens; slot map and token offsets
+ *   dkv_chunk_attn     per layer: append the new K, V; attention
+ * and for a sequence that is admitted after its prefill: dkv_map_pattern,
+ * dkv_page_tables (with the plan), dkv_page_compact.
+ *
+ * status of every call: a device int32 that receives DKV_DEV_* bits, or NULL to
+ * discard them. Values on the device (lengths, counts, page numbers, slots) are
+ * checked there; what is out of range is never followed.
+ * workspace: device scratch, 16-byte aligned, of at least the size named; nothing in
+ * it need be kept or cleared. Calls that share one must be ordered, as must graphs
+ * that were captured with the same one.
+ * All these calls are asynchronous, allocate nothing and can be captured.
+ */
+typedef struct {
+    int32_t L;         /* layers */
+    int32_t B;         /* sequence slots, 1 <= B <= 512 */
+    int32_t H;         /* query heads per layer */
+    int32_t H_kv;      /* KV heads per layer; H % H_kv == 0, H / H_kv <= 8 */
+    int32_t head_dim;  /* must be 128 */
+    int32_t page_rows; /* rows of a page: 16, 32, 64 or 128 */
+    int32_t num_pages; /* pages of each pool; num_pages * page_rows < 2^31 - 16 */
+    int32_t max_pages; /* table entries of a slab; max_pages * page_rows < 2^31 */
+} dkv_pages;
+
+/* Element types of q, the new rows, the pools and out in dkv_chunk_attn. */
+#define DKV_BF16 0
+#define DKV_FP16 1
+
+/*
+ * Pages for new rows: block tables, slot map and token offsets from request lengths.
+ *
+ * tokens     device int32 [B]: new tokens of each slot (0: none), so n_h = tokens[b]
+ *            new rows in every slab of slot b; or NULL, and
+ * plan, seq  a plan of dkv_map_pattern(_inplace) with the geometry's L and H_kv: its
+ *            sequence i goes to slot seq[i], n_h = its slab's kept rows. seq: device
+ *            int32 [plan B], ascending slots; NULL: slot i. Exactly one of tokens and
+ *            plan is given.
+ * len        rows of each slab before the call.
+ * new_len    receives len[h] + n_h (may be len).
+ * table      slab h's entries ceil(len/page_rows) .. ceil((len + n_h)/page_rows) - 1 are
+ *            written; others are kept. The k-th page that the call takes, in slab order,
+ *            is free_pages[free_count - 1 - k].
+ * new_count  receives free_count less the pages taken (may be free_count).
+ * cu_tokens  device int32 [B + 1]: receives the sequences' first tokens in the step's
+ *            batch, cu[0] = 0, cu[b + 1] = cu[b] + tokens[b]; NULL: not written.
+ *            NULL with a plan.
+ * slots      device int32 [L][max_tokens][H_kv]: receives the pool row of each new
+ *            token, slots[l][t][g] for t < cu[B] (the rows behind are kept), for
+ *            callers that write K and V themselves; NULL: not written. Needs cu_tokens.
+ * workspace  dkv_page_workspace_bytes(pages) bytes.
+ *
+ * All or nothing: with fewer free pages than needed (DKV_DEV_PAGES_EXHAUSTED), or a
+ * negative count, a slab past max_pages, more than max_tokens tokens with a slot map,
+ * seq out of order or range (DKV_DEV_PAGE_RANGE), no table entry and no slot is written,
+ * new_len = len, new_count = free_count, and cu_tokens is all 0: a dkv_chunk_attn that
+ * follows then does nothing.
+ * Errors: DKV_ERR_INVALID_ARG, DKV_ERR_CUDA.
+ */
+int64_t dkv_page_workspace_bytes(const dkv_pages* pages);
+dkv_status dkv_page_tables(const dkv_pages* pages, const int32_t* tokens, const dkv_plan* plan, const int32_t* seq,
+                           const int32_t* len, int32_t* new_len, int32_t* table, const int32_t* free_pages,
+                           const int32_t* free_count, int32_t* new_count, int32_t* cu_tokens, int32_t* slots,
+                           int64_t max_tokens, void* workspace, int64_t workspace_bytes, int32_t* status,
+                           cudaStream_t stream);
+
+/*
+ * The pages of ended sequences go back to the free list, in slab order:
+ * ended      device int32 [B]: not 0 for the slots that end.
+ * new_len    receives 0 for their slabs, len[h] for the others (may be len).
+ * free_pages entries free_count .. new_count - 1 are written.
+ * new_count  receives free_count plus the pages given back (may be free_count).
+ * Nothing is changed (new_len = len, new_count = free_count) if the list would
+ * pass num_pages or a length is out of range (DKV_DEV_PAGE_RANGE).
+ * Other arguments and errors are those of dkv_page_tables.
+ */
+dkv_status dkv_page_release(const dkv_pages* pages, const int32_t* ended, const int32_t* len, int32_t* new_len,
+                            const int32_t* table, int32_t* free_pages, const int32_t* free_count, int32_t* new_count,
+                            void* workspace, int64_t workspace_bytes, int32_t* status, cudaStream_t stream);
+
+/*
+ * Prune-and-pack into pages (dkv_compact's paged form): the kept rows of plan
+ * sequence i become the last rows of slot seq[i], rows len[h] - n_h .. len[h] - 1 of
+ * each slab, with len and table as they are after dkv_page_tables with this plan.
+ * K, V       device 16-bit [L][plan B][H_kv][T_stride][128]. T_stride >= max ctx_len.
+ * Bytes are copied exactly; K, V, Kp and Vp are 16-byte aligned. A row whose place is
+ * out of range is skipped (DKV_DEV_PAGE_RANGE). Dense plans are rejected.
+ */
+dkv_status dkv_page_compact(const dkv_pages* pages, const dkv_plan* plan, const int32_t* seq, const void* K,
+                            const void* V, int64_t T_stride, const int32_t* table, const int32_t* len, void* Kp,
+                            void* Vp, int32_t* status, cudaStream_t stream);
+
+/*
+ * One layer's attention of a step's new tokens over the paged cache: any number of
+ * tokens a sequence (the next token, drafted ones, a whole turn), sequences mixed.
+ *
+ * dtype       DKV_BF16 or DKV_FP16: type of q, k_new, v_new, Kp, Vp and out.
+ * num_tokens  rows of q, k_new, v_new and out. Tokens cu_tokens[b] .. cu_tokens[b + 1] - 1
+ *             are sequence b's; cu_tokens (device int32 [B + 1]) ascends from 0. Rows
+ *             from cu_tokens[B] on are no token's: not read, and left as they are in out.
+ * q           [num_tokens][H][128], token t at q + t * q_stride elements.
+ * k_new,      [num_tokens][H_kv][128], token t at t * kv_stride elements, or both
+ * v_new       NULL (the rows are in the pools already). When given they are first
+ *             written to the last rows of their slabs.
+ *             Strides are in elements, multiples of 8, at least H*128 (H_kv*128), so
+ *             that q, k_new and v_new may be slices of one projection; all 16-byte
+ *             aligned. They must not overlap out or the pools.
+ * table, len  as they are after dkv_page_tables: len[h] counts the new tokens.
+ * causal      not 0: token i of a sequence's n new ones attends to the first
+ *             len[h] - n + i + 1 rows of its slab; 0: to all len[h] rows.
+ * scale       softmax scale; <= 0 selects 1/sqrt(128).
+ * out         [num_tokens][H][128]; zeros for a token that has no row to attend to.
+ * workspace   dkv_chunk_workspace_bytes(pages) bytes.
+ * Errors: DKV_ERR_INVALID_ARG, DKV_ERR_CUDA.
+ */
+int64_t dkv_chunk_workspace_bytes(const dkv_pages* pages);
+dkv_status dkv_chunk_attn(const dkv_pages* pages, int32_t layer, int32_t dtype, int32_t num_tokens, const void* q,
+                          int64_t q_stride, const void* k_new, const void* v_new, int64_t kv_stride,
+                          const int32_t* cu_tokens, const int32_t* table, const int32_t* len, void* Kp, void* Vp,
+                          int32_t causal, float scale, void* out, void* workspace, int64_t workspace_bytes,
+                          int32_t* status, cudaStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -4,6 +4,7 @@
 // dkv_decode_mma.cu, dkv_decode.cu and dkv_topk.cu.
 #include "dkv.h"
 #include "dkv_internal.cuh"
+#include "dkv_pages.cuh"
 #include "dkv_pool.cuh"
 
 #include <algorithm>
@@ -297,6 +298,11 @@ dkv_status set_error(dkv_status st, const char* msg)
 {
     snprintf(g_err, sizeof g_err, "%s", msg ? msg : "");
     return st;
+}
+
+PlanView plan_view(const dkv_plan* p)
+{
+    return PlanView{p->s.L, p->B, p->s.H_kv, p->dense != 0, p->kept_rows, p->d_len, p->d_ioff, p->d_idx};
 }
 }  // namespace dkv
 

@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes
 import os
 from dataclasses import dataclass
+from functools import cached_property
 
 import numpy as np
 
@@ -25,6 +26,9 @@ DKV_DEV_APPEND_OVERFLOW = 0x1
 DKV_DEV_TMA_TIMEOUT = 0x2
 DKV_DEV_MERGE_TIMEOUT = 0x4
 DKV_DEV_BOUNDS = 0x8
+DKV_DEV_PAGES_EXHAUSTED = 0x10
+DKV_DEV_PAGE_RANGE = 0x20
+DKV_BF16, DKV_FP16 = 0, 1
 
 # Every entry point include/dkv.h declares.
 EXPORTS = ("dkv_last_error", "dkv_map_pattern", "dkv_plan_dense", "dkv_plan_query", "dkv_plan_read",
@@ -32,7 +36,8 @@ EXPORTS = ("dkv_last_error", "dkv_map_pattern", "dkv_plan_dense", "dkv_plan_quer
            "dkv_plan_status", "dkv_free", "dkv_decode_attn_noalloc", "dkv_budget", "dkv_topk_workspace_bytes",
            "dkv_topk_mask", "dkv_decode_multi", "dkv_map_pattern_inplace", "dkv_compact_inplace",
            "dkv_vmm_alloc", "dkv_vmm_trim", "dkv_vmm_pages_to_keep", "dkv_vmm_mapped_bytes", "dkv_vmm_page_bytes",
-           "dkv_vmm_free")
+           "dkv_vmm_free", "dkv_page_workspace_bytes", "dkv_page_tables", "dkv_page_release", "dkv_page_compact",
+           "dkv_chunk_workspace_bytes", "dkv_chunk_attn")
 
 
 class DkvError(RuntimeError):
@@ -65,6 +70,33 @@ class Shape:
     @property
     def G(self):
         return self.H // self.H_kv
+
+
+class dkv_pages(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("L", "B", "H", "H_kv", "head_dim", "page_rows", "num_pages", "max_pages")]
+
+
+@dataclass(frozen=True)
+class Pages:
+    """Geometry of a paged cache (dkv_pages): B sequence slots, pools of num_pages pages of page_rows rows, tables of
+    max_pages entries a slab."""
+    L: int
+    B: int
+    H: int
+    H_kv: int
+    page_rows: int
+    num_pages: int
+    max_pages: int
+    head_dim: int = 128
+
+    @cached_property
+    def c(self):
+        return dkv_pages(self.L, self.B, self.H, self.H_kv, self.head_dim, self.page_rows, self.num_pages, self.max_pages)
+
+    @property
+    def slabs(self):
+        return self.L * self.B * self.H_kv
 
 
 _lib = None
@@ -133,6 +165,19 @@ def lib(path: str | None = None):
     L.dkv_topk_workspace_bytes.argtypes = []
     L.dkv_topk_mask.restype = ctypes.c_int
     L.dkv_topk_mask.argtypes = [V, I64, I64, V, V, I64, V]
+    PG = ctypes.POINTER(dkv_pages)
+    L.dkv_page_workspace_bytes.restype = I64
+    L.dkv_page_workspace_bytes.argtypes = [PG]
+    L.dkv_page_tables.restype = ctypes.c_int
+    L.dkv_page_tables.argtypes = [PG, V, V, V, V, V, V, V, V, V, V, V, I64, V, I64, V, V]
+    L.dkv_page_release.restype = ctypes.c_int
+    L.dkv_page_release.argtypes = [PG, V, V, V, V, V, V, V, V, I64, V, V]
+    L.dkv_page_compact.restype = ctypes.c_int
+    L.dkv_page_compact.argtypes = [PG, V, V, V, V, I64, V, V, V, V, V, V]
+    L.dkv_chunk_workspace_bytes.restype = I64
+    L.dkv_chunk_workspace_bytes.argtypes = [PG]
+    L.dkv_chunk_attn.restype = ctypes.c_int
+    L.dkv_chunk_attn.argtypes = [PG, I32, I32, I32, V, I64, V, V, I64, V, V, V, V, V, I32, ctypes.c_float, V, V, I64, V, V]
     if path is None:
         _lib = L
     return L
@@ -482,3 +527,142 @@ def dkv_plan_read(plan: Plan, stream=None):
     if plan.dense:
         return ln, off, None, None
     return ln, off, ioff, idx[: info.kept_rows]
+
+
+def _bad(why):
+    raise DkvError(DKV_ERR_INVALID_ARG, "argument check", why)
+
+
+def _work(workspace):
+    return _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
+
+
+def _here(*tensors):
+    """The buffers of a call lie on the current device, whose stream it runs on."""
+    T = _torch()
+    if T.torch.cuda.is_available():
+        at = T.device() if T.device is not None else T.torch.cuda.current_device()
+        for t in tensors:
+            if t is not None and not isinstance(t, int) and t.is_cuda and t.device.index != at:
+                _bad(f"a tensor lies on {t.device}, the current device is cuda:{at}")
+
+
+def _page_args(p: Pages, len, new_len, table, free_pages, free_count, new_count, workspace, status):
+    i32, n = _i32(), p.slabs
+    _here(len, new_len, table, free_pages, free_count, new_count, workspace, status)
+    return ((_dev(len, "len", i32, n), _dev(new_len, "new_len", i32, n), _dev(table, "table", i32, n * p.max_pages),
+             _dev(free_pages, "free_pages", i32, p.num_pages), _dev(free_count, "free_count", i32, 1),
+             _dev(new_count, "new_count", i32, 1)), _work(workspace), _dev(status, "status", i32, min_numel=1))
+
+
+def dkv_page_workspace_bytes(pages: Pages) -> int:
+    n = int(lib().dkv_page_workspace_bytes(ctypes.byref(pages.c)))
+    if n < 0:
+        _check(DKV_ERR_INVALID_ARG, "dkv_page_workspace_bytes")
+    return n
+
+
+def dkv_page_tables(pages: Pages, len, new_len, table, free_pages, free_count, new_count, workspace, tokens=None,
+                    plan: Plan | None = None, seq=None, cu_tokens=None, slots=None, status=None, stream=None):
+    """Pages for tokens[b] new rows of every slab of slot b, or for a plan's kept rows (its sequence i to slot seq[i]);
+    slots int32 [L][max_tokens][H_kv] receives the slot map, cu_tokens int32 [B + 1] the token offsets."""
+    i32 = _i32()
+    _here(tokens, seq, cu_tokens, slots)
+    (ln, nl, tb, fp, fc, nc), (wp, wb), st = _page_args(pages, len, new_len, table, free_pages, free_count, new_count,
+                                                        workspace, status)
+    if isinstance(slots, int):
+        _bad("slots must be a tensor: its size is the most tokens")
+    rows = pages.L * pages.H_kv
+    if slots is not None and slots.numel() % rows:
+        _bad(f"slots has {slots.numel()} elements, not a multiple of L*H_kv={rows}")
+    if plan is not None and seq is not None and not isinstance(seq, int) and seq.numel() != plan.B:
+        _bad(f"seq has {seq.numel()} elements, the plan {plan.B} sequences")
+    _check(lib().dkv_page_tables(
+        ctypes.byref(pages.c), _dev(tokens, "tokens", i32, pages.B), plan.address if plan is not None else None,
+        _dev(seq, "seq", i32), ln, nl, tb, fp, fc, nc, _dev(cu_tokens, "cu_tokens", i32, pages.B + 1),
+        _dev(slots, "slots", i32), 0 if slots is None else slots.numel() // rows, wp, wb, st, _stream(stream)),
+        "dkv_page_tables")
+
+
+def dkv_page_release(pages: Pages, ended, len, new_len, table, free_pages, free_count, new_count, workspace,
+                     status=None, stream=None):
+    """The pages of the slots with ended[b] != 0 go back to the free list."""
+    _here(ended)
+    (ln, nl, tb, fp, fc, nc), (wp, wb), st = _page_args(pages, len, new_len, table, free_pages, free_count, new_count,
+                                                        workspace, status)
+    _check(lib().dkv_page_release(ctypes.byref(pages.c), _dev(ended, "ended", _i32(), pages.B), ln, nl, tb, fp, fc, nc,
+                                  wp, wb, st, _stream(stream)), "dkv_page_release")
+
+
+def _rows16():
+    t = _torch()
+    return (*t.bf16, t.torch.float16)
+
+
+def dkv_page_compact(pages: Pages, plan: Plan, K, V, table, len, Kp, Vp, seq=None, T_stride: int | None = None,
+                     status=None, stream=None):
+    """The kept rows of plan sequence i become the last rows of slot seq[i]'s slabs."""
+    if T_stride is None:
+        T_stride = K.shape[-2]
+    sh, i32, r16 = plan.shape, _i32(), _rows16()
+    plan.address
+    _here(K, V, table, len, Kp, Vp, seq, status)
+    dense = sh.L * plan.B * sh.H_kv * int(T_stride) * 128
+    pool = pages.num_pages * pages.page_rows * 128
+    if seq is not None and not isinstance(seq, int) and seq.numel() != plan.B:
+        _bad(f"seq has {seq.numel()} elements, the plan {plan.B} sequences")
+    _check(lib().dkv_page_compact(
+        ctypes.byref(pages.c), plan.address, _dev(seq, "seq", i32), _dev(K, "K", r16, min_numel=dense),
+        _dev(V, "V", r16, min_numel=dense), int(T_stride), _dev(table, "table", i32, pages.slabs * pages.max_pages),
+        _dev(len, "len", i32, pages.slabs), _dev(Kp, "Kp", r16, pool), _dev(Vp, "Vp", r16, pool),
+        _dev(status, "status", i32, min_numel=1), _stream(stream)), "dkv_page_compact")
+
+
+def dkv_chunk_workspace_bytes(pages: Pages) -> int:
+    n = int(lib().dkv_chunk_workspace_bytes(ctypes.byref(pages.c)))
+    if n < 0:
+        _check(DKV_ERR_INVALID_ARG, "dkv_chunk_workspace_bytes")
+    return n
+
+
+def _token_rows(t, name, dtype, tokens, heads):
+    """Address and token stride (elements) of a [tokens][heads][128] tensor whose tokens may lie apart (a slice of a
+    projection); heads and elements are contiguous."""
+    if not getattr(t, "is_cuda", False):
+        _bad(f"{name} must be a CUDA tensor")
+    if t.dtype != dtype or t.shape != (tokens, heads, 128):
+        _bad(f"{name} is {t.dtype} {tuple(t.shape)}, expected {dtype} {(tokens, heads, 128)}")
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != 128):
+        _bad(f"{name}: heads and elements of a token must be contiguous")
+    return t.data_ptr(), (t.stride(0) if tokens > 1 else heads * 128)
+
+
+def dkv_chunk_attn(pages: Pages, layer: int, q, k_new, v_new, cu_tokens, table, len, Kp, Vp, out, workspace,
+                   causal: bool = True, scale: float = 0.0, status=None, stream=None):
+    """One layer's new tokens: k_new and v_new [T][H_kv][128] appended to their slabs' pages (None: they are there), and
+    the attention of q [T][H][128] -> out [T][H][128], all of q's type (bf16 or fp16). q, k_new and v_new may be slices of
+    one projection; k_new and v_new have the same token stride."""
+    t = _torch().torch
+    i32 = _i32()
+    _here(q, k_new, v_new, cu_tokens, table, len, Kp, Vp, out, workspace, status)
+    if q.dtype not in (t.bfloat16, t.float16) or q.dim() != 3:
+        _bad(f"q is {q.dtype} of {q.dim()} dimensions, expected bfloat16 or float16 [T][H][128]")
+    tokens, one = q.shape[0], (q.dtype,)
+    qp, qs = _token_rows(q, "q", q.dtype, tokens, pages.H)
+    kp = vp = None
+    ks = 0
+    if (k_new is None) != (v_new is None):
+        _bad("k_new and v_new must both be given or both be None")
+    if k_new is not None:
+        kp, ks = _token_rows(k_new, "k_new", q.dtype, tokens, pages.H_kv)
+        vp, vs = _token_rows(v_new, "v_new", q.dtype, tokens, pages.H_kv)
+        if ks != vs:
+            _bad(f"k_new and v_new have token strides {ks} and {vs}")
+    pool = pages.num_pages * pages.page_rows * 128
+    wp, wb = _work(workspace)
+    _check(lib().dkv_chunk_attn(
+        ctypes.byref(pages.c), int(layer), DKV_FP16 if q.dtype == t.float16 else DKV_BF16, tokens, qp, qs, kp, vp, ks,
+        _dev(cu_tokens, "cu_tokens", i32, pages.B + 1), _dev(table, "table", i32, pages.slabs * pages.max_pages),
+        _dev(len, "len", i32, pages.slabs), _dev(Kp, "Kp", one, pool), _dev(Vp, "Vp", one, pool), int(bool(causal)),
+        scale, _dev(out, "out", one, tokens * pages.H * 128), wp, wb, _dev(status, "status", i32, min_numel=1),
+        _stream(stream)), "dkv_chunk_attn")
