@@ -2,22 +2,275 @@
 // rows are appended to their slabs' pages, then token i of the n new ones of sequence b
 // attends, per query head, to the first len - n + i + 1 rows of its slab (causal) or to
 // all len rows:  o = sum_r softmax_r(scale q.k_r) v_r.
-#include "dkv_decode_common.cuh"
+//
+// Unit of work: up to 2 TQ tokens of one sequence and KV head (TQ = 128 / G tokens x G heads
+// fill a 128-row tile of queries, row = token G + head), against the cache rows that its last
+// token sees, in tiles of 128 rows. All (unit, cache tile) pairs, unit after unit, are cut into
+// equal contiguous shares, one a CTA, one CTA an SM, so ragged lengths leave no SM idle; a unit
+// that lies in several CTAs is joined by the one that finishes last.
+//
+//   chunk_prologue_kernel  appends the rows, counts the tiles and finds where each CTA starts.
+//   chunk_attn_kernel      two pipelines of S = Q K^T, softmax, O += P V, one a softmax group:
+//     pair units (more than TQ tokens): group p has query tile p; both use the same K and V tile.
+//     split units (decode, drafts, the rest of a turn): one query tile; group p takes the cache
+//     tiles of parity p, and the groups' (m, l, O) are joined at the unit's end.
+//     warps 0-3, 4-7  softmax groups; thread = query row = TMEM lane. S is read from TMEM, P goes
+//                     back over it as the A operand of the second product.
+//     warp 8          MMA: S(0), S(1), then PV(s), S(s + 2) of step s (group s % 2), in one order, so
+//                     that the tensor pipe itself keeps S(s + 2) behind the PV(s) whose P it overwrites.
+//     warp 9          TMA (10 and 11 idle): Q tiles, and K and V tiles page by page into one ring in the order of use.
+//
+// Every wait is bounded (polls and 2 s); one that runs out sets DKV_DEV_TMA_TIMEOUT, the roles
+// walk on without work so that they meet at the named barriers, copies and products in flight
+// are drained, and the unit's outputs stay unwritten.
 #include "dkv_pages.cuh"
+#include "dkv_tcgen05.cuh"
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+#include <cudaTypedefs.h>
+
+#include <mutex>
 
 namespace dkv {
 namespace {
 
+constexpr int kTile = 128;                 // query rows and cache rows of a tile
+constexpr int kHalf = kTile * 128;         // one 64-dim half of a tile (16 KB)
+constexpr int kOperand = 2 * kHalf;        // a tile: dims 0-63, then 64-127
+constexpr int kStages = 5;                 // ring of K and V tiles
+constexpr int kThreads = 384;
+constexpr int kRegsSoft = 208, kRegsRest = 88;  // a thread's registers after the split; launched with 168
+static_assert(2 * kRegsSoft + kRegsRest <= 3 * 168, "three warpgroups share what they were launched with");
+constexpr int kSoft = 256;                 // threads of the softmax groups
+constexpr int kMaxCtas = 160;              // CTAs of the largest grid (the workspace's size)
+constexpr int kPieceRows = 2 * kTile;      // rows of a piece in the workspace
+constexpr int kTmemCols = 512;             // S of group p at 128 p (P over its first half), O at 256 + 128 p
+
+// Shared memory, from its 1024-byte aligned start (there is no room to align it by hand).
+constexpr int kOffQ = 0;
+constexpr int kOffRing = kOffQ + 2 * kOperand;
+constexpr int kOffBars = kOffRing + kStages * kOperand;
+constexpr int kNumBars = 2 * kStages + 9;  // full[], empty[], q_full, q_empty, s_full[2], p_full[2], o_done[2], fin
+constexpr int kOffMisc = kOffBars + (kNumBars + 1) / 2 * 16;  // int[4]: TMEM address, abort, last
+constexpr int kOffMl = kOffMisc + 16;                           // float2[128]: group 1's (m, l), then group 0's
+constexpr int kSmemBytes = kOffMl + 2 * kTile * 8;
+static_assert(kSmemBytes <= 227 * 1024, "fits one CTA");
+
+// Workspace.
+struct ChunkHead {
+    int64_t tiles;  // of all units
+    int32_t parts;  // CTAs with a share
+    int32_t pad;
+};
+struct ChunkWork {
+    ChunkHead* head;
+    int4* start;      // [kMaxCtas] sequence, KV head, unit of the sequence, first tile of a CTA's share
+    int32_t* done;    // [kMaxCtas] finished pieces of the unit that starts in CTA c and ends in a later one
+    float2* ml;       // [kMaxCtas][2][256]
+    float* o;         // [kMaxCtas][2][256][128]
+};
+constexpr int64_t kOffStart = 256, kOffDone = kOffStart + kMaxCtas * 16, kOffPieceMl = (kOffDone + kMaxCtas * 4 + 255) / 256 * 256,
+                  kOffPieceO = kOffPieceMl + (int64_t)kMaxCtas * 2 * kPieceRows * 8,
+                  kWorkBytes = kOffPieceO + (int64_t)kMaxCtas * 2 * kPieceRows * kHeadDim * 4;
+
+struct ChunkMaps {
+    CacheMaps cache;
+    CUtensorMap q;
+};
+
 __device__ __forceinline__ int cu_at(const ChunkArgs& a, int b) { return min(max(a.cu[b], 0), a.T); }
 
-// The sequence of token t, or -1 behind the last one.
-__device__ __forceinline__ int seq_of(const ChunkArgs& a, int t)
+// ---------------------------------------------------------------- units
+struct Unit {
+    int h;       // slab
+    int t0;      // first token (row of q)
+    int tokens;  // 1 .. 2 TQ
+    int row0;    // rows that the first token sees (causal), before the clamp to [0, len]
+    int len;     // rows of the slab
+    int kv;      // rows that the last token sees
+    bool pair;   // two query tiles
+    __device__ __forceinline__ int tiles() const { return max(1, (kv + kTile - 1) / kTile); }
+};
+
+__device__ __forceinline__ int slab_len(const ChunkArgs& a, int h)
 {
-    if (t >= cu_at(a, a.B)) return -1;
-    int lo = 0, hi = a.B - 1;
+    return (int)min((int64_t)max(a.len[h], 0), (int64_t)a.max_pages * a.P);
+}
+
+// Unit i of the n tokens from row t of q on, over a slab of len rows.
+__device__ __forceinline__ Unit make_unit(const ChunkArgs& a, int h, int t, int n, int len, int i)
+{
+    const int TQ = kTile / a.G, w = 2 * TQ;
+    Unit u;
+    u.h = h;
+    u.t0 = t + i * w;
+    u.tokens = min(w, n - i * w);
+    u.len = len;
+    u.row0 = a.causal ? len - n + i * w + 1 : len;
+    u.kv = a.causal ? max(0, u.row0 + u.tokens - 1) : len;
+    u.pair = u.tokens > TQ;
+    return u;
+}
+
+// The share of one CTA, unit by unit.
+struct Walk {
+    int b, g, i, t, n, j0, j1, tiles;
+    int64_t pos, end;  // tiles of the whole call: the current piece's first, the share's end
+    Unit u;
+    __device__ __forceinline__ void load(const ChunkArgs& a, int off)
+    {
+        t = cu_at(a, b);
+        n = cu_at(a, b + 1) - t;
+        const int h = b * a.Hkv + g;
+        u = make_unit(a, h, t, n, slab_len(a, h), i);
+        tiles = u.tiles();
+        j0 = off;
+        j1 = (int)min((int64_t)tiles, off + (end - pos));
+    }
+    // parts: CTAs with a share (c < parts).
+    __device__ __forceinline__ void begin(const ChunkArgs& a, const ChunkWork& w, const ChunkHead& head, int c)
+    {
+        pos = head.tiles * c / head.parts;
+        end = head.tiles * (c + 1) / head.parts;
+        const int4 s = __ldcg(w.start + c);
+        b = s.x;
+        g = s.y;
+        i = s.z;
+        load(a, s.w);
+    }
+    __device__ __forceinline__ bool next(const ChunkArgs& a)
+    {
+        pos += j1 - j0;
+        if (pos >= end) return false;
+        if (++i * 2 * (kTile / a.G) >= n) {
+            i = 0;
+            if (++g == a.Hkv) {
+                g = 0;
+                do ++b;
+                while (b < a.B - 1 && cu_at(a, b + 1) <= cu_at(a, b));
+            }
+        }
+        load(a, 0);
+        return true;
+    }
+    __device__ __forceinline__ bool whole() const { return j0 == 0 && j1 == tiles; }
+    __device__ __forceinline__ int steps() const { return u.pair ? 2 * (j1 - j0) : j1 - j0; }
+    __device__ __forceinline__ int tile(int s) const { return j0 + (u.pair ? s >> 1 : s); }
+};
+
+// The CTA whose share holds tile x of the call.
+__device__ __forceinline__ int cta_of(const ChunkHead& h, int64_t x) { return (int)(((x + 1) * h.parts - 1) / h.tiles); }
+
+// ---------------------------------------------------------------- append and schedule
+constexpr int kProThreads = 512;
+
+// Sum of x over the block's earlier threads; *total receives the whole sum.
+__device__ __forceinline__ int64_t scan_block(int64_t x, int64_t* sh, int64_t* total)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int64_t v = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(kFull, v, o);
+        if (lane >= o) v += y;
+    }
+    __syncthreads();
+    if (lane == 31) sh[warp] = v;
+    __syncthreads();
+    int64_t before = 0, all = 0;
+#pragma unroll
+    for (int k = 0; k < kProThreads / 32; ++k) {
+        if (k < warp) before += sh[k];
+        all += sh[k];
+    }
+    *total = all;
+    return v - x + before;
+}
+
+__device__ __forceinline__ void report(const ChunkArgs& a, int bits)
+{
+    if (a.status) atomicOr(a.status, bits);
+}
+
+// One block: the tiles of every unit, and where each CTA's share starts.
+__device__ __forceinline__ void schedule(const ChunkArgs& a, const ChunkWork& w, int nctas)
+{
+    __shared__ int64_t sh[kProThreads / 32];
+    __shared__ int32_t first[kMaxSlots + 1];  // units of the sequences before
+    const int tid = threadIdx.x, width = 2 * (kTile / a.G);
+    for (int c = tid; c < kMaxCtas; c += kProThreads) w.done[c] = 0;
+    static_assert(kMaxSlots <= kProThreads, "one thread a sequence");
+    int mine = 0;
+    if (tid < a.B) {
+        const int t0 = a.cu[tid], t1 = a.cu[tid + 1];
+        if (t0 < 0 || t1 < t0 || t1 > a.T || (tid == 0 && t0 != 0)) report(a, DKV_DEV_PAGE_RANGE);
+        mine = (max(cu_at(a, tid + 1) - cu_at(a, tid), 0) + width - 1) / width * a.Hkv;
+    }
+    int64_t units;
+    const int64_t before = scan_block(mine, sh, &units);
+    if (tid < a.B) first[tid] = (int)before;
+    if (tid == 0) first[a.B] = (int)units;
+    __syncthreads();
+    const int64_t per = (units + kProThreads - 1) / kProThreads;
+    const int64_t u0 = min(units, tid * per), u1 = min(units, u0 + per);
+    int b = 0;
+    {
+        int lo = 0, hi = a.B - 1;  // the last sequence with first <= u0 (it has units)
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (first[mid] <= u0)
+                lo = mid;
+            else
+                hi = mid - 1;
+        }
+        b = lo;
+    }
+    int64_t pos = 0, parts = 0, total = 0;
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+        int64_t sum = 0;
+        int bb = b;
+#pragma unroll 1
+        for (int64_t x = u0; x < u1; ++x) {
+            while (first[bb + 1] <= x) ++bb;
+            const int t = cu_at(a, bb), n = cu_at(a, bb + 1) - t, nq = (n + width - 1) / width;
+            const int k = (int)(x - first[bb]), g = k / nq, i = k - g * nq, h = bb * a.Hkv + g;
+            if (pass == 0 && i == 0 && (a.len[h] < n || a.len[h] != slab_len(a, h)) && (a.k_new || a.len[h] != slab_len(a, h)))
+                report(a, DKV_DEV_PAGE_RANGE);
+            const int tiles = make_unit(a, h, t, n, slab_len(a, h), i).tiles();
+            if (pass == 1) {
+                const int64_t s = pos + sum, e = s + tiles;
+#pragma unroll 1
+                for (int64_t c = (s * parts + total - 1) / total; c < parts; ++c) {
+                    const int64_t at = total * c / parts;
+                    if (at >= e) break;
+                    if (at >= s) w.start[c] = make_int4(bb, g, i, (int)(at - s));
+                }
+            }
+            sum += tiles;
+        }
+        if (pass == 0) {
+            pos = scan_block(sum, sh, &total);
+            parts = min(total, (int64_t)nctas);
+        }
+    }
+    if (tid == 0) *w.head = ChunkHead{total, (int)parts, 0};
+}
+
+__global__ void __launch_bounds__(kProThreads) chunk_prologue_kernel(const __grid_constant__ ChunkArgs a, const ChunkWork w, int nctas)
+{
+    pdl_wait();
+    pdl_launch_dependents();
+    if (blockIdx.x == 0) {
+        schedule(a, w, nctas);
+        return;
+    }
+    // Append: a half-warp a row (K and V).
+    const int64_t i = (int64_t)(blockIdx.x - 1) * (kProThreads / 16) + (threadIdx.x >> 4);
+    const int sub = threadIdx.x & 15, t = (int)(i / a.Hkv), g = (int)(i - (int64_t)t * a.Hkv);
+    if (t >= cu_at(a, a.B)) return;
+    int lo = 0, hi = a.B - 1;  // the last sequence that starts at t or before
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (cu_at(a, mid) <= t)
@@ -25,106 +278,654 @@ __device__ __forceinline__ int seq_of(const ChunkArgs& a, int t)
         else
             hi = mid - 1;
     }
-    return lo;
-}
-
-// Pool row of row r of slab h, or -1.
-__device__ __forceinline__ int64_t pool_row(const ChunkArgs& a, int h, int64_t r)
-{
-    if (r < 0 || r >= (int64_t)a.max_pages * a.P) return -1;
-    const int page = a.table[(int64_t)h * a.max_pages + r / a.P];
-    return page < 0 || page >= a.num_pages ? -1 : (int64_t)page * a.P + r % a.P;
-}
-
-__global__ void __launch_bounds__(256) chunk_append_kernel(const ChunkArgs a)
-{
-    const int i = blockIdx.x * 16 + (threadIdx.x >> 4), sub = threadIdx.x & 15;
-    const int t = i / a.Hkv, g = i - t * a.Hkv;
-    if (t >= a.T) return;
-    const int b = seq_of(a, t);
-    if (b < 0) return;
-    const int h = b * a.Hkv + g, n = cu_at(a, b + 1) - cu_at(a, b);
-    const int64_t row = pool_row(a, h, (int64_t)a.len[h] - n + (t - cu_at(a, b)));
-    if (row < 0) {
-        if (sub == 0 && a.status) atomicOr(a.status, DKV_DEV_PAGE_RANGE);
+    const int h = lo * a.Hkv + g;
+    const int64_t r = (int64_t)a.len[h] - cu_at(a, lo + 1) + t;
+    int page = -1;
+    if (r >= 0 && r < (int64_t)a.max_pages * a.P) page = a.table[(int64_t)h * a.max_pages + r / a.P];
+    if (page < 0 || page >= a.num_pages) {
+        if (sub == 0) report(a, DKV_DEV_PAGE_RANGE);
         return;
     }
-    const int64_t src = t * a.kv_stride + g * kHeadDim;
+    const int64_t row = (int64_t)page * a.P + r % a.P, src = t * a.kv_stride + g * kHeadDim;
     reinterpret_cast<uint4*>(a.Kp + row * kHeadDim)[sub] = reinterpret_cast<const uint4*>(a.k_new + src)[sub];
     reinterpret_cast<uint4*>(a.Vp + row * kHeadDim)[sub] = reinterpret_cast<const uint4*>(a.v_new + src)[sub];
 }
 
-template <bool F16>
-__device__ __forceinline__ float4 load4(const uint16_t* p)
+// ---------------------------------------------------------------- attention
+__device__ __forceinline__ bool wait_more(uint32_t bar, uint32_t parity, volatile int* abort, int32_t* status)
 {
-    const uint2 u = *reinterpret_cast<const uint2*>(p);
-    if (F16) {
-        const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&u.x)), y = __half22float2(*reinterpret_cast<const __half2*>(&u.y));
-        return make_float4(x.x, x.y, y.x, y.y);
+    const unsigned long long t0 = global_ns();
+    for (int i = 1; i < kWaitSpins; ++i) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((i & 15) == 0 && (*abort || global_ns() - t0 > kWaitNs)) break;
     }
-    return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
-                       __uint_as_float(u.y & 0xffff0000u));
+    if (!*abort) {
+        *abort = 1;
+        if (status) atomicOr(status, DKV_DEV_TMA_TIMEOUT);
+    }
+    return false;
 }
 
-// One warp a (token, query head): 4 dimensions a lane, one row after another.
+// A bounded wait of a whole warp. After one that ran out (here or in another role) every wait
+// of the CTA returns false at once.
+struct Waits {
+    volatile int* abort;
+    int32_t* status;
+    bool ok;
+    __device__ __forceinline__ bool operator()(uint64_t* b, uint32_t parity)
+    {
+        if (!ok) return false;
+        const uint32_t bar = smem_u32(b);
+        if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
+        ok = __all_sync(kFull, wait_more(bar, parity, abort, status));
+        return ok;
+    }
+};
+
 template <bool F16>
-__global__ void __launch_bounds__(256) chunk_rows_kernel(const ChunkArgs a)
+__device__ __forceinline__ uint32_t pack16(float lo, float hi)
 {
-    const int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31, t = (int)(w / a.H), head = (int)(w - (int64_t)t * a.H);
-    if (t >= a.T) return;
-    const int b = seq_of(a, t);
-    if (b < 0) return;
-    const int h = b * a.Hkv + head / a.G, t0 = cu_at(a, b), n = cu_at(a, b + 1) - t0;
-    const int64_t len = a.len[h], rows = a.causal ? len - n + (t - t0) + 1 : len;
-    const float4 q = load4<F16>(a.q + t * a.q_stride + head * kHeadDim + 4 * lane);
-    float m = -INFINITY, l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int64_t r = 0; r < rows; ++r) {
-        const int64_t row = pool_row(a, h, r);
-        if (row < 0) {
-            if (lane == 0 && a.status) atomicOr(a.status, DKV_DEV_PAGE_RANGE);
-            break;
-        }
-        const float4 k = load4<F16>(a.Kp + row * kHeadDim + 4 * lane), v = load4<F16>(a.Vp + row * kHeadDim + 4 * lane);
-        float s = q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w;
-#pragma unroll
-        for (int x = 16; x >= 1; x >>= 1) s += __shfl_xor_sync(kFull, s, x);
-        s *= a.qscale;
-        const float m1 = fmaxf(m, s), f = ex2(m - m1), p = ex2(s - m1);
-        m = m1;
-        l = l * f + p;
-        o = make_float4(o.x * f + p * v.x, o.y * f + p * v.y, o.z * f + p * v.z, o.w * f + p * v.w);
-    }
-    const float z = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
-    uint2 u;
     if (F16) {
-        const __half2 x = __floats2half2_rn(o.x * z, o.y * z), y = __floats2half2_rn(o.z * z, o.w * z);
-        u = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
-    } else {
-        const __nv_bfloat162 x = __floats2bfloat162_rn(o.x * z, o.y * z), y = __floats2bfloat162_rn(o.z * z, o.w * z);
-        u = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+        const __half2 x = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&x);
     }
-    *reinterpret_cast<uint2*>(a.out + ((int64_t)t * a.H + head) * kHeadDim + 4 * lane) = u;
+    return pack_bf16(lo, hi);
+}
+
+// Zeroes rows [first, 128) of a V tile (one warp).
+__device__ __forceinline__ void zero_rows(unsigned char* v, int first, int lane)
+{
+    for (int e = lane; e < (kTile - first) * 16; e += 32)
+        *reinterpret_cast<uint4*>(v + ((e & 15) >> 3) * kHalf + (first + (e >> 4)) * 128 + (e & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+    fence_proxy_async_smem();
+    __syncwarp();
+}
+
+// P of a score s is 2^(s c - origin(m, c)).
+template <bool F16>
+__device__ __forceinline__ float origin(float m, float c)
+{
+    constexpr float kShift = F16 ? 7.f : 0.f;
+    return (m == -INFINITY ? 0.f : m * c) - kShift;
+}
+
+// One step of a softmax group's warp: scores of 32 query rows x 128 cache rows (TMEM columns of
+// `s`) to P over them, with the running max m (of raw scores), sum l and output `o`. lim: the
+// cache rows of this tile that the thread's query sees (may be outside 0 .. 128).
+// The max moves only when a score tops it by 2^kSlack (then O is rescaled, so `rescale` says
+// whether it holds anything): P stays below 2^kSlack. fp16 P is scaled by 2^7 more, which l shares: the
+// smallest normal P is then 2^-21 of the largest score's.
+template <bool F16>
+__device__ __forceinline__ void softmax_step(uint32_t s, uint32_t o, int lim, bool rescale, float c, float& m, float& l)
+{
+    uint32_t x[4][32];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) tmem_ld32_async(s + 32 * k, x[k]);
+    tmem_wait_ld();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) tmem_fence_regs(x[k]);
+    if (__any_sync(kFull, lim < kTile)) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+                if (32 * k + e >= lim) x[k][e] = 0xff800000u;  // -inf: also over NaN
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < 32; ++e) mx = fmaxf(mx, __uint_as_float(x[k][e]));
+    const bool move = (mx - m) * c > kSlack;
+    if (__any_sync(kFull, move)) {
+        const float alpha = move ? ex2((m - mx) * c) : 1.f;
+        if (move) m = mx;
+        l *= alpha;
+        if (rescale) {
+#pragma unroll 1
+            for (int k = 0; k < 8; ++k) {
+                uint32_t v[16];
+                tmem_ld16_async(o + 16 * k, v);
+                tmem_wait_ld();
+                tmem_fence_regs(v);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * alpha);
+                tmem_st16_async(o + 16 * k, v);
+            }
+        }
+    }
+    const float mc = origin<F16>(m, c);
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        uint32_t p[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float p0 = ex2(fmaf(__uint_as_float(x[k][2 * e]), c, -mc));
+            const float p1 = ex2(fmaf(__uint_as_float(x[k][2 * e + 1]), c, -mc));
+            sum += p0 + p1;
+            p[e] = pack16<F16>(p0, p1);
+        }
+        tmem_st16_async(s + 16 * k, p);
+    }
+    l += sum;
+    tmem_wait_st();
+}
+
+// Elements 32 k .. 32 k + 31 of an output row.
+template <bool F16>
+__device__ __forceinline__ void store_out(uint16_t* row, const float (&v)[32], float z)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        uint4 u;
+        u.x = pack16<F16>(v[8 * k] * z, v[8 * k + 1] * z);
+        u.y = pack16<F16>(v[8 * k + 2] * z, v[8 * k + 3] * z);
+        u.z = pack16<F16>(v[8 * k + 4] * z, v[8 * k + 5] * z);
+        u.w = pack16<F16>(v[8 * k + 6] * z, v[8 * k + 7] * z);
+        reinterpret_cast<uint4*>(row)[k] = u;
+    }
+}
+
+__device__ __forceinline__ void store_piece(float* row, const float (&v)[32])
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        __stcg(reinterpret_cast<float4*>(row) + k, make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]));
+}
+
+// 1 / l; a sum of 0 (no rows) gives 0, NaN stays.
+__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
+
+template <bool F16>
+__device__ __forceinline__ float2 widen(uint32_t u)
+{
+    if (F16) return __half22float2(*reinterpret_cast<const __half2*>(&u));
+    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+}
+
+// Pool row of row r of the unit's slab, or -1.
+__device__ __forceinline__ int64_t pool_row(const ChunkArgs& a, int h, int r)
+{
+    const int page = a.table[(int64_t)h * a.max_pages + r / a.P];
+    return page < 0 || page >= a.num_pages ? -1 : (int64_t)page * a.P + r % a.P;
+}
+
+// A value of V that is not finite, in a later token's row, spoils the rows of the same tile
+// that do not see it (0 NaN is NaN). Rows whose result is not finite (`odd`) and that have
+// such a value in a masked place, rows [lim, end), are computed again without the tensor cores:
+// o = sum over rows [first, lim) of 2^(s - mc) v, dims [d0, d0 + nd). Slow and rare: 4 rows at
+// once, 8 lanes and 16 dims a lane each.
+template <bool F16>
+__device__ __forceinline__ void mend_rows(const ChunkArgs& a, int h, bool odd, int first, int lim, int end, float mc, float z,
+                                          const uint16_t* q, uint16_t* out, float* piece, int d0, int nd)
+{
+    const int lane = threadIdx.x & 31, sub = lane & 7, dim = 16 * sub;
+    const bool mine = dim >= d0 && dim < d0 + nd;
+    __syncwarp();  // the rows' first results are stored
+    unsigned todo = __ballot_sync(kFull, odd);
+#pragma unroll 1
+    while (todo) {
+        const int src = __ffs(todo) - 1;
+        todo &= todo - 1;
+        const int L = __shfl_sync(kFull, lim, src);
+        const float m1 = __shfl_sync(kFull, mc, src), z1 = __shfl_sync(kFull, z, src);
+        const uint16_t* q1 = reinterpret_cast<const uint16_t*>(__shfl_sync(kFull, reinterpret_cast<unsigned long long>(q), src));
+        uint16_t* out1 = reinterpret_cast<uint16_t*>(__shfl_sync(kFull, reinterpret_cast<unsigned long long>(out), src));
+        float* piece1 = reinterpret_cast<float*>(__shfl_sync(kFull, reinterpret_cast<unsigned long long>(piece), src));
+        float spoilt = 0.f;
+#pragma unroll 1
+        for (int r = max(L, first) + (lane >> 3); r < end; r += 4) {
+            const int64_t row = pool_row(a, h, r);
+            if (row < 0 || !mine) continue;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float2 v = widen<F16>(reinterpret_cast<const uint32_t*>(a.Vp + row * kHeadDim + dim)[e]);
+                spoilt += 0.f * v.x + 0.f * v.y;
+            }
+        }
+        if (!__any_sync(kFull, spoilt != spoilt)) continue;
+        float o[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[e] = 0.f;
+        const int last = min(L, end);
+#pragma unroll 1
+        for (int r0 = first; r0 < last; r0 += 4) {
+            const int r = r0 + (lane >> 3);
+            const int64_t row = r < last ? pool_row(a, h, r) : -1;
+            float s = 0.f;
+            if (row >= 0)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float2 x = widen<F16>(reinterpret_cast<const uint32_t*>(q1 + dim)[e]);
+                    const float2 k = widen<F16>(reinterpret_cast<const uint32_t*>(a.Kp + row * kHeadDim + dim)[e]);
+                    s = fmaf(x.x, k.x, fmaf(x.y, k.y, s));
+                }
+#pragma unroll
+            for (int x = 4; x >= 1; x >>= 1) s += __shfl_xor_sync(kFull, s, x);
+            if (row >= 0) {
+                const float p = ex2(fmaf(s, a.qscale, -m1));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float2 v = widen<F16>(reinterpret_cast<const uint32_t*>(a.Vp + row * kHeadDim + dim)[e]);
+                    o[2 * e] = fmaf(p, v.x, o[2 * e]);
+                    o[2 * e + 1] = fmaf(p, v.y, o[2 * e + 1]);
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            o[e] += __shfl_xor_sync(kFull, o[e], 8);
+            o[e] += __shfl_xor_sync(kFull, o[e], 16);
+        }
+        if (lane < 8 && mine) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (piece1)
+                    __stcg(reinterpret_cast<float2*>(piece1 + dim) + e, make_float2(o[2 * e], o[2 * e + 1]));
+                else
+                    reinterpret_cast<uint32_t*>(out1 + dim)[e] = pack16<F16>(o[2 * e] * z1, o[2 * e + 1] * z1);
+            }
+        }
+        __syncwarp();
+    }
+}
+
+// The last piece's CTA joins the pieces of a unit, in the order of the CTAs: one warp a row.
+template <bool F16>
+__device__ __forceinline__ void join_pieces(const ChunkArgs& a, const ChunkWork& w, int t0, int tokens, int g, int c0, int pieces)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, TQ = kTile / a.G, rows = tokens * a.G;
+    const float c = a.qscale;
+#pragma unroll 1
+    for (int x = warp; x < rows; x += kSoft / 32) {
+        const int token = x / a.G, j = x - token * a.G;
+        const int r = token >= TQ ? kTile + (token - TQ) * a.G + j : x;
+        float M = -INFINITY;
+#pragma unroll 1
+        for (int k = lane; k < pieces; k += 32)
+            M = fmaxf(M, __ldcg(w.ml + ((int64_t)(c0 + k) * 2 + (k == 0)) * kPieceRows + r).x);
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(kFull, M, o));
+        float L = 0.f;
+        float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int k = 0; k < pieces; ++k) {
+            const int64_t at = ((int64_t)(c0 + k) * 2 + (k == 0)) * kPieceRows + r;
+            const float2 ml = __ldcg(w.ml + at);
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(w.o + at * kHeadDim) + lane);
+            const float f = ml.x == -INFINITY ? 0.f : ex2((ml.x - M) * c);
+            if (ml.y == 0.f) continue;
+            L = fmaf(ml.y, f, L);
+            O.x = fmaf(v.x, f, O.x);
+            O.y = fmaf(v.y, f, O.y);
+            O.z = fmaf(v.z, f, O.z);
+            O.w = fmaf(v.w, f, O.w);
+        }
+        const float z = inverse(L);
+        uint16_t* out = a.out + ((int64_t)(t0 + token) * a.H + g * a.G + j) * kHeadDim + 4 * lane;
+        *reinterpret_cast<uint2*>(out) = make_uint2(pack16<F16>(O.x * z, O.y * z), pack16<F16>(O.z * z, O.w * z));
+    }
+}
+
+template <bool F16>
+__global__ void __launch_bounds__(kThreads, 1)
+    chunk_attn_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkMaps maps, const __grid_constant__ ChunkWork w)
+{
+    extern __shared__ __align__(1024) unsigned char sm[];
+    if (smem_u32(sm) & 1023) {  // never: the swizzled tiles need it
+        if (threadIdx.x == 0) report(a, DKV_DEV_TMA_TIMEOUT);
+        return;
+    }
+    uint64_t* full = reinterpret_cast<uint64_t*>(sm + kOffBars);  // [kStages] the stage's rows landed
+    uint64_t* empty = full + kStages;                              // [kStages] its products are done
+    uint64_t* q_full = empty + kStages;                            // the unit's Q tiles landed
+    uint64_t* q_empty = q_full + 1;                                // the unit's score products are done
+    uint64_t* s_full = q_empty + 1;                                // [2] S of the group's next step is done
+    uint64_t* p_full = s_full + 2;                                 // [2] its P is written
+    uint64_t* o_done = p_full + 2;                                 // [2] the group's last product of the unit is done
+    uint64_t* fin = o_done + 2;                                    // drain after a timeout
+    volatile int* misc = reinterpret_cast<volatile int*>(sm + kOffMisc);
+    float2* sh_ml = reinterpret_cast<float2*>(sm + kOffMl);        // [2][128]
+
+    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31, c = blockIdx.x;
+    if (warp == 8) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(sm + kOffMisc)),
+                     "r"(kTmemCols));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (tid == 0) {
+        misc[1] = 0;
+        for (int i = 0; i < kNumBars; ++i) mbar_init(smem_u32(full + i), full + i == p_full || full + i == p_full + 1 ? 4 : 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_proxy_async_smem();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = (uint32_t)uniform(misc[0]);
+    pdl_wait();
+    const ChunkHead head{(int64_t)__ldcg(reinterpret_cast<const long long*>(&w.head->tiles)), __ldcg(&w.head->parts), 0};
+    const bool work = c < head.parts;
+    Waits wait{misc + 1, a.status, true};
+    const int TQ = kTile / a.G;
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
+    if (work && warp == 9) {
+        // ---------------------------------------------------------------- TMA
+        asm volatile("fence.proxy.async.global;" ::: "memory");  // the appended rows, written by ordinary stores
+        // Rows that one unit streams once leave L2 first; a turn's units share theirs.
+        const uint64_t stream = evict_first_policy();
+        uint64_t keep;
+        asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(keep));
+        Walk k;
+        k.begin(a, w, head, c);
+        int pos = 0, unit = 0;
+        const int ppt = kTile / a.P;  // pages a tile
+        auto load = [&](const CUtensorMap* map, int j) {
+            const int s = pos % kStages;
+            const int pages = min(max(k.u.kv - j * kTile, 0), kTile);
+            const int np = (pages + a.P - 1) / a.P;
+            int y = 0;
+            if (lane < np) {
+                const int page = a.table[(int64_t)k.u.h * a.max_pages + j * ppt + lane];
+                const bool good = page >= 0 && page < a.num_pages;
+                if (!good) report(a, DKV_DEV_PAGE_RANGE);
+                y = (good ? page : a.num_pages) * a.P;  // behind the pool: zeros
+            }
+            if (pos >= kStages && !wait(&empty[s], (pos / kStages - 1) & 1)) return;
+            const uint32_t bar = smem_u32(&full[s]), dst = smem_u32(sm + kOffRing + s * kOperand);
+            if (lane == 0) mbar_arrive_expect_tx(bar, np * a.P * kRowBytes);
+            __syncwarp();
+            const uint64_t pol = k.u.pair ? keep : stream;
+            if (lane < np) {
+                tma_box(dst + lane * a.P * 128, map, 0, y, bar, pol);
+                tma_box(dst + kHalf + lane * a.P * 128, map, 64, y, bar, pol);
+            }
+            __syncwarp();
+            ++pos;
+        };
+        int qs = 0;  // Q loads issued
+        do {
+            if (unit > 0 && !wait(q_empty, (unit - 1) & 1)) break;
+            if (lane == 0) {
+                const uint32_t bar = smem_u32(q_full), box = 2u * 64 * a.G * TQ;
+                mbar_arrive_expect_tx(bar, (k.u.pair ? 4 : 2) * box);
+                for (int p = 0; p < (k.u.pair ? 2 : 1); ++p)
+                    for (int half = 0; half < 2; ++half)
+                        tma_box3(smem_u32(sm + kOffQ + p * kOperand + half * kHalf), &maps.q, 64 * half, k.g * a.G, k.u.t0 + p * TQ, bar);
+            }
+            __syncwarp();
+            ++qs;
+            const int steps = k.steps(), stride = k.u.pair ? 2 : 1;
+            // K(0), K(1), then V(s), K(s + 2); pair units have one K and one V a pair of steps.
+#pragma unroll 1
+            for (int x = -4; x < 2 * steps && wait.ok; ++x) {
+                const int s = (x >> 1) + 2 * (x & 1);  // even x: V of step x / 2; odd x: K of step x / 2 + 2
+                if (s < 0 || s >= steps || (s & (stride - 1))) continue;
+                load(x & 1 ? &maps.cache.k : &maps.cache.v, k.tile(s));
+            }
+            ++unit;
+        } while (wait.ok && k.next(a));
+        if (!wait.ok) {
+            // Copies in flight land (or run out of time) before the CTA exits.
+            for (int x = max(0, pos - kStages); x < pos; ++x) mbar_wait(smem_u32(&full[x % kStages]), (x / kStages) & 1);
+            if (qs) mbar_wait(smem_u32(q_full), (qs - 1) & 1);
+        }
+    } else if (work && warp == 8) {
+        // ---------------------------------------------------------------- MMA
+        const bool leads = elect_one();
+        const uint32_t id_s = idesc(kTile, kTile, 0, 0, !F16), id_o = idesc(kTile, kTile, 0, 1, !F16);
+        // Operand descriptors: a stride byte offset of 1 KB, version 1, 128-byte swizzle in the high
+        // word; stages and k-steps add to the address field of the low one (16-byte units).
+        const uint32_t dhi = (uint32_t)(sdesc(0, 0, 1024) >> 32);
+        const uint32_t dQ = (uint32_t)sdesc(smem_u32(sm + kOffQ), 16, 1024), dK = (uint32_t)sdesc(smem_u32(sm + kOffRing), 16, 1024),
+                       dV = (uint32_t)sdesc(smem_u32(sm + kOffRing), kHalf, 1024);
+        auto desc = [dhi](uint32_t lo) { return ((uint64_t)dhi << 32) | lo; };
+        Walk k;
+        k.begin(a, w, head, c);
+        int pos = 0, unit = 0, curK = 0, curV = 0;
+        uint32_t phases = 0;  // bit p: parity of the P tiles taken of group p
+        bool issued = false;
+        do {
+            const int steps = k.steps();
+            const bool pair = k.u.pair;
+            if (!wait(q_full, unit & 1)) break;
+#pragma unroll 1
+            for (int x = -2; x < steps; ++x) {
+                const int p = x & 1;
+                if (x >= 0) {  // PV(x)
+                    if (!pair || p == 0) {
+                        curV = pos % kStages;
+                        if (!wait(&full[curV], (pos / kStages) & 1)) break;
+                        ++pos;
+                        // Rows past the unit's last (another token's, or never written) are zeroed: 0 NaN is NaN.
+                        const int valid = max(k.u.kv - k.tile(x) * kTile, 0);
+                        if (valid < kTile) zero_rows(sm + kOffRing + curV * kOperand, valid, lane);
+                    }
+                    if (!wait(&p_full[p], (phases >> p) & 1)) break;
+                    phases ^= 1u << p;
+                    tc_fence_after();
+                    if (leads) {
+                        const uint32_t v = dV + curV * (kOperand >> 4), o = tmem + 256 + p * kTile, pt = tmem + p * kTile;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) umma_ts(o, pt + 8 * e, desc(v + e * (2048 >> 4)), id_o, x > 1 || e > 0);
+                        if (!pair || p == 1) umma_commit(smem_u32(&empty[curV]));
+                        if (x + 2 >= steps) umma_commit(smem_u32(&o_done[p]));
+                    }
+                    __syncwarp();
+                }
+                if (x + 2 < steps) {  // S(x + 2)
+                    if (!pair || p == 0) {
+                        curK = pos % kStages;
+                        if (!wait(&full[curK], (pos / kStages) & 1)) break;
+                        ++pos;
+                    }
+                    tc_fence_after();
+                    if (leads) {
+                        const uint32_t q = dQ + (pair ? p : 0) * (kOperand >> 4), kt = dK + curK * (kOperand >> 4), d = tmem + p * kTile;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const uint32_t off = ((e >> 2) * kHalf + (e & 3) * 32) >> 4;
+                            umma(d, desc(q + off), desc(kt + off), id_s, e > 0);
+                        }
+                        umma_commit(smem_u32(&s_full[p]));
+                        if (!pair || p == 1) umma_commit(smem_u32(&empty[curK]));
+                        if (x + 2 == steps - 1) umma_commit(smem_u32(q_empty));
+                    }
+                    issued = true;
+                    __syncwarp();
+                }
+            }
+            ++unit;
+        } while (wait.ok && k.next(a));
+        if (!wait.ok && issued) {
+            if (leads) {
+                umma_commit(smem_u32(fin));
+                mbar_wait(smem_u32(fin), 0);
+            }
+            __syncwarp();
+        }
+    }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoft));
+        if (work) {
+        // ---------------------------------------------------------------- softmax groups
+        const int p = warp >> 2, r = tid & 127;
+        const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
+        const uint32_t s_at = tmem + lanes + p * kTile, o_at = tmem + lanes + 256;
+        const int token = r / a.G, j = r - token * a.G;
+        const float cs = a.qscale;
+        Walk k;
+        k.begin(a, w, head, c);
+        int ns = 0, no = 0;  // S tiles and O accumulators taken
+        do {
+            const int steps = k.steps();
+            const bool pair = k.u.pair, whole = k.whole();
+            const int tok = token + (pair ? p * TQ : 0);
+            const bool live = token < TQ && tok < k.u.tokens;
+            const int lim = !live ? 0x3fffffff : a.causal ? min(max(k.u.row0 + tok, 0), k.u.len) : k.u.len;
+            const bool any = __any_sync(kFull, live);
+            float m = -INFINITY, l = 0.f;
+#pragma unroll 1
+            for (int s = p; s < steps; s += 2) {
+                if (wait(&s_full[p], ns & 1) && any) {
+                    tc_fence_after();
+                    softmax_step<F16>(s_at, o_at + p * kTile, lim - k.tile(s) * kTile, s > 1, cs, m, l);
+                    tc_fence_before();
+                }
+                ++ns;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&p_full[p]));
+            }
+            if (steps > p) {
+                wait(&o_done[p], no & 1);
+                ++no;
+            }
+            tc_fence_after();
+            uint16_t* out = a.out + ((int64_t)(k.u.t0 + tok) * a.H + k.g * a.G + j) * kHeadDim;
+            const int64_t piece = ((int64_t)c * 2 + (k.j0 == 0)) * kPieceRows + (pair ? p * kTile : 0) + r;
+            // Cache rows of this piece, and whether some of them are hidden from the thread's query.
+            const int first = k.j0 * kTile, end = min(k.u.kv, k.j1 * kTile);
+            const bool hidden = live && lim < end;
+            const uint16_t* q = a.q + (int64_t)(k.u.t0 + tok) * a.q_stride + (k.g * a.G + j) * kHeadDim;
+            float* o_piece = whole ? nullptr : w.o + piece * kHeadDim;
+            float odd = 0.f;  // NaN if a result is not finite
+            if (pair) {
+                if (any && wait.ok) {
+                    const float z = inverse(l);
+#pragma unroll 1
+                    for (int e = 0; e < 4; ++e) {
+                        float v[32];
+                        tmem_ld32(o_at + p * kTile + 32 * e, v);
+#pragma unroll
+                        for (int d = 0; d < 32; ++d) odd = fmaf(v[d], 0.f, odd);
+                        if (live && whole) store_out<F16>(out + 32 * e, v, z);
+                        if (live && !whole) store_piece(o_piece + 32 * e, v);
+                    }
+                    if (__any_sync(kFull, hidden && odd != odd))
+                        mend_rows<F16>(a, k.u.h, hidden && odd != odd, first, lim, end, origin<F16>(m, cs), z, q, out, o_piece, 0, kHeadDim);
+                    if (live && !whole) __stcg(w.ml + piece, make_float2(m, l));
+                }
+            } else {
+                // The groups' halves of the cache rows: each group joins 64 of the dimensions.
+                sh_ml[p * kTile + r] = make_float2(m, l);
+                tc_fence_before();
+                named_sync(1, kSoft);
+                tc_fence_after();
+                const float2 x = sh_ml[r], y = sh_ml[kTile + r];
+                const float M = fmaxf(x.x, y.x);
+                const float fx = x.x == -INFINITY ? 0.f : ex2((x.x - M) * cs), fy = y.x == -INFINITY ? 0.f : ex2((y.x - M) * cs);
+                const float L = x.y * fx + y.y * fy, z = inverse(L);
+                const bool two = steps > 1;
+                if (any && wait.ok) {
+#pragma unroll 1
+                    for (int e = 2 * p; e < 2 * p + 2; ++e) {
+                        float v[32], v1[32];
+                        tmem_ld32(o_at + 32 * e, v);
+                        if (two) tmem_ld32(o_at + kTile + 32 * e, v1);
+#pragma unroll
+                        for (int d = 0; d < 32; ++d) {
+                            v[d] = v[d] * fx + (two ? v1[d] * fy : 0.f);
+                            odd = fmaf(v[d], 0.f, odd);
+                        }
+                        if (live && whole) store_out<F16>(out + 32 * e, v, z);
+                        if (live && !whole) store_piece(o_piece + 32 * e, v);
+                    }
+                    if (__any_sync(kFull, hidden && odd != odd))
+                        mend_rows<F16>(a, k.u.h, hidden && odd != odd, first, lim, end, origin<F16>(M, cs), z, q, out, o_piece, 64 * p, 64);
+                    if (live && !whole && p == 0) __stcg(w.ml + piece, make_float2(M, L));
+                }
+            }
+            if (!whole) {
+                const int c0 = cta_of(head, k.pos - k.j0), pieces = cta_of(head, k.pos - k.j0 + k.tiles - 1) - c0 + 1;
+                __threadfence();
+                named_sync(1, kSoft);
+                if (tid == 0) misc[2] = misc[1] == 0 && atomicAdd(w.done + c0, 1) == pieces - 1;
+                named_sync(1, kSoft);
+                if (misc[2]) {
+                    __threadfence();
+                    join_pieces<F16>(a, w, k.u.t0, k.u.tokens, k.g, c0, pieces);
+                }
+            }
+            if (!pair || !whole) {
+                tc_fence_before();
+                named_sync(1, kSoft);  // O of the other group, sh_ml and misc[2] are read
+            }
+        } while (k.next(a));
+        }
+    }
+    // ---------------------------------------------------------------- teardown
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 8)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols));
+}
+
+PFN_cuTensorMapEncodeTiled_v12000 encode_tiled()
+{
+    static std::once_flag once;
+    static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+    std::call_once(once, [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+    });
+    return fn;
+}
+
+// q as [T][H][128] with its token stride; a box is 64 dims x the heads of a group x TQ tokens.
+cudaError_t make_q_map(const ChunkArgs& a, CUtensorMap* map)
+{
+    PFN_cuTensorMapEncodeTiled_v12000 enc = encode_tiled();
+    if (!enc) return cudaErrorNotSupported;
+    const cuuint64_t dim[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)a.H, (cuuint64_t)a.T};
+    const cuuint64_t stride[2] = {(cuuint64_t)kRowBytes, (cuuint64_t)a.q_stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)a.G, (cuuint32_t)(kTile / a.G)};
+    const cuuint32_t elem[3] = {1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<uint16_t*>(a.q), dim, stride, box, elem,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? cudaSuccess
+               : cudaErrorInvalidValue;
+}
+
+template <bool F16>
+cudaError_t launch_attn(const ChunkArgs& a, const ChunkMaps& maps, const ChunkWork& w, int nctas, cudaStream_t st)
+{
+    const cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel<F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(chunk_attn_kernel<F16>, nctas, kThreads, kSmemBytes, st, a, maps, w);
 }
 
 }  // namespace
 
-int64_t chunk_workspace_bytes() { return 256; }
+int64_t chunk_workspace_bytes() { return kWorkBytes; }
 
-cudaError_t launch_chunk(const ChunkArgs& a, cudaStream_t st)
+cudaError_t launch_chunk(const ChunkArgs& a, bool short_boxes, cudaStream_t st)
 {
-    if (a.k_new) {
-        chunk_append_kernel<<<(unsigned)(((int64_t)a.T * a.Hkv + 15) / 16), 256, 0, st>>>(a);
-        const cudaError_t e = cudaGetLastError();
-        if (e != cudaSuccess) return e;
-    }
-    const unsigned grid = (unsigned)(((int64_t)a.T * a.H + 7) / 8);
-    if (a.fp16)
-        chunk_rows_kernel<true><<<grid, 256, 0, st>>>(a);
-    else
-        chunk_rows_kernel<false><<<grid, 256, 0, st>>>(a);
-    return cudaGetLastError();
+    int dev = 0, sms = 0;
+    cudaError_t e;
+    if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
+    if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
+    const int nctas = sms < kMaxCtas ? sms : kMaxCtas;
+    ChunkMaps maps;
+    if ((e = make_cache_maps(a.Kp, a.Vp, (int64_t)a.num_pages * a.P, &maps.cache, short_boxes, a.P, false)) != cudaSuccess) return e;
+    if ((e = make_q_map(a, &maps.q)) != cudaSuccess) return e;
+    unsigned char* base = static_cast<unsigned char*>(a.work);
+    ChunkWork w;
+    w.head = reinterpret_cast<ChunkHead*>(base);
+    w.start = reinterpret_cast<int4*>(base + kOffStart);
+    w.done = reinterpret_cast<int32_t*>(base + kOffDone);
+    w.ml = reinterpret_cast<float2*>(base + kOffPieceMl);
+    w.o = reinterpret_cast<float*>(base + kOffPieceO);
+    const int64_t rows = a.k_new ? (int64_t)a.T * a.Hkv : 0;
+    const int blocks = 1 + (int)((rows + kProThreads / 16 - 1) / (kProThreads / 16));
+    if ((e = launch_pdl(chunk_prologue_kernel, blocks, kProThreads, 0, st, a, w, nctas)) != cudaSuccess) return e;
+    return a.fp16 ? launch_attn<true>(a, maps, w, nctas, st) : launch_attn<false>(a, maps, w, nctas, st);
 }
 
 }  // namespace dkv

@@ -92,6 +92,8 @@ struct ChunkArgs {
     float qscale;           // softmax scale * log2(e)
 };
 int64_t chunk_workspace_bytes();
-cudaError_t launch_chunk(const ChunkArgs& a, cudaStream_t st);
+// short_boxes (fault injection): page copies deliver half the bytes that a stage expects,
+// inside the stage, so that every wait for them runs out.
+cudaError_t launch_chunk(const ChunkArgs& a, bool short_boxes, cudaStream_t st);
 
 }  // namespace dkv

@@ -20,12 +20,18 @@ dkv_status refuse(const char* fmt, ...)
     return dkv::set_error(DKV_ERR_INVALID_ARG, msg);
 }
 
-// DKV_FAULT=launch: launches report failure, as for the other entry points.
+// DKV_FAULT as for the other entry points: "launch" makes launches report failure, "copy" makes
+// every wait for a page copy of dkv_chunk_attn run out.
+bool fault(const char* what)
+{
+    const char* f = std::getenv("DKV_FAULT");
+    return f && std::strcmp(f, what) == 0;
+}
+
 dkv_status launched(cudaError_t e, const char* where)
 {
     char msg[256];
-    const char* f = std::getenv("DKV_FAULT");
-    if (f && std::strcmp(f, "launch") == 0) {
+    if (fault("launch")) {
         snprintf(msg, sizeof msg, "%s: injected launch failure", where);
         return dkv::set_error(DKV_ERR_CUDA, msg);
     }
@@ -251,7 +257,7 @@ dkv_status dkv_chunk_attn(const dkv_pages* g, int32_t layer, int32_t dtype, int3
     a.fp16 = dtype == DKV_FP16;
     const float sc = scale > 0.f ? scale : 1.0f / std::sqrt((float)dkv::kHeadDim);
     a.qscale = sc * 1.4426950408889634f;  // base-2 softmax: exp(x) = exp2(x log2 e)
-    return launched(dkv::launch_chunk(a, stream), "chunk attention kernels");
+    return launched(dkv::launch_chunk(a, fault("copy"), stream), "chunk attention kernels");
 }
 
 }  // extern "C"
