@@ -40,7 +40,7 @@ constexpr int kHalf = kTile * 128;         // one 64-dim half of a tile (16 KB)
 constexpr int kOperand = 2 * kHalf;        // a tile: dims 0-63, then 64-127
 constexpr int kStages = 5;                 // ring of K and V tiles
 constexpr int kThreads = 384;
-constexpr int kRegsSoft = 208, kRegsRest = 88;  // a thread's registers after the split; launched with 168
+constexpr int kRegsSoft = 216, kRegsRest = 72;  // a thread's registers after the split; launched with 168
 static_assert(2 * kRegsSoft + kRegsRest <= 3 * 168, "three warpgroups share what they were launched with");
 constexpr int kSoft = 256;                 // threads of the softmax groups
 constexpr int kMaxCtas = 160;              // CTAs of the largest grid (the workspace's size)
@@ -51,7 +51,7 @@ constexpr int kTmemCols = 512;             // S of group p at 128 p (P over its 
 constexpr int kOffQ = 0;
 constexpr int kOffRing = kOffQ + 2 * kOperand;
 constexpr int kOffBars = kOffRing + kStages * kOperand;
-constexpr int kNumBars = 2 * kStages + 9;  // full[], empty[], q_full, q_empty, s_full[2], p_full[2], o_done[2], fin
+constexpr int kNumBars = 2 * kStages + 11;  // full[], empty[], q_full, q_empty, s_full[2], p_half[2], p_full[2], o_done[2], fin
 constexpr int kOffMisc = kOffBars + (kNumBars + 1) / 2 * 16;  // int[4]: TMEM address, abort, last
 constexpr int kOffMl = kOffMisc + 16;                           // float2[128]: group 1's (m, l), then group 0's
 constexpr int kSmemBytes = kOffMl + 2 * kTile * 8;
@@ -68,7 +68,7 @@ struct ChunkWork {
     int4* start;      // [kMaxCtas] sequence, KV head, unit of the sequence, first tile of a CTA's share
     int32_t* done;    // [kMaxCtas] finished pieces of the unit that starts in CTA c and ends in a later one
     float2* ml;       // [kMaxCtas][2][256]
-    float* o;         // [kMaxCtas][2][256][128]
+    float4* o;        // [kMaxCtas][2][128 / 4][256]: a warp's rows side by side
 };
 constexpr int64_t kOffStart = 256, kOffDone = kOffStart + kMaxCtas * 16, kOffPieceMl = (kOffDone + kMaxCtas * 4 + 255) / 256 * 256,
                   kOffPieceO = kOffPieceMl + (int64_t)kMaxCtas * 2 * kPieceRows * 8,
@@ -341,6 +341,27 @@ __device__ __forceinline__ void zero_rows(unsigned char* v, int first, int lane)
     __syncwarp();
 }
 
+// Two fp32 values in a register pair, one instruction for both.
+__device__ __forceinline__ uint64_t pack2(float x, float y)
+{
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
+    return v;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t x, uint64_t y, uint64_t z)
+{
+    uint64_t v;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(x), "l"(y), "l"(z));
+    return v;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t x, uint64_t y)
+{
+    uint64_t v;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(x), "l"(y));
+    return v;
+}
+
 // P of a score s is 2^(s c - origin(m, c)).
 template <bool F16>
 __device__ __forceinline__ float origin(float m, float c)
@@ -356,7 +377,7 @@ __device__ __forceinline__ float origin(float m, float c)
 // whether it holds anything): P stays below 2^kSlack. fp16 P is scaled by 2^7 more, which l shares: the
 // smallest normal P is then 2^-21 of the largest score's.
 template <bool F16>
-__device__ __forceinline__ void softmax_step(uint32_t s, uint32_t o, int lim, bool rescale, float c, float& m, float& l)
+__device__ __forceinline__ void softmax_step(uint32_t s, uint32_t o, int lim, bool rescale, float c, float& m, float& l, uint32_t half_bar)
 {
     uint32_t x[4][32];
 #pragma unroll
@@ -371,11 +392,15 @@ __device__ __forceinline__ void softmax_step(uint32_t s, uint32_t o, int lim, bo
             for (int e = 0; e < 32; ++e)
                 if (32 * k + e >= lim) x[k][e] = 0xff800000u;  // -inf: also over NaN
     }
-    float mx = -INFINITY;
+    // Two warps share a scheduler, so the step is latency: independent chains for max and sum.
+    float mxs[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mxs[e] = -INFINITY;
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int e = 0; e < 32; ++e) mx = fmaxf(mx, __uint_as_float(x[k][e]));
+        for (int e = 0; e < 32; ++e) mxs[e & 7] = fmaxf(mxs[e & 7], __uint_as_float(x[k][e]));
+    const float mx = fmaxf(fmaxf(fmaxf(mxs[0], mxs[1]), fmaxf(mxs[2], mxs[3])), fmaxf(fmaxf(mxs[4], mxs[5]), fmaxf(mxs[6], mxs[7])));
     const bool move = (mx - m) * c > kSlack;
     if (__any_sync(kFull, move)) {
         const float alpha = move ? ex2((m - mx) * c) : 1.f;
@@ -395,20 +420,31 @@ __device__ __forceinline__ void softmax_step(uint32_t s, uint32_t o, int lim, bo
         }
     }
     const float mc = origin<F16>(m, c);
-    float sum = 0.f;
+    const uint64_t c2 = pack2(c, c), o2 = pack2(-mc, -mc);
+    uint64_t sum[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         uint32_t p[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            const float p0 = ex2(fmaf(__uint_as_float(x[k][2 * e]), c, -mc));
-            const float p1 = ex2(fmaf(__uint_as_float(x[k][2 * e + 1]), c, -mc));
-            sum += p0 + p1;
+            float p0, p1;
+            unpack2(fma2(pack2(__uint_as_float(x[k][2 * e]), __uint_as_float(x[k][2 * e + 1])), c2, o2), p0, p1);
+            p0 = ex2(p0);
+            p1 = ex2(p1);
+            sum[e & 3] = add2(sum[e & 3], pack2(p0, p1));
             p[e] = pack16<F16>(p0, p1);
         }
         tmem_st16_async(s + 16 * k, p);
+        if (k == 1) {
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0) mbar_arrive(half_bar);
+        }
     }
-    l += sum;
+    float s0, s1;
+    unpack2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), s0, s1);
+    l += s0 + s1;
     tmem_wait_st();
 }
 
@@ -427,11 +463,11 @@ __device__ __forceinline__ void store_out(uint16_t* row, const float (&v)[32], f
     }
 }
 
-__device__ __forceinline__ void store_piece(float* row, const float (&v)[32])
+// Elements 32 k .. 32 k + 31 of a row of a piece (at: its element 32 k).
+__device__ __forceinline__ void store_piece(float4* at, const float (&v)[32])
 {
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-        __stcg(reinterpret_cast<float4*>(row) + k, make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]));
+    for (int k = 0; k < 8; ++k) __stcg(at + k * kPieceRows, make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]));
 }
 
 // 1 / l; a sum of 0 (no rows) gives 0, NaN stays.
@@ -458,7 +494,7 @@ __device__ __forceinline__ int64_t pool_row(const ChunkArgs& a, int h, int r)
 // once, 8 lanes and 16 dims a lane each.
 template <bool F16>
 __device__ __forceinline__ void mend_rows(const ChunkArgs& a, int h, bool odd, int first, int lim, int end, float mc, float z,
-                                          const uint16_t* q, uint16_t* out, float* piece, int d0, int nd)
+                                          const uint16_t* q, uint16_t* out, float4* piece, int d0, int nd)
 {
     const int lane = threadIdx.x & 31, sub = lane & 7, dim = 16 * sub;
     const bool mine = dim >= d0 && dim < d0 + nd;
@@ -472,7 +508,7 @@ __device__ __forceinline__ void mend_rows(const ChunkArgs& a, int h, bool odd, i
         const float m1 = __shfl_sync(kFull, mc, src), z1 = __shfl_sync(kFull, z, src);
         const uint16_t* q1 = reinterpret_cast<const uint16_t*>(__shfl_sync(kFull, reinterpret_cast<unsigned long long>(q), src));
         uint16_t* out1 = reinterpret_cast<uint16_t*>(__shfl_sync(kFull, reinterpret_cast<unsigned long long>(out), src));
-        float* piece1 = reinterpret_cast<float*>(__shfl_sync(kFull, reinterpret_cast<unsigned long long>(piece), src));
+        float4* piece1 = reinterpret_cast<float4*>(__shfl_sync(kFull, reinterpret_cast<unsigned long long>(piece), src));
         float spoilt = 0.f;
 #pragma unroll 1
         for (int r = max(L, first) + (lane >> 3); r < end; r += 4) {
@@ -522,7 +558,7 @@ __device__ __forceinline__ void mend_rows(const ChunkArgs& a, int h, bool odd, i
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 if (piece1)
-                    __stcg(reinterpret_cast<float2*>(piece1 + dim) + e, make_float2(o[2 * e], o[2 * e + 1]));
+                    __stcg(reinterpret_cast<float2*>(piece1 + (dim / 4 + e / 2) * kPieceRows) + (e & 1), make_float2(o[2 * e], o[2 * e + 1]));
                 else
                     reinterpret_cast<uint32_t*>(out1 + dim)[e] = pack16<F16>(o[2 * e] * z1, o[2 * e + 1] * z1);
             }
@@ -531,40 +567,62 @@ __device__ __forceinline__ void mend_rows(const ChunkArgs& a, int h, bool odd, i
     }
 }
 
-// The last piece's CTA joins the pieces of a unit, in the order of the CTAs: one warp a row.
+// The last piece's CTA joins the pieces of a unit, in the order of the CTAs. `scale` (shared):
+// each row's max and 1 / sum over the pieces.
 template <bool F16>
-__device__ __forceinline__ void join_pieces(const ChunkArgs& a, const ChunkWork& w, int t0, int tokens, int g, int c0, int pieces)
+__device__ __forceinline__ void join_pieces(const ChunkArgs& a, const ChunkWork& w, float2* scale, int t0, int tokens, int g, int c0, int pieces)
 {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, TQ = kTile / a.G, rows = tokens * a.G;
+    const int tid = threadIdx.x, lane = tid & 31, TQ = kTile / a.G, rows = tokens * a.G, low = TQ * a.G;
     const float c = a.qscale;
+    auto piece = [c0](int k) { return (int64_t)(c0 + k) * 2 + (k == 0); };
+    auto place = [low](int x) { return x < low ? x : x - low + kTile; };
+    // A warp a row with few rows (then the pieces may be many), a thread a row else.
+    const bool few = rows <= 64;
 #pragma unroll 1
-    for (int x = warp; x < rows; x += kSoft / 32) {
-        const int token = x / a.G, j = x - token * a.G;
-        const int r = token >= TQ ? kTile + (token - TQ) * a.G + j : x;
-        float M = -INFINITY;
-#pragma unroll 1
-        for (int k = lane; k < pieces; k += 32)
-            M = fmaxf(M, __ldcg(w.ml + ((int64_t)(c0 + k) * 2 + (k == 0)) * kPieceRows + r).x);
+    for (int x = few ? tid >> 5 : tid; x < rows; x += few ? kSoft / 32 : kSoft) {
+        float M = -INFINITY, L = 0.f;
+#pragma unroll 2
+        for (int k = few ? lane : 0; k < pieces; k += few ? 32 : 1) {
+            const float2 ml = __ldcg(w.ml + piece(k) * kPieceRows + place(x));
+            if (ml.x == -INFINITY && ml.y == 0.f) continue;  // a piece that the row does not see
+            const float M1 = fmaxf(M, ml.x);
+            L = L * (M == -INFINITY ? 0.f : ex2((M - M1) * c)) + ml.y * (ml.x == -INFINITY ? 0.f : ex2((ml.x - M1) * c));
+            M = M1;
+        }
+        if (few) {
+            float M1 = M;
 #pragma unroll
-        for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(kFull, M, o));
-        float L = 0.f;
-        float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int o = 16; o >= 1; o >>= 1) M1 = fmaxf(M1, __shfl_xor_sync(kFull, M1, o));
+            L *= M == -INFINITY && L == 0.f ? 0.f : ex2((M - M1) * c);
+            M = M1;
+#pragma unroll
+            for (int o = 16; o >= 1; o >>= 1) L += __shfl_xor_sync(kFull, L, o);
+        }
+        if (!few || lane == 0) scale[x] = make_float2(M, inverse(L));
+    }
+    named_sync(1, kSoft);
+    // Eight elements of a row a thread, neighbouring rows in neighbouring lanes.
+#pragma unroll 1
+    for (int i = tid; i < rows * (kHeadDim / 8); i += kSoft) {
+        const int ch = i / rows, x = i - ch * rows, r = place(x);
+        const float2 mz = scale[x];
+        float4 A = make_float4(0.f, 0.f, 0.f, 0.f), B = A;
 #pragma unroll 4
         for (int k = 0; k < pieces; ++k) {
-            const int64_t at = ((int64_t)(c0 + k) * 2 + (k == 0)) * kPieceRows + r;
-            const float2 ml = __ldcg(w.ml + at);
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(w.o + at * kHeadDim) + lane);
-            const float f = ml.x == -INFINITY ? 0.f : ex2((ml.x - M) * c);
-            if (ml.y == 0.f) continue;
-            L = fmaf(ml.y, f, L);
-            O.x = fmaf(v.x, f, O.x);
-            O.y = fmaf(v.y, f, O.y);
-            O.z = fmaf(v.z, f, O.z);
-            O.w = fmaf(v.w, f, O.w);
+            const float2 ml = __ldcg(w.ml + piece(k) * kPieceRows + r);
+            const float4* o = w.o + (piece(k) * (kHeadDim / 4) + 2 * ch) * kPieceRows + r;
+            const float4 u = __ldcg(o), v = __ldcg(o + kPieceRows);
+            const bool none = ml.x == -INFINITY && ml.y == 0.f;
+            const float f = none ? 0.f : ex2((ml.x - mz.x) * c);
+            if (none) continue;
+            A = make_float4(fmaf(u.x, f, A.x), fmaf(u.y, f, A.y), fmaf(u.z, f, A.z), fmaf(u.w, f, A.w));
+            B = make_float4(fmaf(v.x, f, B.x), fmaf(v.y, f, B.y), fmaf(v.z, f, B.z), fmaf(v.w, f, B.w));
         }
-        const float z = inverse(L);
-        uint16_t* out = a.out + ((int64_t)(t0 + token) * a.H + g * a.G + j) * kHeadDim + 4 * lane;
-        *reinterpret_cast<uint2*>(out) = make_uint2(pack16<F16>(O.x * z, O.y * z), pack16<F16>(O.z * z, O.w * z));
+        const int token = x / a.G, j = x - token * a.G;
+        const float z = mz.y;
+        *reinterpret_cast<uint4*>(a.out + ((int64_t)(t0 + token) * a.H + g * a.G + j) * kHeadDim + 8 * ch) =
+            make_uint4(pack16<F16>(A.x * z, A.y * z), pack16<F16>(A.z * z, A.w * z), pack16<F16>(B.x * z, B.y * z),
+                       pack16<F16>(B.z * z, B.w * z));
     }
 }
 
@@ -582,7 +640,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint64_t* q_full = empty + kStages;                            // the unit's Q tiles landed
     uint64_t* q_empty = q_full + 1;                                // the unit's score products are done
     uint64_t* s_full = q_empty + 1;                                // [2] S of the group's next step is done
-    uint64_t* p_full = s_full + 2;                                 // [2] its P is written
+    uint64_t* p_half = s_full + 2;                                 // [2] the first half of its P is written
+    uint64_t* p_full = p_half + 2;                                 // [2] all of it
     uint64_t* o_done = p_full + 2;                                 // [2] the group's last product of the unit is done
     uint64_t* fin = o_done + 2;                                    // drain after a timeout
     volatile int* misc = reinterpret_cast<volatile int*>(sm + kOffMisc);
@@ -596,7 +655,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     if (tid == 0) {
         misc[1] = 0;
-        for (int i = 0; i < kNumBars; ++i) mbar_init(smem_u32(full + i), full + i == p_full || full + i == p_full + 1 ? 4 : 1);
+        for (int i = 0; i < kNumBars; ++i) mbar_init(smem_u32(full + i), full + i >= p_half && full + i < p_full + 2 ? 4 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_proxy_async_smem();
     }
@@ -703,13 +762,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const int valid = max(k.u.kv - k.tile(x) * kTile, 0);
                         if (valid < kTile) zero_rows(sm + kOffRing + curV * kOperand, valid, lane);
                     }
+                    if (!wait(&p_half[p], (phases >> p) & 1)) break;
+                    tc_fence_after();
+                    const uint32_t v = dV + curV * (kOperand >> 4), o = tmem + 256 + p * kTile, pt = tmem + p * kTile;
+                    if (leads) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) umma_ts(o, pt + 8 * e, desc(v + e * (2048 >> 4)), id_o, x > 1 || e > 0);
+                    }
+                    __syncwarp();
                     if (!wait(&p_full[p], (phases >> p) & 1)) break;
                     phases ^= 1u << p;
                     tc_fence_after();
                     if (leads) {
-                        const uint32_t v = dV + curV * (kOperand >> 4), o = tmem + 256 + p * kTile, pt = tmem + p * kTile;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) umma_ts(o, pt + 8 * e, desc(v + e * (2048 >> 4)), id_o, x > 1 || e > 0);
+                        for (int e = 4; e < 8; ++e) umma_ts(o, pt + 8 * e, desc(v + e * (2048 >> 4)), id_o, x > 1 || e > 0);
                         if (!pair || p == 1) umma_commit(smem_u32(&empty[curV]));
                         if (x + 2 >= steps) umma_commit(smem_u32(&o_done[p]));
                     }
@@ -771,8 +837,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int s = p; s < steps; s += 2) {
                 if (wait(&s_full[p], ns & 1) && any) {
                     tc_fence_after();
-                    softmax_step<F16>(s_at, o_at + p * kTile, lim - k.tile(s) * kTile, s > 1, cs, m, l);
+                    softmax_step<F16>(s_at, o_at + p * kTile, lim - k.tile(s) * kTile, s > 1, cs, m, l, smem_u32(&p_half[p]));
                     tc_fence_before();
+                } else if (lane == 0) {
+                    mbar_arrive(smem_u32(&p_half[p]));
                 }
                 ++ns;
                 __syncwarp();
@@ -784,12 +852,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             tc_fence_after();
             uint16_t* out = a.out + ((int64_t)(k.u.t0 + tok) * a.H + k.g * a.G + j) * kHeadDim;
-            const int64_t piece = ((int64_t)c * 2 + (k.j0 == 0)) * kPieceRows + (pair ? p * kTile : 0) + r;
+            const int64_t slot = (int64_t)c * 2 + (k.j0 == 0);
+            const int prow = (pair ? p * kTile : 0) + r;
             // Cache rows of this piece, and whether some of them are hidden from the thread's query.
             const int first = k.j0 * kTile, end = min(k.u.kv, k.j1 * kTile);
             const bool hidden = live && lim < end;
             const uint16_t* q = a.q + (int64_t)(k.u.t0 + tok) * a.q_stride + (k.g * a.G + j) * kHeadDim;
-            float* o_piece = whole ? nullptr : w.o + piece * kHeadDim;
+            float4* o_piece = whole ? nullptr : w.o + slot * (kHeadDim / 4) * kPieceRows + prow;
             float odd = 0.f;  // NaN if a result is not finite
             if (pair) {
                 if (any && wait.ok) {
@@ -801,11 +870,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                         for (int d = 0; d < 32; ++d) odd = fmaf(v[d], 0.f, odd);
                         if (live && whole) store_out<F16>(out + 32 * e, v, z);
-                        if (live && !whole) store_piece(o_piece + 32 * e, v);
+                        if (live && !whole) store_piece(o_piece + 8 * e * kPieceRows, v);
                     }
                     if (__any_sync(kFull, hidden && odd != odd))
                         mend_rows<F16>(a, k.u.h, hidden && odd != odd, first, lim, end, origin<F16>(m, cs), z, q, out, o_piece, 0, kHeadDim);
-                    if (live && !whole) __stcg(w.ml + piece, make_float2(m, l));
+                    if (live && !whole) __stcg(w.ml + slot * kPieceRows + prow, make_float2(m, l));
                 }
             } else {
                 // The groups' halves of the cache rows: each group joins 64 of the dimensions.
@@ -830,11 +899,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                             odd = fmaf(v[d], 0.f, odd);
                         }
                         if (live && whole) store_out<F16>(out + 32 * e, v, z);
-                        if (live && !whole) store_piece(o_piece + 32 * e, v);
+                        if (live && !whole) store_piece(o_piece + 8 * e * kPieceRows, v);
                     }
                     if (__any_sync(kFull, hidden && odd != odd))
                         mend_rows<F16>(a, k.u.h, hidden && odd != odd, first, lim, end, origin<F16>(M, cs), z, q, out, o_piece, 64 * p, 64);
-                    if (live && !whole && p == 0) __stcg(w.ml + piece, make_float2(M, L));
+                    if (live && !whole && p == 0) __stcg(w.ml + slot * kPieceRows + prow, make_float2(M, L));
                 }
             }
             if (!whole) {
@@ -845,7 +914,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 named_sync(1, kSoft);
                 if (misc[2]) {
                     __threadfence();
-                    join_pieces<F16>(a, w, k.u.t0, k.u.tokens, k.g, c0, pieces);
+                    join_pieces<F16>(a, w, sh_ml, k.u.t0, k.u.tokens, k.g, c0, pieces);
                 }
             }
             if (!pair || !whole) {
@@ -921,7 +990,7 @@ cudaError_t launch_chunk(const ChunkArgs& a, bool short_boxes, cudaStream_t st)
     w.start = reinterpret_cast<int4*>(base + kOffStart);
     w.done = reinterpret_cast<int32_t*>(base + kOffDone);
     w.ml = reinterpret_cast<float2*>(base + kOffPieceMl);
-    w.o = reinterpret_cast<float*>(base + kOffPieceO);
+    w.o = reinterpret_cast<float4*>(base + kOffPieceO);
     const int64_t rows = a.k_new ? (int64_t)a.T * a.Hkv : 0;
     const int blocks = 1 + (int)((rows + kProThreads / 16 - 1) / (kProThreads / 16));
     if ((e = launch_pdl(chunk_prologue_kernel, blocks, kProThreads, 0, st, a, w, nctas)) != cudaSuccess) return e;
