@@ -58,19 +58,21 @@ constexpr int kSmemBytes = kOffMl + 2 * kTile * 8;
 static_assert(kSmemBytes <= 227 * 1024, "fits one CTA");
 
 // Workspace.
-struct ChunkHead {
-    int64_t tiles;  // of all units
-    int32_t parts;  // CTAs with a share
-    int32_t pad;
+struct alignas(16) ChunkStart {  // a CTA's share
+    int64_t tiles;   // of the whole call
+    int32_t parts;   // CTAs with a share; 0 tiles: none, and nothing else is set
+    int32_t b, g, i, first;  // sequence, KV head, unit of the sequence, and its first tile in the share
+    int32_t t, n, len;       // the sequence's first token and tokens, rows of the slab
+    int32_t pad[2];
 };
+static_assert(sizeof(ChunkStart) == 48, "three 16-byte loads");
 struct ChunkWork {
-    ChunkHead* head;
-    int4* start;      // [kMaxCtas] sequence, KV head, unit of the sequence, first tile of a CTA's share
-    int32_t* done;    // [kMaxCtas] finished pieces of the unit that starts in CTA c and ends in a later one
-    float2* ml;       // [kMaxCtas][2][256]
-    float4* o;        // [kMaxCtas][2][128 / 4][256]: a warp's rows side by side
+    ChunkStart* start;  // [kMaxCtas]
+    int32_t* done;      // [kMaxCtas] finished pieces of the unit that starts in CTA c and ends in a later one
+    float2* ml;         // [kMaxCtas][2][256]
+    float4* o;          // [kMaxCtas][2][128 / 4][256]: a warp's rows side by side
 };
-constexpr int64_t kOffStart = 256, kOffDone = kOffStart + kMaxCtas * 16, kOffPieceMl = (kOffDone + kMaxCtas * 4 + 255) / 256 * 256,
+constexpr int64_t kOffDone = kMaxCtas * sizeof(ChunkStart), kOffPieceMl = (kOffDone + kMaxCtas * 4 + 255) / 256 * 256,
                   kOffPieceO = kOffPieceMl + (int64_t)kMaxCtas * 2 * kPieceRows * 8,
                   kWorkBytes = kOffPieceO + (int64_t)kMaxCtas * 2 * kPieceRows * kHeadDim * 4;
 
@@ -118,26 +120,23 @@ struct Walk {
     int b, g, i, t, n, j0, j1, tiles;
     int64_t pos, end;  // tiles of the whole call: the current piece's first, the share's end
     Unit u;
-    __device__ __forceinline__ void load(const ChunkArgs& a, int off)
+    __device__ __forceinline__ void enter(const ChunkArgs& a, int len, int off)
     {
-        t = cu_at(a, b);
-        n = cu_at(a, b + 1) - t;
-        const int h = b * a.Hkv + g;
-        u = make_unit(a, h, t, n, slab_len(a, h), i);
+        u = make_unit(a, b * a.Hkv + g, t, n, len, i);
         tiles = u.tiles();
         j0 = off;
         j1 = (int)min((int64_t)tiles, off + (end - pos));
     }
-    // parts: CTAs with a share (c < parts).
-    __device__ __forceinline__ void begin(const ChunkArgs& a, const ChunkWork& w, const ChunkHead& head, int c)
+    __device__ __forceinline__ void begin(const ChunkArgs& a, const ChunkStart& s, int c)
     {
-        pos = head.tiles * c / head.parts;
-        end = head.tiles * (c + 1) / head.parts;
-        const int4 s = __ldcg(w.start + c);
-        b = s.x;
-        g = s.y;
-        i = s.z;
-        load(a, s.w);
+        pos = s.tiles * c / s.parts;
+        end = s.tiles * (c + 1) / s.parts;
+        b = s.b;
+        g = s.g;
+        i = s.i;
+        t = s.t;
+        n = s.n;
+        enter(a, s.len, s.first);
     }
     __device__ __forceinline__ bool next(const ChunkArgs& a)
     {
@@ -149,9 +148,11 @@ struct Walk {
                 g = 0;
                 do ++b;
                 while (b < a.B - 1 && cu_at(a, b + 1) <= cu_at(a, b));
+                t = cu_at(a, b);
+                n = cu_at(a, b + 1) - t;
             }
         }
-        load(a, 0);
+        enter(a, slab_len(a, b * a.Hkv + g), 0);
         return true;
     }
     __device__ __forceinline__ bool whole() const { return j0 == 0 && j1 == tiles; }
@@ -160,7 +161,7 @@ struct Walk {
 };
 
 // The CTA whose share holds tile x of the call.
-__device__ __forceinline__ int cta_of(const ChunkHead& h, int64_t x) { return (int)(((x + 1) * h.parts - 1) / h.tiles); }
+__device__ __forceinline__ int cta_of(const ChunkStart& s, int64_t x) { return (int)(((x + 1) * s.parts - 1) / s.tiles); }
 
 // ---------------------------------------------------------------- append and schedule
 constexpr int kProThreads = 512;
@@ -193,102 +194,113 @@ __device__ __forceinline__ void report(const ChunkArgs& a, int bits)
     if (a.status) atomicOr(a.status, bits);
 }
 
-// One block: the tiles of every unit, and where each CTA's share starts.
-__device__ __forceinline__ void schedule(const ChunkArgs& a, const ChunkWork& w, int nctas)
+constexpr int kMaxSlabs = 4096;  // of a layer, whose prefix sums fit shared memory; more are summed in groups
+
+// One block: the tiles of every slab, and where each CTA's share starts.
+__device__ __forceinline__ void schedule(const ChunkArgs& a, const ChunkWork& w, const int32_t* cu, int nctas)
 {
     __shared__ int64_t sh[kProThreads / 32];
-    __shared__ int32_t first[kMaxSlots + 1];  // units of the sequences before
-    const int tid = threadIdx.x, width = 2 * (kTile / a.G);
+    __shared__ int64_t before[kMaxSlabs];  // tiles of the groups of slabs before
+    const int tid = threadIdx.x, width = 2 * (kTile / a.G), slabs = a.B * a.Hkv;
+    const int group = (slabs + kMaxSlabs - 1) / kMaxSlabs, groups = (slabs + group - 1) / group;
     for (int c = tid; c < kMaxCtas; c += kProThreads) w.done[c] = 0;
-    static_assert(kMaxSlots <= kProThreads, "one thread a sequence");
-    int mine = 0;
     if (tid < a.B) {
         const int t0 = a.cu[tid], t1 = a.cu[tid + 1];
         if (t0 < 0 || t1 < t0 || t1 > a.T || (tid == 0 && t0 != 0)) report(a, DKV_DEV_PAGE_RANGE);
-        mine = (max(cu_at(a, tid + 1) - cu_at(a, tid), 0) + width - 1) / width * a.Hkv;
     }
-    int64_t units;
-    const int64_t before = scan_block(mine, sh, &units);
-    if (tid < a.B) first[tid] = (int)before;
-    if (tid == 0) first[a.B] = (int)units;
+    auto slab_tiles = [&](int h, int& t, int& n, int& len) -> int64_t {
+        const int b = h / a.Hkv, raw = a.len[h];
+        t = cu[b];
+        n = max(cu[b + 1] - t, 0);
+        len = slab_len(a, h);
+        if (n > 0 && (raw != len || (a.k_new && raw < n))) report(a, DKV_DEV_PAGE_RANGE);
+        int64_t sum = 0;
+#pragma unroll 1
+        for (int i = 0; i * width < n; ++i) sum += make_unit(a, h, t, n, len, i).tiles();
+        return sum;
+    };
+    // A contiguous piece of the groups a thread.
+    const int per = (groups + kProThreads - 1) / kProThreads, g0 = min(groups, tid * per), g1 = min(groups, g0 + per);
+    int64_t mine = 0;
+    int t, n, len;
+#pragma unroll 1
+    for (int x = g0; x < g1; ++x) {
+        before[x] = mine;
+#pragma unroll 1
+        for (int h = x * group; h < min(slabs, (x + 1) * group); ++h) mine += slab_tiles(h, t, n, len);
+    }
+    int64_t total;
+    const int64_t base = scan_block(mine, sh, &total);
+#pragma unroll 1
+    for (int x = g0; x < g1; ++x) before[x] += base;
     __syncthreads();
-    const int64_t per = (units + kProThreads - 1) / kProThreads;
-    const int64_t u0 = min(units, tid * per), u1 = min(units, u0 + per);
-    int b = 0;
-    {
-        int lo = 0, hi = a.B - 1;  // the last sequence with first <= u0 (it has units)
+    const int parts = (int)min(total, (int64_t)nctas);
+    if (tid >= nctas) return;
+    ChunkStart s{total, parts};
+    if (tid < parts) {
+        const int64_t at = total * tid / parts;
+        int lo = 0, hi = groups - 1;  // the last group that starts at tile `at` or before (it has tiles)
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if (first[mid] <= u0)
+            if (before[mid] <= at)
                 lo = mid;
             else
                 hi = mid - 1;
         }
-        b = lo;
+        int64_t off = at - before[lo];
+        int h = lo * group;
+        if (group > 1)
+            for (int64_t x = slab_tiles(h, t, n, len); off >= x; x = slab_tiles(++h, t, n, len)) off -= x;
+        s.b = h / a.Hkv;
+        s.g = h - s.b * a.Hkv;
+        s.t = cu[s.b];
+        s.n = max(cu[s.b + 1] - s.t, 0);
+        s.len = slab_len(a, h);
+#pragma unroll 1
+        for (int x; off >= (x = make_unit(a, h, s.t, s.n, s.len, s.i).tiles()); ++s.i) off -= x;
+        s.first = (int)off;
     }
-    int64_t pos = 0, parts = 0, total = 0;
-#pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {
-        int64_t sum = 0;
-        int bb = b;
-#pragma unroll 1
-        for (int64_t x = u0; x < u1; ++x) {
-            while (first[bb + 1] <= x) ++bb;
-            const int t = cu_at(a, bb), n = cu_at(a, bb + 1) - t, nq = (n + width - 1) / width;
-            const int k = (int)(x - first[bb]), g = k / nq, i = k - g * nq, h = bb * a.Hkv + g;
-            if (pass == 0 && i == 0 && (a.len[h] < n || a.len[h] != slab_len(a, h)) && (a.k_new || a.len[h] != slab_len(a, h)))
-                report(a, DKV_DEV_PAGE_RANGE);
-            const int tiles = make_unit(a, h, t, n, slab_len(a, h), i).tiles();
-            if (pass == 1) {
-                const int64_t s = pos + sum, e = s + tiles;
-#pragma unroll 1
-                for (int64_t c = (s * parts + total - 1) / total; c < parts; ++c) {
-                    const int64_t at = total * c / parts;
-                    if (at >= e) break;
-                    if (at >= s) w.start[c] = make_int4(bb, g, i, (int)(at - s));
-                }
-            }
-            sum += tiles;
-        }
-        if (pass == 0) {
-            pos = scan_block(sum, sh, &total);
-            parts = min(total, (int64_t)nctas);
-        }
-    }
-    if (tid == 0) *w.head = ChunkHead{total, (int)parts, 0};
+    w.start[tid] = s;
 }
 
-__global__ void __launch_bounds__(kProThreads) chunk_prologue_kernel(const __grid_constant__ ChunkArgs a, const ChunkWork w, int nctas)
+__global__ void __launch_bounds__(kProThreads) chunk_prologue_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkWork w, int nctas)
 {
+    __shared__ int32_t cu[kMaxSlots + 1];
+    static_assert(kMaxSlots <= kProThreads && kMaxCtas <= kProThreads, "one thread each");
     pdl_wait();
     pdl_launch_dependents();
+    if (threadIdx.x < a.B) cu[threadIdx.x] = cu_at(a, threadIdx.x);
+    if (threadIdx.x == 0) cu[a.B] = cu_at(a, a.B);
+    __syncthreads();
     if (blockIdx.x == 0) {
-        schedule(a, w, nctas);
+        schedule(a, w, cu, nctas);
         return;
     }
     // Append: a half-warp a row (K and V).
     const int64_t i = (int64_t)(blockIdx.x - 1) * (kProThreads / 16) + (threadIdx.x >> 4);
     const int sub = threadIdx.x & 15, t = (int)(i / a.Hkv), g = (int)(i - (int64_t)t * a.Hkv);
-    if (t >= cu_at(a, a.B)) return;
+    if (t >= cu[a.B]) return;
+    const int64_t src = t * a.kv_stride + g * kHeadDim;
+    const uint4 kv = __ldcs(reinterpret_cast<const uint4*>(a.k_new + src) + sub), vv = __ldcs(reinterpret_cast<const uint4*>(a.v_new + src) + sub);
     int lo = 0, hi = a.B - 1;  // the last sequence that starts at t or before
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (cu_at(a, mid) <= t)
+        if (cu[mid] <= t)
             lo = mid;
         else
             hi = mid - 1;
     }
     const int h = lo * a.Hkv + g;
-    const int64_t r = (int64_t)a.len[h] - cu_at(a, lo + 1) + t;
+    const int64_t r = (int64_t)a.len[h] - cu[lo + 1] + t;
     int page = -1;
-    if (r >= 0 && r < (int64_t)a.max_pages * a.P) page = a.table[(int64_t)h * a.max_pages + r / a.P];
+    if (r >= 0 && r < (int64_t)a.max_pages * a.P) page = a.table[(int64_t)h * a.max_pages + (int)r / a.P];
     if (page < 0 || page >= a.num_pages) {
         if (sub == 0) report(a, DKV_DEV_PAGE_RANGE);
         return;
     }
-    const int64_t row = (int64_t)page * a.P + r % a.P, src = t * a.kv_stride + g * kHeadDim;
-    reinterpret_cast<uint4*>(a.Kp + row * kHeadDim)[sub] = reinterpret_cast<const uint4*>(a.k_new + src)[sub];
-    reinterpret_cast<uint4*>(a.Vp + row * kHeadDim)[sub] = reinterpret_cast<const uint4*>(a.v_new + src)[sub];
+    const int64_t row = (int64_t)page * a.P + (int)r % a.P;
+    reinterpret_cast<uint4*>(a.Kp + row * kHeadDim)[sub] = kv;
+    reinterpret_cast<uint4*>(a.Vp + row * kHeadDim)[sub] = vv;
 }
 
 // ---------------------------------------------------------------- attention
@@ -664,7 +676,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_after();
     const uint32_t tmem = (uint32_t)uniform(misc[0]);
     pdl_wait();
-    const ChunkHead head{(int64_t)__ldcg(reinterpret_cast<const long long*>(&w.head->tiles)), __ldcg(&w.head->parts), 0};
+    union {
+        uint4 u[3];
+        ChunkStart s;
+    } given;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) given.u[i] = ld_prev(reinterpret_cast<const uint4*>(w.start + c) + i);
+    const ChunkStart& head = given.s;
     const bool work = c < head.parts;
     Waits wait{misc + 1, a.status, true};
     const int TQ = kTile / a.G;
@@ -678,7 +696,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint64_t keep;
         asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(keep));
         Walk k;
-        k.begin(a, w, head, c);
+        k.begin(a, head, c);
         int pos = 0, unit = 0;
         const int ppt = kTile / a.P;  // pages a tile
         auto load = [&](const CUtensorMap* map, int j) {
@@ -742,7 +760,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                        dV = (uint32_t)sdesc(smem_u32(sm + kOffRing), kHalf, 1024);
         auto desc = [dhi](uint32_t lo) { return ((uint64_t)dhi << 32) | lo; };
         Walk k;
-        k.begin(a, w, head, c);
+        k.begin(a, head, c);
         int pos = 0, unit = 0, curK = 0, curV = 0;
         uint32_t phases = 0;  // bit p: parity of the P tiles taken of group p
         bool issued = false;
@@ -823,7 +841,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int token = r / a.G, j = r - token * a.G;
         const float cs = a.qscale;
         Walk k;
-        k.begin(a, w, head, c);
+        k.begin(a, head, c);
         int ns = 0, no = 0;  // S tiles and O accumulators taken
         do {
             const int steps = k.steps();
@@ -965,8 +983,6 @@ cudaError_t make_q_map(const ChunkArgs& a, CUtensorMap* map)
 template <bool F16>
 cudaError_t launch_attn(const ChunkArgs& a, const ChunkMaps& maps, const ChunkWork& w, int nctas, cudaStream_t st)
 {
-    const cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel<F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-    if (e != cudaSuccess) return e;
     return launch_pdl(chunk_attn_kernel<F16>, nctas, kThreads, kSmemBytes, st, a, maps, w);
 }
 
@@ -974,20 +990,25 @@ cudaError_t launch_attn(const ChunkArgs& a, const ChunkMaps& maps, const ChunkWo
 
 int64_t chunk_workspace_bytes() { return kWorkBytes; }
 
+cudaError_t chunk_setup()
+{
+    cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(chunk_attn_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    return e;
+}
+
 cudaError_t launch_chunk(const ChunkArgs& a, bool short_boxes, cudaStream_t st)
 {
-    int dev = 0, sms = 0;
-    cudaError_t e;
-    if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
-    if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
+    int sms = 0;
+    cudaError_t e = page_setup(&sms);
+    if (e != cudaSuccess) return e;
     const int nctas = sms < kMaxCtas ? sms : kMaxCtas;
     ChunkMaps maps;
     if ((e = make_cache_maps(a.Kp, a.Vp, (int64_t)a.num_pages * a.P, &maps.cache, short_boxes, a.P, false)) != cudaSuccess) return e;
     if ((e = make_q_map(a, &maps.q)) != cudaSuccess) return e;
     unsigned char* base = static_cast<unsigned char*>(a.work);
     ChunkWork w;
-    w.head = reinterpret_cast<ChunkHead*>(base);
-    w.start = reinterpret_cast<int4*>(base + kOffStart);
+    w.start = reinterpret_cast<ChunkStart*>(base);
     w.done = reinterpret_cast<int32_t*>(base + kOffDone);
     w.ml = reinterpret_cast<float2*>(base + kOffPieceMl);
     w.o = reinterpret_cast<float4*>(base + kOffPieceO);

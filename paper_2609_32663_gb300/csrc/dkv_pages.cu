@@ -15,6 +15,9 @@
 // the free list's) and the slot map from the scan.
 #include "dkv_decode_common.cuh"
 #include "dkv_pages.cuh"
+#include "dkv_pool.cuh"
+
+#include <mutex>
 
 namespace dkv {
 namespace {
@@ -242,12 +245,38 @@ __global__ void __launch_bounds__(kPcThreads) page_compact_kernel(const PageComp
 
 }  // namespace
 
+cudaError_t page_setup(int* sms)
+{
+    struct Known {
+        unsigned long long context;
+        int sms;
+    };
+    constexpr int kMost = 64;  // contexts; later ones are looked up on every call
+    static std::mutex mu;
+    static Known known[kMost];
+    static int count = 0;
+    unsigned long long id = 0;
+    cudaError_t e = current_context_id(&id);
+    if (e != cudaSuccess) return e;
+    std::lock_guard<std::mutex> lock(mu);
+    for (int i = 0; i < count; ++i)
+        if (known[i].context == id) {
+            *sms = known[i].sms;
+            return cudaSuccess;
+        }
+    int dev = 0;
+    if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
+    if ((e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
+    if ((e = chunk_setup()) != cudaSuccess) return e;
+    if (count < kMost) known[count++] = Known{id, *sms};
+    return cudaSuccess;
+}
+
 cudaError_t launch_page_tables(const PageArgs& a, cudaStream_t st)
 {
-    int dev = 0, sms = 0;
-    cudaError_t e;
-    if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
-    if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
+    int sms = 0;
+    cudaError_t e = page_setup(&sms);
+    if (e != cudaSuccess) return e;
     if ((e = launch_pdl(page_scan_kernel, 1, kScanThreads, 0, st, a)) != cudaSuccess) return e;
     return launch_pdl(page_fill_kernel, 4 * sms, kFillThreads, 0, st, a);
 }

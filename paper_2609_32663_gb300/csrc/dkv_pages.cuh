@@ -92,6 +92,10 @@ struct ChunkArgs {
     float qscale;           // softmax scale * log2(e)
 };
 int64_t chunk_workspace_bytes();
+cudaError_t chunk_setup();  // the kernels' attributes in the current context
+// SMs of the current device; the kernels' attributes are set once a context (a lock and a
+// look-up, where the runtime calls take microseconds).
+cudaError_t page_setup(int* sms);
 // short_boxes (fault injection): page copies deliver half the bytes that a stage expects,
 // inside the stage, so that every wait for them runs out.
 cudaError_t launch_chunk(const ChunkArgs& a, bool short_boxes, cudaStream_t st);

@@ -94,7 +94,11 @@ class Pages:
     def c(self):
         return dkv_pages(self.L, self.B, self.H, self.H_kv, self.head_dim, self.page_rows, self.num_pages, self.max_pages)
 
-    @property
+    @cached_property
+    def ref(self):
+        return ctypes.byref(self.c)
+
+    @cached_property
     def slabs(self):
         return self.L * self.B * self.H_kv
 
@@ -533,26 +537,42 @@ def _bad(why):
     raise DkvError(DKV_ERR_INVALID_ARG, "argument check", why)
 
 
-def _work(workspace):
-    return _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
-
-
-def _here(*tensors):
-    """The buffers of a call lie on the current device, whose stream it runs on."""
+def _at():
+    """The current device, on whose stream a call runs and where its buffers lie."""
     T = _torch()
-    if T.torch.cuda.is_available():
-        at = T.device() if T.device is not None else T.torch.cuda.current_device()
-        for t in tensors:
-            if t is not None and not isinstance(t, int) and t.is_cuda and t.device.index != at:
-                _bad(f"a tensor lies on {t.device}, the current device is cuda:{at}")
+    if T.device is not None and T.torch.cuda.is_initialized():
+        return T.device()
+    return T.torch.cuda.current_device() if T.torch.cuda.is_available() else 0
 
 
-def _page_args(p: Pages, len, new_len, table, free_pages, free_count, new_count, workspace, status):
-    i32, n = _i32(), p.slabs
-    _here(len, new_len, table, free_pages, free_count, new_count, workspace, status)
-    return ((_dev(len, "len", i32, n), _dev(new_len, "new_len", i32, n), _dev(table, "table", i32, n * p.max_pages),
-             _dev(free_pages, "free_pages", i32, p.num_pages), _dev(free_count, "free_count", i32, 1),
-             _dev(new_count, "new_count", i32, 1)), _work(workspace), _dev(status, "status", i32, min_numel=1))
+def _on(t, name, at, dtypes, numel=None):
+    """_dev for a buffer of the paged cache, which must lie on device `at` (the look-ups of t are the binding's time)."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.get_device() == at and t.is_contiguous() and t.dtype in dtypes and (numel is None or t.numel() == numel):
+        return t.data_ptr()
+    if t.is_cuda and t.get_device() != at:
+        _bad(f"{name} lies on {t.device}, the current device is cuda:{at}")
+    return _dev(t, name, dtypes, numel)
+
+
+def _work(workspace, at):
+    if workspace.get_device() != at or not workspace.is_contiguous():
+        _bad(f"workspace must be a contiguous tensor on cuda:{at}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _word(status, at):
+    if status is not None and not isinstance(status, int) and status.numel() < 1:
+        _bad("status has no element")
+    return _on(status, "status", at, _torch().i32)
+
+
+def _page_args(p: Pages, at, len, new_len, table, free_pages, free_count, new_count, workspace, status):
+    i32, n = _torch().i32, p.slabs
+    return ((_on(len, "len", at, i32, n), _on(new_len, "new_len", at, i32, n), _on(table, "table", at, i32, n * p.max_pages),
+             _on(free_pages, "free_pages", at, i32, p.num_pages), _on(free_count, "free_count", at, i32, 1),
+             _on(new_count, "new_count", at, i32, 1)), _work(workspace, at), _word(status, at))
 
 
 def dkv_page_workspace_bytes(pages: Pages) -> int:
@@ -566,37 +586,31 @@ def dkv_page_tables(pages: Pages, len, new_len, table, free_pages, free_count, n
                     plan: Plan | None = None, seq=None, cu_tokens=None, slots=None, status=None, stream=None):
     """Pages for tokens[b] new rows of every slab of slot b, or for a plan's kept rows (its sequence i to slot seq[i]);
     slots int32 [L][max_tokens][H_kv] receives the slot map, cu_tokens int32 [B + 1] the token offsets."""
-    i32 = _i32()
-    _here(tokens, seq, cu_tokens, slots)
-    (ln, nl, tb, fp, fc, nc), (wp, wb), st = _page_args(pages, len, new_len, table, free_pages, free_count, new_count,
+    i32, at = _torch().i32, _at()
+    (ln, nl, tb, fp, fc, nc), (wp, wb), st = _page_args(pages, at, len, new_len, table, free_pages, free_count, new_count,
                                                         workspace, status)
-    if isinstance(slots, int):
-        _bad("slots must be a tensor: its size is the most tokens")
-    rows = pages.L * pages.H_kv
-    if slots is not None and slots.numel() % rows:
-        _bad(f"slots has {slots.numel()} elements, not a multiple of L*H_kv={rows}")
-    if plan is not None and seq is not None and not isinstance(seq, int) and seq.numel() != plan.B:
-        _bad(f"seq has {seq.numel()} elements, the plan {plan.B} sequences")
+    most = 0
+    if slots is not None:
+        if isinstance(slots, int):
+            _bad("slots must be a tensor: its size is the most tokens")
+        most, rest = divmod(slots.numel(), pages.L * pages.H_kv)
+        if rest:
+            _bad(f"slots has {slots.numel()} elements, not a multiple of L*H_kv={pages.L * pages.H_kv}")
     _check(lib().dkv_page_tables(
-        ctypes.byref(pages.c), _dev(tokens, "tokens", i32, pages.B), plan.address if plan is not None else None,
-        _dev(seq, "seq", i32), ln, nl, tb, fp, fc, nc, _dev(cu_tokens, "cu_tokens", i32, pages.B + 1),
-        _dev(slots, "slots", i32), 0 if slots is None else slots.numel() // rows, wp, wb, st, _stream(stream)),
+        pages.ref, _on(tokens, "tokens", at, i32, pages.B), None if plan is None else plan.address,
+        _on(seq, "seq", at, i32, None if plan is None else plan.B), ln, nl, tb, fp, fc, nc,
+        _on(cu_tokens, "cu_tokens", at, i32, pages.B + 1), _on(slots, "slots", at, i32), most, wp, wb, st, _stream(stream)),
         "dkv_page_tables")
 
 
 def dkv_page_release(pages: Pages, ended, len, new_len, table, free_pages, free_count, new_count, workspace,
                      status=None, stream=None):
     """The pages of the slots with ended[b] != 0 go back to the free list."""
-    _here(ended)
-    (ln, nl, tb, fp, fc, nc), (wp, wb), st = _page_args(pages, len, new_len, table, free_pages, free_count, new_count,
+    at = _at()
+    (ln, nl, tb, fp, fc, nc), (wp, wb), st = _page_args(pages, at, len, new_len, table, free_pages, free_count, new_count,
                                                         workspace, status)
-    _check(lib().dkv_page_release(ctypes.byref(pages.c), _dev(ended, "ended", _i32(), pages.B), ln, nl, tb, fp, fc, nc,
-                                  wp, wb, st, _stream(stream)), "dkv_page_release")
-
-
-def _rows16():
-    t = _torch()
-    return (*t.bf16, t.torch.float16)
+    _check(lib().dkv_page_release(pages.ref, _on(ended, "ended", at, _torch().i32, pages.B), ln, nl, tb, fp, fc, nc, wp, wb,
+                                  st, _stream(stream)), "dkv_page_release")
 
 
 def dkv_page_compact(pages: Pages, plan: Plan, K, V, table, len, Kp, Vp, seq=None, T_stride: int | None = None,
@@ -604,18 +618,18 @@ def dkv_page_compact(pages: Pages, plan: Plan, K, V, table, len, Kp, Vp, seq=Non
     """The kept rows of plan sequence i become the last rows of slot seq[i]'s slabs."""
     if T_stride is None:
         T_stride = K.shape[-2]
-    sh, i32, r16 = plan.shape, _i32(), _rows16()
-    plan.address
-    _here(K, V, table, len, Kp, Vp, seq, status)
+    T, sh, at = _torch(), plan.shape, _at()
+    r16 = (*T.bf16, T.torch.float16)
+    handle = plan.address
     dense = sh.L * plan.B * sh.H_kv * int(T_stride) * 128
     pool = pages.num_pages * pages.page_rows * 128
-    if seq is not None and not isinstance(seq, int) and seq.numel() != plan.B:
-        _bad(f"seq has {seq.numel()} elements, the plan {plan.B} sequences")
+    for t, name in ((K, "K"), (V, "V")):
+        if not isinstance(t, int) and t.numel() < dense:
+            _bad(f"{name} has {t.numel()} elements, needs at least {dense}")
     _check(lib().dkv_page_compact(
-        ctypes.byref(pages.c), plan.address, _dev(seq, "seq", i32), _dev(K, "K", r16, min_numel=dense),
-        _dev(V, "V", r16, min_numel=dense), int(T_stride), _dev(table, "table", i32, pages.slabs * pages.max_pages),
-        _dev(len, "len", i32, pages.slabs), _dev(Kp, "Kp", r16, pool), _dev(Vp, "Vp", r16, pool),
-        _dev(status, "status", i32, min_numel=1), _stream(stream)), "dkv_page_compact")
+        pages.ref, handle, _on(seq, "seq", at, T.i32, plan.B), _on(K, "K", at, r16), _on(V, "V", at, r16), int(T_stride),
+        _on(table, "table", at, T.i32, pages.slabs * pages.max_pages), _on(len, "len", at, T.i32, pages.slabs),
+        _on(Kp, "Kp", at, r16, pool), _on(Vp, "Vp", at, r16, pool), _word(status, at), _stream(stream)), "dkv_page_compact")
 
 
 def dkv_chunk_workspace_bytes(pages: Pages) -> int:
@@ -625,16 +639,17 @@ def dkv_chunk_workspace_bytes(pages: Pages) -> int:
     return n
 
 
-def _token_rows(t, name, dtype, tokens, heads):
+def _token_rows(t, name, at, dtype, tokens, heads):
     """Address and token stride (elements) of a [tokens][heads][128] tensor whose tokens may lie apart (a slice of a
     projection); heads and elements are contiguous."""
-    if not getattr(t, "is_cuda", False):
-        _bad(f"{name} must be a CUDA tensor")
+    if t.get_device() != at:
+        _bad(f"{name} must be a CUDA tensor on cuda:{at}")
     if t.dtype != dtype or t.shape != (tokens, heads, 128):
         _bad(f"{name} is {t.dtype} {tuple(t.shape)}, expected {dtype} {(tokens, heads, 128)}")
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != 128):
+    stride = t.stride()
+    if stride[2] != 1 or (heads > 1 and stride[1] != 128):
         _bad(f"{name}: heads and elements of a token must be contiguous")
-    return t.data_ptr(), (t.stride(0) if tokens > 1 else heads * 128)
+    return t.data_ptr(), stride[0] if tokens > 1 else heads * 128
 
 
 def dkv_chunk_attn(pages: Pages, layer: int, q, k_new, v_new, cu_tokens, table, len, Kp, Vp, out, workspace,
@@ -642,27 +657,26 @@ def dkv_chunk_attn(pages: Pages, layer: int, q, k_new, v_new, cu_tokens, table, 
     """One layer's new tokens: k_new and v_new [T][H_kv][128] appended to their slabs' pages (None: they are there), and
     the attention of q [T][H][128] -> out [T][H][128], all of q's type (bf16 or fp16). q, k_new and v_new may be slices of
     one projection; k_new and v_new have the same token stride."""
-    t = _torch().torch
-    i32 = _i32()
-    _here(q, k_new, v_new, cu_tokens, table, len, Kp, Vp, out, workspace, status)
-    if q.dtype not in (t.bfloat16, t.float16) or q.dim() != 3:
-        _bad(f"q is {q.dtype} of {q.dim()} dimensions, expected bfloat16 or float16 [T][H][128]")
-    tokens, one = q.shape[0], (q.dtype,)
-    qp, qs = _token_rows(q, "q", q.dtype, tokens, pages.H)
+    T, at, dtype = _torch(), _at(), q.dtype
+    half = dtype == T.torch.float16
+    if not (half or dtype == T.torch.bfloat16) or q.dim() != 3:
+        _bad(f"q is {dtype} of {q.dim()} dimensions, expected bfloat16 or float16 [T][H][128]")
+    tokens, one = q.shape[0], (dtype,)
+    qp, qs = _token_rows(q, "q", at, dtype, tokens, pages.H)
     kp = vp = None
     ks = 0
-    if (k_new is None) != (v_new is None):
-        _bad("k_new and v_new must both be given or both be None")
-    if k_new is not None:
-        kp, ks = _token_rows(k_new, "k_new", q.dtype, tokens, pages.H_kv)
-        vp, vs = _token_rows(v_new, "v_new", q.dtype, tokens, pages.H_kv)
+    if k_new is not None and v_new is not None:
+        kp, ks = _token_rows(k_new, "k_new", at, dtype, tokens, pages.H_kv)
+        vp, vs = _token_rows(v_new, "v_new", at, dtype, tokens, pages.H_kv)
         if ks != vs:
             _bad(f"k_new and v_new have token strides {ks} and {vs}")
+    elif k_new is not None or v_new is not None:
+        _bad("k_new and v_new must both be given or both be None")
     pool = pages.num_pages * pages.page_rows * 128
-    wp, wb = _work(workspace)
+    wp, wb = _work(workspace, at)
     _check(lib().dkv_chunk_attn(
-        ctypes.byref(pages.c), int(layer), DKV_FP16 if q.dtype == t.float16 else DKV_BF16, tokens, qp, qs, kp, vp, ks,
-        _dev(cu_tokens, "cu_tokens", i32, pages.B + 1), _dev(table, "table", i32, pages.slabs * pages.max_pages),
-        _dev(len, "len", i32, pages.slabs), _dev(Kp, "Kp", one, pool), _dev(Vp, "Vp", one, pool), int(bool(causal)),
-        scale, _dev(out, "out", one, tokens * pages.H * 128), wp, wb, _dev(status, "status", i32, min_numel=1),
+        pages.ref, layer, DKV_FP16 if half else DKV_BF16, tokens, qp, qs, kp, vp, ks,
+        _on(cu_tokens, "cu_tokens", at, T.i32, pages.B + 1), _on(table, "table", at, T.i32, pages.slabs * pages.max_pages),
+        _on(len, "len", at, T.i32, pages.slabs), _on(Kp, "Kp", at, one, pool), _on(Vp, "Vp", at, one, pool),
+        1 if causal else 0, scale, _on(out, "out", at, one, tokens * pages.H * 128), wp, wb, _word(status, at),
         _stream(stream)), "dkv_chunk_attn")
