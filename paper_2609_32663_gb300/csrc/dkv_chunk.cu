@@ -579,63 +579,103 @@ __device__ __forceinline__ void mend_rows(const ChunkArgs& a, int h, bool odd, i
     }
 }
 
-// The last piece's CTA joins the pieces of a unit, in the order of the CTAs. `scale` (shared):
-// each row's max and 1 / sum over the pieces.
+// Joining the pieces of a unit: eight elements of a row an item, neighbouring rows in
+// neighbouring lanes, the sums in the order of the CTAs. Loads are most of it, so ITEMS items of
+// a thread and PIECES of their pieces are on the way at once (16 loads of 16 bytes).
+template <bool F16, int ITEMS, int PIECES>
+__device__ __forceinline__ void join_items(const ChunkArgs& a, const ChunkWork& w, const float2* scale, int t0, int rows, int g, int c0, int pieces)
+{
+    const int low = kTile / a.G * a.G, items = rows * (kHeadDim / 8);
+    const float c = a.qscale;
+#pragma unroll 1
+    for (int i0 = threadIdx.x; i0 < items; i0 += ITEMS * kSoft) {
+        int x[ITEMS], ch[ITEMS], at[ITEMS];
+        float4 A[ITEMS], B[ITEMS];
+        float2 mz[ITEMS];
+#pragma unroll
+        for (int y = 0; y < ITEMS; ++y) {
+            const int i = min(i0 + y * kSoft, items - 1);
+            ch[y] = i / rows;
+            x[y] = i - ch[y] * rows;
+            at[y] = x[y] < low ? x[y] : x[y] - low + kTile;
+            mz[y] = scale[x[y]];
+            A[y] = B[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll 1
+        for (int k0 = 0; k0 < pieces; k0 += PIECES) {
+            float2 ml[ITEMS][PIECES];
+            float4 u[ITEMS][PIECES], v[ITEMS][PIECES];
+#pragma unroll
+            for (int z = 0; z < PIECES; ++z) {
+                const int k = min(k0 + z, pieces - 1);
+                const int64_t piece = (int64_t)(c0 + k) * 2 + (k == 0);
+#pragma unroll
+                for (int y = 0; y < ITEMS; ++y) {
+                    const float4* o = w.o + (piece * (kHeadDim / 4) + 2 * ch[y]) * kPieceRows + at[y];
+                    ml[y][z] = __ldcg(w.ml + piece * kPieceRows + at[y]);
+                    u[y][z] = __ldcg(o);
+                    v[y][z] = __ldcg(o + kPieceRows);
+                }
+            }
+#pragma unroll
+            for (int z = 0; z < PIECES; ++z)
+#pragma unroll
+                for (int y = 0; y < ITEMS; ++y) {
+                    const float2 m = ml[y][z];
+                    if (k0 + z >= pieces || (m.x == -INFINITY && m.y == 0.f)) continue;  // a piece that the row does not see
+                    const float f = ex2((m.x - mz[y].x) * c);
+                    const float4 p = u[y][z], q = v[y][z];
+                    A[y] = make_float4(fmaf(p.x, f, A[y].x), fmaf(p.y, f, A[y].y), fmaf(p.z, f, A[y].z), fmaf(p.w, f, A[y].w));
+                    B[y] = make_float4(fmaf(q.x, f, B[y].x), fmaf(q.y, f, B[y].y), fmaf(q.z, f, B[y].z), fmaf(q.w, f, B[y].w));
+                }
+        }
+#pragma unroll
+        for (int y = 0; y < ITEMS; ++y) {
+            if (i0 + y * kSoft >= items) break;
+            const int token = x[y] / a.G, j = x[y] - token * a.G;
+            const float z = mz[y].y;
+            *reinterpret_cast<uint4*>(a.out + ((int64_t)(t0 + token) * a.H + g * a.G + j) * kHeadDim + 8 * ch[y]) =
+                make_uint4(pack16<F16>(A[y].x * z, A[y].y * z), pack16<F16>(A[y].z * z, A[y].w * z), pack16<F16>(B[y].x * z, B[y].y * z),
+                           pack16<F16>(B[y].z * z, B[y].w * z));
+        }
+    }
+}
+
+// The last piece's CTA joins the pieces. `scale` (shared): each row's max and 1 / sum over them.
 template <bool F16>
 __device__ __forceinline__ void join_pieces(const ChunkArgs& a, const ChunkWork& w, float2* scale, int t0, int tokens, int g, int c0, int pieces)
 {
-    const int tid = threadIdx.x, lane = tid & 31, TQ = kTile / a.G, rows = tokens * a.G, low = TQ * a.G;
+    const int tid = threadIdx.x, rows = tokens * a.G, low = kTile / a.G * a.G;
     const float c = a.qscale;
-    auto piece = [c0](int k) { return (int64_t)(c0 + k) * 2 + (k == 0); };
-    auto place = [low](int x) { return x < low ? x : x - low + kTile; };
-    // A warp a row with few rows (then the pieces may be many), a thread a row else.
-    const bool few = rows <= 64;
-#pragma unroll 1
-    for (int x = few ? tid >> 5 : tid; x < rows; x += few ? kSoft / 32 : kSoft) {
-        float M = -INFINITY, L = 0.f;
-#pragma unroll 2
-        for (int k = few ? lane : 0; k < pieces; k += few ? 32 : 1) {
-            const float2 ml = __ldcg(w.ml + piece(k) * kPieceRows + place(x));
-            if (ml.x == -INFINITY && ml.y == 0.f) continue;  // a piece that the row does not see
+    // As many lanes a row as there are threads for (a power of 2).
+    int lanes = 32;
+    while (lanes > 1 && lanes * rows > kSoft) lanes >>= 1;
+    const int x = tid / lanes, first = tid & (lanes - 1), at = x < low ? x : x - low + kTile;
+    float M = -INFINITY, L = 0.f;
+    if (x < rows) {
+#pragma unroll 4
+        for (int k = first; k < pieces; k += lanes) {
+            const float2 ml = __ldcg(w.ml + ((int64_t)(c0 + k) * 2 + (k == 0)) * kPieceRows + at);
+            if (ml.x == -INFINITY && ml.y == 0.f) continue;
             const float M1 = fmaxf(M, ml.x);
             L = L * (M == -INFINITY ? 0.f : ex2((M - M1) * c)) + ml.y * (ml.x == -INFINITY ? 0.f : ex2((ml.x - M1) * c));
             M = M1;
         }
-        if (few) {
-            float M1 = M;
-#pragma unroll
-            for (int o = 16; o >= 1; o >>= 1) M1 = fmaxf(M1, __shfl_xor_sync(kFull, M1, o));
-            L *= M == -INFINITY && L == 0.f ? 0.f : ex2((M - M1) * c);
-            M = M1;
-#pragma unroll
-            for (int o = 16; o >= 1; o >>= 1) L += __shfl_xor_sync(kFull, L, o);
-        }
-        if (!few || lane == 0) scale[x] = make_float2(M, inverse(L));
     }
-    named_sync(1, kSoft);
-    // Eight elements of a row a thread, neighbouring rows in neighbouring lanes.
 #pragma unroll 1
-    for (int i = tid; i < rows * (kHeadDim / 8); i += kSoft) {
-        const int ch = i / rows, x = i - ch * rows, r = place(x);
-        const float2 mz = scale[x];
-        float4 A = make_float4(0.f, 0.f, 0.f, 0.f), B = A;
-#pragma unroll 4
-        for (int k = 0; k < pieces; ++k) {
-            const float2 ml = __ldcg(w.ml + piece(k) * kPieceRows + r);
-            const float4* o = w.o + (piece(k) * (kHeadDim / 4) + 2 * ch) * kPieceRows + r;
-            const float4 u = __ldcg(o), v = __ldcg(o + kPieceRows);
-            const bool none = ml.x == -INFINITY && ml.y == 0.f;
-            const float f = none ? 0.f : ex2((ml.x - mz.x) * c);
-            if (none) continue;
-            A = make_float4(fmaf(u.x, f, A.x), fmaf(u.y, f, A.y), fmaf(u.z, f, A.z), fmaf(u.w, f, A.w));
-            B = make_float4(fmaf(v.x, f, B.x), fmaf(v.y, f, B.y), fmaf(v.z, f, B.z), fmaf(v.w, f, B.w));
-        }
-        const int token = x / a.G, j = x - token * a.G;
-        const float z = mz.y;
-        *reinterpret_cast<uint4*>(a.out + ((int64_t)(t0 + token) * a.H + g * a.G + j) * kHeadDim + 8 * ch) =
-            make_uint4(pack16<F16>(A.x * z, A.y * z), pack16<F16>(A.z * z, A.w * z), pack16<F16>(B.x * z, B.y * z),
-                       pack16<F16>(B.z * z, B.w * z));
+    for (int o = lanes >> 1; o >= 1; o >>= 1) {
+        const float M0 = __shfl_xor_sync(kFull, M, o), L0 = __shfl_xor_sync(kFull, L, o), M1 = fmaxf(M, M0);
+        L = (L == 0.f ? 0.f : L * ex2((M - M1) * c)) + (L0 == 0.f ? 0.f : L0 * ex2((M0 - M1) * c));
+        M = M1;
     }
+    if (x < rows && first == 0) scale[x] = make_float2(M, inverse(L));
+    named_sync(1, kSoft);
+    if (pieces <= 2)
+        join_items<F16, 4, 2>(a, w, scale, t0, rows, g, c0, pieces);
+    else if (rows > 16)
+        join_items<F16, 2, 4>(a, w, scale, t0, rows, g, c0, pieces);
+    else
+        join_items<F16, 1, 8>(a, w, scale, t0, rows, g, c0, pieces);
 }
 
 template <bool F16>
