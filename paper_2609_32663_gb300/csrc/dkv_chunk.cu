@@ -20,9 +20,9 @@
 //                     that the tensor pipe itself keeps S(s + 2) behind the PV(s) whose P it overwrites.
 //     warp 9          TMA (10 and 11 idle): Q tiles, and K and V tiles page by page into one ring in the order of use.
 //
-// Every wait is bounded (polls and 2 s); one that runs out sets DKV_DEV_TMA_TIMEOUT, the roles
-// walk on without work so that they meet at the named barriers, copies and products in flight
-// are drained, and the unit's outputs stay unwritten.
+// Every wait is bounded (polls and 2 s), and so are the softmax warps' meetings (Waits::meet); one
+// that runs out sets DKV_DEV_TMA_TIMEOUT, the roles leave, copies and products in flight are
+// drained, and the outputs of the CTA's unfinished units stay unwritten.
 #include "dkv_pages.cuh"
 #include "dkv_tcgen05.cuh"
 
@@ -51,21 +51,24 @@ constexpr int kTmemCols = 512;             // S of group p at 128 p (P over its 
 constexpr int kOffQ = 0;
 constexpr int kOffRing = kOffQ + 2 * kOperand;
 constexpr int kOffBars = kOffRing + kStages * kOperand;
-constexpr int kNumBars = 2 * kStages + 11;  // full[], empty[], q_full, q_empty, s_full[2], p_half[2], p_full[2], o_done[2], fin
+constexpr int kAhead = 4;                  // ring of unit descriptors
+constexpr int kNumBars = 2 * kStages + 2 * kAhead + 11;  // full[], empty[], q_full[], late[], q_empty[2], s_full[2], p_half[2], p_full[2], o_done[2], fin
 constexpr int kOffMisc = kOffBars + (kNumBars + 1) / 2 * 16;  // int[4]: TMEM address, abort, last
-constexpr int kOffMl = kOffMisc + 16;                           // float2[128]: group 1's (m, l), then group 0's
+constexpr int kOffPieces = kOffMisc + 16;                      // Piece[kAhead]
+constexpr int kOffMl = kOffPieces + kAhead * 48;                           // float2[128]: group 1's (m, l), then group 0's
 constexpr int kSmemBytes = kOffMl + 2 * kTile * 8;
 static_assert(kSmemBytes <= 227 * 1024, "fits one CTA");
 
 // Workspace.
 struct alignas(16) ChunkStart {  // a CTA's share
     int64_t tiles;   // of the whole call
-    int32_t parts;   // CTAs with a share; 0 tiles: none, and nothing else is set
+    int64_t pos, end;  // the share's
+    int32_t parts;   // CTAs with a share; 0: none, and nothing else is set
     int32_t b, g, i, first;  // sequence, KV head, unit of the sequence, and its first tile in the share
     int32_t t, n, len;       // the sequence's first token and tokens, rows of the slab
     int32_t pad[2];
 };
-static_assert(sizeof(ChunkStart) == 48, "three 16-byte loads");
+static_assert(sizeof(ChunkStart) == 64, "four 16-byte loads");
 struct ChunkWork {
     ChunkStart* start;  // [kMaxCtas]
     int32_t* done;      // [kMaxCtas] finished pieces of the unit that starts in CTA c and ends in a later one
@@ -127,10 +130,10 @@ struct Walk {
         j0 = off;
         j1 = (int)min((int64_t)tiles, off + (end - pos));
     }
-    __device__ __forceinline__ void begin(const ChunkArgs& a, const ChunkStart& s, int c)
+    __device__ __forceinline__ void begin(const ChunkArgs& a, const ChunkStart& s)
     {
-        pos = s.tiles * c / s.parts;
-        end = s.tiles * (c + 1) / s.parts;
+        pos = s.pos;
+        end = s.end;
         b = s.b;
         g = s.g;
         i = s.i;
@@ -156,9 +159,37 @@ struct Walk {
         return true;
     }
     __device__ __forceinline__ bool whole() const { return j0 == 0 && j1 == tiles; }
-    __device__ __forceinline__ int steps() const { return u.pair ? 2 * (j1 - j0) : j1 - j0; }
-    __device__ __forceinline__ int tile(int s) const { return j0 + (u.pair ? s >> 1 : s); }
 };
+
+// What the other roles need of a CTA's part of a unit; the TMA warp walks and describes it.
+struct alignas(16) Piece {
+    int t0, tokens, row0, len;  // as in Unit
+    int kv, h, g, j0;
+    int j1, flags;
+    int c0, pieces;             // CTAs c0 .. c0 + pieces - 1 hold the unit (written after the rest: `late`)
+    static constexpr int kPair = 1, kWhole = 2, kMore = 4;
+    __device__ __forceinline__ bool pair() const { return flags & kPair; }
+    __device__ __forceinline__ bool whole() const { return flags & kWhole; }
+    __device__ __forceinline__ bool more() const { return flags & kMore; }  // the CTA has a unit after this
+    __device__ __forceinline__ int steps() const { return pair() ? 2 * (j1 - j0) : j1 - j0; }
+    __device__ __forceinline__ int tile(int s) const { return j0 + (pair() ? s >> 1 : s); }
+};
+static_assert(sizeof(Piece) == 48, "three 16-byte words");
+
+__device__ __forceinline__ Piece read_piece(const unsigned char* at)
+{
+    union {
+        uint4 u[3];
+        Piece p;
+    } x;
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(x.u[i].x), "=r"(x.u[i].y), "=r"(x.u[i].z), "=r"(x.u[i].w)
+                     : "r"(smem_u32(at) + 16 * i)
+                     : "memory");
+    return x.p;
+}
 
 // The CTA whose share holds tile x of the call.
 __device__ __forceinline__ int cta_of(const ChunkStart& s, int64_t x) { return (int)(((x + 1) * s.parts - 1) / s.tiles); }
@@ -236,9 +267,11 @@ __device__ __forceinline__ void schedule(const ChunkArgs& a, const ChunkWork& w,
     __syncthreads();
     const int parts = (int)min(total, (int64_t)nctas);
     if (tid >= nctas) return;
-    ChunkStart s{total, parts};
+    ChunkStart s{total, 0, 0, parts};
     if (tid < parts) {
         const int64_t at = total * tid / parts;
+        s.pos = at;
+        s.end = total * (tid + 1) / parts;
         int lo = 0, hi = groups - 1;  // the last group that starts at tile `at` or before (it has tiles)
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
@@ -318,12 +351,13 @@ __device__ __forceinline__ bool wait_more(uint32_t bar, uint32_t parity, volatil
     return false;
 }
 
-// A bounded wait of a whole warp. After one that ran out (here or in another role) every wait
+// Bounded waits of a whole warp. After one that ran out (here or in another role) every wait
 // of the CTA returns false at once.
 struct Waits {
     volatile int* abort;
     int32_t* status;
     bool ok;
+    bool left;  // this softmax warp goes to no further meeting
     __device__ __forceinline__ bool operator()(uint64_t* b, uint32_t parity)
     {
         if (!ok) return false;
@@ -331,6 +365,26 @@ struct Waits {
         if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
         ok = __all_sync(kFull, wait_more(bar, parity, abort, status));
         return ok;
+    }
+    // All softmax warps meet at a named barrier, which has no bound: a warp whose wait ran out
+    // still goes to one more meeting and says so there, to whichever the others come next (all
+    // go to one after their last unit); every warp then leaves.
+    __device__ __forceinline__ bool meet()
+    {
+        if (left) return false;
+        uint32_t r;
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+            "bar.red.or.pred p, 1, %2, q;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(r)
+            : "r"(ok ? 0 : 1), "n"(kSoft)
+            : "memory");
+        if (r) {
+            ok = false;
+            left = true;
+        }
+        return r == 0;
     }
 };
 
@@ -374,6 +428,14 @@ __device__ __forceinline__ uint64_t add2(uint64_t x, uint64_t y)
     return v;
 }
 
+// The larger of three, NaN only if all are.
+__device__ __forceinline__ float max3(float x, float y, float z)
+{
+    float v;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(v) : "f"(x), "f"(y), "f"(z));
+    return v;
+}
+
 // P of a score s is 2^(s c - origin(m, c)).
 template <bool F16>
 __device__ __forceinline__ float origin(float m, float c)
@@ -382,12 +444,29 @@ __device__ __forceinline__ float origin(float m, float c)
     return (m == -INFINITY ? 0.f : m * c) - kShift;
 }
 
+// P of 32 scores as 16 packed words; their sums are added to sum[].
+template <bool F16>
+__device__ __forceinline__ void exponentials(const uint32_t (&x)[32], uint64_t c2, uint64_t o2, uint32_t (&p)[16], uint64_t (&sum)[4])
+{
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        float p0, p1;
+        unpack2(fma2(pack2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), c2, o2), p0, p1);
+        p0 = ex2(p0);
+        p1 = ex2(p1);
+        sum[e & 3] = add2(sum[e & 3], pack2(p0, p1));
+        p[e] = pack16<F16>(p0, p1);
+    }
+}
+
 // One step of a softmax group's warp: scores of 32 query rows x 128 cache rows (TMEM columns of
 // `s`) to P over them, with the running max m (of raw scores), sum l and output `o`. lim: the
 // cache rows of this tile that the thread's query sees (may be outside 0 .. 128).
 // The max moves only when a score tops it by 2^kSlack (then O is rescaled, so `rescale` says
-// whether it holds anything): P stays below 2^kSlack. fp16 P is scaled by 2^7 more, which l shares: the
-// smallest normal P is then 2^-21 of the largest score's.
+// whether it holds anything): P stays below 2^kSlack. So the first half of P is computed with the
+// max as it was, beside the tile's own max, and again in the rare step that moves it: the max is off the
+// path from S to P. fp16 P is scaled by 2^7 more, which l shares: the smallest normal P is then 2^-21 of the
+// largest score's.
 template <bool F16>
 __device__ __forceinline__ void softmax_step(uint32_t s, uint32_t o, int lim, bool rescale, float c, float& m, float& l, uint32_t half_bar)
 {
@@ -411,8 +490,9 @@ __device__ __forceinline__ void softmax_step(uint32_t s, uint32_t o, int lim, bo
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int e = 0; e < 32; ++e) mxs[e & 7] = fmaxf(mxs[e & 7], __uint_as_float(x[k][e]));
-    const float mx = fmaxf(fmaxf(fmaxf(mxs[0], mxs[1]), fmaxf(mxs[2], mxs[3])), fmaxf(fmaxf(mxs[4], mxs[5]), fmaxf(mxs[6], mxs[7])));
+        for (int e = 0; e < 32; e += 2)
+            mxs[(e >> 1) & 7] = max3(mxs[(e >> 1) & 7], __uint_as_float(x[k][e]), __uint_as_float(x[k][e + 1]));
+    const float mx = max3(max3(mxs[0], mxs[1], mxs[2]), max3(mxs[3], mxs[4], mxs[5]), fmaxf(mxs[6], mxs[7]));
     const bool move = (mx - m) * c > kSlack;
     if (__any_sync(kFull, move)) {
         const float alpha = move ? ex2((m - mx) * c) : 1.f;
@@ -434,26 +514,19 @@ __device__ __forceinline__ void softmax_step(uint32_t s, uint32_t o, int lim, bo
     const float mc = origin<F16>(m, c);
     const uint64_t c2 = pack2(c, c), o2 = pack2(-mc, -mc);
     uint64_t sum[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        uint32_t p[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            float p0, p1;
-            unpack2(fma2(pack2(__uint_as_float(x[k][2 * e]), __uint_as_float(x[k][2 * e + 1])), c2, o2), p0, p1);
-            p0 = ex2(p0);
-            p1 = ex2(p1);
-            sum[e & 3] = add2(sum[e & 3], pack2(p0, p1));
-            p[e] = pack16<F16>(p0, p1);
-        }
-        tmem_st16_async(s + 16 * k, p);
-        if (k == 1) {
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if ((threadIdx.x & 31) == 0) mbar_arrive(half_bar);
-        }
-    }
+    uint32_t p[16];
+    exponentials<F16>(x[0], c2, o2, p, sum);
+    tmem_st16_async(s, p);
+    exponentials<F16>(x[1], c2, o2, p, sum);
+    tmem_st16_async(s + 16, p);
+    tmem_wait_st();
+    tc_fence_before();
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(half_bar);
+    exponentials<F16>(x[2], c2, o2, p, sum);
+    tmem_st16_async(s + 32, p);
+    exponentials<F16>(x[3], c2, o2, p, sum);
+    tmem_st16_async(s + 48, p);
     float s0, s1;
     unpack2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), s0, s1);
     l += s0 + s1;
@@ -579,6 +652,20 @@ __device__ __forceinline__ void mend_rows(const ChunkArgs& a, int h, bool odd, i
     }
 }
 
+// Loads from L2 that stay ahead of their use, a batch together (volatile).
+__device__ __forceinline__ float4 load_l2(const float4* p)
+{
+    float4 v;
+    asm volatile("ld.global.cg.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ float2 load_l2(const float2* p)
+{
+    float2 v;
+    asm volatile("ld.global.cg.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p));
+    return v;
+}
+
 // Joining the pieces of a unit: eight elements of a row an item, neighbouring rows in
 // neighbouring lanes, the sums in the order of the CTAs. Loads are most of it, so ITEMS items of
 // a thread and PIECES of their pieces are on the way at once (16 loads of 16 bytes).
@@ -612,9 +699,9 @@ __device__ __forceinline__ void join_items(const ChunkArgs& a, const ChunkWork& 
 #pragma unroll
                 for (int y = 0; y < ITEMS; ++y) {
                     const float4* o = w.o + (piece * (kHeadDim / 4) + 2 * ch[y]) * kPieceRows + at[y];
-                    ml[y][z] = __ldcg(w.ml + piece * kPieceRows + at[y]);
-                    u[y][z] = __ldcg(o);
-                    v[y][z] = __ldcg(o + kPieceRows);
+                    ml[y][z] = load_l2(w.ml + piece * kPieceRows + at[y]);
+                    u[y][z] = load_l2(o);
+                    v[y][z] = load_l2(o + kPieceRows);
                 }
             }
 #pragma unroll
@@ -643,7 +730,7 @@ __device__ __forceinline__ void join_items(const ChunkArgs& a, const ChunkWork& 
 
 // The last piece's CTA joins the pieces. `scale` (shared): each row's max and 1 / sum over them.
 template <bool F16>
-__device__ __forceinline__ void join_pieces(const ChunkArgs& a, const ChunkWork& w, float2* scale, int t0, int tokens, int g, int c0, int pieces)
+__device__ __forceinline__ void join_pieces(const ChunkArgs& a, const ChunkWork& w, Waits& wait, float2* scale, int t0, int tokens, int g, int c0, int pieces)
 {
     const int tid = threadIdx.x, rows = tokens * a.G, low = kTile / a.G * a.G;
     const float c = a.qscale;
@@ -669,7 +756,7 @@ __device__ __forceinline__ void join_pieces(const ChunkArgs& a, const ChunkWork&
         M = M1;
     }
     if (x < rows && first == 0) scale[x] = make_float2(M, inverse(L));
-    named_sync(1, kSoft);
+    if (!wait.meet()) return;
     if (pieces <= 2)
         join_items<F16, 4, 2>(a, w, scale, t0, rows, g, c0, pieces);
     else if (rows > 16)
@@ -689,9 +776,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     uint64_t* full = reinterpret_cast<uint64_t*>(sm + kOffBars);  // [kStages] the stage's rows landed
     uint64_t* empty = full + kStages;                              // [kStages] its products are done
-    uint64_t* q_full = empty + kStages;                            // the unit's Q tiles landed
-    uint64_t* q_empty = q_full + 1;                                // the unit's score products are done
-    uint64_t* s_full = q_empty + 1;                                // [2] S of the group's next step is done
+    uint64_t* q_full = empty + kStages;                            // [kAhead] the unit is described and its Q landed
+    uint64_t* late = q_full + kAhead;                              // [kAhead] the unit's CTAs are described
+    uint64_t* q_empty = late + kAhead;                             // [2] the unit's score products are done
+    uint64_t* s_full = q_empty + 2;                                // [2] S of the group's next step is done
     uint64_t* p_half = s_full + 2;                                 // [2] the first half of its P is written
     uint64_t* p_full = p_half + 2;                                 // [2] all of it
     uint64_t* o_done = p_full + 2;                                 // [2] the group's last product of the unit is done
@@ -717,14 +805,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t tmem = (uint32_t)uniform(misc[0]);
     pdl_wait();
     union {
-        uint4 u[3];
+        uint4 u[4];
         ChunkStart s;
     } given;
 #pragma unroll
-    for (int i = 0; i < 3; ++i) given.u[i] = ld_prev(reinterpret_cast<const uint4*>(w.start + c) + i);
+    for (int i = 0; i < 4; ++i) given.u[i] = ld_prev(reinterpret_cast<const uint4*>(w.start + c) + i);
     const ChunkStart& head = given.s;
     const bool work = c < head.parts;
-    Waits wait{misc + 1, a.status, true};
+    Waits wait{misc + 1, a.status, true, false};
     const int TQ = kTile / a.G;
     if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
@@ -736,25 +824,24 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint64_t keep;
         asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(keep));
         Walk k;
-        k.begin(a, head, c);
+        k.begin(a, head);
         int pos = 0, unit = 0;
         const int ppt = kTile / a.P;  // pages a tile
-        auto load = [&](const CUtensorMap* map, int j) {
-            const int s = pos % kStages;
-            const int pages = min(max(k.u.kv - j * kTile, 0), kTile);
-            const int np = (pages + a.P - 1) / a.P;
-            int y = 0;
-            if (lane < np) {
-                const int page = a.table[(int64_t)k.u.h * a.max_pages + j * ppt + lane];
-                const bool good = page >= 0 && page < a.num_pages;
-                if (!good) report(a, DKV_DEV_PAGE_RANGE);
-                y = (good ? page : a.num_pages) * a.P;  // behind the pool: zeros
-            }
+        // Pages of tile j, and the lane's page number.
+        auto pages_in = [&](const Unit& u, int j) { return (min(max(u.kv - j * kTile, 0), kTile) + a.P - 1) / a.P; };
+        auto page_of = [&](const Unit& u, int j) {
+            return lane < pages_in(u, j) ? a.table[(int64_t)u.h * a.max_pages + j * ppt + lane] : 0;
+        };
+        auto load = [&](const CUtensorMap* map, const Unit& u, int j, int page) {
+            const int s = pos % kStages, np = pages_in(u, j);
+            const bool good = page >= 0 && page < a.num_pages;
+            if (!good) report(a, DKV_DEV_PAGE_RANGE);
+            const int y = (good ? page : a.num_pages) * a.P;  // behind the pool: zeros
             if (pos >= kStages && !wait(&empty[s], (pos / kStages - 1) & 1)) return;
             const uint32_t bar = smem_u32(&full[s]), dst = smem_u32(sm + kOffRing + s * kOperand);
             if (lane == 0) mbar_arrive_expect_tx(bar, np * a.P * kRowBytes);
             __syncwarp();
-            const uint64_t pol = k.u.pair ? keep : stream;
+            const uint64_t pol = u.pair ? keep : stream;
             if (lane < np) {
                 tma_box(dst + lane * a.P * 128, map, 0, y, bar, pol);
                 tma_box(dst + kHalf + lane * a.P * 128, map, 64, y, bar, pol);
@@ -762,32 +849,59 @@ __global__ void __launch_bounds__(kThreads, 1)
             __syncwarp();
             ++pos;
         };
-        int qs = 0;  // Q loads issued
+        int qs = 0;  // units described
+        bool more = true, pair_before = false;
         do {
-            if (unit > 0 && !wait(q_empty, (unit - 1) & 1)) break;
+            const Unit u = k.u;
+            const int j0 = k.j0, j1 = k.j1;
+            // Q buffers: both for a pair unit, the unit's parity's for a split one, so that these run ahead.
+            if (unit > 1 && !wait(&q_empty[unit & 1], (unit / 2 - 1) & 1)) break;
+            if (unit > 0 && (u.pair || pair_before) && !wait(&q_empty[(unit - 1) & 1], ((unit - 1) / 2) & 1)) break;
+            pair_before = u.pair;
+            const int64_t from = k.pos - j0;
+            const int g = k.g, unit_tiles = k.tiles;
+            const bool whole = k.whole();
+            more = k.pos + (j1 - j0) < k.end;
+            int page = page_of(u, j0);  // on its way while Q is
+            Piece* d = reinterpret_cast<Piece*>(sm + kOffPieces) + unit % kAhead;
             if (lane == 0) {
-                const uint32_t bar = smem_u32(q_full), box = 2u * 64 * a.G * TQ;
-                mbar_arrive_expect_tx(bar, (k.u.pair ? 4 : 2) * box);
-                for (int p = 0; p < (k.u.pair ? 2 : 1); ++p)
+                *reinterpret_cast<int4*>(&d->t0) = make_int4(u.t0, u.tokens, u.row0, u.len);
+                *reinterpret_cast<int4*>(&d->kv) = make_int4(u.kv, u.h, g, j0);
+                *reinterpret_cast<int2*>(&d->j1) =
+                    make_int2(j1, (u.pair ? Piece::kPair : 0) | (whole ? Piece::kWhole : 0) | (more ? Piece::kMore : 0));
+                const uint32_t bar = smem_u32(&q_full[unit % kAhead]), box = 2u * 64 * a.G * TQ;
+                mbar_arrive_expect_tx(bar, (u.pair ? 4 : 2) * box);
+                for (int p = 0; p < (u.pair ? 2 : 1); ++p)
                     for (int half = 0; half < 2; ++half)
-                        tma_box3(smem_u32(sm + kOffQ + p * kOperand + half * kHalf), &maps.q, 64 * half, k.g * a.G, k.u.t0 + p * TQ, bar);
+                        tma_box3(smem_u32(sm + kOffQ + (u.pair ? p : unit & 1) * kOperand + half * kHalf), &maps.q, 64 * half, g * a.G,
+                                 u.t0 + p * TQ, bar);
             }
-            __syncwarp();
             ++qs;
-            const int steps = k.steps(), stride = k.u.pair ? 2 : 1;
+            __syncwarp();
+            const int steps = u.pair ? 2 * (j1 - j0) : j1 - j0, stride = u.pair ? 2 : 1;
             // K(0), K(1), then V(s), K(s + 2); pair units have one K and one V a pair of steps.
 #pragma unroll 1
-            for (int x = -4; x < 2 * steps && wait.ok; ++x) {
+            for (int x = -3; x < 2 * steps && wait.ok; ++x) {
                 const int s = (x >> 1) + 2 * (x & 1);  // even x: V of step x / 2; odd x: K of step x / 2 + 2
                 if (s < 0 || s >= steps || (s & (stride - 1))) continue;
-                load(x & 1 ? &maps.cache.k : &maps.cache.v, k.tile(s));
+                const int j = j0 + (u.pair ? s >> 1 : s);
+                load(x & 1 ? &maps.cache.k : &maps.cache.v, u, j, x == -3 ? page : page_of(u, j));
+                if (x == -3) {  // with the first copies on their way
+                    const int c0 = whole ? c : cta_of(head, from), last = whole ? c : cta_of(head, from + unit_tiles - 1);
+                    if (lane == 0) {
+                        d->c0 = c0;
+                        d->pieces = last - c0 + 1;
+                        mbar_arrive(smem_u32(&late[unit % kAhead]));
+                    }
+                    if (more) k.next(a);
+                }
             }
             ++unit;
-        } while (wait.ok && k.next(a));
+        } while (wait.ok && more);
         if (!wait.ok) {
             // Copies in flight land (or run out of time) before the CTA exits.
             for (int x = max(0, pos - kStages); x < pos; ++x) mbar_wait(smem_u32(&full[x % kStages]), (x / kStages) & 1);
-            if (qs) mbar_wait(smem_u32(q_full), (qs - 1) & 1);
+            for (int x = max(0, qs - 2); x < qs; ++x) mbar_wait(smem_u32(&q_full[x % kAhead]), (x / kAhead) & 1);
         }
     } else if (work && warp == 8) {
         // ---------------------------------------------------------------- MMA
@@ -799,15 +913,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t dQ = (uint32_t)sdesc(smem_u32(sm + kOffQ), 16, 1024), dK = (uint32_t)sdesc(smem_u32(sm + kOffRing), 16, 1024),
                        dV = (uint32_t)sdesc(smem_u32(sm + kOffRing), kHalf, 1024);
         auto desc = [dhi](uint32_t lo) { return ((uint64_t)dhi << 32) | lo; };
-        Walk k;
-        k.begin(a, head, c);
+        Piece k;
         int pos = 0, unit = 0, curK = 0, curV = 0;
         uint32_t phases = 0;  // bit p: parity of the P tiles taken of group p
         bool issued = false;
         do {
+            if (!wait(&q_full[unit % kAhead], (unit / kAhead) & 1)) break;
+            k = read_piece(sm + kOffPieces + unit % kAhead * sizeof(Piece));
             const int steps = k.steps();
-            const bool pair = k.u.pair;
-            if (!wait(q_full, unit & 1)) break;
+            const bool pair = k.pair();
+            const uint32_t qbuf = dQ + (pair ? 0 : unit & 1) * (kOperand >> 4);
 #pragma unroll 1
             for (int x = -2; x < steps; ++x) {
                 const int p = x & 1;
@@ -817,7 +932,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (!wait(&full[curV], (pos / kStages) & 1)) break;
                         ++pos;
                         // Rows past the unit's last (another token's, or never written) are zeroed: 0 NaN is NaN.
-                        const int valid = max(k.u.kv - k.tile(x) * kTile, 0);
+                        const int valid = max(k.kv - k.tile(x) * kTile, 0);
                         if (valid < kTile) zero_rows(sm + kOffRing + curV * kOperand, valid, lane);
                     }
                     if (!wait(&p_half[p], (phases >> p) & 1)) break;
@@ -847,7 +962,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     tc_fence_after();
                     if (leads) {
-                        const uint32_t q = dQ + (pair ? p : 0) * (kOperand >> 4), kt = dK + curK * (kOperand >> 4), d = tmem + p * kTile;
+                        const uint32_t q = qbuf + (pair ? p : 0) * (kOperand >> 4), kt = dK + curK * (kOperand >> 4), d = tmem + p * kTile;
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             const uint32_t off = ((e >> 2) * kHalf + (e & 3) * 32) >> 4;
@@ -855,14 +970,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                         umma_commit(smem_u32(&s_full[p]));
                         if (!pair || p == 1) umma_commit(smem_u32(&empty[curK]));
-                        if (x + 2 == steps - 1) umma_commit(smem_u32(q_empty));
+                        if (x + 2 == steps - 1) umma_commit(smem_u32(&q_empty[unit & 1]));
                     }
                     issued = true;
                     __syncwarp();
                 }
             }
             ++unit;
-        } while (wait.ok && k.next(a));
+        } while (wait.ok && k.more());
         if (!wait.ok && issued) {
             if (leads) {
                 umma_commit(smem_u32(fin));
@@ -880,46 +995,46 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t s_at = tmem + lanes + p * kTile, o_at = tmem + lanes + 256;
         const int token = r / a.G, j = r - token * a.G;
         const float cs = a.qscale;
-        Walk k;
-        k.begin(a, head, c);
+        Piece k;
         int ns = 0, no = 0;  // S tiles and O accumulators taken
+        int unit = 0;
         do {
+            if (!wait(&q_full[unit % kAhead], (unit / kAhead) & 1)) break;
+            k = read_piece(sm + kOffPieces + unit % kAhead * sizeof(Piece));
             const int steps = k.steps();
-            const bool pair = k.u.pair, whole = k.whole();
+            const bool pair = k.pair(), whole = k.whole();
             const int tok = token + (pair ? p * TQ : 0);
-            const bool live = token < TQ && tok < k.u.tokens;
-            const int lim = !live ? 0x3fffffff : a.causal ? min(max(k.u.row0 + tok, 0), k.u.len) : k.u.len;
+            const bool live = token < TQ && tok < k.tokens;
+            const int lim = !live ? 0x3fffffff : a.causal ? min(max(k.row0 + tok, 0), k.len) : k.len;
             const bool any = __any_sync(kFull, live);
             float m = -INFINITY, l = 0.f;
 #pragma unroll 1
             for (int s = p; s < steps; s += 2) {
-                if (wait(&s_full[p], ns & 1) && any) {
+                if (!wait(&s_full[p], ns++ & 1)) break;
+                if (any) {
                     tc_fence_after();
                     softmax_step<F16>(s_at, o_at + p * kTile, lim - k.tile(s) * kTile, s > 1, cs, m, l, smem_u32(&p_half[p]));
                     tc_fence_before();
                 } else if (lane == 0) {
                     mbar_arrive(smem_u32(&p_half[p]));
                 }
-                ++ns;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&p_full[p]));
             }
-            if (steps > p) {
-                wait(&o_done[p], no & 1);
-                ++no;
-            }
+            if (!wait.ok) break;
+            if (steps > p && !wait(&o_done[p], no++ & 1)) break;
             tc_fence_after();
-            uint16_t* out = a.out + ((int64_t)(k.u.t0 + tok) * a.H + k.g * a.G + j) * kHeadDim;
+            uint16_t* out = a.out + ((int64_t)(k.t0 + tok) * a.H + k.g * a.G + j) * kHeadDim;
             const int64_t slot = (int64_t)c * 2 + (k.j0 == 0);
             const int prow = (pair ? p * kTile : 0) + r;
             // Cache rows of this piece, and whether some of them are hidden from the thread's query.
-            const int first = k.j0 * kTile, end = min(k.u.kv, k.j1 * kTile);
+            const int first = k.j0 * kTile, end = min(k.kv, k.j1 * kTile);
             const bool hidden = live && lim < end;
-            const uint16_t* q = a.q + (int64_t)(k.u.t0 + tok) * a.q_stride + (k.g * a.G + j) * kHeadDim;
+            const uint16_t* q = a.q + (int64_t)(k.t0 + tok) * a.q_stride + (k.g * a.G + j) * kHeadDim;
             float4* o_piece = whole ? nullptr : w.o + slot * (kHeadDim / 4) * kPieceRows + prow;
             float odd = 0.f;  // NaN if a result is not finite
             if (pair) {
-                if (any && wait.ok) {
+                if (any) {
                     const float z = inverse(l);
 #pragma unroll 1
                     for (int e = 0; e < 4; ++e) {
@@ -931,21 +1046,21 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (live && !whole) store_piece(o_piece + 8 * e * kPieceRows, v);
                     }
                     if (__any_sync(kFull, hidden && odd != odd))
-                        mend_rows<F16>(a, k.u.h, hidden && odd != odd, first, lim, end, origin<F16>(m, cs), z, q, out, o_piece, 0, kHeadDim);
+                        mend_rows<F16>(a, k.h, hidden && odd != odd, first, lim, end, origin<F16>(m, cs), z, q, out, o_piece, 0, kHeadDim);
                     if (live && !whole) __stcg(w.ml + slot * kPieceRows + prow, make_float2(m, l));
                 }
             } else {
                 // The groups' halves of the cache rows: each group joins 64 of the dimensions.
                 sh_ml[p * kTile + r] = make_float2(m, l);
                 tc_fence_before();
-                named_sync(1, kSoft);
+                if (!wait.meet()) break;
                 tc_fence_after();
                 const float2 x = sh_ml[r], y = sh_ml[kTile + r];
                 const float M = fmaxf(x.x, y.x);
                 const float fx = x.x == -INFINITY ? 0.f : ex2((x.x - M) * cs), fy = y.x == -INFINITY ? 0.f : ex2((y.x - M) * cs);
                 const float L = x.y * fx + y.y * fy, z = inverse(L);
                 const bool two = steps > 1;
-                if (any && wait.ok) {
+                if (any) {
 #pragma unroll 1
                     for (int e = 2 * p; e < 2 * p + 2; ++e) {
                         float v[32], v1[32];
@@ -960,26 +1075,30 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (live && !whole) store_piece(o_piece + 8 * e * kPieceRows, v);
                     }
                     if (__any_sync(kFull, hidden && odd != odd))
-                        mend_rows<F16>(a, k.u.h, hidden && odd != odd, first, lim, end, origin<F16>(M, cs), z, q, out, o_piece, 64 * p, 64);
+                        mend_rows<F16>(a, k.h, hidden && odd != odd, first, lim, end, origin<F16>(M, cs), z, q, out, o_piece, 64 * p, 64);
                     if (live && !whole && p == 0) __stcg(w.ml + slot * kPieceRows + prow, make_float2(M, L));
                 }
             }
             if (!whole) {
-                const int c0 = cta_of(head, k.pos - k.j0), pieces = cta_of(head, k.pos - k.j0 + k.tiles - 1) - c0 + 1;
                 __threadfence();
-                named_sync(1, kSoft);
-                if (tid == 0) misc[2] = misc[1] == 0 && atomicAdd(w.done + c0, 1) == pieces - 1;
-                named_sync(1, kSoft);
+                if (!wait(&late[unit % kAhead], (unit / kAhead) & 1)) break;
+                const volatile Piece* d = reinterpret_cast<const volatile Piece*>(sm + kOffPieces) + unit % kAhead;
+                const int c0 = d->c0, pieces = d->pieces;
+                if (!wait.meet()) break;
+                if (tid == 0) misc[2] = atomicAdd(w.done + c0, 1) == pieces - 1;
+                if (!wait.meet()) break;
                 if (misc[2]) {
                     __threadfence();
-                    join_pieces<F16>(a, w, sh_ml, k.u.t0, k.u.tokens, k.g, c0, pieces);
+                    join_pieces<F16>(a, w, wait, sh_ml, k.t0, k.tokens, k.g, c0, pieces);
                 }
             }
             if (!pair || !whole) {
                 tc_fence_before();
-                named_sync(1, kSoft);  // O of the other group, sh_ml and misc[2] are read
+                if (!wait.meet()) break;  // O of the other group, sh_ml and misc[2] are read
             }
-        } while (k.next(a));
+            ++unit;
+        } while (k.more());
+        wait.meet();
         }
     }
     // ---------------------------------------------------------------- teardown

@@ -238,3 +238,33 @@ def test_long_cache_offsets_pass_32_bits(cuda):
     c.run()
     assert int(c.status) == 0
     paged.assert_attention(c.out, want, size, cache.dtype)
+
+
+def test_copies_that_never_land_are_reported(cuda, monkeypatch):
+    """Page copies that deliver half their bytes: every wait runs out, the call ends with the status bit, outputs stay
+    unwritten, and the next call is right."""
+    tokens = [1, 70]
+    cache = paged.Cache(lens_of(1, 2, 1, [500, 90], tokens, 1), 16, H=4)
+    cu, qkv = inputs(cache, tokens, 3)
+    c = Call(cache, 0, qkv, cu)
+    monkeypatch.setenv("DKV_FAULT", "copy")
+    c.run()
+    torch.cuda.synchronize()
+    monkeypatch.delenv("DKV_FAULT")
+    assert int(c.status) & dkv.DKV_DEV_TMA_TIMEOUT
+    assert torch.isnan(c.out).all()
+    c.status.zero_()
+    c.run()
+    want, size, _, _ = paged.attention(cache, 0, *qkv, cu, True)
+    assert int(c.status) == 0
+    paged.assert_attention(c.out, want, size, cache.dtype)
+
+
+def test_many_short_units_in_one_share(cuda):
+    """Sequences of few rows, so that a CTA has many units of one or two tiles, with turns between them."""
+    tokens = [1, 3, 1, 80, 1, 0, 2, 1] * 12
+    cache = paged.Cache(lens_of(1, len(tokens), 4, [20, 200, 140, 5, 300, 9, 0, 127] * 12, tokens, 6), 16, H=16)
+    cu, qkv = inputs(cache, tokens, 3)
+    c = Call(cache, 0, qkv, cu).run()
+    want, size, _, _ = paged.attention(cache, 0, *qkv, cu, True)
+    paged.assert_attention(c.out, want, size, cache.dtype)
