@@ -9,10 +9,14 @@
 //            takes is free[count - 1 - k].
 //   release  an ended slab gives back its pages, in slab order behind the free list's end.
 //
-// Two launches: page_scan_kernel checks every argument that lives on the device, scans the
-// slabs' page counts and writes lengths, counts and token offsets (nothing, if a check
-// fails or the free list is too short); page_fill_kernel then writes the table entries (or
-// the free list's) and the slot map from the scan.
+// The whole call needs the scan of all slabs' page counts, and every CTA its part of it. Up to
+// kFusedSlabs slabs each CTA scans them all itself (64 KB through L2 at 16,384 slabs, 2-3 us) into
+// shared memory and then fills its share: one launch, where a scan kernel and a fill kernel
+// behind it took 12.4 us for a step of 4,096 slabs. Lengths and counts that are updated in place
+// are committed by a second, tiny launch, as CTAs may still be reading them. More slabs: one
+// CTA scans into the workspace, then all fill.
+// Every value that lives on the device is checked in the scan: nothing is written if a check fails
+// or the free list is too short.
 #include "dkv_decode_common.cuh"
 #include "dkv_pages.cuh"
 #include "dkv_pool.cuh"
@@ -22,7 +26,8 @@
 namespace dkv {
 namespace {
 
-constexpr int kScanThreads = 1024;
+constexpr int kThreads = 1024;
+constexpr int kFusedSlabs = 48 * 1024;  // prefix sums in shared memory: 192 KB
 constexpr int kDevExhausted = DKV_DEV_PAGES_EXHAUSTED;
 constexpr int kDevRange = DKV_DEV_PAGE_RANGE;
 
@@ -39,134 +44,204 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* sh, int64_t* t
     __syncthreads();
     if (lane == 31) sh[warp] = v;
     __syncthreads();
-    if (warp == 0) {
-        int64_t w = lane < (int)(blockDim.x >> 5) ? sh[lane] : 0;
+    int64_t w = sh[lane];
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t y = __shfl_up_sync(kFull, w, o);
-            if (lane >= o) w += y;
-        }
-        sh[lane] = w;
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(kFull, w, o);
+        if (lane >= o) w += y;
     }
-    __syncthreads();
-    *total = sh[31];
-    return v - x + (warp ? sh[warp - 1] : 0);
+    *total = __shfl_sync(kFull, w, 31);
+    const int64_t before = __shfl_sync(kFull, w, (warp + 31) & 31);
+    return v - x + (warp ? before : 0);
 }
 
-// Rows that slab h of the pool gains (grow; negative: out of range) or gives up (release).
-// per_slot: per sequence slot, the new tokens, the ended flag or the plan's sequence (-1: none).
-__device__ __forceinline__ int slab_rows(const PageArgs& a, const int32_t* per_slot, int h, int len)
+__device__ __forceinline__ int pages_of(const PageArgs& a, int64_t rows) { return (int)((rows + a.P - 1) >> a.log_P); }
+
+// Rows that slab h gains (grow; negative: out of range), or whether it ends (release).
+// per_slot: new tokens, ended flags or the plan's sequence (-1: none) of each slot.
+__device__ __forceinline__ int slab_rows(const PageArgs& a, const int32_t* per_slot, int h)
 {
-    const int b = h / a.Hkv % a.B;
-    const int x = per_slot[b];
-    if (a.mode == kGrowTokens) return x;
-    if (a.mode == kRelease) return x ? len : 0;
-    const int l = h / (a.Hkv * a.B);
-    return x < 0 ? 0 : a.plan_len[((int64_t)l * a.planB + x) * a.Hkv + h % a.Hkv];
+    const int lb = h / a.Hkv, l = lb / a.B, x = per_slot[lb - l * a.B];
+    if (a.mode != kGrowPlan) return x;
+    return x < 0 ? 0 : a.plan_len[((int64_t)l * a.planB + x) * a.Hkv + (h - lb * a.Hkv)];
 }
 
-__device__ __forceinline__ int pages_of(int64_t rows, int P) { return (int)((rows + P - 1) / P); }
-
-__global__ void __launch_bounds__(kScanThreads) page_scan_kernel(const PageArgs a)
+// Pages that a slab of len rows takes (n new rows) or gives back (n: it ends).
+__device__ __forceinline__ int slab_pages(const PageArgs& a, int len, int n)
 {
-    __shared__ int64_t sh[32];
-    __shared__ int32_t per_slot[kMaxSlots];
-    __shared__ int bad;
+    if (a.mode == kRelease) return n ? pages_of(a, len) : 0;
+    return pages_of(a, (int64_t)len + n) - pages_of(a, len);
+}
+
+__device__ __forceinline__ int slab_after(const PageArgs& a, int len, int n)
+{
+    return a.mode == kRelease ? (n ? 0 : len) : len + n;
+}
+
+struct ScanShared {
+    int64_t sums[32];
+    int32_t per_slot[kMaxSlots];
+    int32_t cu[kMaxSlots + 1];
+    int bad;
+};
+
+// One CTA's scan of all slabs: first[h] = pages of the slabs before h. Returns whether all is in
+// range; then *head and, in token mode, sh->cu hold. Reads nothing that a commit writes after it.
+__device__ __forceinline__ bool scan_slabs(const PageArgs& a, ScanShared* sh, int32_t* first, PageHead* head)
+{
     const int tid = threadIdx.x;
-    pdl_wait();
-    pdl_launch_dependents();
-    if (tid == 0) bad = 0;
-    for (int b = tid; b < a.B; b += kScanThreads) per_slot[b] = a.mode == kGrowPlan ? -1 : a.tokens[b];
+    if (tid == 0) sh->bad = 0;
+    // A contiguous piece of the slabs a warp, 32 at a time; the first lengths are on their way at once.
+    constexpr int kRound = 4;
+    const int lane = tid & 31, per = (a.NH + kThreads - 1) / kThreads * 32;
+    const int h0 = (int)min((int64_t)a.NH, (int64_t)(tid >> 5) * per), h1 = (int)min((int64_t)a.NH, (int64_t)h0 + per);
+    int lens[kRound];
+    auto fetch = [&](int h) {
+#pragma unroll
+        for (int i = 0; i < kRound; ++i) lens[i] = h + 32 * i + lane < h1 ? a.len[h + 32 * i + lane] : 0;
+    };
+    fetch(h0);
+    const int count = *a.free_count;
+    for (int b = tid; b < a.B; b += kThreads) sh->per_slot[b] = a.mode == kGrowPlan ? -1 : a.tokens[b];
     __syncthreads();
     int flags = 0;
     if (a.mode == kGrowPlan) {
-        for (int i = tid; i < a.planB; i += kScanThreads) {
+        for (int i = tid; i < a.planB; i += kThreads) {
             const int b = a.seq ? a.seq[i] : i;
             if (b < 0 || b >= a.B || (a.seq && i > 0 && a.seq[i - 1] >= b))
                 flags |= kDevRange;  // slots ascend, so that no slot is named twice
             else
-                per_slot[b] = i;
+                sh->per_slot[b] = i;
         }
         __syncthreads();
     }
-    // Token offsets.
     int64_t tokens = 0;
     if (a.mode == kGrowTokens) {
-        const int n = tid < a.B ? per_slot[tid] : 0;
+        static_assert(kMaxSlots <= kThreads, "one thread a slot");
+        const int n = tid < a.B ? sh->per_slot[tid] : 0;
         if (n < 0) flags |= kDevRange;
-        const int64_t before = block_scan(max(n, 0), sh, &tokens);
-        if (a.cu && tid < a.B) a.cu[tid] = (int)min(before, (int64_t)INT32_MAX);
-        if (a.cu && tid == 0) a.cu[a.B] = (int)min(tokens, (int64_t)INT32_MAX);
+        const int64_t before = block_scan(max(n, 0), sh->sums, &tokens);
+        if (tid < a.B) sh->cu[tid] = (int)min(before, (int64_t)INT32_MAX);
+        if (tid == 0) sh->cu[a.B] = (int)min(tokens, (int64_t)INT32_MAX);
         if (tokens > (a.slots ? a.max_tokens : (int64_t)INT32_MAX)) flags |= kDevRange;
     }
-    // Pages of this thread's slabs, a contiguous piece of them.
-    const int64_t per = (a.NH + kScanThreads - 1) / kScanThreads;
-    const int64_t h0 = min((int64_t)a.NH, tid * per), h1 = min((int64_t)a.NH, h0 + per);
-    const int64_t cap = (int64_t)a.max_pages * a.P;
-    int64_t mine = 0;
-    for (int64_t h = h0; h < h1; ++h) {
-        const int len = a.len[h], n = slab_rows(a, per_slot, (int)h, len);
-        if (len < 0 || n < 0 || (int64_t)len + (a.mode == kRelease ? 0 : n) > cap) {
-            flags |= kDevRange;
-            continue;
+    const int64_t cap = (int64_t)a.max_pages << a.log_P;
+    int64_t mine = 0;  // this lane's pages; `run`: the warp's so far (32 bits do: it is used only if the sum fits)
+    int run = 0;
+#pragma unroll 1
+    for (int h = h0; h < h1; h += 32 * kRound) {
+        int v[kRound];
+#pragma unroll
+        for (int i = 0; i < kRound; ++i) {
+            const int x = h + 32 * i + lane, len = lens[i];
+            v[i] = 0;
+            if (x >= h1) continue;
+            const int n = slab_rows(a, sh->per_slot, x);
+            if (len < 0 || len > cap || (a.mode != kRelease && (n < 0 || (int64_t)len + n > cap)))
+                flags |= kDevRange;
+            else
+                v[i] = slab_pages(a, len, n);
         }
-        mine += a.mode == kRelease ? (n ? pages_of(len, a.P) : 0) : pages_of((int64_t)len + n, a.P) - pages_of(len, a.P);
+        if (h + 32 * kRound < h1) fetch(h + 32 * kRound);
+#pragma unroll
+        for (int i = 0; i < kRound; ++i) {
+            mine += v[i];
+            int up = v[i];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(kFull, up, o);
+                if (lane >= o) up += y;
+            }
+            if (h + 32 * i + lane < h1) first[h + 32 * i + lane] = run + up - v[i];
+            run += __shfl_sync(kFull, up, 31);
+        }
     }
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) mine += __shfl_xor_sync(kFull, mine, o);
     int64_t pages;
-    int64_t at = block_scan(mine, sh, &pages);
-    const int count = *a.free_count;
+    const int64_t at = block_scan(lane == 31 ? mine : 0, sh->sums, &pages);
     if (count < 0 || count > a.num_pages)
         flags |= kDevRange;
     else if (a.mode == kRelease ? count + pages > a.num_pages : pages > count)
         flags |= a.mode == kRelease ? kDevRange : kDevExhausted;
-    if (flags) atomicOr(&bad, flags);
+    if (flags) atomicOr(&sh->bad, flags);
+    const int base = __shfl_sync(kFull, (int)at, 0);  // pages of the warps before
+    for (int h = h0 + lane; h < h1; h += 32) first[h] += base;
     __syncthreads();
-    const bool ok = bad == 0;
-    if (!ok && a.cu)
-        for (int b = tid; b <= a.B; b += kScanThreads) a.cu[b] = 0;
-    for (int64_t h = h0; h < h1; ++h) {
-        const int len = a.len[h], n = ok ? slab_rows(a, per_slot, (int)h, len) : 0;
-        a.before[h] = len;
-        a.first[h] = (int)at;
-        if (ok) at += a.mode == kRelease ? (n ? pages_of(len, a.P) : 0) : pages_of((int64_t)len + n, a.P) - pages_of(len, a.P);
-        a.new_len[h] = a.mode == kRelease ? len - n : len + n;
-    }
+    *head = PageHead{sh->bad == 0, count, (int)min(tokens, (int64_t)INT32_MAX), (int)pages};
+    return sh->bad == 0;
+}
+
+// What one CTA of the call writes besides pages and slots: status, token offsets, counts.
+__device__ __forceinline__ void write_totals(const PageArgs& a, const ScanShared* sh, const PageHead& head, int32_t* new_count)
+{
+    const int tid = threadIdx.x;
+    if (a.cu)
+        for (int b = tid; b <= a.B; b += kThreads) a.cu[b] = head.ok ? sh->cu[b] : 0;
     if (tid == 0) {
-        *a.head = PageHead{ok, count, (int)min(tokens, (int64_t)INT32_MAX), (int)pages};
-        *a.new_count = ok ? (int)(a.mode == kRelease ? count + pages : count - pages) : count;
-        if (!ok && a.status) atomicOr(a.status, bad);
+        if (!head.ok && a.status) atomicOr(a.status, sh->bad);
+        *new_count = !head.ok ? head.count : a.mode == kRelease ? head.count + head.pages : head.count - head.pages;
     }
 }
 
-constexpr int kFillThreads = 256;
+constexpr int kPagesLane = 8;  // pages of a lane at a time: a warp's 256 are usually of one slab, or of very many
 
-__global__ void __launch_bounds__(kFillThreads) page_fill_kernel(const PageArgs a)
+// For N values j[]: the last slab h in [lo, hi] with first[h] <= j, the one that page j belongs to.
+template <int N>
+__device__ __forceinline__ void slabs_of_pages(const int32_t* first, int lo, int hi, const int (&j)[N], int (&h)[N])
 {
-    __shared__ int32_t cu[kMaxSlots + 1];
-    pdl_wait();
-    const PageHead head = *a.head;
-    if (!head.ok) return;
-    const int lane = threadIdx.x & 31;
-    // Pages: one warp a slab.
-    for (int h = (blockIdx.x * kFillThreads + threadIdx.x) >> 5; h < a.NH; h += gridDim.x * (kFillThreads / 32)) {
-        const int first = a.first[h], next = h + 1 < a.NH ? a.first[h + 1] : head.pages;
-        int32_t* row = a.table + (int64_t)h * a.max_pages;
+#pragma unroll
+    for (int i = 0; i < N; ++i) h[i] = lo;
+    int step = 1;
+    while (step <= hi - lo) step <<= 1;
+#pragma unroll 1
+    for (step >>= 1; step >= 1; step >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (h[i] + step <= hi && first[min(h[i] + step, hi)] <= j[i]) h[i] += step;
+}
+
+// This CTA's share of the table entries (or of the free list's) and of the slot map. first: the
+// scan (shared or global); len: rows of the slabs before the call; cu: token offsets.
+__device__ __forceinline__ void fill(const PageArgs& a, const PageHead& head, const int32_t* first, const int32_t* len, const int32_t* cu)
+{
+    const int tid = threadIdx.x, lane = tid & 31;
+    constexpr int kChunk = 32 * kPagesLane;
+    const int64_t stride = (int64_t)gridDim.x * (kThreads / 32) * kChunk;
+    for (int64_t c0 = ((int64_t)(tid >> 5) * gridDim.x + blockIdx.x) * kChunk; c0 < head.pages; c0 += stride) {
+        const int j0 = (int)c0, j1 = (int)min((int64_t)head.pages, c0 + kChunk);
+        // Lanes 0 and 1 look for the slab of the first and of the last page.
+        const int ends[1] = {lane & 1 ? j1 - 1 : j0};
+        int found[1], j[kPagesLane], h[kPagesLane], page[kPagesLane];
+        slabs_of_pages(first, 0, a.NH - 1, ends, found);
+        const int ha = __shfl_sync(kFull, found[0], 0), hb = __shfl_sync(kFull, found[0], 1);
+#pragma unroll
+        for (int i = 0; i < kPagesLane; ++i) j[i] = min(j0 + 32 * i + lane, j1 - 1);
+        slabs_of_pages(first, ha, hb, j, h);
         if (a.mode == kRelease) {
-            for (int j = lane; j < next - first; j += 32) a.free_pages[head.count + first + j] = row[j];
+#pragma unroll
+            for (int i = 0; i < kPagesLane; ++i) page[i] = a.table[(int64_t)h[i] * a.max_pages + (j[i] - first[h[i]])];
+#pragma unroll
+            for (int i = 0; i < kPagesLane; ++i)
+                if (j0 + 32 * i + lane < j1) a.free_pages[head.count + j[i]] = page[i];
         } else {
-            row += pages_of(a.before[h], a.P);
-            for (int j = lane; j < next - first; j += 32) row[j] = a.free_pages[head.count - 1 - first - j];
+#pragma unroll
+            for (int i = 0; i < kPagesLane; ++i) page[i] = a.free_pages[head.count - 1 - j[i]];
+#pragma unroll
+            for (int i = 0; i < kPagesLane; ++i)
+                if (j0 + 32 * i + lane < j1) a.table[(int64_t)h[i] * a.max_pages + pages_of(a, len[h[i]]) + (j[i] - first[h[i]])] = page[i];
         }
     }
     if (!a.slots) return;
-    for (int b = threadIdx.x; b <= a.B; b += kFillThreads) cu[b] = a.cu[b];
-    __syncthreads();
-    // Slot map: [L][t][Hkv], one thread an entry.
-    const int64_t per_layer = (int64_t)head.total * a.Hkv, n = per_layer * a.L;
-    for (int64_t i = (int64_t)blockIdx.x * kFillThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kFillThreads) {
-        const int l = (int)(i / per_layer);
-        const int64_t x = i - l * per_layer;
-        const int t = (int)(x / a.Hkv), g = (int)(x - (int64_t)t * a.Hkv);
+    // Slot map: [L][t][Hkv], a.slot_vec neighbouring heads a thread. Pages that this call takes
+    // are read from the free list: their table entries may not be written yet.
+    const int vec = a.slot_vec, row = a.Hkv / vec;  // 1 or 4
+    const int64_t per_layer = (int64_t)head.total * row, chunks = (per_layer + kThreads - 1) / kThreads;
+    for (int64_t x = blockIdx.x; x < chunks * a.L; x += gridDim.x) {
+        const int l = (int)(x / chunks);
+        const int64_t i = (x - l * chunks) * kThreads + tid;
+        if (i >= per_layer) continue;
+        const int t = (int)(i / row), g = (int)(i - (int64_t)t * row) * vec;
         int lo = 0, hi = a.B - 1;  // the last sequence that starts at t or before
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
@@ -175,11 +250,73 @@ __global__ void __launch_bounds__(kFillThreads) page_fill_kernel(const PageArgs 
             else
                 hi = mid - 1;
         }
-        const int h = (l * a.B + lo) * a.Hkv + g;
-        const int before = a.before[h], r = before + t - cu[lo], p = r / a.P, had = pages_of(before, a.P);
-        const int page = p < had ? a.table[(int64_t)h * a.max_pages + p] : a.free_pages[head.count - 1 - a.first[h] - (p - had)];
-        a.slots[((int64_t)l * a.max_tokens + t) * a.Hkv + g] = page * a.P + r % a.P;
+        const int h = (l * a.B + lo) * a.Hkv + g, k = t - cu[lo];
+        auto slot = [&](int hh) {
+            const int before = len[hh], r = before + k, p = r >> a.log_P, had = pages_of(a, before);
+            const int page = p < had ? a.table[(int64_t)hh * a.max_pages + p] : a.free_pages[head.count - 1 - first[hh] - (p - had)];
+            return (page << a.log_P) + (r & (a.P - 1));
+        };
+        int32_t* to = a.slots + ((int64_t)l * a.max_tokens + t) * a.Hkv + g;
+        if (vec == 4)
+            *reinterpret_cast<int4*>(to) = make_int4(slot(h), slot(h + 1), slot(h + 2), slot(h + 3));
+        else
+            *to = slot(h);
     }
+}
+
+// The whole call. new_len: the caller's, or the workspace's where that is len itself (then
+// page_commit_kernel follows); new_count the same.
+__global__ void __launch_bounds__(kThreads, 1) page_fused_kernel(const __grid_constant__ PageArgs a, int32_t* new_len, int32_t* new_count)
+{
+    extern __shared__ int32_t first[];
+    __shared__ ScanShared sh;
+    pdl_wait();
+    pdl_launch_dependents();
+    PageHead head;
+    const bool ok = scan_slabs(a, &sh, first, &head);
+    if (blockIdx.x == 0) write_totals(a, &sh, head, new_count);
+    if (ok) fill(a, head, first, a.len, sh.cu);
+    for (int h = blockIdx.x * kThreads + threadIdx.x; h < a.NH; h += gridDim.x * kThreads) {
+        const int len = a.len[h];
+        new_len[h] = ok ? slab_after(a, len, slab_rows(a, sh.per_slot, h)) : len;
+    }
+}
+
+__global__ void __launch_bounds__(kThreads) page_commit_kernel(const __grid_constant__ PageArgs a, const int32_t* from_len, const int32_t* from_count)
+{
+    pdl_wait();
+    const int h = blockIdx.x * kThreads + threadIdx.x;
+    if (a.new_len != from_len && h < a.NH) a.new_len[h] = from_len[h];
+    if (h == 0 && a.new_count != from_count) *a.new_count = *from_count;
+}
+
+// Many slabs: one CTA scans into the workspace and writes lengths and counts; then all fill.
+__global__ void __launch_bounds__(kThreads, 1) page_scan_kernel(const __grid_constant__ PageArgs a)
+{
+    __shared__ ScanShared sh;
+    pdl_wait();
+    pdl_launch_dependents();
+    PageHead head;
+    const bool ok = scan_slabs(a, &sh, a.first, &head);
+    write_totals(a, &sh, head, a.new_count);
+    if (threadIdx.x == 0) *a.head = head;
+    for (int h = threadIdx.x; h < a.NH; h += kThreads) {
+        const int len = a.len[h];
+        a.before[h] = len;
+        a.new_len[h] = ok ? slab_after(a, len, slab_rows(a, sh.per_slot, h)) : len;
+    }
+}
+
+__global__ void __launch_bounds__(kThreads, 1) page_fill_kernel(const __grid_constant__ PageArgs a)
+{
+    __shared__ int32_t cu[kMaxSlots + 1];
+    pdl_wait();
+    const PageHead head = *a.head;
+    if (!head.ok) return;
+    if (a.slots)
+        for (int b = threadIdx.x; b <= a.B; b += kThreads) cu[b] = a.cu[b];
+    __syncthreads();
+    fill(a, head, a.first, a.before, cu);
 }
 
 // ---------------------------------------------------------------- prune-and-pack into pages
@@ -268,6 +405,7 @@ cudaError_t page_setup(int* sms)
     if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
     if ((e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
     if ((e = chunk_setup()) != cudaSuccess) return e;
+    if ((e = cudaFuncSetAttribute(page_fused_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFusedSlabs * 4)) != cudaSuccess) return e;
     if (count < kMost) known[count++] = Known{id, *sms};
     return cudaSuccess;
 }
@@ -277,8 +415,17 @@ cudaError_t launch_page_tables(const PageArgs& a, cudaStream_t st)
     int sms = 0;
     cudaError_t e = page_setup(&sms);
     if (e != cudaSuccess) return e;
-    if ((e = launch_pdl(page_scan_kernel, 1, kScanThreads, 0, st, a)) != cudaSuccess) return e;
-    return launch_pdl(page_fill_kernel, 4 * sms, kFillThreads, 0, st, a);
+    if (a.NH > kFusedSlabs) {
+        if ((e = launch_pdl(page_scan_kernel, 1, kThreads, 0, st, a)) != cudaSuccess) return e;
+        return launch_pdl(page_fill_kernel, sms, kThreads, 0, st, a);
+    }
+    const bool len_in_place = a.new_len == a.len, count_in_place = a.new_count == a.free_count;
+    int32_t* new_len = len_in_place ? a.before : a.new_len;
+    int32_t* new_count = count_in_place ? &a.head->count : a.new_count;
+    if ((e = launch_pdl(page_fused_kernel, sms, kThreads, a.NH * 4, st, a, new_len, new_count)) != cudaSuccess) return e;
+    if (!len_in_place && !count_in_place) return cudaSuccess;
+    const int32_t *from_len = new_len, *from_count = new_count;
+    return launch_pdl(page_commit_kernel, len_in_place ? (a.NH + kThreads - 1) / kThreads : 1, kThreads, 0, st, a, from_len, from_count);
 }
 
 cudaError_t launch_page_compact(const PageCompactArgs& a, cudaStream_t st)

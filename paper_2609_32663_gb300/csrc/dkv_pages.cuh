@@ -24,7 +24,8 @@ PlanView plan_view(const dkv_plan* p);
 dkv_status set_error(dkv_status st, const char* msg);
 
 // Workspace of dkv_page_tables and dkv_page_release: a header, then for every slab the
-// position of its first page among the pages that the call moves, and its rows before.
+// position of its first page among the pages that the call moves, and its rows before (or,
+// where the lengths are updated in place by one kernel and committed by another, after).
 struct PageHead {
     int32_t ok;      // 0: the call changes nothing
     int32_t count;   // free pages before the call
@@ -37,7 +38,8 @@ inline int64_t page_workspace_bytes(int64_t NH) { return kPageHeadBytes + 2 * ((
 enum PageMode { kGrowTokens, kGrowPlan, kRelease };
 
 struct PageArgs {
-    int L, B, Hkv, NH, P, num_pages, max_pages;
+    int L, B, Hkv, NH, P, log_P, num_pages, max_pages;
+    int slot_vec;              // entries of the slot map a thread writes at once: 4 where they are aligned, else 1
     int mode;                  // PageMode
     const int32_t* tokens;     // [B] new tokens (kGrowTokens) or ended flags (kRelease)
     const int32_t* plan_len;   // kGrowPlan: [L][planB][Hkv] kept rows

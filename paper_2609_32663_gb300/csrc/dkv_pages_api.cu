@@ -94,6 +94,7 @@ dkv_status page_args(const dkv_pages* g, const int32_t* len, int32_t* new_len, c
     a->Hkv = g->H_kv;
     a->NH = (int)NH;
     a->P = g->page_rows;
+    while ((1 << a->log_P) < a->P) ++a->log_P;
     a->num_pages = g->num_pages;
     a->max_pages = g->max_pages;
     a->len = len;
@@ -150,6 +151,7 @@ dkv_status dkv_page_tables(const dkv_pages* g, const int32_t* tokens, const dkv_
     a.cu = cu_tokens;
     a.slots = slots;
     a.max_tokens = max_tokens;
+    a.slot_vec = g->H_kv % 4 == 0 && aligned(slots, 16) ? 4 : 1;
     return launched(dkv::launch_page_tables(a, stream), "page table kernels");
 }
 

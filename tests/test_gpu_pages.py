@@ -79,6 +79,35 @@ def test_tables(cuda, page, L, B, Hkv, most, tokens, alias):
     assert np.array_equal(slots.cpu().numpy(), want_slots)
 
 
+def test_more_slabs_than_one_launch_takes(cuda):
+    """Past 49,152 slabs the scan is a launch of its own."""
+    L, B, Hkv = 2, 100, 251
+    r = np.random.default_rng(1)
+    lens, tokens = r.integers(0, 41, (L, B, Hkv)), [i % 4 for i in range(100)]
+    n = np.broadcast_to(np.asarray(tokens)[None, :, None], lens.shape)
+    cache = paged.Cache(np.zeros((1, 1, 1), int), 16)
+    cache.L, cache.B, cache.Hkv, cache.lens = L, B, Hkv, lens.reshape(-1).astype(np.int64)
+    pages = -(-cache.lens // 16)
+    order = r.permutation(int(pages.sum()) + 20000).astype(np.int32)
+    cache.table = np.full((cache.lens.size, 6), -1, np.int32)
+    cache.table[np.arange(6)[None] < pages[:, None]] = order[:int(pages.sum())]
+    cache.free, cache.count = np.concatenate([order[int(pages.sum()):], np.full(int(pages.sum()), -7, np.int32)]), 20000
+    cache.pages = dkv.Pages(L=L, B=B, H=Hkv, H_kv=Hkv, page_rows=16, num_pages=order.size, max_pages=6)
+    for alias in (False, True):
+        s = State(cache)
+        if alias:
+            s.new_len, s.new_count = s.len, s.count
+        cu, slots = dev(np.zeros(B + 1)), dev(np.full((L, sum(tokens) + 1, Hkv), -3))
+        s.tables(tokens=dev(tokens), cu_tokens=cu, slots=slots)
+        table, free, count, ln = paged.tables_after(cache, n)
+        s.same(table, free, count, ln)
+        assert np.array_equal(slots.cpu().numpy(), slot_map(cache, table, tokens, sum(tokens) + 1)[1])
+        s = State(cache)
+        ended = r.integers(0, 2, B)
+        s.release(ended)
+        s.same(*paged.tables_after(cache, np.broadcast_to(ended[None, :, None], lens.shape), release=True))
+
+
 def test_tables_without_slot_map_or_offsets(cuda):
     cache = paged.Cache(np.array([[[5], [16]]]), 16, spare=4)
     for kw in ({}, {"cu_tokens": dev([7, 7, 7])}):
