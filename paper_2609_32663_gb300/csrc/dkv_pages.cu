@@ -57,14 +57,51 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* sh, int64_t* t
 
 __device__ __forceinline__ int pages_of(const PageArgs& a, int64_t rows) { return (int)((rows + a.P - 1) >> a.log_P); }
 
-// Rows that slab h gains (grow; negative: out of range), or whether it ends (release).
-// per_slot: new tokens, ended flags or the plan's sequence (-1: none) of each slot.
-__device__ __forceinline__ int slab_rows(const PageArgs& a, const int32_t* per_slot, int h)
-{
-    const int lb = h / a.Hkv, l = lb / a.B, x = per_slot[lb - l * a.B];
-    if (a.mode != kGrowPlan) return x;
-    return x < 0 ? 0 : a.plan_len[((int64_t)l * a.planB + x) * a.Hkv + (h - lb * a.Hkv)];
-}
+// A slab's place, moved on without divisions.
+struct Slab {
+    int l, b, g;
+    __device__ __forceinline__ void at(const PageArgs& a, int h)
+    {
+        const int lb = h / a.Hkv;
+        g = h - lb * a.Hkv;
+        l = lb / a.B;
+        b = lb - l * a.B;
+    }
+    __device__ __forceinline__ void carry(const PageArgs& a)
+    {
+        while (b >= a.B) {
+            b -= a.B;
+            ++l;
+        }
+    }
+    __device__ __forceinline__ void next(const PageArgs& a)
+    {
+        if (++g == a.Hkv) {
+            g = 0;
+            ++b;
+            carry(a);
+        }
+    }
+    // 124 slabs on (a.skip_b slots and a.skip_g heads).
+    __device__ __forceinline__ void skip(const PageArgs& a)
+    {
+        b += a.skip_b;
+        g += a.skip_g;
+        if (g >= a.Hkv) {
+            g -= a.Hkv;
+            ++b;
+        }
+        carry(a);
+    }
+    // Rows that the slab gains (grow; negative: out of range), or whether it ends (release).
+    // per_slot: new tokens, ended flags or the plan's sequence (-1: none) of each slot.
+    __device__ __forceinline__ int rows(const PageArgs& a, const int32_t* per_slot) const
+    {
+        const int x = per_slot[b];
+        if (a.mode != kGrowPlan) return x;
+        return x < 0 ? 0 : a.plan_len[((int64_t)l * a.planB + x) * a.Hkv + g];
+    }
+};
 
 // Pages that a slab of len rows takes (n new rows) or gives back (n: it ends).
 __device__ __forceinline__ int slab_pages(const PageArgs& a, int len, int n)
@@ -91,16 +128,16 @@ __device__ __forceinline__ bool scan_slabs(const PageArgs& a, ScanShared* sh, in
 {
     const int tid = threadIdx.x;
     if (tid == 0) sh->bad = 0;
-    // A contiguous piece of the slabs a warp, 32 at a time; the first lengths are on their way at once.
-    constexpr int kRound = 4;
-    const int lane = tid & 31, per = (a.NH + kThreads - 1) / kThreads * 32;
-    const int h0 = (int)min((int64_t)a.NH, (int64_t)(tid >> 5) * per), h1 = (int)min((int64_t)a.NH, (int64_t)h0 + per);
-    int lens[kRound];
+    // A contiguous piece of the slabs a warp, 128 at a time, four neighbours a lane; the first
+    // lengths are on their way at once.
+    const int lane = tid & 31, warp = tid >> 5, per = (a.NH + 128 * (kThreads / 32) - 1) / (128 * (kThreads / 32)) * 128;
+    const int h0 = (int)min((int64_t)a.NH, (int64_t)warp * per), h1 = (int)min((int64_t)a.NH, (int64_t)h0 + per);
+    int lens[4];
     auto fetch = [&](int h) {
 #pragma unroll
-        for (int i = 0; i < kRound; ++i) lens[i] = h + 32 * i + lane < h1 ? a.len[h + 32 * i + lane] : 0;
+        for (int i = 0; i < 4; ++i) lens[i] = h + i < h1 ? a.len[h + i] : 0;
     };
-    fetch(h0);
+    fetch(h0 + 4 * lane);
     const int count = *a.free_count;
     for (int b = tid; b < a.B; b += kThreads) sh->per_slot[b] = a.mode == kGrowPlan ? -1 : a.tokens[b];
     __syncthreads();
@@ -115,46 +152,63 @@ __device__ __forceinline__ bool scan_slabs(const PageArgs& a, ScanShared* sh, in
         }
         __syncthreads();
     }
-    int64_t tokens = 0;
-    if (a.mode == kGrowTokens) {
-        static_assert(kMaxSlots <= kThreads, "one thread a slot");
-        const int n = tid < a.B ? sh->per_slot[tid] : 0;
-        if (n < 0) flags |= kDevRange;
-        const int64_t before = block_scan(max(n, 0), sh->sums, &tokens);
-        if (tid < a.B) sh->cu[tid] = (int)min(before, (int64_t)INT32_MAX);
-        if (tid == 0) sh->cu[a.B] = (int)min(tokens, (int64_t)INT32_MAX);
-        if (tokens > (a.slots ? a.max_tokens : (int64_t)INT32_MAX)) flags |= kDevRange;
+    if (a.mode == kGrowTokens && warp == kThreads / 32 - 1) {
+        // The last warp scans the tokens.
+        int64_t sum = 0;
+        for (int b0 = 0; b0 < a.B; b0 += 32) {
+            const int n = b0 + lane < a.B ? sh->per_slot[b0 + lane] : 0;
+            if (n < 0) flags |= kDevRange;
+            int64_t up = max(n, 0);
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int64_t y = __shfl_up_sync(kFull, up, o);
+                if (lane >= o) up += y;
+            }
+            if (b0 + lane < a.B) sh->cu[b0 + lane + 1] = (int)min(sum + up, (int64_t)INT32_MAX);
+            sum += __shfl_sync(kFull, up, 31);
+        }
+        if (lane == 0) sh->cu[0] = 0;
+        if (sum > (a.slots ? a.max_tokens : (int64_t)INT32_MAX)) flags |= kDevRange;
     }
     const int64_t cap = (int64_t)a.max_pages << a.log_P;
     int64_t mine = 0;  // this lane's pages; `run`: the warp's so far (32 bits do: it is used only if the sum fits)
     int run = 0;
+    Slab s;
+    s.at(a, h0 + 4 * lane);
 #pragma unroll 1
-    for (int h = h0; h < h1; h += 32 * kRound) {
-        int v[kRound];
+    for (int h = h0; h < h1; h += 128) {
+        const int x = h + 4 * lane;
+        int v[4], sum = 0;
 #pragma unroll
-        for (int i = 0; i < kRound; ++i) {
-            const int x = h + 32 * i + lane, len = lens[i];
-            v[i] = 0;
-            if (x >= h1) continue;
-            const int n = slab_rows(a, sh->per_slot, x);
-            if (len < 0 || len > cap || (a.mode != kRelease && (n < 0 || (int64_t)len + n > cap)))
-                flags |= kDevRange;
-            else
-                v[i] = slab_pages(a, len, n);
-        }
-        if (h + 32 * kRound < h1) fetch(h + 32 * kRound);
-#pragma unroll
-        for (int i = 0; i < kRound; ++i) {
-            mine += v[i];
-            int up = v[i];
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(kFull, up, o);
-                if (lane >= o) up += y;
+        for (int i = 0; i < 4; ++i) {
+            const int len = lens[i];
+            v[i] = sum;
+            if (x + i < h1) {
+                const int n = s.rows(a, sh->per_slot);
+                if (len < 0 || len > cap || (a.mode != kRelease && (n < 0 || (int64_t)len + n > cap))) {
+                    flags |= kDevRange;
+                } else {
+                    const int pages = slab_pages(a, len, n);
+                    sum += pages;
+                    mine += pages;
+                }
             }
-            if (h + 32 * i + lane < h1) first[h + 32 * i + lane] = run + up - v[i];
-            run += __shfl_sync(kFull, up, 31);
+            s.next(a);
         }
+        s.skip(a);
+        if (h + 128 < h1) fetch(x + 128);
+        int up = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(kFull, up, o);
+            if (lane >= o) up += y;
+        }
+        const int before = run + up - sum;
+        if (x + 3 < h1)
+            *reinterpret_cast<int4*>(first + x) = make_int4(before + v[0], before + v[1], before + v[2], before + v[3]);
+        else
+            for (int i = 0; x + i < h1; ++i) first[x + i] = before + (i == 0 ? v[0] : i == 1 ? v[1] : v[2]);
+        run += __shfl_sync(kFull, up, 31);
     }
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1) mine += __shfl_xor_sync(kFull, mine, o);
@@ -168,7 +222,7 @@ __device__ __forceinline__ bool scan_slabs(const PageArgs& a, ScanShared* sh, in
     const int base = __shfl_sync(kFull, (int)at, 0);  // pages of the warps before
     for (int h = h0 + lane; h < h1; h += 32) first[h] += base;
     __syncthreads();
-    *head = PageHead{sh->bad == 0, count, (int)min(tokens, (int64_t)INT32_MAX), (int)pages};
+    *head = PageHead{sh->bad == 0, count, a.mode == kGrowTokens ? sh->cu[a.B] : 0, (int)pages};
     return sh->bad == 0;
 }
 
@@ -184,7 +238,13 @@ __device__ __forceinline__ void write_totals(const PageArgs& a, const ScanShared
     }
 }
 
-constexpr int kPagesLane = 8;  // pages of a lane at a time: a warp's 256 are usually of one slab, or of very many
+// A load that stays ahead of what follows it (volatile).
+__device__ __forceinline__ int load_now(const int32_t* p)
+{
+    int v;
+    asm volatile("ld.global.s32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
 
 // For N values j[]: the last slab h in [lo, hi] with first[h] <= j, the one that page j belongs to.
 template <int N>
@@ -201,47 +261,82 @@ __device__ __forceinline__ void slabs_of_pages(const int32_t* first, int lo, int
             if (h[i] + step <= hi && first[min(h[i] + step, hi)] <= j[i]) h[i] += step;
 }
 
+// Pages c0 + 32 i + lane (i < N; up to `end`) of the call, of slabs ha .. hb (one warp).
+template <int N>
+__device__ __forceinline__ void fill_pages(const PageArgs& a, const PageHead& head, const int32_t* first, const int32_t* len, int c0, int end, int ha, int hb)
+{
+    const int lane = threadIdx.x & 31;
+    int j[N], h[N], page[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) j[i] = min(end - 1, c0 + 32 * i + lane);
+    slabs_of_pages(first, ha, hb, j, h);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        page[i] = a.mode == kRelease ? a.table[(int64_t)h[i] * a.max_pages + (j[i] - first[h[i]])] : a.free_pages[head.count - 1 - j[i]];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (c0 + 32 * i + lane >= end) continue;
+        if (a.mode == kRelease)
+            a.free_pages[head.count + j[i]] = page[i];
+        else
+            a.table[(int64_t)h[i] * a.max_pages + pages_of(a, len[h[i]]) + (j[i] - first[h[i]])] = page[i];
+    }
+}
+
+constexpr int kLong = 8;  // pages of a lane on their way at once in a run of one slab
+
+// Chunk after chunk of 32 kLong pages (one warp): a run of one slab, as most are when there are so
+// many pages, is copied as it is.
+__device__ __forceinline__ void fill_chunks(const PageArgs& a, const PageHead& head, const int32_t* first, const int32_t* len, int64_t c0, int64_t stride)
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (; c0 < head.pages; c0 += stride) {
+        const int j0 = (int)c0, end = (int)min((int64_t)head.pages, c0 + 32 * kLong);
+        const int one[1] = {lane & 1 ? end - 1 : j0};  // lanes 0 and 1: the slabs of the first and the last page
+        int found[1];
+        slabs_of_pages(first, 0, a.NH - 1, one, found);
+        const int ha = __shfl_sync(kFull, found[0], 0), hb = __shfl_sync(kFull, found[0], 1);
+        if (ha != hb) {
+#pragma unroll 1
+            for (int j = j0; j < end; j += 128) fill_pages<4>(a, head, first, len, j, end, ha, hb);
+            continue;
+        }
+        const int32_t* from = a.mode == kRelease ? a.table + ((int64_t)ha * a.max_pages + (j0 - first[ha])) : a.free_pages + (head.count - 1 - j0);
+        int32_t* to = a.mode == kRelease ? a.free_pages + head.count + j0 : a.table + ((int64_t)ha * a.max_pages + pages_of(a, len[ha]) + (j0 - first[ha]));
+        const int step = a.mode == kRelease ? 1 : -1, n = end - j0;
+        int page[kLong];
+#pragma unroll
+        for (int i = 0; i < kLong; ++i) page[i] = 32 * i + lane < n ? load_now(from + step * (32 * i + lane)) : 0;
+#pragma unroll
+        for (int i = 0; i < kLong; ++i)
+            if (32 * i + lane < n) to[32 * i + lane] = page[i];
+    }
+}
+
 // This CTA's share of the table entries (or of the free list's) and of the slot map. first: the
 // scan (shared or global); len: rows of the slabs before the call; cu: token offsets.
 __device__ __forceinline__ void fill(const PageArgs& a, const PageHead& head, const int32_t* first, const int32_t* len, const int32_t* cu)
 {
-    const int tid = threadIdx.x, lane = tid & 31;
-    constexpr int kChunk = 32 * kPagesLane;
-    const int64_t stride = (int64_t)gridDim.x * (kThreads / 32) * kChunk;
-    for (int64_t c0 = ((int64_t)(tid >> 5) * gridDim.x + blockIdx.x) * kChunk; c0 < head.pages; c0 += stride) {
-        const int j0 = (int)c0, j1 = (int)min((int64_t)head.pages, c0 + kChunk);
-        // Lanes 0 and 1 look for the slab of the first and of the last page.
-        const int ends[1] = {lane & 1 ? j1 - 1 : j0};
-        int found[1], j[kPagesLane], h[kPagesLane], page[kPagesLane];
-        slabs_of_pages(first, 0, a.NH - 1, ends, found);
-        const int ha = __shfl_sync(kFull, found[0], 0), hb = __shfl_sync(kFull, found[0], 1);
-#pragma unroll
-        for (int i = 0; i < kPagesLane; ++i) j[i] = min(j0 + 32 * i + lane, j1 - 1);
-        slabs_of_pages(first, ha, hb, j, h);
-        if (a.mode == kRelease) {
-#pragma unroll
-            for (int i = 0; i < kPagesLane; ++i) page[i] = a.table[(int64_t)h[i] * a.max_pages + (j[i] - first[h[i]])];
-#pragma unroll
-            for (int i = 0; i < kPagesLane; ++i)
-                if (j0 + 32 * i + lane < j1) a.free_pages[head.count + j[i]] = page[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < kPagesLane; ++i) page[i] = a.free_pages[head.count - 1 - j[i]];
-#pragma unroll
-            for (int i = 0; i < kPagesLane; ++i)
-                if (j0 + 32 * i + lane < j1) a.table[(int64_t)h[i] * a.max_pages + pages_of(a, len[h[i]]) + (j[i] - first[h[i]])] = page[i];
-        }
-    }
+    const int warps = gridDim.x * (kThreads / 32), warp = (threadIdx.x >> 5) * gridDim.x + blockIdx.x;
+    // One page a lane while that is enough (latency counts). Chunks of neighbouring warps lie side by side:
+    // a contiguous piece a warp took 54 us where this takes 40, for the release of 12.8 M pages.
+    if (head.pages > warps * 32)
+        fill_chunks(a, head, first, len, (int64_t)warp * 32 * kLong, (int64_t)warps * 32 * kLong);
+    else if (warp * 32 < head.pages)
+        fill_pages<1>(a, head, first, len, warp * 32, head.pages, 0, a.NH - 1);
     if (!a.slots) return;
-    // Slot map: [L][t][Hkv], a.slot_vec neighbouring heads a thread. Pages that this call takes
+    // Slot map [L][t][Hkv], a.slot_vec neighbouring heads (1 or 4) a thread. Pages that this call takes
     // are read from the free list: their table entries may not be written yet.
-    const int vec = a.slot_vec, row = a.Hkv / vec;  // 1 or 4
+    const int vec = a.slot_vec, row = a.Hkv / vec;
     const int64_t per_layer = (int64_t)head.total * row, chunks = (per_layer + kThreads - 1) / kThreads;
+    const bool small = chunks * a.L <= INT32_MAX && per_layer <= INT32_MAX - kThreads;  // 32-bit divisions
+#pragma unroll 1
     for (int64_t x = blockIdx.x; x < chunks * a.L; x += gridDim.x) {
-        const int l = (int)(x / chunks);
-        const int64_t i = (x - l * chunks) * kThreads + tid;
+        const int l = small ? (int)((unsigned)x / (unsigned)chunks) : (int)(x / chunks);
+        const int64_t i = (x - l * chunks) * kThreads + threadIdx.x;
         if (i >= per_layer) continue;
-        const int t = (int)(i / row), g = (int)(i - (int64_t)t * row) * vec;
+        const int t = small ? (int)((unsigned)i / (unsigned)row) : (int)(i / row), g = (int)(i - (int64_t)t * row) * vec;
         int lo = 0, hi = a.B - 1;  // the last sequence that starts at t or before
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
@@ -253,8 +348,8 @@ __device__ __forceinline__ void fill(const PageArgs& a, const PageHead& head, co
         const int h = (l * a.B + lo) * a.Hkv + g, k = t - cu[lo];
         auto slot = [&](int hh) {
             const int before = len[hh], r = before + k, p = r >> a.log_P, had = pages_of(a, before);
-            const int page = p < had ? a.table[(int64_t)hh * a.max_pages + p] : a.free_pages[head.count - 1 - first[hh] - (p - had)];
-            return (page << a.log_P) + (r & (a.P - 1));
+            const int* from = p < had ? a.table + (int64_t)hh * a.max_pages + p : a.free_pages + (head.count - 1 - first[hh] - (p - had));
+            return (*from << a.log_P) + (r & (a.P - 1));
         };
         int32_t* to = a.slots + ((int64_t)l * a.max_tokens + t) * a.Hkv + g;
         if (vec == 4)
@@ -268,7 +363,7 @@ __device__ __forceinline__ void fill(const PageArgs& a, const PageHead& head, co
 // page_commit_kernel follows); new_count the same.
 __global__ void __launch_bounds__(kThreads, 1) page_fused_kernel(const __grid_constant__ PageArgs a, int32_t* new_len, int32_t* new_count)
 {
-    extern __shared__ int32_t first[];
+    extern __shared__ __align__(16) int32_t first[];
     __shared__ ScanShared sh;
     pdl_wait();
     pdl_launch_dependents();
@@ -277,8 +372,10 @@ __global__ void __launch_bounds__(kThreads, 1) page_fused_kernel(const __grid_co
     if (blockIdx.x == 0) write_totals(a, &sh, head, new_count);
     if (ok) fill(a, head, first, a.len, sh.cu);
     for (int h = blockIdx.x * kThreads + threadIdx.x; h < a.NH; h += gridDim.x * kThreads) {
+        Slab s;
+        s.at(a, h);
         const int len = a.len[h];
-        new_len[h] = ok ? slab_after(a, len, slab_rows(a, sh.per_slot, h)) : len;
+        new_len[h] = ok ? slab_after(a, len, s.rows(a, sh.per_slot)) : len;
     }
 }
 
@@ -301,9 +398,11 @@ __global__ void __launch_bounds__(kThreads, 1) page_scan_kernel(const __grid_con
     write_totals(a, &sh, head, a.new_count);
     if (threadIdx.x == 0) *a.head = head;
     for (int h = threadIdx.x; h < a.NH; h += kThreads) {
+        Slab s;
+        s.at(a, h);
         const int len = a.len[h];
         a.before[h] = len;
-        a.new_len[h] = ok ? slab_after(a, len, slab_rows(a, sh.per_slot, h)) : len;
+        a.new_len[h] = ok ? slab_after(a, len, s.rows(a, sh.per_slot)) : len;
     }
 }
 
