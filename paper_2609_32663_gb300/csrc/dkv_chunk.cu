@@ -9,8 +9,9 @@
 // equal contiguous shares, one a CTA, one CTA an SM, so ragged lengths leave no SM idle; a unit
 // that lies in several CTAs is joined by the one that finishes last.
 //
-//   chunk_prologue_kernel  appends the rows, counts the tiles and finds where each CTA starts.
-//   chunk_attn_kernel      two pipelines of S = Q K^T, softmax, O += P V, one a softmax group:
+//   chunk_append_kernel  appends the rows.
+//   chunk_attn_kernel    starts beside it, finds its shares, and waits for the append only where a
+//                        tile holds new rows. Two pipelines of S = Q K^T, softmax, O += P V, one a softmax group:
 //     pair units (more than TQ tokens): group p has query tile p; both use the same K and V tile.
 //     split units (decode, drafts, the rest of a turn): one query tile; group p takes the cache
 //     tiles of parity p, and the groups' (m, l, O) are joined at the unit's end.
@@ -60,23 +61,12 @@ constexpr int kSmemBytes = kOffMl + 2 * kTile * 8;
 static_assert(kSmemBytes <= 227 * 1024, "fits one CTA");
 
 // Workspace.
-struct alignas(16) ChunkStart {  // a CTA's share
-    int64_t tiles;   // of the whole call
-    int64_t pos, end;  // the share's
-    int32_t parts;   // CTAs with a share; 0: none, and nothing else is set
-    int32_t b, g, i, first;  // sequence, KV head, unit of the sequence, and its first tile in the share
-    int32_t t, n, len;       // the sequence's first token and tokens, rows of the slab
-    int32_t pad[2];
-};
-static_assert(sizeof(ChunkStart) == 64, "four 16-byte loads");
 struct ChunkWork {
-    ChunkStart* start;  // [kMaxCtas]
     int32_t* done;      // [kMaxCtas] finished pieces of the unit that starts in CTA c and ends in a later one
     float2* ml;         // [kMaxCtas][2][256]
     float4* o;          // [kMaxCtas][2][128 / 4][256]: a warp's rows side by side
 };
-constexpr int64_t kOffDone = kMaxCtas * sizeof(ChunkStart), kOffPieceMl = (kOffDone + kMaxCtas * 4 + 255) / 256 * 256,
-                  kOffPieceO = kOffPieceMl + (int64_t)kMaxCtas * 2 * kPieceRows * 8,
+constexpr int64_t kOffPieceMl = (kMaxCtas * 4 + 255) / 256 * 256, kOffPieceO = kOffPieceMl + (int64_t)kMaxCtas * 2 * kPieceRows * 8,
                   kWorkBytes = kOffPieceO + (int64_t)kMaxCtas * 2 * kPieceRows * kHeadDim * 4;
 
 struct ChunkMaps {
@@ -94,6 +84,7 @@ struct Unit {
     int row0;    // rows that the first token sees (causal), before the clamp to [0, len]
     int len;     // rows of the slab
     int kv;      // rows that the last token sees
+    int fresh;   // rows that this call appends to the slab
     bool pair;   // two query tiles
     __device__ __forceinline__ int tiles() const { return max(1, (kv + kTile - 1) / kTile); }
 };
@@ -115,6 +106,7 @@ __device__ __forceinline__ Unit make_unit(const ChunkArgs& a, int h, int t, int 
     u.row0 = a.causal ? len - n + i * w + 1 : len;
     u.kv = a.causal ? max(0, u.row0 + u.tokens - 1) : len;
     u.pair = u.tokens > TQ;
+    u.fresh = n;
     return u;
 }
 
@@ -129,17 +121,6 @@ struct Walk {
         tiles = u.tiles();
         j0 = off;
         j1 = (int)min((int64_t)tiles, off + (end - pos));
-    }
-    __device__ __forceinline__ void begin(const ChunkArgs& a, const ChunkStart& s)
-    {
-        pos = s.pos;
-        end = s.end;
-        b = s.b;
-        g = s.g;
-        i = s.i;
-        t = s.t;
-        n = s.n;
-        enter(a, s.len, s.first);
     }
     __device__ __forceinline__ bool next(const ChunkArgs& a)
     {
@@ -191,130 +172,56 @@ __device__ __forceinline__ Piece read_piece(const unsigned char* at)
     return x.p;
 }
 
+// The whole call: cache tiles of all units, and CTAs with a share of them.
+struct Extent {
+    int64_t tiles;
+    int parts;
+};
+
 // The CTA whose share holds tile x of the call.
-__device__ __forceinline__ int cta_of(const ChunkStart& s, int64_t x) { return (int)(((x + 1) * s.parts - 1) / s.tiles); }
-
-// ---------------------------------------------------------------- append and schedule
-constexpr int kProThreads = 512;
-
-// Sum of x over the block's earlier threads; *total receives the whole sum.
-__device__ __forceinline__ int64_t scan_block(int64_t x, int64_t* sh, int64_t* total)
-{
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int64_t v = x;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(kFull, v, o);
-        if (lane >= o) v += y;
-    }
-    __syncthreads();
-    if (lane == 31) sh[warp] = v;
-    __syncthreads();
-    int64_t before = 0, all = 0;
-#pragma unroll
-    for (int k = 0; k < kProThreads / 32; ++k) {
-        if (k < warp) before += sh[k];
-        all += sh[k];
-    }
-    *total = all;
-    return v - x + before;
-}
+__device__ __forceinline__ int cta_of(const Extent& e, int64_t x) { return (int)(((x + 1) * e.parts - 1) / e.tiles); }
 
 __device__ __forceinline__ void report(const ChunkArgs& a, int bits)
 {
     if (a.status) atomicOr(a.status, bits);
 }
 
-constexpr int kMaxSlabs = 4096;  // of a layer, whose prefix sums fit shared memory; more are summed in groups
+// ---------------------------------------------------------------- append
+constexpr int kAppThreads = 512;
 
-// One block: the tiles of every slab, and where each CTA's share starts.
-__device__ __forceinline__ void schedule(const ChunkArgs& a, const ChunkWork& w, const int32_t* cu, int nctas)
-{
-    __shared__ int64_t sh[kProThreads / 32];
-    __shared__ int64_t before[kMaxSlabs];  // tiles of the groups of slabs before
-    const int tid = threadIdx.x, width = 2 * (kTile / a.G), slabs = a.B * a.Hkv;
-    const int group = (slabs + kMaxSlabs - 1) / kMaxSlabs, groups = (slabs + group - 1) / group;
-    for (int c = tid; c < kMaxCtas; c += kProThreads) w.done[c] = 0;
-    if (tid < a.B) {
-        const int t0 = a.cu[tid], t1 = a.cu[tid + 1];
-        if (t0 < 0 || t1 < t0 || t1 > a.T || (tid == 0 && t0 != 0)) report(a, DKV_DEV_PAGE_RANGE);
-    }
-    auto slab_tiles = [&](int h, int& t, int& n, int& len) -> int64_t {
-        const int b = h / a.Hkv, raw = a.len[h];
-        t = cu[b];
-        n = max(cu[b + 1] - t, 0);
-        len = slab_len(a, h);
-        if (n > 0 && (raw != len || (a.k_new && raw < n))) report(a, DKV_DEV_PAGE_RANGE);
-        int64_t sum = 0;
-#pragma unroll 1
-        for (int i = 0; i * width < n; ++i) sum += make_unit(a, h, t, n, len, i).tiles();
-        return sum;
-    };
-    // A contiguous piece of the groups a thread.
-    const int per = (groups + kProThreads - 1) / kProThreads, g0 = min(groups, tid * per), g1 = min(groups, g0 + per);
-    int64_t mine = 0;
-    int t, n, len;
-#pragma unroll 1
-    for (int x = g0; x < g1; ++x) {
-        before[x] = mine;
-#pragma unroll 1
-        for (int h = x * group; h < min(slabs, (x + 1) * group); ++h) mine += slab_tiles(h, t, n, len);
-    }
-    int64_t total;
-    const int64_t base = scan_block(mine, sh, &total);
-#pragma unroll 1
-    for (int x = g0; x < g1; ++x) before[x] += base;
-    __syncthreads();
-    const int parts = (int)min(total, (int64_t)nctas);
-    if (tid >= nctas) return;
-    ChunkStart s{total, 0, 0, parts};
-    if (tid < parts) {
-        const int64_t at = total * tid / parts;
-        s.pos = at;
-        s.end = total * (tid + 1) / parts;
-        int lo = 0, hi = groups - 1;  // the last group that starts at tile `at` or before (it has tiles)
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (before[mid] <= at)
-                lo = mid;
-            else
-                hi = mid - 1;
-        }
-        int64_t off = at - before[lo];
-        int h = lo * group;
-        if (group > 1)
-            for (int64_t x = slab_tiles(h, t, n, len); off >= x; x = slab_tiles(++h, t, n, len)) off -= x;
-        s.b = h / a.Hkv;
-        s.g = h - s.b * a.Hkv;
-        s.t = cu[s.b];
-        s.n = max(cu[s.b + 1] - s.t, 0);
-        s.len = slab_len(a, h);
-#pragma unroll 1
-        for (int x; off >= (x = make_unit(a, h, s.t, s.n, s.len, s.i).tiles()); ++s.i) off -= x;
-        s.first = (int)off;
-    }
-    w.start[tid] = s;
-}
-
-__global__ void __launch_bounds__(kProThreads) chunk_prologue_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkWork w, int nctas)
+__global__ void __launch_bounds__(kAppThreads) chunk_append_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkWork w)
 {
     __shared__ int32_t cu[kMaxSlots + 1];
-    static_assert(kMaxSlots <= kProThreads && kMaxCtas <= kProThreads, "one thread each");
+    static_assert(kMaxSlots <= kAppThreads && kMaxCtas <= kAppThreads, "one thread each");
+    const int tid = threadIdx.x;
     pdl_wait();
     pdl_launch_dependents();
-    if (threadIdx.x < a.B) cu[threadIdx.x] = cu_at(a, threadIdx.x);
-    if (threadIdx.x == 0) cu[a.B] = cu_at(a, a.B);
-    __syncthreads();
     if (blockIdx.x == 0) {
-        schedule(a, w, cu, nctas);
+        // The attention kernel's counters, and the checks of what lives on the device.
+        if (tid < kMaxCtas) w.done[tid] = 0;
+        if (tid < a.B) {
+            const int t0 = a.cu[tid], t1 = a.cu[tid + 1];
+            if (t0 < 0 || t1 < t0 || t1 > a.T || (tid == 0 && t0 != 0)) report(a, DKV_DEV_PAGE_RANGE);
+        }
+        for (int h = tid; h < a.B * a.Hkv; h += kAppThreads) {
+            const int b = h / a.Hkv, n = cu_at(a, b + 1) - cu_at(a, b), len = a.len[h];
+            if (n > 0 && (len != slab_len(a, h) || (a.k_new && len < n))) report(a, DKV_DEV_PAGE_RANGE);
+        }
         return;
     }
-    // Append: a half-warp a row (K and V).
-    const int64_t i = (int64_t)(blockIdx.x - 1) * (kProThreads / 16) + (threadIdx.x >> 4);
-    const int sub = threadIdx.x & 15, t = (int)(i / a.Hkv), g = (int)(i - (int64_t)t * a.Hkv);
-    if (t >= cu[a.B]) return;
+    if (tid < a.B) cu[tid] = cu_at(a, tid);
+    if (tid == 0) cu[a.B] = cu_at(a, a.B);
+    // A half-warp a row (K and V).
+    const int64_t i = (int64_t)(blockIdx.x - 1) * (kAppThreads / 16) + (tid >> 4);
+    const int sub = tid & 15, t = (int)(i / a.Hkv), g = (int)(i - (int64_t)t * a.Hkv);
     const int64_t src = t * a.kv_stride + g * kHeadDim;
-    const uint4 kv = __ldcs(reinterpret_cast<const uint4*>(a.k_new + src) + sub), vv = __ldcs(reinterpret_cast<const uint4*>(a.v_new + src) + sub);
+    uint4 kv, vv;
+    if (t < a.T) {
+        kv = __ldcs(reinterpret_cast<const uint4*>(a.k_new + src) + sub);
+        vv = __ldcs(reinterpret_cast<const uint4*>(a.v_new + src) + sub);
+    }
+    __syncthreads();
+    if (t >= cu[a.B]) return;
     int lo = 0, hi = a.B - 1;  // the last sequence that starts at t or before
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -334,6 +241,83 @@ __global__ void __launch_bounds__(kProThreads) chunk_prologue_kernel(const __gri
     const int64_t row = (int64_t)page * a.P + (int)r % a.P;
     reinterpret_cast<uint4*>(a.Kp + row * kHeadDim)[sub] = kv;
     reinterpret_cast<uint4*>(a.Vp + row * kHeadDim)[sub] = vv;
+}
+
+// ---------------------------------------------------------------- schedule
+constexpr int kMaxGroups = kStages * kOperand / 8;  // prefix sums in the ring before its first use
+
+// Tiles of slab h.
+__device__ __forceinline__ int64_t slab_tiles(const ChunkArgs& a, int h)
+{
+    const int b = h / a.Hkv, t = cu_at(a, b), n = cu_at(a, b + 1) - t, len = slab_len(a, h), width = 2 * (kTile / a.G);
+    int64_t sum = 0;
+#pragma unroll 1
+    for (int i = 0; i * width < n; ++i) sum += make_unit(a, h, t, n, len, i).tiles();
+    return sum;
+}
+
+// All threads of the CTA: the tiles of every slab (or group of slabs, where there are more than
+// fit), summed into `before`. Every CTA does it for itself, beside the append: as a kernel's
+// job in front of this one it was 2 us on the way of a small call.
+__device__ __forceinline__ Extent count_tiles(const ChunkArgs& a, int64_t* before, int64_t* sums, int nctas, int& group)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, slabs = a.B * a.Hkv;
+    group = (slabs + kMaxGroups - 1) / kMaxGroups;
+    const int groups = (slabs + group - 1) / group, per = (groups + kThreads - 1) / kThreads;
+    const int g0 = min(groups, tid * per), g1 = min(groups, g0 + per);
+    int64_t mine = 0;
+#pragma unroll 1
+    for (int x = g0; x < g1; ++x) {
+        before[x] = mine;
+#pragma unroll 1
+        for (int h = x * group; h < min(slabs, (x + 1) * group); ++h) mine += slab_tiles(a, h);
+    }
+    int64_t up = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(kFull, up, o);
+        if (lane >= o) up += y;
+    }
+    if (lane == 31) sums[warp] = up;
+    __syncthreads();
+    int64_t base = up - mine, total = 0;
+#pragma unroll
+    for (int k = 0; k < kThreads / 32; ++k) {
+        if (k < warp) base += sums[k];
+        total += sums[k];
+    }
+#pragma unroll 1
+    for (int x = g0; x < g1; ++x) before[x] += base;
+    __syncthreads();
+    return Extent{total, (int)min(total, (int64_t)nctas)};
+}
+
+// Where the share of CTA c (which has one) starts.
+__device__ __forceinline__ void seek(const ChunkArgs& a, const Extent& e, const int64_t* before, int group, int c, Walk& k)
+{
+    k.pos = e.tiles * c / e.parts;
+    k.end = e.tiles * (c + 1) / e.parts;
+    int lo = 0, hi = (a.B * a.Hkv + group - 1) / group - 1;  // the last group that starts at `pos` or before (it has tiles)
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (before[mid] <= k.pos)
+            lo = mid;
+        else
+            hi = mid - 1;
+    }
+    int64_t off = k.pos - before[lo];
+    int h = lo * group;
+    if (group > 1)
+        for (int64_t x; off >= (x = slab_tiles(a, h)); ++h) off -= x;
+    k.b = h / a.Hkv;
+    k.g = h - k.b * a.Hkv;
+    k.t = cu_at(a, k.b);
+    k.n = cu_at(a, k.b + 1) - k.t;
+    const int len = slab_len(a, h);
+    k.i = 0;
+#pragma unroll 1
+    for (int x; off >= (x = make_unit(a, h, k.t, k.n, len, k.i).tiles()); ++k.i) off -= x;
+    k.enter(a, len, (int)off);
 }
 
 // ---------------------------------------------------------------- attention
@@ -584,6 +568,7 @@ __device__ __forceinline__ void mend_rows(const ChunkArgs& a, int h, bool odd, i
     const int lane = threadIdx.x & 31, sub = lane & 7, dim = 16 * sub;
     const bool mine = dim >= d0 && dim < d0 + nd;
     __syncwarp();  // the rows' first results are stored
+    pdl_wait();    // the appended rows are read from the pools
     unsigned todo = __ballot_sync(kFull, odd);
 #pragma unroll 1
     while (todo) {
@@ -767,7 +752,7 @@ __device__ __forceinline__ void join_pieces(const ChunkArgs& a, const ChunkWork&
 
 template <bool F16>
 __global__ void __launch_bounds__(kThreads, 1)
-    chunk_attn_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkMaps maps, const __grid_constant__ ChunkWork w)
+    chunk_attn_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkMaps maps, const __grid_constant__ ChunkWork w, int nctas)
 {
     extern __shared__ __align__(1024) unsigned char sm[];
     if (smem_u32(sm) & 1023) {  // never: the swizzled tiles need it
@@ -799,18 +784,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_proxy_async_smem();
     }
+    // The append kernel started only after every kernel before it had completed, and this one after
+    // that: what those wrote (lengths, tables, q, earlier rows) may be read now. The appended rows and the
+    // counters may not before pdl_wait().
+    int64_t* before = reinterpret_cast<int64_t*>(sm + kOffRing);
+    int group;
     tc_fence_before();
-    __syncthreads();
+    const Extent head = count_tiles(a, before, reinterpret_cast<int64_t*>(sm + kOffMl), nctas, group);
     tc_fence_after();
     const uint32_t tmem = (uint32_t)uniform(misc[0]);
-    pdl_wait();
-    union {
-        uint4 u[4];
-        ChunkStart s;
-    } given;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) given.u[i] = ld_prev(reinterpret_cast<const uint4*>(w.start + c) + i);
-    const ChunkStart& head = given.s;
     const bool work = c < head.parts;
     Waits wait{misc + 1, a.status, true, false};
     const int TQ = kTile / a.G;
@@ -818,13 +800,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
     if (work && warp == 9) {
         // ---------------------------------------------------------------- TMA
-        asm volatile("fence.proxy.async.global;" ::: "memory");  // the appended rows, written by ordinary stores
         // Rows that one unit streams once leave L2 first; a turn's units share theirs.
         const uint64_t stream = evict_first_policy();
         uint64_t keep;
         asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(keep));
         Walk k;
-        k.begin(a, head);
+        seek(a, head, before, group, c, k);
+        __syncwarp();
+        fence_proxy_async_smem();  // `before` lies in the ring, which the copies write next
+        bool appended = !a.k_new;
         int pos = 0, unit = 0;
         const int ppt = kTile / a.P;  // pages a tile
         // Pages of tile j, and the lane's page number.
@@ -837,6 +821,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             const bool good = page >= 0 && page < a.num_pages;
             if (!good) report(a, DKV_DEV_PAGE_RANGE);
             const int y = (good ? page : a.num_pages) * a.P;  // behind the pool: zeros
+            if (!appended && (j + 1) * kTile > u.len - u.fresh) {
+                pdl_wait();
+                asm volatile("fence.proxy.async.global;" ::: "memory");  // the rows were written by ordinary stores
+                appended = true;
+            }
             if (pos >= kStages && !wait(&empty[s], (pos / kStages - 1) & 1)) return;
             const uint32_t bar = smem_u32(&full[s]), dst = smem_u32(sm + kOffRing + s * kOperand);
             if (lane == 0) mbar_arrive_expect_tx(bar, np * a.P * kRowBytes);
@@ -1085,7 +1074,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const volatile Piece* d = reinterpret_cast<const volatile Piece*>(sm + kOffPieces) + unit % kAhead;
                 const int c0 = d->c0, pieces = d->pieces;
                 if (!wait.meet()) break;
-                if (tid == 0) misc[2] = atomicAdd(w.done + c0, 1) == pieces - 1;
+                if (tid == 0) {
+                    pdl_wait();  // the counters are cleared
+                    misc[2] = atomicAdd(w.done + c0, 1) == pieces - 1;
+                }
                 if (!wait.meet()) break;
                 if (misc[2]) {
                     __threadfence();
@@ -1102,6 +1094,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
     }
     // ---------------------------------------------------------------- teardown
+    pdl_wait();  // the call is not over before its append
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -1142,7 +1135,7 @@ cudaError_t make_q_map(const ChunkArgs& a, CUtensorMap* map)
 template <bool F16>
 cudaError_t launch_attn(const ChunkArgs& a, const ChunkMaps& maps, const ChunkWork& w, int nctas, cudaStream_t st)
 {
-    return launch_pdl(chunk_attn_kernel<F16>, nctas, kThreads, kSmemBytes, st, a, maps, w);
+    return launch_pdl(chunk_attn_kernel<F16>, nctas, kThreads, kSmemBytes, st, a, maps, w, nctas);
 }
 
 }  // namespace
@@ -1167,13 +1160,12 @@ cudaError_t launch_chunk(const ChunkArgs& a, bool short_boxes, cudaStream_t st)
     if ((e = make_q_map(a, &maps.q)) != cudaSuccess) return e;
     unsigned char* base = static_cast<unsigned char*>(a.work);
     ChunkWork w;
-    w.start = reinterpret_cast<ChunkStart*>(base);
-    w.done = reinterpret_cast<int32_t*>(base + kOffDone);
+    w.done = reinterpret_cast<int32_t*>(base);
     w.ml = reinterpret_cast<float2*>(base + kOffPieceMl);
     w.o = reinterpret_cast<float4*>(base + kOffPieceO);
     const int64_t rows = a.k_new ? (int64_t)a.T * a.Hkv : 0;
-    const int blocks = 1 + (int)((rows + kProThreads / 16 - 1) / (kProThreads / 16));
-    if ((e = launch_pdl(chunk_prologue_kernel, blocks, kProThreads, 0, st, a, w, nctas)) != cudaSuccess) return e;
+    const int blocks = 1 + (int)((rows + kAppThreads / 16 - 1) / (kAppThreads / 16));
+    if ((e = launch_pdl(chunk_append_kernel, blocks, kAppThreads, 0, st, a, w)) != cudaSuccess) return e;
     return a.fp16 ? launch_attn<true>(a, maps, w, nctas, st) : launch_attn<false>(a, maps, w, nctas, st);
 }
 
