@@ -335,6 +335,15 @@ __device__ __forceinline__ bool wait_more(uint32_t bar, uint32_t parity, volatil
     return false;
 }
 
+// The drain after a wait that ran out: the phase completes, or the bound passes (in line: a warp
+// whose registers were split calls no function).
+__device__ __forceinline__ void land(uint64_t* bar, uint32_t parity)
+{
+    const unsigned long long t0 = global_ns();
+    for (int i = 1; i < kWaitSpins && !mbar_try_wait(smem_u32(bar), parity); ++i)
+        if ((i & 63) == 0 && global_ns() - t0 > kWaitNs) break;
+}
+
 // Bounded waits of a whole warp. After one that ran out (here or in another role) every wait
 // of the CTA returns false at once.
 struct Waits {
@@ -889,8 +898,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         } while (wait.ok && more);
         if (!wait.ok) {
             // Copies in flight land (or run out of time) before the CTA exits.
-            for (int x = max(0, pos - kStages); x < pos; ++x) mbar_wait(smem_u32(&full[x % kStages]), (x / kStages) & 1);
-            for (int x = max(0, qs - 2); x < qs; ++x) mbar_wait(smem_u32(&q_full[x % kAhead]), (x / kAhead) & 1);
+            for (int x = max(0, pos - kStages); x < pos; ++x) land(&full[x % kStages], (x / kStages) & 1);
+            for (int x = max(0, qs - 2); x < qs; ++x) land(&q_full[x % kAhead], (x / kAhead) & 1);
         }
     } else if (work && warp == 8) {
         // ---------------------------------------------------------------- MMA
@@ -970,7 +979,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!wait.ok && issued) {
             if (leads) {
                 umma_commit(smem_u32(fin));
-                mbar_wait(smem_u32(fin), 0);
+                land(fin, 0);
             }
             __syncwarp();
         }
