@@ -6,8 +6,8 @@
 // Unit of work: up to 2 TQ tokens of one sequence and KV head (TQ = 128 / G tokens x G heads
 // fill a 128-row tile of queries, row = token G + head), against the cache rows that its last
 // token sees, in tiles of 128 rows. All (unit, cache tile) pairs, unit after unit, are cut into
-// equal contiguous shares, one a CTA, one CTA an SM, so ragged lengths leave no SM idle; a unit
-// that lies in several CTAs is joined by the one that finishes last.
+// contiguous shares of equal cost, one a CTA, one CTA an SM, so ragged lengths leave no SM idle; a
+// unit that lies in several CTAs is joined by the one that finishes last.
 //
 //   chunk_append_kernel  appends the rows.
 //   chunk_attn_kernel    starts beside it, finds its shares, and waits for the append only where a
@@ -19,7 +19,8 @@
 //                     back over it as the A operand of the second product.
 //     warp 8          MMA: S(0), S(1), then PV(s), S(s + 2) of step s (group s % 2), in one order, so
 //                     that the tensor pipe itself keeps S(s + 2) behind the PV(s) whose P it overwrites.
-//     warp 9          TMA (10 and 11 idle): Q tiles, and K and V tiles page by page into one ring in the order of use.
+//     warp 9          TMA: Q tiles, and K and V tiles page by page into one ring in the order of use.
+//     warp 10         walks the CTA's share and describes its units to the others (11 is idle).
 //
 // Every wait is bounded (polls and 2 s), and so are the softmax warps' meetings (Waits::meet); one
 // that runs out sets DKV_DEV_TMA_TIMEOUT, the roles leave, copies and products in flight are
@@ -53,10 +54,10 @@ constexpr int kOffQ = 0;
 constexpr int kOffRing = kOffQ + 2 * kOperand;
 constexpr int kOffBars = kOffRing + kStages * kOperand;
 constexpr int kAhead = 4;                  // ring of unit descriptors
-constexpr int kNumBars = 2 * kStages + 2 * kAhead + 11;  // full[], empty[], q_full[], late[], q_empty[2], s_full[2], p_half[2], p_full[2], o_done[2], fin
+constexpr int kNumBars = 2 * kStages + 3 * kAhead + 11;  // full[], empty[], said[], q_full[], late[], q_empty[2], s_full[2], p_half[2], p_full[2], o_done[2], fin
 constexpr int kOffMisc = kOffBars + (kNumBars + 1) / 2 * 16;  // int[4]: TMEM address, abort, last
 constexpr int kOffPieces = kOffMisc + 16;                      // Piece[kAhead]
-constexpr int kOffMl = kOffPieces + kAhead * 48;                           // float2[128]: group 1's (m, l), then group 0's
+constexpr int kOffMl = kOffPieces + kAhead * 64;                           // float2[128]: group 1's (m, l), then group 0's
 constexpr int kSmemBytes = kOffMl + 2 * kTile * 8;
 static_assert(kSmemBytes <= 227 * 1024, "fits one CTA");
 
@@ -110,22 +111,36 @@ __device__ __forceinline__ Unit make_unit(const ChunkArgs& a, int h, int t, int 
     return u;
 }
 
-// The share of one CTA, unit by unit.
+// What a cache tile costs: a pair unit's has twice the products, a split unit's waits for its rows.
+// Measured side by side 1.63 and 1.15 us (with one weight for both, the SMs with next tokens only were
+// done at 225 us of 320, in a step of two turns and ten next tokens).
+constexpr int kPairCost = 3, kSplitCost = 2;
+
+// The share of one CTA, unit by unit. Units lie end to end on a line of costs; a tile is the
+// CTA's in whose part of the line it starts.
 struct Walk {
     int b, g, i, t, n, j0, j1, tiles;
-    int64_t pos, end;  // tiles of the whole call: the current piece's first, the share's end
+    int64_t start, end;  // of the unit, of the share
     Unit u;
+    __device__ __forceinline__ int cost() const { return kSplitCost + (int)u.pair; }
+    // Tiles that start before point x of the unit (a unit costs less than 2^26).
+    __device__ __forceinline__ int before(unsigned x) const
+    {
+        const unsigned w = cost();
+        return (int)((x + w - 1) / w);
+    }
+    // The unit (b, g, i), its start set, from its tile at `off` behind its start.
     __device__ __forceinline__ void enter(const ChunkArgs& a, int len, int off)
     {
         u = make_unit(a, b * a.Hkv + g, t, n, len, i);
         tiles = u.tiles();
-        j0 = off;
-        j1 = (int)min((int64_t)tiles, off + (end - pos));
+        j0 = min(tiles, before((unsigned)off));
+        j1 = min(tiles, before((unsigned)min(end - start, (int64_t)1 << 28)));
     }
-    __device__ __forceinline__ bool next(const ChunkArgs& a)
+    __device__ __forceinline__ bool more() const { return j1 == tiles && start + tiles * cost() < end; }
+    __device__ __forceinline__ void next(const ChunkArgs& a)
     {
-        pos += j1 - j0;
-        if (pos >= end) return false;
+        start += tiles * cost();
         if (++i * 2 * (kTile / a.G) >= n) {
             i = 0;
             if (++g == a.Hkv) {
@@ -137,17 +152,16 @@ struct Walk {
             }
         }
         enter(a, slab_len(a, b * a.Hkv + g), 0);
-        return true;
     }
     __device__ __forceinline__ bool whole() const { return j0 == 0 && j1 == tiles; }
 };
 
-// What the other roles need of a CTA's part of a unit; the TMA warp walks and describes it.
+// What the other roles need of a CTA's part of a unit, described by the walking warp.
 struct alignas(16) Piece {
     int t0, tokens, row0, len;  // as in Unit
     int kv, h, g, j0;
-    int j1, flags;
-    int c0, pieces;             // CTAs c0 .. c0 + pieces - 1 hold the unit (written after the rest: `late`)
+    int j1, flags, fresh, pad0;
+    int c0, pieces, pad1, pad2;  // CTAs c0 .. c0 + pieces - 1 hold the unit (written after the rest: `late`)
     static constexpr int kPair = 1, kWhole = 2, kMore = 4;
     __device__ __forceinline__ bool pair() const { return flags & kPair; }
     __device__ __forceinline__ bool whole() const { return flags & kWhole; }
@@ -155,12 +169,12 @@ struct alignas(16) Piece {
     __device__ __forceinline__ int steps() const { return pair() ? 2 * (j1 - j0) : j1 - j0; }
     __device__ __forceinline__ int tile(int s) const { return j0 + (pair() ? s >> 1 : s); }
 };
-static_assert(sizeof(Piece) == 48, "three 16-byte words");
+static_assert(sizeof(Piece) == 64, "four 16-byte words, of which read_piece reads three");
 
 __device__ __forceinline__ Piece read_piece(const unsigned char* at)
 {
     union {
-        uint4 u[3];
+        uint4 u[4];
         Piece p;
     } x;
 #pragma unroll
@@ -172,14 +186,21 @@ __device__ __forceinline__ Piece read_piece(const unsigned char* at)
     return x.p;
 }
 
-// The whole call: cache tiles of all units, and CTAs with a share of them.
+// The whole call: the cost of all units, and CTAs with a share of it.
 struct Extent {
-    int64_t tiles;
+    int64_t cost;
     int parts;
 };
 
-// The CTA whose share holds tile x of the call.
-__device__ __forceinline__ int cta_of(const Extent& e, int64_t x) { return (int)(((x + 1) * e.parts - 1) / e.tiles); }
+// x / y of values >= 0 (most calls are small enough for the short division).
+__device__ __forceinline__ int64_t divide(int64_t x, int64_t y)
+{
+    return x <= UINT32_MAX && y <= UINT32_MAX ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+}
+
+// Where share c starts, and the CTA whose share holds point x of the line.
+__device__ __forceinline__ int64_t share_start(const Extent& e, int c) { return divide(e.cost * c, e.parts); }
+__device__ __forceinline__ int cta_of(const Extent& e, int64_t x) { return (int)divide((x + 1) * e.parts - 1, e.cost); }
 
 __device__ __forceinline__ void report(const ChunkArgs& a, int bits)
 {
@@ -246,31 +267,34 @@ __global__ void __launch_bounds__(kAppThreads) chunk_append_kernel(const __grid_
 // ---------------------------------------------------------------- schedule
 constexpr int kMaxGroups = kStages * kOperand / 8;  // prefix sums in the ring before its first use
 
-// Tiles of slab h.
-__device__ __forceinline__ int64_t slab_tiles(const ChunkArgs& a, int h)
+// Cost of a unit, and of slab h. any_pair is set if there is a pair unit.
+__device__ __forceinline__ int unit_cost(const Unit& u) { return u.tiles() * (kSplitCost + (int)u.pair); }
+__device__ __forceinline__ int64_t slab_cost(const ChunkArgs& a, int h, int& any_pair)
 {
-    const int b = h / a.Hkv, t = cu_at(a, b), n = cu_at(a, b + 1) - t, len = slab_len(a, h), width = 2 * (kTile / a.G);
+    const int b = h / a.Hkv, t = cu_at(a, b), n = cu_at(a, b + 1) - t, len = slab_len(a, h), TQ = kTile / a.G;
+    any_pair |= n > TQ;
     int64_t sum = 0;
 #pragma unroll 1
-    for (int i = 0; i * width < n; ++i) sum += make_unit(a, h, t, n, len, i).tiles();
+    for (int i = 0; i * 2 * TQ < n; ++i) sum += unit_cost(make_unit(a, h, t, n, len, i));
     return sum;
 }
 
-// All threads of the CTA: the tiles of every slab (or group of slabs, where there are more than
+// All threads of the CTA: the cost of every slab (or group of slabs, where there are more than
 // fit), summed into `before`. Every CTA does it for itself, beside the append: as a kernel's
 // job in front of this one it was 2 us on the way of a small call.
-__device__ __forceinline__ Extent count_tiles(const ChunkArgs& a, int64_t* before, int64_t* sums, int nctas, int& group)
+__device__ __forceinline__ Extent count_cost(const ChunkArgs& a, int64_t* before, int64_t* sums, int nctas, int& group)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, slabs = a.B * a.Hkv;
     group = (slabs + kMaxGroups - 1) / kMaxGroups;
     const int groups = (slabs + group - 1) / group, per = (groups + kThreads - 1) / kThreads;
     const int g0 = min(groups, tid * per), g1 = min(groups, g0 + per);
     int64_t mine = 0;
+    int any_pair = 0;
 #pragma unroll 1
     for (int x = g0; x < g1; ++x) {
         before[x] = mine;
 #pragma unroll 1
-        for (int h = x * group; h < min(slabs, (x + 1) * group); ++h) mine += slab_tiles(a, h);
+        for (int h = x * group; h < min(slabs, (x + 1) * group); ++h) mine += slab_cost(a, h, any_pair);
     }
     int64_t up = mine;
 #pragma unroll
@@ -278,37 +302,45 @@ __device__ __forceinline__ Extent count_tiles(const ChunkArgs& a, int64_t* befor
         const int64_t y = __shfl_up_sync(kFull, up, o);
         if (lane >= o) up += y;
     }
-    if (lane == 31) sums[warp] = up;
+    // Whether there is a pair unit goes along in the sums' upper bits (a barrier that votes, instead,
+    // cost the whole kernel 5 %).
+    constexpr int kFlag = 56;
+    const int64_t pairs = __any_sync(kFull, any_pair) ? (int64_t)1 << kFlag : 0;
+    if (lane == 31) sums[warp] = up + pairs;
     __syncthreads();
     int64_t base = up - mine, total = 0;
 #pragma unroll
     for (int k = 0; k < kThreads / 32; ++k) {
-        if (k < warp) base += sums[k];
+        if (k < warp) base += sums[k] & (((int64_t)1 << kFlag) - 1);
         total += sums[k];
     }
+    const int dearest = total >> kFlag ? kPairCost : kSplitCost;
+    total &= ((int64_t)1 << kFlag) - 1;
 #pragma unroll 1
     for (int x = g0; x < g1; ++x) before[x] += base;
     __syncthreads();
-    return Extent{total, (int)min(total, (int64_t)nctas)};
+    // A share is at least as long as the dearest tile, so that one starts in every share of a unit.
+    static_assert(kPairCost >= kSplitCost, "the dearest tile");
+    return Extent{total, total >= (int64_t)nctas * dearest ? nctas : (int)((unsigned)total / (unsigned)dearest)};
 }
 
 // Where the share of CTA c (which has one) starts.
 __device__ __forceinline__ void seek(const ChunkArgs& a, const Extent& e, const int64_t* before, int group, int c, Walk& k)
 {
-    k.pos = e.tiles * c / e.parts;
-    k.end = e.tiles * (c + 1) / e.parts;
-    int lo = 0, hi = (a.B * a.Hkv + group - 1) / group - 1;  // the last group that starts at `pos` or before (it has tiles)
+    const int64_t pos = share_start(e, c);
+    k.end = share_start(e, c + 1);
+    int lo = 0, hi = (a.B * a.Hkv + group - 1) / group - 1;  // the last group that starts at `pos` or before (it has units)
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (before[mid] <= k.pos)
+        if (before[mid] <= pos)
             lo = mid;
         else
             hi = mid - 1;
     }
-    int64_t off = k.pos - before[lo];
-    int h = lo * group;
+    int64_t off = pos - before[lo];
+    int h = lo * group, any = 0;
     if (group > 1)
-        for (int64_t x; off >= (x = slab_tiles(a, h)); ++h) off -= x;
+        for (int64_t x; off >= (x = slab_cost(a, h, any)); ++h) off -= x;
     k.b = h / a.Hkv;
     k.g = h - k.b * a.Hkv;
     k.t = cu_at(a, k.b);
@@ -316,8 +348,10 @@ __device__ __forceinline__ void seek(const ChunkArgs& a, const Extent& e, const 
     const int len = slab_len(a, h);
     k.i = 0;
 #pragma unroll 1
-    for (int x; off >= (x = make_unit(a, h, k.t, k.n, len, k.i).tiles()); ++k.i) off -= x;
+    for (int x; off >= (x = unit_cost(make_unit(a, h, k.t, k.n, len, k.i))); ++k.i) off -= x;
+    k.start = pos - off;
     k.enter(a, len, (int)off);
+    if (k.j0 == k.tiles) k.next(a);  // the unit's last tile starts before this share
 }
 
 // ---------------------------------------------------------------- attention
@@ -770,7 +804,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     uint64_t* full = reinterpret_cast<uint64_t*>(sm + kOffBars);  // [kStages] the stage's rows landed
     uint64_t* empty = full + kStages;                              // [kStages] its products are done
-    uint64_t* q_full = empty + kStages;                            // [kAhead] the unit is described and its Q landed
+    uint64_t* said = empty + kStages;                              // [kAhead] the unit is described
+    uint64_t* q_full = said + kAhead;                              // [kAhead] its Q landed
     uint64_t* late = q_full + kAhead;                              // [kAhead] the unit's CTAs are described
     uint64_t* q_empty = late + kAhead;                             // [2] the unit's score products are done
     uint64_t* s_full = q_empty + 2;                                // [2] S of the group's next step is done
@@ -799,7 +834,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     int64_t* before = reinterpret_cast<int64_t*>(sm + kOffRing);
     int group;
     tc_fence_before();
-    const Extent head = count_tiles(a, before, reinterpret_cast<int64_t*>(sm + kOffMl), nctas, group);
+    const Extent head = count_cost(a, before, reinterpret_cast<int64_t*>(sm + kOffMl), nctas, group);
     tc_fence_after();
     const uint32_t tmem = (uint32_t)uniform(misc[0]);
     const bool work = c < head.parts;
@@ -807,30 +842,49 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int TQ = kTile / a.G;
     if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
-    if (work && warp == 9) {
-        // ---------------------------------------------------------------- TMA
-        // Rows that one unit streams once leave L2 first; a turn's units share theirs.
-        const uint64_t stream = evict_first_policy();
-        uint64_t keep;
-        asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(keep));
+    if (work && warp == 10) {
+        // ---------------------------------------------------------------- walk
         Walk k;
         seek(a, head, before, group, c, k);
-        __syncwarp();
         fence_proxy_async_smem();  // `before` lies in the ring, which the copies write next
-        bool appended = !a.k_new;
-        int pos = 0, unit = 0;
+        __syncwarp();
+#pragma unroll 1
+        for (int unit = 0;; ++unit) {
+            // Two units ahead of the score products at most: the slot's readers are past it.
+            if (unit > 1 && !wait(&q_empty[unit & 1], (unit / 2 - 1) & 1)) break;
+            const bool whole = k.whole(), more = k.more();
+            Piece* d = reinterpret_cast<Piece*>(sm + kOffPieces) + unit % kAhead;
+            if (lane == 0) {
+                *reinterpret_cast<int4*>(&d->t0) = make_int4(k.u.t0, k.u.tokens, k.u.row0, k.u.len);
+                *reinterpret_cast<int4*>(&d->kv) = make_int4(k.u.kv, k.u.h, k.g, k.j0);
+                *reinterpret_cast<int4*>(&d->j1) = make_int4(
+                    k.j1, (k.u.pair ? Piece::kPair : 0) | (whole ? Piece::kWhole : 0) | (more ? Piece::kMore : 0), k.u.fresh, 0);
+                mbar_arrive(smem_u32(&said[unit % kAhead]));
+            }
+            const int c0 = whole ? c : cta_of(head, k.start), last = whole ? c : cta_of(head, k.start + (k.tiles - 1) * k.cost());
+            if (lane == 0) {
+                d->c0 = c0;
+                d->pieces = last - c0 + 1;
+                mbar_arrive(smem_u32(&late[unit % kAhead]));
+            }
+            if (!more) break;
+            k.next(a);
+        }
+    } else if (work && warp == 9) {
+        // ---------------------------------------------------------------- TMA
         const int ppt = kTile / a.P;  // pages a tile
+        bool appended = !a.k_new, pair_before = false;
+        int pos = 0, unit = 0;
+        Piece k;
         // Pages of tile j, and the lane's page number.
-        auto pages_in = [&](const Unit& u, int j) { return (min(max(u.kv - j * kTile, 0), kTile) + a.P - 1) / a.P; };
-        auto page_of = [&](const Unit& u, int j) {
-            return lane < pages_in(u, j) ? a.table[(int64_t)u.h * a.max_pages + j * ppt + lane] : 0;
-        };
-        auto load = [&](const CUtensorMap* map, const Unit& u, int j, int page) {
-            const int s = pos % kStages, np = pages_in(u, j);
+        auto pages_in = [&](int j) { return (min(max(k.kv - j * kTile, 0), kTile) + a.P - 1) / a.P; };
+        auto page_of = [&](int j) { return lane < pages_in(j) ? a.table[(int64_t)k.h * a.max_pages + j * ppt + lane] : 0; };
+        auto load = [&](const CUtensorMap* map, int j, int page) {
+            const int s = pos % kStages, np = pages_in(j);
             const bool good = page >= 0 && page < a.num_pages;
             if (!good) report(a, DKV_DEV_PAGE_RANGE);
             const int y = (good ? page : a.num_pages) * a.P;  // behind the pool: zeros
-            if (!appended && (j + 1) * kTile > u.len - u.fresh) {
+            if (!appended && (j + 1) * kTile > k.len - k.fresh) {
                 pdl_wait();
                 asm volatile("fence.proxy.async.global;" ::: "memory");  // the rows were written by ordinary stores
                 appended = true;
@@ -839,7 +893,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint32_t bar = smem_u32(&full[s]), dst = smem_u32(sm + kOffRing + s * kOperand);
             if (lane == 0) mbar_arrive_expect_tx(bar, np * a.P * kRowBytes);
             __syncwarp();
-            const uint64_t pol = u.pair ? keep : stream;
+            // Rows that one unit streams once leave L2 first; a turn's units share theirs.
+            uint64_t pol;
+            if (k.pair())
+                asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol));
+            else
+                pol = evict_first_policy();
             if (lane < np) {
                 tma_box(dst + lane * a.P * 128, map, 0, y, bar, pol);
                 tma_box(dst + kHalf + lane * a.P * 128, map, 64, y, bar, pol);
@@ -847,59 +906,40 @@ __global__ void __launch_bounds__(kThreads, 1)
             __syncwarp();
             ++pos;
         };
-        int qs = 0;  // units described
-        bool more = true, pair_before = false;
         do {
-            const Unit u = k.u;
-            const int j0 = k.j0, j1 = k.j1;
+            if (!wait(&said[unit % kAhead], (unit / kAhead) & 1)) break;
+            k = read_piece(sm + kOffPieces + unit % kAhead * sizeof(Piece));
+            const bool pair = k.pair();
             // Q buffers: both for a pair unit, the unit's parity's for a split one, so that these run ahead.
             if (unit > 1 && !wait(&q_empty[unit & 1], (unit / 2 - 1) & 1)) break;
-            if (unit > 0 && (u.pair || pair_before) && !wait(&q_empty[(unit - 1) & 1], ((unit - 1) / 2) & 1)) break;
-            pair_before = u.pair;
-            const int64_t from = k.pos - j0;
-            const int g = k.g, unit_tiles = k.tiles;
-            const bool whole = k.whole();
-            more = k.pos + (j1 - j0) < k.end;
-            int page = page_of(u, j0);  // on its way while Q is
-            Piece* d = reinterpret_cast<Piece*>(sm + kOffPieces) + unit % kAhead;
+            if (unit > 0 && (pair || pair_before) && !wait(&q_empty[(unit - 1) & 1], ((unit - 1) / 2) & 1)) break;
+            pair_before = pair;
+            const int page = page_of(k.j0);  // on its way while Q is
             if (lane == 0) {
-                *reinterpret_cast<int4*>(&d->t0) = make_int4(u.t0, u.tokens, u.row0, u.len);
-                *reinterpret_cast<int4*>(&d->kv) = make_int4(u.kv, u.h, g, j0);
-                *reinterpret_cast<int2*>(&d->j1) =
-                    make_int2(j1, (u.pair ? Piece::kPair : 0) | (whole ? Piece::kWhole : 0) | (more ? Piece::kMore : 0));
                 const uint32_t bar = smem_u32(&q_full[unit % kAhead]), box = 2u * 64 * a.G * TQ;
-                mbar_arrive_expect_tx(bar, (u.pair ? 4 : 2) * box);
-                for (int p = 0; p < (u.pair ? 2 : 1); ++p)
+                mbar_arrive_expect_tx(bar, (pair ? 4 : 2) * box);
+                for (int p = 0; p < (pair ? 2 : 1); ++p)
                     for (int half = 0; half < 2; ++half)
-                        tma_box3(smem_u32(sm + kOffQ + (u.pair ? p : unit & 1) * kOperand + half * kHalf), &maps.q, 64 * half, g * a.G,
-                                 u.t0 + p * TQ, bar);
-            }
-            ++qs;
-            __syncwarp();
-            const int steps = u.pair ? 2 * (j1 - j0) : j1 - j0, stride = u.pair ? 2 : 1;
-            // K(0), K(1), then V(s), K(s + 2); pair units have one K and one V a pair of steps.
-#pragma unroll 1
-            for (int x = -3; x < 2 * steps && wait.ok; ++x) {
-                const int s = (x >> 1) + 2 * (x & 1);  // even x: V of step x / 2; odd x: K of step x / 2 + 2
-                if (s < 0 || s >= steps || (s & (stride - 1))) continue;
-                const int j = j0 + (u.pair ? s >> 1 : s);
-                load(x & 1 ? &maps.cache.k : &maps.cache.v, u, j, x == -3 ? page : page_of(u, j));
-                if (x == -3) {  // with the first copies on their way
-                    const int c0 = whole ? c : cta_of(head, from), last = whole ? c : cta_of(head, from + unit_tiles - 1);
-                    if (lane == 0) {
-                        d->c0 = c0;
-                        d->pieces = last - c0 + 1;
-                        mbar_arrive(smem_u32(&late[unit % kAhead]));
-                    }
-                    if (more) k.next(a);
-                }
+                        tma_box3(smem_u32(sm + kOffQ + (pair ? p : unit & 1) * kOperand + half * kHalf), &maps.q, 64 * half, k.g * a.G,
+                                 k.t0 + p * TQ, bar);
             }
             ++unit;
-        } while (wait.ok && more);
+            __syncwarp();
+            const int steps = k.steps();
+            // K(0), K(1), then V(s), K(s + 2); pair units have one K and one V a pair of steps.
+            load(&maps.cache.k, k.tile(0), page);
+#pragma unroll 1
+            for (int x = -1; x < 2 * steps && wait.ok; ++x) {
+                const int s = (x >> 1) + 2 * (x & 1);  // even x: V of step x / 2; odd x: K of step x / 2 + 2
+                if (s >= steps || (pair && (s & 1))) continue;
+                const int j = k.tile(s);
+                load(x & 1 ? &maps.cache.k : &maps.cache.v, j, page_of(j));
+            }
+        } while (wait.ok && k.more());
         if (!wait.ok) {
             // Copies in flight land (or run out of time) before the CTA exits.
             for (int x = max(0, pos - kStages); x < pos; ++x) land(&full[x % kStages], (x / kStages) & 1);
-            for (int x = max(0, qs - 2); x < qs; ++x) land(&q_full[x % kAhead], (x / kAhead) & 1);
+            for (int x = max(0, unit - 2); x < unit; ++x) land(&q_full[x % kAhead], (x / kAhead) & 1);
         }
     } else if (work && warp == 8) {
         // ---------------------------------------------------------------- MMA
@@ -997,7 +1037,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         int ns = 0, no = 0;  // S tiles and O accumulators taken
         int unit = 0;
         do {
-            if (!wait(&q_full[unit % kAhead], (unit / kAhead) & 1)) break;
+            if (!wait(&said[unit % kAhead], (unit / kAhead) & 1)) break;
             k = read_piece(sm + kOffPieces + unit % kAhead * sizeof(Piece));
             const int steps = k.steps();
             const bool pair = k.pair(), whole = k.whole();
