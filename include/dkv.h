@@ -13,7 +13,8 @@
  *   dkv_decode_attn   split-K decode attention over the packed cache
  *   dkv_free          release a plan
  *
- * and the step before them, the export of the pattern from learned retention
+ * the same over a paged cache, whose sequences grow, come and go (dkv_page_tables,
+ * dkv_page_release, dkv_page_compact, dkv_chunk_attn), and the step before them, the export of the pattern from learned retention
  * probabilities with an exact budget (dkv_budget, dkv_topk_mask; Eq. 3).
  *
  * Conventions used by every entry point
@@ -436,7 +437,7 @@ typedef struct {
     int32_t head_dim;  /* must be 128 */
     int32_t page_rows; /* rows of a page: 16, 32, 64 or 128 */
     int32_t num_pages; /* pages of each pool; num_pages * page_rows < 2^31 - 16 */
-    int32_t max_pages; /* table entries of a slab; max_pages * page_rows < 2^31 */
+    int32_t max_pages; /* table entries of a slab; max_pages * page_rows <= 2^31 - 256 */
 } dkv_pages;
 
 /* Element types of q, the new rows, the pools and out in dkv_chunk_attn. */
@@ -464,7 +465,7 @@ typedef struct {
  * slots      device int32 [L][max_tokens][H_kv]: receives the pool row of each new
  *            token, slots[l][t][g] for t < cu[B] (the rows behind are kept), for
  *            callers that write K and V themselves; NULL: not written. Needs cu_tokens.
- * workspace  dkv_page_workspace_bytes(pages) bytes.
+ * workspace  dkv_page_workspace_bytes(pages) bytes (-1: a bad geometry).
  *
  * All or nothing: with fewer free pages than needed (DKV_DEV_PAGES_EXHAUSTED), or a
  * negative count, a slab past max_pages, more than max_tokens tokens with a slot map,
@@ -511,7 +512,7 @@ dkv_status dkv_page_compact(const dkv_pages* pages, const dkv_plan* plan, const 
  * tokens a sequence (the next token, drafted ones, a whole turn), sequences mixed.
  *
  * dtype       DKV_BF16 or DKV_FP16: type of q, k_new, v_new, Kp, Vp and out.
- * num_tokens  rows of q, k_new, v_new and out. Tokens cu_tokens[b] .. cu_tokens[b + 1] - 1
+ * num_tokens  rows of q, k_new, v_new and out; num_tokens * H <= 2^30. Tokens cu_tokens[b] .. cu_tokens[b + 1] - 1
  *             are sequence b's; cu_tokens (device int32 [B + 1]) ascends from 0. Rows
  *             from cu_tokens[B] on are no token's: not read, and left as they are in out.
  * q           [num_tokens][H][128], token t at q + t * q_stride elements.
@@ -526,7 +527,12 @@ dkv_status dkv_page_compact(const dkv_pages* pages, const dkv_plan* plan, const 
  *             len[h] - n + i + 1 rows of its slab; 0: to all len[h] rows.
  * scale       softmax scale; <= 0 selects 1/sqrt(128).
  * out         [num_tokens][H][128]; zeros for a token that has no row to attend to.
- * workspace   dkv_chunk_workspace_bytes(pages) bytes.
+ *             Scores, softmax statistics and sums are fp32; each softmax weight is
+ *             rounded to dtype for the second product, and the output once.
+ * workspace   dkv_chunk_workspace_bytes(pages) bytes (-1: a bad geometry), about 43 MB.
+ * Results do not depend on the order in which the GPU runs the call's parts. A value that
+ * is not finite in K or V of a row that a token does not see does not reach it. A wait
+ * that runs out (DKV_DEV_TMA_TIMEOUT) leaves outputs unwritten.
  * Errors: DKV_ERR_INVALID_ARG, DKV_ERR_CUDA.
  */
 int64_t dkv_chunk_workspace_bytes(const dkv_pages* pages);

@@ -55,8 +55,8 @@ int64_t check_pages(const dkv_pages* g)
         return refuse("page_rows=%d: 16, 32, 64 or 128", g->page_rows), -1;
     if (g->num_pages < 1 || (int64_t)g->num_pages * g->page_rows >= dkv::kMaxMmaRows)
         return refuse("num_pages=%d of %d rows: need 1 to 2^31 - 17 rows", g->num_pages, g->page_rows), -1;
-    if (g->max_pages < 1 || (int64_t)g->max_pages * g->page_rows > 0x7fffffffLL)
-        return refuse("max_pages=%d of %d rows: need 1 to 2^31 - 1 rows", g->max_pages, g->page_rows), -1;
+    if (g->max_pages < 1 || (int64_t)g->max_pages * g->page_rows > 0x7fffff00LL)
+        return refuse("max_pages=%d of %d rows: need 1 to 2^31 - 256 rows", g->max_pages, g->page_rows), -1;
     const int64_t NH = (int64_t)g->L * g->B * g->H_kv;
     if (g->L > (1 << 20) || g->H_kv > (1 << 20) || NH > (1 << 26))
         return refuse("L*B*H_kv=%lld slabs (more than 2^26)", (long long)NH), -1;
@@ -213,8 +213,8 @@ dkv_status dkv_chunk_attn(const dkv_pages* g, int32_t layer, int32_t dtype, int3
     if (check_pages(g) < 0) return DKV_ERR_INVALID_ARG;
     if (layer < 0 || layer >= g->L) return refuse("layer=%d out of [0, %d)", layer, g->L);
     if (dtype != DKV_BF16 && dtype != DKV_FP16) return refuse("dtype=%d: DKV_BF16 or DKV_FP16", dtype);
-    if (num_tokens < 0 || (int64_t)num_tokens * g->H > 0x7fffffffLL)
-        return refuse("num_tokens=%d: need 0 <= num_tokens and num_tokens*H < 2^31", num_tokens);
+    if (num_tokens < 0 || (int64_t)num_tokens * g->H > (1 << 30))
+        return refuse("num_tokens=%d: need 0 <= num_tokens and num_tokens*H <= 2^30", num_tokens);
     if (!std::isfinite(scale)) return refuse("scale is not finite");
     if ((k_new == nullptr) != (v_new == nullptr)) return refuse("k_new and v_new must both be given or both be NULL");
     if (num_tokens == 0) return dkv::set_error(DKV_OK, "");

@@ -26,7 +26,7 @@ def test_workspace_sizes(dkv):
 @pytest.mark.parametrize("kw", [
     dict(L=0), dict(B=0), dict(B=513), dict(H=7), dict(H=18), dict(H_kv=0), dict(head_dim=64), dict(page_rows=8),
     dict(page_rows=48), dict(page_rows=256), dict(num_pages=0), dict(num_pages=1 << 27), dict(max_pages=0),
-    dict(max_pages=1 << 27, page_rows=16), dict(L=1 << 20, B=512),
+    dict(max_pages=1 << 27, page_rows=16), dict(max_pages=(1 << 27) - 1, page_rows=16), dict(L=1 << 20, B=512),
 ])
 def test_bad_geometry(dkv, kw):
     for f in (dkv.dkv_page_workspace_bytes, dkv.dkv_chunk_workspace_bytes):
