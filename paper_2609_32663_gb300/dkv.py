@@ -537,12 +537,13 @@ def _bad(why):
     raise DkvError(DKV_ERR_INVALID_ARG, "argument check", why)
 
 
-def _at():
-    """The current device, on whose stream a call runs and where its buffers lie."""
+def _where(stream):
+    """The current device, where a call's buffers lie, and the stream it runs on."""
     T = _torch()
-    if T.device is not None and T.torch.cuda.is_initialized():
-        return T.device()
-    return T.torch.cuda.current_device() if T.torch.cuda.is_available() else 0
+    if T.raw_stream is not None and T.device is not None and T.torch.cuda.is_initialized():
+        at = T.device()
+        return at, T.raw_stream(at) if stream is None else _stream(stream)
+    return (T.torch.cuda.current_device() if T.torch.cuda.is_available() else 0), _stream(stream)
 
 
 def _on(t, name, at, dtypes, numel=None):
@@ -586,7 +587,8 @@ def dkv_page_tables(pages: Pages, len, new_len, table, free_pages, free_count, n
                     plan: Plan | None = None, seq=None, cu_tokens=None, slots=None, status=None, stream=None):
     """Pages for tokens[b] new rows of every slab of slot b, or for a plan's kept rows (its sequence i to slot seq[i]);
     slots int32 [L][max_tokens][H_kv] receives the slot map, cu_tokens int32 [B + 1] the token offsets."""
-    i32, at = _torch().i32, _at()
+    i32 = _torch().i32
+    at, queue = _where(stream)
     (ln, nl, tb, fp, fc, nc), (wp, wb), st = _page_args(pages, at, len, new_len, table, free_pages, free_count, new_count,
                                                         workspace, status)
     most = 0
@@ -599,18 +601,18 @@ def dkv_page_tables(pages: Pages, len, new_len, table, free_pages, free_count, n
     _check(lib().dkv_page_tables(
         pages.ref, _on(tokens, "tokens", at, i32, pages.B), None if plan is None else plan.address,
         _on(seq, "seq", at, i32, None if plan is None else plan.B), ln, nl, tb, fp, fc, nc,
-        _on(cu_tokens, "cu_tokens", at, i32, pages.B + 1), _on(slots, "slots", at, i32), most, wp, wb, st, _stream(stream)),
+        _on(cu_tokens, "cu_tokens", at, i32, pages.B + 1), _on(slots, "slots", at, i32), most, wp, wb, st, queue),
         "dkv_page_tables")
 
 
 def dkv_page_release(pages: Pages, ended, len, new_len, table, free_pages, free_count, new_count, workspace,
                      status=None, stream=None):
     """The pages of the slots with ended[b] != 0 go back to the free list."""
-    at = _at()
+    at, queue = _where(stream)
     (ln, nl, tb, fp, fc, nc), (wp, wb), st = _page_args(pages, at, len, new_len, table, free_pages, free_count, new_count,
                                                         workspace, status)
     _check(lib().dkv_page_release(pages.ref, _on(ended, "ended", at, _torch().i32, pages.B), ln, nl, tb, fp, fc, nc, wp, wb,
-                                  st, _stream(stream)), "dkv_page_release")
+                                  st, queue), "dkv_page_release")
 
 
 def dkv_page_compact(pages: Pages, plan: Plan, K, V, table, len, Kp, Vp, seq=None, T_stride: int | None = None,
@@ -618,7 +620,8 @@ def dkv_page_compact(pages: Pages, plan: Plan, K, V, table, len, Kp, Vp, seq=Non
     """The kept rows of plan sequence i become the last rows of slot seq[i]'s slabs."""
     if T_stride is None:
         T_stride = K.shape[-2]
-    T, sh, at = _torch(), plan.shape, _at()
+    T, sh = _torch(), plan.shape
+    at, queue = _where(stream)
     r16 = (*T.bf16, T.torch.float16)
     handle = plan.address
     dense = sh.L * plan.B * sh.H_kv * int(T_stride) * 128
@@ -629,7 +632,7 @@ def dkv_page_compact(pages: Pages, plan: Plan, K, V, table, len, Kp, Vp, seq=Non
     _check(lib().dkv_page_compact(
         pages.ref, handle, _on(seq, "seq", at, T.i32, plan.B), _on(K, "K", at, r16), _on(V, "V", at, r16), int(T_stride),
         _on(table, "table", at, T.i32, pages.slabs * pages.max_pages), _on(len, "len", at, T.i32, pages.slabs),
-        _on(Kp, "Kp", at, r16, pool), _on(Vp, "Vp", at, r16, pool), _word(status, at), _stream(stream)), "dkv_page_compact")
+        _on(Kp, "Kp", at, r16, pool), _on(Vp, "Vp", at, r16, pool), _word(status, at), queue), "dkv_page_compact")
 
 
 def dkv_chunk_workspace_bytes(pages: Pages) -> int:
@@ -657,7 +660,8 @@ def dkv_chunk_attn(pages: Pages, layer: int, q, k_new, v_new, cu_tokens, table, 
     """One layer's new tokens: k_new and v_new [T][H_kv][128] appended to their slabs' pages (None: they are there), and
     the attention of q [T][H][128] -> out [T][H][128], all of q's type (bf16 or fp16). q, k_new and v_new may be slices of
     one projection; k_new and v_new have the same token stride."""
-    T, at, dtype = _torch(), _at(), q.dtype
+    T, dtype = _torch(), q.dtype
+    at, queue = _where(stream)
     half = dtype == T.torch.float16
     if not (half or dtype == T.torch.bfloat16) or q.dim() != 3:
         _bad(f"q is {dtype} of {q.dim()} dimensions, expected bfloat16 or float16 [T][H][128]")
@@ -679,4 +683,4 @@ def dkv_chunk_attn(pages: Pages, layer: int, q, k_new, v_new, cu_tokens, table, 
         _on(cu_tokens, "cu_tokens", at, T.i32, pages.B + 1), _on(table, "table", at, T.i32, pages.slabs * pages.max_pages),
         _on(len, "len", at, T.i32, pages.slabs), _on(Kp, "Kp", at, one, pool), _on(Vp, "Vp", at, one, pool),
         1 if causal else 0, scale, _on(out, "out", at, one, tokens * pages.H * 128), wp, wb, _word(status, at),
-        _stream(stream)), "dkv_chunk_attn")
+        queue), "dkv_chunk_attn")
