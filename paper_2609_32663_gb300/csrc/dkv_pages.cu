@@ -11,12 +11,16 @@
 //
 // The whole call needs the scan of all slabs' page counts, and every CTA its part of it. Up to
 // kFusedSlabs slabs each CTA scans them all itself (64 KB through L2 at 16,384 slabs, 2-3 us) into
-// shared memory and then fills its share: one launch, where a scan kernel and a fill kernel
-// behind it took 12.4 us for a step of 4,096 slabs. Lengths and counts that are updated in place
+// shared memory and then fills its share: one launch and 6.9 us for a step of 4,096 slabs, where a
+// scan kernel and a fill kernel behind it took 12.4. Lengths and counts that are updated in place
 // are committed by a second, tiny launch, as CTAs may still be reading them. More slabs: one
 // CTA scans into the workspace, then all fill.
 // Every value that lives on the device is checked in the scan: nothing is written if a check fails
 // or the free list is too short.
+//
+// What bounds it: launches and the scan for a decode step (4.4 us of its 6.9); instructions more than bytes for
+// the large calls: 12.8 M pages given back, 103 MB, in 28.5 us, of which the scan takes 5 and whole runs of one slab go at
+// 6.4 TB/s; 256 K pages and 4.1 M slots, 17.7 MB, in 11.6 us.
 #include "dkv_decode_common.cuh"
 #include "dkv_pages.cuh"
 #include "dkv_pool.cuh"
@@ -56,7 +60,8 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* sh, int64_t* t
     return v - x + (warp ? before : 0);
 }
 
-__device__ __forceinline__ int pages_of(const PageArgs& a, int64_t rows) { return (int)((rows + a.P - 1) >> a.log_P); }
+// rows: at most max_pages * P, which the host keeps to 2^31 - 256.
+__device__ __forceinline__ int pages_of(const PageArgs& a, int rows) { return (rows + a.P - 1) >> a.log_P; }
 
 // A slab's place, moved on without divisions.
 struct Slab {
@@ -83,7 +88,7 @@ struct Slab {
             carry(a);
         }
     }
-    // 124 slabs on (a.skip_b slots and a.skip_g heads).
+    // 128 slabs on (a.skip_b slots and a.skip_g heads).
     __device__ __forceinline__ void skip(const PageArgs& a)
     {
         b += a.skip_b;
@@ -108,7 +113,7 @@ struct Slab {
 __device__ __forceinline__ int slab_pages(const PageArgs& a, int len, int n)
 {
     if (a.mode == kRelease) return n ? pages_of(a, len) : 0;
-    return pages_of(a, (int64_t)len + n) - pages_of(a, len);
+    return pages_of(a, len + n) - pages_of(a, len);
 }
 
 __device__ __forceinline__ int slab_after(const PageArgs& a, int len, int n)
@@ -171,33 +176,36 @@ __device__ __forceinline__ bool scan_slabs(const PageArgs& a, ScanShared* sh, in
         if (lane == 0) sh->cu[0] = 0;
         if (sum > (a.slots ? a.max_tokens : (int64_t)INT32_MAX)) flags |= kDevRange;
     }
-    const int64_t cap = (int64_t)a.max_pages << a.log_P;
+    const int cap = a.max_pages << a.log_P;
     int64_t mine = 0;  // this lane's pages; `run`: the warp's so far (32 bits do: it is used only if the sum fits)
     int run = 0;
+    const bool quads = a.Hkv % 4 == 0;
     Slab s;
     s.at(a, h0 + 4 * lane);
 #pragma unroll 1
     for (int h = h0; h < h1; h += 128) {
         const int x = h + 4 * lane;
         int v[4], sum = 0;
+        Slab one = s;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int len = lens[i];
             v[i] = sum;
             if (x + i < h1) {
-                const int n = s.rows(a, sh->per_slot);
-                if (len < 0 || len > cap || (a.mode != kRelease && (n < 0 || (int64_t)len + n > cap))) {
+                const int n = one.rows(a, sh->per_slot);
+                if (len < 0 || len > cap || (a.mode != kRelease && (n < 0 || n > cap - len)))
                     flags |= kDevRange;
-                } else {
-                    const int pages = slab_pages(a, len, n);
-                    sum += pages;
-                    mine += pages;
-                }
+                else
+                    sum += slab_pages(a, len, n);
             }
-            s.next(a);
+            if (quads)
+                ++one.g;  // four neighbours of one slot
+            else
+                one.next(a);
         }
         s.skip(a);
         if (h + 128 < h1) fetch(x + 128);
+        mine += sum;  // four slabs: at most 2^29
         int up = sum;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -262,6 +270,20 @@ __device__ __forceinline__ void slabs_of_pages(const int32_t* first, int lo, int
             if (h[i] + step <= hi && first[min(h[i] + step, hi)] <= j[i]) h[i] += step;
 }
 
+// The same for one value, all lanes of a warp together: 32 probes a round.
+__device__ __forceinline__ int slab_of_page(const int32_t* first, int NH, int j)
+{
+    const int lane = threadIdx.x & 31;
+    int lo = 0, n = NH;  // in [lo, lo + n)
+    while (n > 1) {
+        const int step = (n + 31) >> 5, x = lane * step;
+        const int k = 31 - __clz(__ballot_sync(kFull, x < n && first[lo + x] <= j) | 1u);
+        lo += k * step;
+        n = min(step, n - k * step);
+    }
+    return lo;
+}
+
 // Pages c0 + 32 i + lane (i < N; up to `end`) of the call, of slabs ha .. hb (one warp).
 template <int N>
 __device__ __forceinline__ void fill_pages(const PageArgs& a, const PageHead& head, const int32_t* first, const int32_t* len, int c0, int end, int ha, int hb)
@@ -294,13 +316,10 @@ __device__ __forceinline__ void fill_chunks(const PageArgs& a, const PageHead& h
 #pragma unroll 1
     for (; c0 < head.pages; c0 += stride) {
         const int j0 = (int)c0, end = (int)min((int64_t)head.pages, c0 + 32 * kLong);
-        const int one[1] = {lane & 1 ? end - 1 : j0};  // lanes 0 and 1: the slabs of the first and the last page
-        int found[1];
-        slabs_of_pages(first, 0, a.NH - 1, one, found);
-        const int ha = __shfl_sync(kFull, found[0], 0), hb = __shfl_sync(kFull, found[0], 1);
-        if (ha != hb) {
-#pragma unroll 1
-            for (int j = j0; j < end; j += 128) fill_pages<4>(a, head, first, len, j, end, ha, hb);
+        const int ha = slab_of_page(first, a.NH, j0);
+        if (ha + 1 < a.NH && first[ha + 1] < end) {
+            const int hb = ha + slab_of_page(first + ha, a.NH - ha, end - 1);
+            fill_pages<kLong>(a, head, first, len, j0, end, ha, hb);
             continue;
         }
         const int32_t* from = a.mode == kRelease ? a.table + ((int64_t)ha * a.max_pages + (j0 - first[ha])) : a.free_pages + (head.count - 1 - j0);
@@ -315,49 +334,102 @@ __device__ __forceinline__ void fill_chunks(const PageArgs& a, const PageHead& h
     }
 }
 
+// a / b of numbers that are not negative; in 32 bits where they fit.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b)
+{
+    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// Slot map [L][t][Hkv], V neighbouring heads a lane. A warp takes a contiguous piece of the map, a unit of 32 / (Hkv / V)
+// tokens (of one token's 32 V heads, where it has more) after the other, and looks sequence, lengths and
+// scan up again only where they change (all of it for each entry: 14.3 us instead of 11.6 for 4.1 M
+// entries). Pages that this call takes are read from the free list: their table entries may not be
+// written yet.
+template <int V>
+__device__ __forceinline__ void fill_slots(const PageArgs& a, const PageHead& head, const int32_t* first, const int32_t* len, const int32_t* cu, int warp, int warps)
+{
+    const int lane = threadIdx.x & 31, row = a.Hkv / V, width = min(row, 32), per = 32 / width, parts = (row + 31) / 32;
+    const int groups = (int)(((uint32_t)head.total + per - 1) / per);
+    const int64_t per_layer = (int64_t)groups * parts, units = per_layer * a.L;
+    const int64_t each = quotient(units, warps), more = units - each * warps;  // `more` warps take one unit more
+    const int count = (int)each + (warp < more);
+    if (count == 0) return;
+    const int64_t u0 = each * warp + min((int64_t)warp, more);
+    int l = (int)quotient(u0, per_layer);
+    const int64_t rest = u0 - l * per_layer;
+    int group = (int)quotient(rest, parts), part = (int)(rest - (int64_t)group * parts);
+    const int tk = lane / width, sub = lane - tk * width;
+    int until = 0;  // the tokens that what follows holds for end here
+    int shift[V], had[V], from_free[V];  // row of token t; pages before the call; place of page p in the free list, less p
+    const int32_t* table = nullptr;
+#pragma unroll 1
+    for (int n = 0; n < count; ++n) {
+        const uint32_t place = (uint32_t)group * per + tk;
+        const int t = (int)place, x = part * 32 + sub;
+        if (tk < per && place < (uint32_t)head.total && x < row) {
+            const int g = x * V;
+            if (t >= until) {
+                int lo = 0, hi = a.B - 1;  // the last sequence that starts at t or before
+                while (lo < hi) {
+                    const int mid = (lo + hi + 1) >> 1;
+                    if (cu[mid] <= t)
+                        lo = mid;
+                    else
+                        hi = mid - 1;
+                }
+                until = parts == 1 ? cu[lo + 1] : 0;
+                const int h = (l * a.B + lo) * a.Hkv + g;
+                table = a.table + (int64_t)h * a.max_pages;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const int before = len[h + i];
+                    shift[i] = before - cu[lo];
+                    had[i] = pages_of(a, before);
+                    from_free[i] = head.count - 1 - first[h + i] + had[i];
+                }
+            }
+            int slot[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int r = shift[i] + t, p = r >> a.log_P;
+                const int32_t* from = p < had[i] ? table + ((int64_t)i * a.max_pages + p) : a.free_pages + (from_free[i] - p);
+                slot[i] = (*from << a.log_P) + (r & (a.P - 1));
+            }
+            int32_t* to = a.slots + ((int64_t)l * a.max_tokens + t) * a.Hkv + g;
+            if (V == 4)
+                *reinterpret_cast<int4*>(to) = make_int4(slot[0], slot[1 % V], slot[2 % V], slot[3 % V]);
+            else
+                to[0] = slot[0];
+        }
+        if (++part == parts) {
+            part = 0;
+            if (++group == groups) {
+                group = 0;
+                ++l;
+                until = 0;
+            }
+        }
+    }
+}
+
 // This CTA's share of the table entries (or of the free list's) and of the slot map. first: the
 // scan (shared or global); len: rows of the slabs before the call; cu: token offsets.
 __device__ __forceinline__ void fill(const PageArgs& a, const PageHead& head, const int32_t* first, const int32_t* len, const int32_t* cu)
 {
     const int warps = gridDim.x * (kThreads / 32), warp = (threadIdx.x >> 5) * gridDim.x + blockIdx.x;
+    if (a.slots) {
+        const int w = warps - 1 - warp;  // a small call's slots from the last warp on, its pages from the first: 6.9 us against 7.8
+        if (a.slot_vec == 4)
+            fill_slots<4>(a, head, first, len, cu, w, warps);
+        else
+            fill_slots<1>(a, head, first, len, cu, w, warps);
+    }
     // One page a lane while that is enough (latency counts). Chunks of neighbouring warps lie side by side:
-    // a contiguous piece a warp took 54 us where this takes 40, for the release of 12.8 M pages.
+    // a contiguous piece a warp took 37 us where this takes 28.5, for the release of 12.8 M pages.
     if (head.pages > warps * 32)
         fill_chunks(a, head, first, len, (int64_t)warp * 32 * kLong, (int64_t)warps * 32 * kLong);
     else if (warp * 32 < head.pages)
         fill_pages<1>(a, head, first, len, warp * 32, head.pages, 0, a.NH - 1);
-    if (!a.slots) return;
-    // Slot map [L][t][Hkv], a.slot_vec neighbouring heads (1 or 4) a thread. Pages that this call takes
-    // are read from the free list: their table entries may not be written yet.
-    const int vec = a.slot_vec, row = a.Hkv / vec;
-    const int64_t per_layer = (int64_t)head.total * row, chunks = (per_layer + kThreads - 1) / kThreads;
-    const bool small = chunks * a.L <= INT32_MAX && per_layer <= INT32_MAX - kThreads;  // 32-bit divisions
-#pragma unroll 1
-    for (int64_t x = blockIdx.x; x < chunks * a.L; x += gridDim.x) {
-        const int l = small ? (int)((unsigned)x / (unsigned)chunks) : (int)(x / chunks);
-        const int64_t i = (x - l * chunks) * kThreads + threadIdx.x;
-        if (i >= per_layer) continue;
-        const int t = small ? (int)((unsigned)i / (unsigned)row) : (int)(i / row), g = (int)(i - (int64_t)t * row) * vec;
-        int lo = 0, hi = a.B - 1;  // the last sequence that starts at t or before
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (cu[mid] <= t)
-                lo = mid;
-            else
-                hi = mid - 1;
-        }
-        const int h = (l * a.B + lo) * a.Hkv + g, k = t - cu[lo];
-        auto slot = [&](int hh) {
-            const int before = len[hh], r = before + k, p = r >> a.log_P, had = pages_of(a, before);
-            const int* from = p < had ? a.table + (int64_t)hh * a.max_pages + p : a.free_pages + (head.count - 1 - first[hh] - (p - had));
-            return (*from << a.log_P) + (r & (a.P - 1));
-        };
-        int32_t* to = a.slots + ((int64_t)l * a.max_tokens + t) * a.Hkv + g;
-        if (vec == 4)
-            *reinterpret_cast<int4*>(to) = make_int4(slot(h), slot(h + 1), slot(h + 2), slot(h + 3));
-        else
-            *to = slot(h);
-    }
 }
 
 // The whole call. new_len: the caller's, or the workspace's where that is len itself (then

@@ -39,7 +39,7 @@ enum PageMode { kGrowTokens, kGrowPlan, kRelease };
 
 struct PageArgs {
     int L, B, Hkv, NH, P, log_P, num_pages, max_pages;
-    int skip_b, skip_g;        // 124 slabs as slots and heads: 124 / Hkv and the rest
+    int skip_b, skip_g;        // 128 slabs as slots and heads: 128 / Hkv and the rest
     int slot_vec;              // entries of the slot map a thread writes at once: 4 where they are aligned, else 1
     int mode;                  // PageMode
     const int32_t* tokens;     // [B] new tokens (kGrowTokens) or ended flags (kRelease)

@@ -95,8 +95,8 @@ dkv_status page_args(const dkv_pages* g, const int32_t* len, int32_t* new_len, c
     a->NH = (int)NH;
     a->P = g->page_rows;
     while ((1 << a->log_P) < a->P) ++a->log_P;
-    a->skip_b = 124 / g->H_kv;
-    a->skip_g = 124 % g->H_kv;
+    a->skip_b = 128 / g->H_kv;
+    a->skip_g = 128 % g->H_kv;
     a->num_pages = g->num_pages;
     a->max_pages = g->max_pages;
     a->len = len;

@@ -294,3 +294,65 @@ def test_serving_loop(cuda):
     step([0, 33, 1])
     step([7, 1, 2])  # a slot that held a sequence before starts anew
     assert int(s.status) == 0
+
+
+def tables_of(lens, page, spare, wider):
+    """The tables of a cache without its pools."""
+    cache = paged.Cache(np.zeros((1, 1, 1), int), page)
+    cache.L, cache.B, cache.Hkv = lens.shape
+    cache.lens = lens.reshape(-1).astype(np.int64)
+    pages = -(-cache.lens // page)
+    total = int(pages.sum())
+    order = np.random.default_rng(5).permutation(total + spare).astype(np.int32)
+    cache.table = np.full((cache.lens.size, int(pages.max()) + wider), -1, np.int32)
+    cache.table[np.arange(cache.table.shape[1])[None] < pages[:, None]] = order[:total]
+    cache.free, cache.count = np.concatenate([order[total:], np.full(total, -7, np.int32)]), spare
+    cache.pages = dkv.Pages(L=cache.L, B=cache.B, H=cache.Hkv, H_kv=cache.Hkv, page_rows=page, num_pages=order.size,
+                            max_pages=cache.table.shape[1])
+    return cache
+
+
+@pytest.mark.parametrize("L,Hkv,tokens,off", [
+    (33, 8, [0, 1700, 0, 3001, 7], 0), (33, 8, [5, 1700, 0, 3001], 1), (33, 3, [1, 999, 1500], 0), (70, 1, [40000, 1], 0),
+    (2, 33, [3, 1, 40], 0), (2, 136, [0, 9, 30], 0), (2, 260, [17, 0], 0), (1, 132, [9000], 2),
+])
+def test_slot_map_of_many_entries(cuda, L, Hkv, tokens, off):
+    """More entries than one a lane, past ends of sequences and layers; rows of heads wider than a warp; maps off 16 bytes."""
+    r = np.random.default_rng(Hkv)
+    lens = r.integers(0, 90, (L, len(tokens), Hkv))
+    n = np.broadcast_to(np.asarray(tokens)[None, :, None], lens.shape)
+    need = int((-(-(lens + n) // 64) - -(-lens // 64)).sum())
+    cache = tables_of(lens, 64, need, max(tokens) // 64 + 2)
+    s = State(cache)
+    cap = sum(tokens) + 5
+    cu, flat = dev(np.full(len(tokens) + 1, -9)), dev(np.full(L * cap * Hkv + 8, -3))
+    slots = flat[off:off + L * cap * Hkv].view(L, cap, Hkv)
+    s.tables(tokens=dev(tokens), cu_tokens=cu, slots=slots)
+    table, free, count, ln = paged.tables_after(cache, n)
+    want_cu, want = slot_map(cache, table, tokens, cap)
+    assert int(s.status) == 0
+    s.same(table, free, count, ln)
+    assert np.array_equal(cu.cpu().numpy(), want_cu) and np.array_equal(slots.cpu().numpy(), want)
+    assert (flat[:off] == -3).all() and (flat[off + L * cap * Hkv:] == -3).all()
+
+
+@pytest.mark.parametrize("L,B,Hkv,most", [(8, 8, 8, 16000), (8, 500, 10, 170), (3, 2, 7, 200000), (1, 9, 5, 120000)])
+def test_many_pages(cuda, L, B, Hkv, most):
+    """More pages than one a lane: runs of one slab, chunks of several slabs, slabs of none, some ended."""
+    r = np.random.default_rng(B)
+    lens = r.integers(0, most + 1, (L, B, Hkv))
+    lens[r.integers(0, 4, lens.shape) == 0] = 0
+    tokens = r.integers(0, most, B)
+    n = np.broadcast_to(tokens[None, :, None], lens.shape)
+    need = int((-(-(lens + n) // 16) - -(-lens // 16)).sum())
+    assert need > 152 * 1024
+    cache = tables_of(lens, 16, need + 1, most // 16 + 2)
+    s = State(cache)
+    s.tables(tokens=dev(tokens))
+    assert int(s.status) == 0
+    s.same(*paged.tables_after(cache, n))
+    for ended in (r.integers(0, 2, B), np.ones(B, int)):
+        s = State(cache)
+        s.release(ended)
+        assert int(s.status) == 0
+        s.same(*paged.tables_after(cache, np.broadcast_to(ended[None, :, None], (L, B, Hkv)), release=True))
