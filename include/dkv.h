@@ -452,7 +452,7 @@ typedef struct {
  * plan, seq  a plan of dkv_map_pattern(_inplace) with the geometry's L and H_kv: its
  *            sequence i goes to slot seq[i], n_h = its slab's kept rows. seq: device
  *            int32 [plan B], ascending slots; NULL: slot i. Exactly one of tokens and
- *            plan is given.
+ *            plan is given; seq is NULL with tokens.
  * len        rows of each slab before the call.
  * new_len    receives len[h] + n_h (may be len).
  * table      slab h's entries ceil(len/page_rows) .. ceil((len + n_h)/page_rows) - 1 are
@@ -500,7 +500,7 @@ dkv_status dkv_page_release(const dkv_pages* pages, const int32_t* ended, const 
  * sequence i become the last rows of slot seq[i], rows len[h] - n_h .. len[h] - 1 of
  * each slab, with len and table as they are after dkv_page_tables with this plan.
  * K, V       device 16-bit [L][plan B][H_kv][T_stride][128]. T_stride >= max ctx_len.
- * Bytes are copied exactly; K, V, Kp and Vp are 16-byte aligned. A row whose place is
+ * Bytes are copied exactly; K, V, Kp and Vp are 16-byte aligned and do not overlap. A row whose place is
  * out of range is skipped (DKV_DEV_PAGE_RANGE). Dense plans are rejected.
  */
 dkv_status dkv_page_compact(const dkv_pages* pages, const dkv_plan* plan, const int32_t* seq, const void* K,
@@ -525,7 +525,7 @@ dkv_status dkv_page_compact(const dkv_pages* pages, const dkv_plan* plan, const 
  * table, len  as they are after dkv_page_tables: len[h] counts the new tokens.
  * causal      not 0: token i of a sequence's n new ones attends to the first
  *             len[h] - n + i + 1 rows of its slab; 0: to all len[h] rows.
- * scale       softmax scale; <= 0 selects 1/sqrt(128).
+ * scale       softmax scale; <= 0 selects 1/sqrt(128). scale * log2(e) must be a finite float.
  * out         [num_tokens][H][128]; zeros for a token that has no row to attend to.
  *             Scores, softmax statistics and sums are fp32; each softmax weight is
  *             rounded to dtype for the second product, and the output once.

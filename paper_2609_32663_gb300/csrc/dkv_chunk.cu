@@ -22,6 +22,18 @@
 //     warp 9          TMA: Q tiles, and K and V tiles page by page into one ring in the order of use.
 //     warp 10         walks the CTA's share and describes its units to the others (11 is idle).
 //
+// What bounds it. Next tokens stream the cache: 16 sequences of 3K-24K rows, 847 MB, in 129.6 us, 6.5
+// TB/s of the 6.8 of a plain copy. Turns and queries: a pair unit's tile (four products, 2,048 cycles
+// of the tensor pipe) takes 2,650. Q K^T reads both operands from shared memory, 8 KB a 64-cycle
+// instruction and so the 128 B a cycle that it gives, beside the copies into the ring: about 670 cycles
+// instead of 512, which makes 2,400 the least of this form. The rest are the hand-offs between MMA and
+// softmax warps (without any softmax the queries below take 121 us of 137). 200-777 queries over
+// 5K-13K rows: 137 us, 1.16 PFLOP/s with the shares' ends; 4K tokens over 45K rows: 1,723 us, 1.44
+// PFLOP/s, 0.85 of what the library's matrix product sustains. One token over 1.8K rows: 14.5 us, all of
+// it latency: two launches, the count of the cost, one tile, the join.
+// Two MMA warps, a group each, took 173 us for the queries (their products alternate on the pipe), four
+// softmax warpgroups 152; stages freed by the softmax warps instead of by commits 136.
+//
 // Every wait is bounded (polls and 2 s), and so are the softmax warps' meetings (Waits::meet); one
 // that runs out sets DKV_DEV_TMA_TIMEOUT, the roles leave, copies and products in flight are
 // drained, and the outputs of the CTA's unfinished units stay unwritten.
@@ -490,10 +502,11 @@ __device__ __forceinline__ void exponentials(const uint32_t (&x)[32], uint64_t c
 // `s`) to P over them, with the running max m (of raw scores), sum l and output `o`. lim: the
 // cache rows of this tile that the thread's query sees (may be outside 0 .. 128).
 // The max moves only when a score tops it by 2^kSlack (then O is rescaled, so `rescale` says
-// whether it holds anything): P stays below 2^kSlack. So the first half of P is computed with the
-// max as it was, beside the tile's own max, and again in the rare step that moves it: the max is off the
-// path from S to P. fp16 P is scaled by 2^7 more, which l shares: the smallest normal P is then 2^-21 of the
-// largest score's.
+// whether it holds anything): P stays below 2^kSlack. fp16 P is scaled by 2^7 more, which l shares: the
+// smallest normal P is then 2^-21 of the largest score's. The first half of P is signalled alone, so that
+// its products run beside the second half's exponentials (signalled at 96 of the 128 columns: 144 us
+// instead of 141 for 777 queries over 13K rows; with that half computed by the old max, beside the tile's own
+// max: 163 instead of 145).
 template <bool F16>
 __device__ __forceinline__ void softmax_step(uint32_t s, uint32_t o, int lim, bool rescale, float c, float& m, float& l, uint32_t half_bar)
 {

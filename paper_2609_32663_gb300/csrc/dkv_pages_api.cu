@@ -134,6 +134,7 @@ dkv_status dkv_page_tables(const dkv_pages* g, const int32_t* tokens, const dkv_
                                     status, &a);
     if (st != DKV_OK) return st;
     if ((tokens != nullptr) == (plan != nullptr)) return refuse("exactly one of tokens and plan is given");
+    if (seq && !plan) return refuse("seq goes with a plan");
     if (plan && (cu_tokens || slots)) return refuse("cu_tokens and slots go with tokens, not with a plan");
     if (slots && !cu_tokens) return refuse("slots needs cu_tokens");
     if (slots && (max_tokens < 0 || max_tokens > 0x7fffffffLL))
@@ -215,7 +216,9 @@ dkv_status dkv_chunk_attn(const dkv_pages* g, int32_t layer, int32_t dtype, int3
     if (dtype != DKV_BF16 && dtype != DKV_FP16) return refuse("dtype=%d: DKV_BF16 or DKV_FP16", dtype);
     if (num_tokens < 0 || (int64_t)num_tokens * g->H > (1 << 30))
         return refuse("num_tokens=%d: need 0 <= num_tokens and num_tokens*H <= 2^30", num_tokens);
-    if (!std::isfinite(scale)) return refuse("scale is not finite");
+    const float sc = scale > 0.f ? scale : 1.0f / std::sqrt((float)dkv::kHeadDim);
+    const float qscale = sc * 1.4426950408889634f;  // base-2 softmax: exp(x) = exp2(x log2 e)
+    if (!std::isfinite(scale) || !std::isfinite(qscale)) return refuse("scale=%g is not finite, or too large", scale);
     if ((k_new == nullptr) != (v_new == nullptr)) return refuse("k_new and v_new must both be given or both be NULL");
     if (num_tokens == 0) return dkv::set_error(DKV_OK, "");
     if (!q || !cu_tokens || !table || !len || !Kp || !Vp || !out) return refuse("NULL q/cu_tokens/table/len/Kp/Vp/out");
@@ -259,8 +262,7 @@ dkv_status dkv_chunk_attn(const dkv_pages* g, int32_t layer, int32_t dtype, int3
     a.max_pages = g->max_pages;
     a.causal = causal != 0;
     a.fp16 = dtype == DKV_FP16;
-    const float sc = scale > 0.f ? scale : 1.0f / std::sqrt((float)dkv::kHeadDim);
-    a.qscale = sc * 1.4426950408889634f;  // base-2 softmax: exp(x) = exp2(x log2 e)
+    a.qscale = qscale;
     return launched(dkv::launch_chunk(a, fault("copy"), stream), "chunk attention kernels");
 }
 

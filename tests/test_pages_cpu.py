@@ -128,3 +128,15 @@ def test_injected_launch_failure(dkv, monkeypatch):
         g = geometry(dkv).c
         assert dkv.lib().dkv_page_tables(ctypes.byref(g), *tables_args(), None) == dkv.DKV_ERR_CUDA
         assert b"page table" in dkv.lib().dkv_last_error()
+
+
+@pytest.mark.parametrize("scale", [3e38, float("inf"), float("-inf")])
+def test_scale_past_the_base_2_softmax_is_refused(dkv, scale):
+    """Its product with log2(e) is infinite: every score of 0 would give NaN."""
+    g = geometry(dkv).c
+    refused(dkv, dkv.lib().dkv_chunk_attn(ctypes.byref(g), *chunk_args(scale=scale), None), "scale")
+
+
+def test_seq_without_a_plan_is_refused(dkv):
+    g = geometry(dkv).c
+    refused(dkv, dkv.lib().dkv_page_tables(ctypes.byref(g), *tables_args(seq=A), None), "seq")
