@@ -13,13 +13,13 @@
 // kFusedSlabs slabs each CTA scans them all itself (64 KB through L2 at 16,384 slabs, 2-3 us) into
 // shared memory and then fills its share: one launch and 6.9 us for a step of 4,096 slabs, where a
 // scan kernel and a fill kernel behind it took 12.4. Lengths and counts that are updated in place
-// are committed by a second, tiny launch, as CTAs may still be reading them. More slabs: one
+// are committed by a second, tiny launch (1.2 us), as CTAs may still be reading them. More slabs: one
 // CTA scans into the workspace, then all fill.
 // Every value that lives on the device is checked in the scan: nothing is written if a check fails
 // or the free list is too short.
 //
-// What bounds it: launches and the scan for a decode step (4.4 us of its 6.9); instructions more than bytes for
-// the large calls: 12.8 M pages given back, 103 MB, in 28.5 us, of which the scan takes 5 and whole runs of one slab go at
+// What bounds it: the launch and the scan for a decode step (4.4 us of its 6.9); instructions more than bytes for
+// the large calls: 12.8 M pages given back, 103 MB, in 28.5 us, of which the scan takes 4 and whole runs of one slab go at
 // 6.4 TB/s; 256 K pages and 4.1 M slots, 17.7 MB, in 11.6 us.
 #include "dkv_decode_common.cuh"
 #include "dkv_pages.cuh"
