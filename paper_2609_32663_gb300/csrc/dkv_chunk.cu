@@ -27,12 +27,12 @@
 // of the tensor pipe) takes 2,650. Q K^T reads both operands from shared memory, 8 KB a 64-cycle
 // instruction and so the 128 B a cycle that it gives, beside the copies into the ring: about 670 cycles
 // instead of 512, which makes 2,400 the least of this form. The rest are the hand-offs between MMA and
-// softmax warps (without any softmax the queries below take 121 us of 137). 200-777 queries over
-// 5K-13K rows: 137 us, 1.16 PFLOP/s with the shares' ends; 4K tokens over 45K rows: 1,723 us, 1.44
-// PFLOP/s, 0.85 of what the library's matrix product sustains. One token over 1.8K rows: 14.5 us, all of
+// softmax warps. 200-777 queries over 5K-13K rows: 125.5 us, 1.27 PFLOP/s, 100 us of it in the loop;
+// 4K tokens over 45K rows: 1,700 us, 1.46 PFLOP/s, 0.86 of what the library's matrix product sustains
+// (1,531 us before the clocks fall under the power limit). One token over 1.8K rows: 14.5 us, all of
 // it latency: two launches, the count of the cost, one tile, the join.
-// Two MMA warps, a group each, took 173 us for the queries (their products alternate on the pipe), four
-// softmax warpgroups 152; stages freed by the softmax warps instead of by commits 136.
+// Two MMA warps, a group each, took 173 us for the queries where one took 137 (their products alternate on
+// the pipe), four softmax warpgroups 152; stages freed by the softmax warps instead of by commits 136.
 //
 // Every wait is bounded (polls and 2 s), and so are the softmax warps' meetings (Waits::meet); one
 // that runs out sets DKV_DEV_TMA_TIMEOUT, the roles leave, copies and products in flight are
@@ -707,6 +707,87 @@ __device__ __forceinline__ float2 load_l2(const float2* p)
     return v;
 }
 
+__device__ __forceinline__ int load_acquire(const int32_t* p)
+{
+    int v;
+    asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+
+// A row's max and sum over the pieces of its unit, one after the other. (The roundings are written out:
+// what joins the pieces must not show in the result.)
+struct RowSum {
+    float M, L;
+    __device__ __forceinline__ void add(float2 ml, float c)
+    {
+        if (ml.x == -INFINITY && ml.y == 0.f) return;  // a piece that the row does not see
+        const float M1 = fmaxf(M, ml.x);
+        const float of_ml = __fmul_rn(ml.y, ml.x == -INFINITY ? 0.f : ex2((ml.x - M1) * c));
+        L = __fmaf_rn(L, M == -INFINITY ? 0.f : ex2((M - M1) * c), of_ml);
+        M = M1;
+    }
+};
+
+// Pieces that one thread adds up, in their order. A turn's units are cut in two or three, all but the last stored
+// long before; with that one stored and all read again as items of join_items the last CTAs took 9 to 17 us
+// longer (200-777 queries over 5K-13K rows: 137 us, 125.5 so).
+constexpr int kFew = 3;
+
+// Where piece k of the unit that starts in CTA c0 lies.
+__device__ __forceinline__ int64_t piece_at(int c0, int k) { return (int64_t)(c0 + k) * 2 + (k == 0); }
+
+// Joining a pair unit's few pieces, this CTA's (`own`) still in TMEM: the thread of each row adds the
+// others to it. The sums are those of join_items.
+template <bool F16>
+__device__ __forceinline__ void join_own(const ChunkArgs& a, const ChunkWork& w, int c0, int pieces, int own, int prow, bool live, float2 mine,
+                                         uint32_t o_at, uint16_t* out)
+{
+    const float c = a.qscale;
+    float2 ml[kFew];
+#pragma unroll
+    for (int k = 0; k < kFew; ++k) {
+        ml[k] = k == own ? mine : make_float2(-INFINITY, 0.f);
+        if (k < pieces && k != own && live) ml[k] = load_l2(w.ml + piece_at(c0, k) * kPieceRows + prow);
+    }
+    RowSum sum{-INFINITY, 0.f};
+#pragma unroll
+    for (int k = 0; k < kFew; ++k) sum.add(ml[k], c);
+    const float z = inverse(sum.L);
+#pragma unroll 1
+    for (int e = 0; e < kHeadDim / 32; ++e) {
+        float acc[32];
+#pragma unroll
+        for (int d = 0; d < 32; ++d) acc[d] = 0.f;
+#pragma unroll
+        for (int k = 0; k < kFew; ++k) {
+            if (k >= pieces) continue;
+            __syncwarp();
+            const bool seen = live && !(ml[k].x == -INFINITY && ml[k].y == 0.f);
+            const float f = ex2((ml[k].x - sum.M) * c);
+            if (k == own) {
+                float v[32];
+                tmem_ld32(o_at + 32 * e, v);
+                if (seen)
+#pragma unroll
+                    for (int d = 0; d < 32; ++d) acc[d] = fmaf(v[d], f, acc[d]);
+            } else if (seen) {
+                const float4* o = w.o + (piece_at(c0, k) * (kHeadDim / 4) + 8 * e) * kPieceRows + prow;
+                float4 u[8];
+#pragma unroll
+                for (int d = 0; d < 8; ++d) u[d] = load_l2(o + d * kPieceRows);
+#pragma unroll
+                for (int d = 0; d < 8; ++d) {
+                    acc[4 * d] = fmaf(u[d].x, f, acc[4 * d]);
+                    acc[4 * d + 1] = fmaf(u[d].y, f, acc[4 * d + 1]);
+                    acc[4 * d + 2] = fmaf(u[d].z, f, acc[4 * d + 2]);
+                    acc[4 * d + 3] = fmaf(u[d].w, f, acc[4 * d + 3]);
+                }
+            }
+        }
+        if (live) store_out<F16>(out + 32 * e, acc, z);
+    }
+}
+
 // Joining the pieces of a unit: eight elements of a row an item, neighbouring rows in
 // neighbouring lanes, the sums in the order of the CTAs. Loads are most of it, so ITEMS items of
 // a thread and PIECES of their pieces are on the way at once (16 loads of 16 bytes).
@@ -736,7 +817,7 @@ __device__ __forceinline__ void join_items(const ChunkArgs& a, const ChunkWork& 
 #pragma unroll
             for (int z = 0; z < PIECES; ++z) {
                 const int k = min(k0 + z, pieces - 1);
-                const int64_t piece = (int64_t)(c0 + k) * 2 + (k == 0);
+                const int64_t piece = piece_at(c0, k);
 #pragma unroll
                 for (int y = 0; y < ITEMS; ++y) {
                     const float4* o = w.o + (piece * (kHeadDim / 4) + 2 * ch[y]) * kPieceRows + at[y];
@@ -775,21 +856,16 @@ __device__ __forceinline__ void join_pieces(const ChunkArgs& a, const ChunkWork&
 {
     const int tid = threadIdx.x, rows = tokens * a.G, low = kTile / a.G * a.G;
     const float c = a.qscale;
-    // As many lanes a row as there are threads for (a power of 2).
-    int lanes = 32;
+    // As many lanes a row as there are threads for (a power of 2), one for few pieces.
+    int lanes = pieces <= kFew ? 1 : 32;
     while (lanes > 1 && lanes * rows > kSoft) lanes >>= 1;
     const int x = tid / lanes, first = tid & (lanes - 1), at = x < low ? x : x - low + kTile;
-    float M = -INFINITY, L = 0.f;
+    RowSum sum{-INFINITY, 0.f};
     if (x < rows) {
 #pragma unroll 4
-        for (int k = first; k < pieces; k += lanes) {
-            const float2 ml = __ldcg(w.ml + ((int64_t)(c0 + k) * 2 + (k == 0)) * kPieceRows + at);
-            if (ml.x == -INFINITY && ml.y == 0.f) continue;
-            const float M1 = fmaxf(M, ml.x);
-            L = L * (M == -INFINITY ? 0.f : ex2((M - M1) * c)) + ml.y * (ml.x == -INFINITY ? 0.f : ex2((ml.x - M1) * c));
-            M = M1;
-        }
+        for (int k = first; k < pieces; k += lanes) sum.add(__ldcg(w.ml + piece_at(c0, k) * kPieceRows + at), c);
     }
+    float M = sum.M, L = sum.L;
 #pragma unroll 1
     for (int o = lanes >> 1; o >= 1; o >>= 1) {
         const float M0 = __shfl_xor_sync(kFull, M, o), L0 = __shfl_xor_sync(kFull, L, o), M1 = fmaxf(M, M0);
@@ -1076,6 +1152,26 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (steps > p && !wait(&o_done[p], no++ & 1)) break;
             tc_fence_after();
             uint16_t* out = a.out + ((int64_t)(k.t0 + tok) * a.H + k.g * a.G + j) * kHeadDim;
+            // Of a pair unit with few pieces, all others may be done: then this one is not stored. (Not if some of
+            // its rows may have to be mended.)
+            int c0 = c, pieces = 1;
+            bool few = false, last = false;
+            if (!whole) {
+                if (!wait(&late[unit % kAhead], (unit / kAhead) & 1)) break;
+                const volatile Piece* d = reinterpret_cast<const volatile Piece*>(sm + kOffPieces) + unit % kAhead;
+                c0 = d->c0;
+                pieces = d->pieces;
+                few = pair && pieces <= kFew && min(k.kv, k.j1 * kTile) <= k.row0;
+                if (few) {
+                    if (tid == 0) {
+                        pdl_wait();  // the counters are cleared
+                        misc[2] = load_acquire(w.done + c0) == pieces - 1;
+                    }
+                    if (!wait.meet()) break;
+                    last = misc[2];
+                    if (last) __threadfence();
+                }
+            }
             const int64_t slot = (int64_t)c * 2 + (k.j0 == 0);
             const int prow = (pair ? p * kTile : 0) + r;
             // Cache rows of this piece, and whether some of them are hidden from the thread's query.
@@ -1085,7 +1181,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             float4* o_piece = whole ? nullptr : w.o + slot * (kHeadDim / 4) * kPieceRows + prow;
             float odd = 0.f;  // NaN if a result is not finite
             if (pair) {
-                if (any) {
+                if (any && !last) {
                     const float z = inverse(l);
 #pragma unroll 1
                     for (int e = 0; e < 4; ++e) {
@@ -1130,22 +1226,19 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (live && !whole && p == 0) __stcg(w.ml + slot * kPieceRows + prow, make_float2(M, L));
                 }
             }
-            if (!whole) {
+            if (!whole && !last) {
                 __threadfence();
-                if (!wait(&late[unit % kAhead], (unit / kAhead) & 1)) break;
-                const volatile Piece* d = reinterpret_cast<const volatile Piece*>(sm + kOffPieces) + unit % kAhead;
-                const int c0 = d->c0, pieces = d->pieces;
                 if (!wait.meet()) break;
                 if (tid == 0) {
                     pdl_wait();  // the counters are cleared
                     misc[2] = atomicAdd(w.done + c0, 1) == pieces - 1;
                 }
                 if (!wait.meet()) break;
-                if (misc[2]) {
-                    __threadfence();
-                    join_pieces<F16>(a, w, wait, sh_ml, k.t0, k.tokens, k.g, c0, pieces);
-                }
+                last = misc[2];
+                if (last) __threadfence();
+                if (last && !few) join_pieces<F16>(a, w, wait, sh_ml, k.t0, k.tokens, k.g, c0, pieces);
             }
+            if (few && last && any) join_own<F16>(a, w, c0, pieces, c - c0, prow, live, make_float2(m, l), o_at + p * kTile, out);
             if (!pair || !whole) {
                 tc_fence_before();
                 if (!wait.meet()) break;  // O of the other group, sh_ml and misc[2] are read

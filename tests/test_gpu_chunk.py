@@ -268,3 +268,27 @@ def test_many_short_units_in_one_share(cuda):
     c = Call(cache, 0, qkv, cu).run()
     want, size, _, _ = paged.attention(cache, 0, *qkv, cu, True)
     paged.assert_attention(c.out, want, size, cache.dtype)
+
+
+@pytest.mark.parametrize("causal,dtype", [(True, torch.bfloat16), (False, torch.float16)])
+def test_units_of_two_and_three_pieces(cuda, causal, dtype):
+    """Units a little longer than a CTA's share: whichever CTA is last joins them, from what is stored and what it
+    still holds, and the result is the same bits beside other work."""
+    tokens, H, Hkv = [640], 32, 4
+    cache = paged.Cache(lens_of(1, 1, Hkv, [1450], tokens, 3), 32, dtype=dtype, H=H)
+    cu, qkv = inputs(cache, tokens, 5)
+    c = Call(cache, 0, qkv, cu, causal).run()
+    torch.cuda.synchronize()
+    want, size, _, _ = paged.attention(cache, 0, *qkv, cu, causal)
+    paged.assert_attention(c.out, want, size, dtype, "pieces")
+    first, side, x = c.out.clone(), torch.cuda.Stream(), torch.randn((2048, 2048), device="cuda")
+    for i in range(60):
+        c.out.fill_(NAN)
+        if i % 2:
+            with torch.cuda.stream(side):
+                for _ in range(1 + i % 5):
+                    x = torch.sin(x)
+        c.run()
+        torch.cuda.synchronize()
+        assert torch.equal(c.out.view(torch.int16), first.view(torch.int16)), f"call {i} differs"
+    assert int(c.status) == 0
