@@ -24,10 +24,11 @@
 //
 // What bounds it. Next tokens stream the cache: 16 sequences of 3K-24K rows, 847 MB, in 129.6 us, 6.5
 // TB/s of the 6.8 of a plain copy. Turns and queries: a pair unit's tile (four products, 2,048 cycles
-// of the tensor pipe) takes 2,650. Q K^T reads both operands from shared memory, 8 KB a 64-cycle
-// instruction and so the 128 B a cycle that it gives, beside the copies into the ring: about 670 cycles
-// instead of 512, which makes 2,400 the least of this form. The rest are the hand-offs between MMA and
-// softmax warps. 200-777 queries over 5K-13K rows: 125.5 us, 1.27 PFLOP/s, 100 us of it in the loop;
+// of the tensor pipe at its best) takes 1.52 us, 2,900 cycles. Q K^T reads both operands from shared
+// memory, 8 KB a 64-cycle instruction and so the 128 B a cycle that it gives, beside the copies into
+// the ring: about 630 cycles instead of 512, so the pipe is busy for 2,280. What bounds it is each
+// group's chain, as TMEM holds one S a group: 950 cycles from S to the first half of P, P V and the
+// next Q K^T behind it, and four hand-offs of 100 to 150 cycles. 200-777 queries over 5K-13K rows: 125.5 us, 1.27 PFLOP/s, 100 us of it in the loop;
 // 4K tokens over 45K rows: 1,700 us, 1.46 PFLOP/s, 0.86 of what the library's matrix product sustains
 // (1,531 us before the clocks fall under the power limit). One token over 1.8K rows: 14.5 us, all of
 // it latency: two launches, the count of the cost, one tile, the join.
