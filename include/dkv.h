@@ -526,7 +526,8 @@ dkv_status dkv_page_compact(const dkv_pages* pages, const dkv_plan* plan, const 
  * causal      not 0: token i of a sequence's n new ones attends to the first
  *             len[h] - n + i + 1 rows of its slab; 0: to all len[h] rows.
  * scale       softmax scale; <= 0 selects 1/sqrt(128). scale * log2(e) must be a finite float.
- * out         [num_tokens][H][128]; zeros for a token that has no row to attend to.
+ * out         [num_tokens][H][128]; zeros for a token that has no row to attend to, or
+ *             whose scores are all -infinity.
  *             Scores, softmax statistics and sums are fp32; each softmax weight is
  *             rounded to dtype for the second product, and the output once.
  * workspace   dkv_chunk_workspace_bytes(pages) bytes (-1: a bad geometry), about 43 MB.

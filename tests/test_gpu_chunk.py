@@ -292,3 +292,25 @@ def test_units_of_two_and_three_pieces(cuda, causal, dtype):
         torch.cuda.synchronize()
         assert torch.equal(c.out.view(torch.int16), first.view(torch.int16)), f"call {i} differs"
     assert int(c.status) == 0
+
+
+def test_more_slabs_than_costs_fit(cuda):
+    """Past 20,480 slabs a layer the costs are kept for groups of slabs."""
+    B, Hkv = 512, 42
+    tokens = [1 + b % 3 if b % 9 == 0 else 0 for b in range(B)]
+    tokens[301] = 150
+    ctx = np.array([b % 4 * 37 if tokens[b] else 0 for b in range(B)])
+    lens = np.broadcast_to((ctx + tokens)[None, :, None], (1, B, Hkv)).copy()
+    lens[0, 301, 5:] += 90
+    check(paged.Cache(lens, 16), 0, tokens)
+
+
+@pytest.mark.parametrize("tokens,ctx", [([1], 300), ([40], 200), ([1, 5], 0)])
+def test_scores_of_minus_infinity_alone_give_zeros(cuda, tokens, ctx):
+    cache = paged.Cache(lens_of(1, len(tokens), 2, [ctx] * len(tokens), tokens, 2), 16, H=8)
+    cu, qkv = inputs(cache, tokens, 1, fused=False)
+    qkv[0] = qkv[0].abs() + 1
+    c = Call(cache, 0, qkv, cu, append=False)
+    c.Kp.fill_(-float("inf"))
+    c.run()
+    assert int(c.status) == 0 and (c.out == 0).all()
