@@ -513,7 +513,8 @@ dkv_status dkv_page_compact(const dkv_pages* pages, const dkv_plan* plan, const 
  *
  * dtype       DKV_BF16 or DKV_FP16: type of q, k_new, v_new, Kp, Vp and out.
  * num_tokens  rows of q, k_new, v_new and out; num_tokens * H <= 2^30. Tokens cu_tokens[b] .. cu_tokens[b + 1] - 1
- *             are sequence b's; cu_tokens (device int32 [B + 1]) ascends from 0. Rows
+ *             are sequence b's; cu_tokens (device int32 [B + 1]) ascends from 0 to at most
+ *             num_tokens (else nothing is written and DKV_DEV_PAGE_RANGE is set). Rows
  *             from cu_tokens[B] on are no token's: not read, and left as they are in out.
  * q           [num_tokens][H][128], token t at q + t * q_stride elements.
  * k_new,      [num_tokens][H_kv][128], token t at t * kv_stride elements, or both

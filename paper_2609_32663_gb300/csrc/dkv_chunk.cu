@@ -220,6 +220,15 @@ __device__ __forceinline__ void report(const ChunkArgs& a, int bits)
     if (a.status) atomicOr(a.status, bits);
 }
 
+// Token offsets hold if they start at 0, ascend and end within the batch; whether the pair (b, b + 1) breaks
+// that. Every CTA of both kernels looks at all pairs: with one that breaks it the call does nothing (followed
+// as far as they go, such offsets would lead to rows of earlier tokens).
+__device__ __forceinline__ bool bad_offsets(const ChunkArgs& a, int b)
+{
+    const int t0 = a.cu[b], t1 = a.cu[b + 1];
+    return t1 < t0 || t1 > a.T || (b == 0 && t0 != 0);
+}
+
 // ---------------------------------------------------------------- append
 constexpr int kAppThreads = 512;
 
@@ -233,18 +242,16 @@ __global__ void __launch_bounds__(kAppThreads) chunk_append_kernel(const __grid_
     if (blockIdx.x == 0) {
         // The attention kernel's counters, and the checks of what lives on the device.
         if (tid < kMaxCtas) w.done[tid] = 0;
-        if (tid < a.B) {
-            const int t0 = a.cu[tid], t1 = a.cu[tid + 1];
-            if (t0 < 0 || t1 < t0 || t1 > a.T || (tid == 0 && t0 != 0)) report(a, DKV_DEV_PAGE_RANGE);
-        }
+        if (tid < a.B && bad_offsets(a, tid)) report(a, DKV_DEV_PAGE_RANGE);
         for (int h = tid; h < a.B * a.Hkv; h += kAppThreads) {
             const int b = h / a.Hkv, n = cu_at(a, b + 1) - cu_at(a, b), len = a.len[h];
             if (n > 0 && (len != slab_len(a, h) || (a.k_new && len < n))) report(a, DKV_DEV_PAGE_RANGE);
         }
         return;
     }
-    if (tid < a.B) cu[tid] = cu_at(a, tid);
-    if (tid == 0) cu[a.B] = cu_at(a, a.B);
+    const bool bad = tid < a.B && bad_offsets(a, tid);
+    if (tid < a.B) cu[tid] = a.cu[tid];
+    if (tid == 0) cu[a.B] = a.cu[a.B];
     // A half-warp a row (K and V).
     const int64_t i = (int64_t)(blockIdx.x - 1) * (kAppThreads / 16) + (tid >> 4);
     const int sub = tid & 15, t = (int)(i / a.Hkv), g = (int)(i - (int64_t)t * a.Hkv);
@@ -254,8 +261,7 @@ __global__ void __launch_bounds__(kAppThreads) chunk_append_kernel(const __grid_
         kv = __ldcs(reinterpret_cast<const uint4*>(a.k_new + src) + sub);
         vv = __ldcs(reinterpret_cast<const uint4*>(a.v_new + src) + sub);
     }
-    __syncthreads();
-    if (t >= cu[a.B]) return;
+    if (__syncthreads_or(bad) || t >= cu[a.B]) return;
     int lo = 0, hi = a.B - 1;  // the last sequence that starts at t or before
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -315,11 +321,16 @@ __device__ __forceinline__ Extent count_cost(const ChunkArgs& a, int64_t* before
         const int64_t y = __shfl_up_sync(kFull, up, o);
         if (lane >= o) up += y;
     }
-    // Whether there is a pair unit goes along in the sums' upper bits (a barrier that votes, instead,
-    // cost the whole kernel 5 %).
-    constexpr int kFlag = 56;
-    const int64_t pairs = __any_sync(kFull, any_pair) ? (int64_t)1 << kFlag : 0;
-    if (lane == 31) sums[warp] = up + pairs;
+    // Whether there is a pair unit, and whether the offsets are bad, goes along in the sums' upper bits (a
+    // barrier that votes, instead, cost the whole kernel 5 %). The cost itself is below 2^52: at most 2^26
+    // slabs' last units and 2^23 full ones, 2^24 tiles each.
+    constexpr int kFlag = 52, kBad = kFlag + 4;
+    static_assert(kThreads / 32 < 16, "a field of 4 bits counts the warps");
+    bool bad = false;
+#pragma unroll 1
+    for (int b = tid; b < a.B; b += kThreads) bad |= bad_offsets(a, b);
+    const int64_t flags = (__any_sync(kFull, any_pair) ? (int64_t)1 << kFlag : 0) + (__any_sync(kFull, bad) ? (int64_t)1 << kBad : 0);
+    if (lane == 31) sums[warp] = up + flags;
     __syncthreads();
     int64_t base = up - mine, total = 0;
 #pragma unroll
@@ -327,11 +338,13 @@ __device__ __forceinline__ Extent count_cost(const ChunkArgs& a, int64_t* before
         if (k < warp) base += sums[k] & (((int64_t)1 << kFlag) - 1);
         total += sums[k];
     }
-    const int dearest = total >> kFlag ? kPairCost : kSplitCost;
+    const bool skip = total >> kBad;
+    const int dearest = (total >> kFlag) & 15 ? kPairCost : kSplitCost;
     total &= ((int64_t)1 << kFlag) - 1;
 #pragma unroll 1
     for (int x = g0; x < g1; ++x) before[x] += base;
     __syncthreads();
+    if (skip) return Extent{0, 0};
     // A share is at least as long as the dearest tile, so that one starts in every share of a unit.
     static_assert(kPairCost >= kSplitCost, "the dearest tile");
     return Extent{total, total >= (int64_t)nctas * dearest ? nctas : (int)((unsigned)total / (unsigned)dearest)};
