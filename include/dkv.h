@@ -523,7 +523,9 @@ dkv_status dkv_page_compact(const dkv_pages* pages, const dkv_plan* plan, const 
  *             Strides are in elements, multiples of 8, at least H*128 (H_kv*128), so
  *             that q, k_new and v_new may be slices of one projection; all 16-byte
  *             aligned. They must not overlap out or the pools.
- * table, len  as they are after dkv_page_tables: len[h] counts the new tokens.
+ * table, len  as they are after dkv_page_tables: len[h] counts the new tokens. A slab whose
+ *             length is out of [0, max_pages * page_rows] counts as empty, and the tokens
+ *             that a slab has no row for are not appended (DKV_DEV_PAGE_RANGE).
  * causal      not 0: token i of a sequence's n new ones attends to the first
  *             len[h] - n + i + 1 rows of its slab; 0: to all len[h] rows.
  * scale       softmax scale; <= 0 selects 1/sqrt(128). scale * log2(e) must be a finite float.

@@ -103,9 +103,11 @@ struct Unit {
     __device__ __forceinline__ int tiles() const { return max(1, (kv + kTile - 1) / kTile); }
 };
 
+// Rows of slab h; none if its length is out of range.
 __device__ __forceinline__ int slab_len(const ChunkArgs& a, int h)
 {
-    return (int)min((int64_t)max(a.len[h], 0), (int64_t)a.max_pages * a.P);
+    const int len = a.len[h];
+    return len >= 0 && len <= a.max_pages * a.P ? len : 0;  // (the product is below 2^31)
 }
 
 // Unit i of the n tokens from row t of q on, over a slab of len rows.
@@ -271,14 +273,14 @@ __global__ void __launch_bounds__(kAppThreads) chunk_append_kernel(const __grid_
             hi = mid - 1;
     }
     const int h = lo * a.Hkv + g;
-    const int64_t r = (int64_t)a.len[h] - cu[lo + 1] + t;
+    const int r = slab_len(a, h) - cu[lo + 1] + t;  // below the slab's length
     int page = -1;
-    if (r >= 0 && r < (int64_t)a.max_pages * a.P) page = a.table[(int64_t)h * a.max_pages + (int)r / a.P];
+    if (r >= 0) page = a.table[(int64_t)h * a.max_pages + r / a.P];
     if (page < 0 || page >= a.num_pages) {
         if (sub == 0) report(a, DKV_DEV_PAGE_RANGE);
         return;
     }
-    const int64_t row = (int64_t)page * a.P + (int)r % a.P;
+    const int64_t row = (int64_t)page * a.P + r % a.P;
     reinterpret_cast<uint4*>(a.Kp + row * kHeadDim)[sub] = kv;
     reinterpret_cast<uint4*>(a.Vp + row * kHeadDim)[sub] = vv;
 }

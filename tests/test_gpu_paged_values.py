@@ -56,3 +56,41 @@ def test_bad_token_offsets_of_many_slots(cuda):
         assert int(c.status) == dkv.DKV_DEV_PAGE_RANGE
         for got, old in zip((c.Kp, c.Vp, c.out), before):
             assert torch.equal(bits(got), old)
+
+
+@pytest.mark.parametrize("over", [1, 2, 3, 100, -1])
+def test_a_length_out_of_range_counts_as_empty(cuda, over):
+    """A slab whose length passes its table (or is negative): none of its rows is written or read, though some of the
+    new tokens' places would lie in the table."""
+    tokens = [2, 3, 2]
+    cache = paged.Cache(lens_of(1, 3, 1, [40, 61, 60], tokens, 1), 16, H=4, wider=0)
+    cap = cache.pages.max_pages * 16
+    assert cache.lens[1] == cap
+    cu, qkv = inputs(cache, tokens, 3)
+    want, size, Kp, Vp = paged.attention(cache, 0, *qkv, cu, True)
+    c = Call(cache, 0, qkv, cu)
+    c.len[1] = cap + over if over > 0 else over
+    before = bits(c.Kp), bits(c.Vp)
+    c.run()
+    assert int(c.status) == dkv.DKV_DEV_PAGE_RANGE
+    mine = torch.from_numpy(cache.rows(1))
+    for got, old in zip((c.Kp, c.Vp), before):
+        assert torch.equal(bits(got)[mine], old[mine])
+    assert not c.out[2:5].any()
+    for t in (slice(0, 2), slice(5, 7)):
+        paged.assert_attention(c.out[t], want[t], size[t], cache.dtype)
+    for h in (0, 2):
+        assert torch.equal(c.Kp.cpu()[cache.rows(h)].double(), Kp[cache.rows(h)])
+
+
+def test_a_slab_shorter_than_its_new_tokens(cuda):
+    """Tokens that the slab has no row for are skipped and reported, the others are placed."""
+    tokens = [5, 1]
+    cache = paged.Cache(np.array([[[3], [40]]]), 16, H=4)
+    cu, qkv = inputs(cache, tokens, 3)
+    c = Call(cache, 0, qkv, cu).run()
+    assert int(c.status) == dkv.DKV_DEV_PAGE_RANGE
+    Kp = cache.Kp.clone()
+    Kp[cache.rows(0)] = qkv[1][2:5, 0]
+    Kp[cache.rows(1)[-1]] = qkv[1][5, 0]
+    assert torch.equal(bits(c.Kp.cpu()), bits(Kp))
