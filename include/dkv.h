@@ -471,7 +471,9 @@ typedef struct {
  * negative count, a slab past max_pages, more than max_tokens tokens with a slot map,
  * seq out of order or range (DKV_DEV_PAGE_RANGE), no table entry and no slot is written,
  * new_len = len, new_count = free_count, and cu_tokens is all 0: a dkv_chunk_attn that
- * follows then does nothing.
+ * follows then does nothing. Page numbers are outside of this rule: one that is out of
+ * [0, num_pages) in the free list or in a table is found where it is used, sets
+ * DKV_DEV_PAGE_RANGE, and -1 stands in its place in the table entry or the slots.
  * Errors: DKV_ERR_INVALID_ARG, DKV_ERR_CUDA.
  */
 int64_t dkv_page_workspace_bytes(const dkv_pages* pages);
@@ -488,7 +490,8 @@ dkv_status dkv_page_tables(const dkv_pages* pages, const int32_t* tokens, const 
  * free_pages entries free_count .. new_count - 1 are written.
  * new_count  receives free_count plus the pages given back (may be free_count).
  * Nothing is changed (new_len = len, new_count = free_count) if the list would
- * pass num_pages or a length is out of range (DKV_DEV_PAGE_RANGE).
+ * pass num_pages or a length is out of range (DKV_DEV_PAGE_RANGE). A page number out of
+ * [0, num_pages) in a table sets the same bit and goes into the list as -1.
  * Other arguments and errors are those of dkv_page_tables.
  */
 dkv_status dkv_page_release(const dkv_pages* pages, const int32_t* ended, const int32_t* len, int32_t* new_len,

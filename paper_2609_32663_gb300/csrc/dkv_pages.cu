@@ -15,12 +15,13 @@
 // scan kernel and a fill kernel behind it took 12.4. Lengths and counts that are updated in place
 // are committed by a second, tiny launch (1.2 us), as CTAs may still be reading them. More slabs: one
 // CTA scans into the workspace, then all fill.
-// Every value that lives on the device is checked in the scan: nothing is written if a check fails
-// or the free list is too short.
+// Lengths, counts and slots are checked in the scan: nothing is written if a check fails or the free list is
+// too short. The page numbers themselves are looked at where they move: one that is out of range is reported,
+// and -1 (no page) moves in its place, so that no table, list or slot map ever leads out of the pools.
 //
 // What bounds it: the launch and the scan for a decode step (4.4 us of its 6.9); instructions more than bytes for
-// the large calls: 12.8 M pages given back, 103 MB, in 28.5 us, of which the scan takes 4 and whole runs of one slab go at
-// 6.4 TB/s; 256 K pages and 4.1 M slots, 17.7 MB, in 11.6 us.
+// the large calls: 12.8 M pages given back, 103 MB, in 29.4 us, of which the scan takes 4 and whole runs of one slab go at
+// 6.2 TB/s; 256 K pages and 4.1 M slots, 17.7 MB, in 12.2 us.
 #include "dkv_decode_common.cuh"
 #include "dkv_pages.cuh"
 #include "dkv_pool.cuh"
@@ -255,6 +256,23 @@ __device__ __forceinline__ int load_now(const int32_t* p)
     return v;
 }
 
+// Whether all N page numbers that move are in range; if not, those that are none become -1 (reported). A
+// compare of the largest: 12.8 M pages given back take 29.4 us (28.6 without any look, 31.4 with one at each),
+// 4.1 M slots 12.2 (11.6, 14.7).
+template <int N>
+__device__ __forceinline__ bool pages_hold(const PageArgs& a, int (&page)[N])
+{
+    unsigned most = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) most = max(most, (unsigned)page[i]);
+    if (most < (unsigned)a.num_pages) return true;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if ((unsigned)page[i] >= (unsigned)a.num_pages) page[i] = -1;
+    if (a.status) atomicOr(a.status, kDevRange);
+    return false;
+}
+
 // For N values j[]: the last slab h in [lo, hi] with first[h] <= j, the one that page j belongs to.
 template <int N>
 __device__ __forceinline__ void slabs_of_pages(const int32_t* first, int lo, int hi, const int (&j)[N], int (&h)[N])
@@ -296,6 +314,7 @@ __device__ __forceinline__ void fill_pages(const PageArgs& a, const PageHead& he
 #pragma unroll
     for (int i = 0; i < N; ++i)
         page[i] = a.mode == kRelease ? a.table[(int64_t)h[i] * a.max_pages + (j[i] - first[h[i]])] : a.free_pages[head.count - 1 - j[i]];
+    pages_hold(a, page);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         if (c0 + 32 * i + lane >= end) continue;
@@ -328,6 +347,7 @@ __device__ __forceinline__ void fill_chunks(const PageArgs& a, const PageHead& h
         int page[kLong];
 #pragma unroll
         for (int i = 0; i < kLong; ++i) page[i] = 32 * i + lane < n ? load_now(from + step * (32 * i + lane)) : 0;
+        pages_hold(a, page);
 #pragma unroll
         for (int i = 0; i < kLong; ++i)
             if (32 * i + lane < n) to[32 * i + lane] = page[i];
@@ -388,13 +408,18 @@ __device__ __forceinline__ void fill_slots(const PageArgs& a, const PageHead& he
                     from_free[i] = head.count - 1 - first[h + i] + had[i];
                 }
             }
-            int slot[V];
+            int page[V], slot[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int r = shift[i] + t, p = r >> a.log_P;
                 const int32_t* from = p < had[i] ? table + ((int64_t)i * a.max_pages + p) : a.free_pages + (from_free[i] - p);
-                slot[i] = (*from << a.log_P) + (r & (a.P - 1));
+                page[i] = *from;
+                slot[i] = (int)((unsigned)page[i] << a.log_P) + (r & (a.P - 1));
             }
+            if (!pages_hold(a, page))
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (page[i] < 0) slot[i] = -1;
             int32_t* to = a.slots + ((int64_t)l * a.max_tokens + t) * a.Hkv + g;
             if (V == 4)
                 *reinterpret_cast<int4*>(to) = make_int4(slot[0], slot[1 % V], slot[2 % V], slot[3 % V]);

@@ -7,6 +7,7 @@ import torch
 import paged
 from paper_2609_32663_gb300 import dkv
 from test_gpu_chunk import Call, inputs, lens_of
+from test_gpu_pages import State, dev, slot_map, tables_of
 
 pytestmark = pytest.mark.gpu
 
@@ -94,3 +95,99 @@ def test_a_slab_shorter_than_its_new_tokens(cuda):
     Kp[cache.rows(0)] = qkv[1][2:5, 0]
     Kp[cache.rows(1)[-1]] = qkv[1][5, 0]
     assert torch.equal(bits(c.Kp.cpu()), bits(Kp))
+
+
+BAD = [-1, 1 << 30, -(1 << 31), None]  # None: the number of pages, the first that is none
+
+
+def spoil(a, at, pages):
+    """The entries `at` of a table or list out of range; the array, and what the definition then has in it."""
+    for i, x in enumerate(at):
+        a[tuple(np.atleast_1d(x))] = pages if BAD[i % 4] is None else BAD[i % 4]
+
+
+def none_out_of_range(a, pages):
+    return np.where((a >= 0) & (a < pages), a, -1)
+
+
+@pytest.mark.parametrize("V", [4, 1])
+def test_tables_pass_no_bad_page_on(cuda, V):
+    """Bad entries of the free list and of the tables' last pages: -1 in the new entries and in the slot map, all else as
+    it would be."""
+    r = np.random.default_rng(V)
+    lens = r.integers(0, 90, (3, 5, 4 if V == 4 else 3))
+    tokens = [20, 0, 1, 40, 7]
+    n = np.broadcast_to(np.asarray(tokens)[None, :, None], lens.shape)
+    need = int((-(-(lens + n) // 16) - -(-lens // 16)).sum())
+    cache = paged.Cache(lens, 16, spare=need + 3, wider=4)
+    pages = cache.pages.num_pages
+    spoil(cache.free, [cache.count - 1, cache.count - 4, cache.count - need, 4], pages)
+    some = [h for h in range(cache.lens.size) if cache.lens[h] % 16][:9]
+    spoil(cache.table, [(h, cache.lens[h] // 16) for h in some], pages)
+    s = State(cache)
+    cap = sum(tokens) + 2
+    cu, slots = dev(np.full(6, -9)), dev(np.full((3, cap, lens.shape[2]), -3))
+    s.tables(tokens=dev(tokens), cu_tokens=cu, slots=slots)
+    table, free, count, ln = paged.tables_after(cache, n)
+    had, has = -(-cache.lens // 16), -(-ln // 16)
+    for h in range(cache.lens.size):  # only entries that the call writes are changed
+        table[h, had[h]:has[h]] = none_out_of_range(table[h, had[h]:has[h]], pages)
+    assert int(s.status) == dkv.DKV_DEV_PAGE_RANGE
+    s.same(table, free, count, ln)
+    seen = np.where((table >= 0) & (table < pages), table, -(1 << 20))
+    want = slot_map(cache, seen, tokens, cap)[1]
+    want[want < -3] = -1
+    assert (want == -1).any() and np.array_equal(slots.cpu().numpy(), want)
+
+
+def test_release_passes_no_bad_page_on(cuda):
+    lens = np.array([[[40, 17], [300, 16], [5, 5]]])
+    cache = paged.Cache(lens, 16, spare=2)
+    pages = cache.pages.num_pages
+    spoil(cache.table, [(0, 0), (0, 2), (3, 0), (5, 0), (2, 1)], pages)
+    s = State(cache)
+    s.release([1, 0, 1])
+    table, free, count, ln = paged.tables_after(cache, [1, 1, 0, 0, 1, 1], release=True)
+    free[2:count] = none_out_of_range(free[2:count], pages)
+    assert int(s.status) == dkv.DKV_DEV_PAGE_RANGE
+    s.same(table, free, count, ln)
+    # What came back as -1 is no page for the next sequence either.
+    s.len, s.count, s.status = s.new_len.clone(), s.new_count.clone(), torch.zeros_like(s.status)
+    s.tables(tokens=dev([0, 0, 60]))
+    assert int(s.status) == dkv.DKV_DEV_PAGE_RANGE
+    got = s.table.cpu().numpy()[4:6, :4]
+    assert np.array_equal(got.reshape(-1), free[:count][::-1][:8]) and (got == -1).any()
+
+
+@pytest.mark.parametrize("release", [False, True])
+def test_bad_pages_among_many(cuda, release):
+    """More pages than one a lane: runs of one slab and chunks of several."""
+    r = np.random.default_rng(2)
+    lens = r.integers(0, 60000, (4, 8, 6))
+    lens[:, 3] = r.integers(0, 400, (4, 6))
+    tokens = r.integers(0, 40000, 8)
+    tokens[3] = 200
+    n = np.broadcast_to(tokens[None, :, None], lens.shape)
+    need = int((-(-(lens + n) // 16) - -(-lens // 16)).sum())
+    cache = tables_of(lens, 16, need + 1, 40000 // 16 + 2)
+    pages = cache.pages.num_pages
+    had = -(-cache.lens // 16)
+    if release:
+        assert int(had.sum()) > 152 * 1024
+        spoil(cache.table, [(h, int(x)) for h in range(cache.lens.size) for x in r.integers(0, had[h], 3) if had[h]], pages)
+    else:
+        assert need > 152 * 1024
+        spoil(cache.free, list(r.integers(1, need + 1, 300)), pages)
+    s = State(cache)
+    if release:
+        s.release(np.ones(8, int))
+        table, free, count, ln = paged.tables_after(cache, np.ones(lens.size), release=True)
+        free[need + 1:count] = none_out_of_range(free[need + 1:count], pages)
+    else:
+        s.tables(tokens=dev(tokens))
+        table, free, count, ln = paged.tables_after(cache, n)
+        has = -(-ln // 16)
+        for h in range(lens.size):
+            table[h, had[h]:has[h]] = none_out_of_range(table[h, had[h]:has[h]], pages)
+    assert int(s.status) == dkv.DKV_DEV_PAGE_RANGE
+    s.same(table, free, count, ln)
