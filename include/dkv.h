@@ -503,8 +503,9 @@ dkv_status dkv_page_release(const dkv_pages* pages, const int32_t* ended, const 
  * sequence i become the last rows of slot seq[i], rows len[h] - n_h .. len[h] - 1 of
  * each slab, with len and table as they are after dkv_page_tables with this plan.
  * K, V       device 16-bit [L][plan B][H_kv][T_stride][128]. T_stride >= max ctx_len.
- * Bytes are copied exactly; K, V, Kp and Vp are 16-byte aligned and do not overlap. A row whose place is
- * out of range is skipped (DKV_DEV_PAGE_RANGE). Dense plans are rejected.
+ * Bytes are copied exactly, so K, V, Kp and Vp are of one type; they are 16-byte aligned and
+ * do not overlap. A row whose place is out of range is skipped (DKV_DEV_PAGE_RANGE). Dense
+ * plans are rejected.
  */
 dkv_status dkv_page_compact(const dkv_pages* pages, const dkv_plan* plan, const int32_t* seq, const void* K,
                             const void* V, int64_t T_stride, const int32_t* table, const int32_t* len, void* Kp,

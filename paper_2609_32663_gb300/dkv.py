@@ -569,6 +569,13 @@ def _word(status, at):
     return _on(status, "status", at, _torch().i32)
 
 
+def _one_type(names, *tensors):
+    """Refuses tensors of 16-bit rows that are not of one type (int16, an address and None say nothing of it)."""
+    types = {t.dtype for t in tensors if t is not None and not isinstance(t, int)} - {_torch().torch.int16}
+    if len(types) > 1:
+        _bad(f"{names} are of different types: {sorted(map(str, types))}")
+
+
 def _page_args(p: Pages, at, len, new_len, table, free_pages, free_count, new_count, workspace, status):
     i32, n = _torch().i32, p.slabs
     return ((_on(len, "len", at, i32, n), _on(new_len, "new_len", at, i32, n), _on(table, "table", at, i32, n * p.max_pages),
@@ -617,7 +624,8 @@ def dkv_page_release(pages: Pages, ended, len, new_len, table, free_pages, free_
 
 def dkv_page_compact(pages: Pages, plan: Plan, K, V, table, len, Kp, Vp, seq=None, T_stride: int | None = None,
                      status=None, stream=None):
-    """The kept rows of plan sequence i become the last rows of slot seq[i]'s slabs."""
+    """The kept rows of plan sequence i become the last rows of slot seq[i]'s slabs. Bytes are copied, so K, V, Kp and Vp
+    are of one type (int16, like an address, says nothing of it)."""
     if T_stride is None:
         T_stride = K.shape[-2]
     T, sh = _torch(), plan.shape
@@ -629,6 +637,7 @@ def dkv_page_compact(pages: Pages, plan: Plan, K, V, table, len, Kp, Vp, seq=Non
     for t, name in ((K, "K"), (V, "V")):
         if not isinstance(t, int) and t.numel() < dense:
             _bad(f"{name} has {t.numel()} elements, needs at least {dense}")
+    _one_type("K, V, Kp and Vp", K, V, Kp, Vp)
     _check(lib().dkv_page_compact(
         pages.ref, handle, _on(seq, "seq", at, T.i32, plan.B), _on(K, "K", at, r16), _on(V, "V", at, r16), int(T_stride),
         _on(table, "table", at, T.i32, pages.slabs * pages.max_pages), _on(len, "len", at, T.i32, pages.slabs),

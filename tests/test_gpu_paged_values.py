@@ -7,7 +7,7 @@ import torch
 import paged
 from paper_2609_32663_gb300 import dkv
 from test_gpu_chunk import Call, inputs, lens_of
-from test_gpu_pages import State, dev, slot_map, tables_of
+from test_gpu_pages import State, dev, plan_of, slot_map, tables_of
 
 pytestmark = pytest.mark.gpu
 
@@ -191,3 +191,23 @@ def test_bad_pages_among_many(cuda, release):
             table[h, had[h]:has[h]] = none_out_of_range(table[h, had[h]:has[h]], pages)
     assert int(s.status) == dkv.DKV_DEV_PAGE_RANGE
     s.same(table, free, count, ln)
+
+
+def test_rows_of_another_type_are_not_packed(cuda):
+    plan, _ = plan_of(1, 2, 1, [100])
+    cache = paged.Cache(np.zeros((1, 1, 1), int), 16, spare=9, wider=9, H=2, dtype=torch.bfloat16)
+    s = State(cache)
+    s.tables(plan=plan)
+    K = torch.ones((1, 1, 1, 100, 128), dtype=torch.float16, device="cuda")
+    Kp, Vp = cache.Kp.cuda(), cache.Vp.cuda()
+    with pytest.raises(dkv.DkvError, match="types"):
+        dkv.dkv_page_compact(s.p, plan, K, K, s.table, s.new_len, Kp, Vp, status=s.status)
+    torch.cuda.synchronize()
+    assert int(s.status) == 0 and torch.isnan(Kp).all() and torch.isnan(Vp).all()
+    # 16-bit words without a type go into pools of either.
+    dkv.dkv_page_compact(s.p, plan, K.view(torch.int16), K.view(torch.int16), s.table, s.new_len, Kp, Vp, status=s.status)
+    n = int(s.new_len[0])
+    cache.table, cache.lens = s.table.cpu().numpy(), np.array([n])
+    at = torch.from_numpy(cache.rows(0))
+    assert n > 0 and int(s.status) == 0 and (Kp.cpu()[at].view(torch.float16) == 1).all()
+    plan.close()

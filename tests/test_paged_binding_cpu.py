@@ -1,0 +1,41 @@
+"""What the binding of the paged cache refuses before a call is made: it answers without a GPU."""
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+BF, HALF, I16 = torch.bfloat16, torch.float16, torch.int16
+
+
+@pytest.fixture(scope="module")
+def dkv():
+    from paper_2609_32663_gb300 import build
+    build.build_library()
+    import paper_2609_32663_gb300.dkv as dkv
+    return dkv
+
+
+def refused(dkv, word, call, *args, **kw):
+    with pytest.raises(dkv.DkvError, match=word) as e:
+        call(*args, **kw)
+    assert e.value.status == dkv.DKV_ERR_INVALID_ARG
+
+
+def compact_args(dkv, K=BF, V=BF, Kp=BF, Vp=BF):
+    g = dkv.Pages(L=1, B=1, H=2, H_kv=1, page_rows=16, num_pages=4, max_pages=4)
+    plan = SimpleNamespace(shape=dkv.Shape(L=1, H=2, H_kv=1, D=1), B=1, address=1 << 20)
+    i = torch.zeros(4, dtype=torch.int32)
+    return [g, plan, torch.zeros((1, 1, 1, 40, 128), dtype=K), torch.zeros((1, 1, 1, 40, 128), dtype=V), i, i[:1],
+            torch.zeros((64, 128), dtype=Kp), torch.zeros((64, 128), dtype=Vp)]
+
+
+@pytest.mark.parametrize("types", [(HALF, HALF, BF, BF), (BF, HALF, BF, BF), (BF, BF, BF, HALF), (I16, I16, BF, HALF),
+                                   (HALF, BF, HALF, BF), (torch.float32, BF, BF, BF)])
+def test_rows_of_another_type_are_not_packed(dkv, types):
+    refused(dkv, "different types", dkv.dkv_page_compact, *compact_args(dkv, *types), stream=0)
+
+
+@pytest.mark.parametrize("types", [(BF,) * 4, (HALF,) * 4, (I16, I16, BF, BF), (HALF, HALF, I16, I16), (I16,) * 4])
+def test_rows_of_one_type_pass_that_check(dkv, types):
+    """The next check refuses them, as they lie on the host."""
+    refused(dkv, "CUDA tensor", dkv.dkv_page_compact, *compact_args(dkv, *types), stream=0)
