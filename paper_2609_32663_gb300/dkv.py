@@ -546,32 +546,47 @@ def _where(stream):
     return (T.torch.cuda.current_device() if T.torch.cuda.is_available() else 0), _stream(stream)
 
 
+def _device_of(t, name):
+    """The device of a tensor (-1: the host); what is none is refused."""
+    try:
+        return t.get_device()
+    except AttributeError:
+        _bad(f"{name} must be a CUDA tensor, not {type(t).__name__}")
+
+
 def _on(t, name, at, dtypes, numel=None):
     """_dev for a buffer of the paged cache, which must lie on device `at` (the look-ups of t are the binding's time)."""
     if t is None or isinstance(t, int):
         return t
-    if t.get_device() == at and t.is_contiguous() and t.dtype in dtypes and (numel is None or t.numel() == numel):
-        return t.data_ptr()
-    if t.is_cuda and t.get_device() != at:
+    try:
+        if t.get_device() == at and t.is_contiguous() and t.dtype in dtypes and (numel is None or t.numel() == numel):
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    if _device_of(t, name) != at and t.is_cuda:
         _bad(f"{name} lies on {t.device}, the current device is cuda:{at}")
     return _dev(t, name, dtypes, numel)
 
 
 def _work(workspace, at):
-    if workspace.get_device() != at or not workspace.is_contiguous():
+    """Address and bytes (so an address alone will not do)."""
+    if _device_of(workspace, "workspace") != at or not workspace.is_contiguous():
         _bad(f"workspace must be a contiguous tensor on cuda:{at}")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def _word(status, at):
-    if status is not None and not isinstance(status, int) and status.numel() < 1:
+    if status is None or isinstance(status, int):
+        return status
+    _device_of(status, "status")
+    if status.numel() < 1:
         _bad("status has no element")
     return _on(status, "status", at, _torch().i32)
 
 
 def _one_type(names, *tensors):
     """Refuses tensors of 16-bit rows that are not of one type (int16, an address and None say nothing of it)."""
-    types = {t.dtype for t in tensors if t is not None and not isinstance(t, int)} - {_torch().torch.int16}
+    types = {t.dtype for t in tensors if hasattr(t, "dtype")} - {_torch().torch.int16}
     if len(types) > 1:
         _bad(f"{names} are of different types: {sorted(map(str, types))}")
 
@@ -627,6 +642,7 @@ def dkv_page_compact(pages: Pages, plan: Plan, K, V, table, len, Kp, Vp, seq=Non
     """The kept rows of plan sequence i become the last rows of slot seq[i]'s slabs. Bytes are copied, so K, V, Kp and Vp
     are of one type (int16, like an address, says nothing of it)."""
     if T_stride is None:
+        _device_of(K, "K (without T_stride)")
         T_stride = K.shape[-2]
     T, sh = _torch(), plan.shape
     at, queue = _where(stream)
@@ -635,7 +651,10 @@ def dkv_page_compact(pages: Pages, plan: Plan, K, V, table, len, Kp, Vp, seq=Non
     dense = sh.L * plan.B * sh.H_kv * int(T_stride) * 128
     pool = pages.num_pages * pages.page_rows * 128
     for t, name in ((K, "K"), (V, "V")):
-        if not isinstance(t, int) and t.numel() < dense:
+        if t is None or isinstance(t, int):
+            continue
+        _device_of(t, name)
+        if t.numel() < dense:
             _bad(f"{name} has {t.numel()} elements, needs at least {dense}")
     _one_type("K, V, Kp and Vp", K, V, Kp, Vp)
     _check(lib().dkv_page_compact(
@@ -654,7 +673,7 @@ def dkv_chunk_workspace_bytes(pages: Pages) -> int:
 def _token_rows(t, name, at, dtype, tokens, heads):
     """Address and token stride (elements) of a [tokens][heads][128] tensor whose tokens may lie apart (a slice of a
     projection); heads and elements are contiguous."""
-    if t.get_device() != at:
+    if _device_of(t, name) != at:
         _bad(f"{name} must be a CUDA tensor on cuda:{at}")
     if t.dtype != dtype or t.shape != (tokens, heads, 128):
         _bad(f"{name} is {t.dtype} {tuple(t.shape)}, expected {dtype} {(tokens, heads, 128)}")
@@ -669,6 +688,7 @@ def dkv_chunk_attn(pages: Pages, layer: int, q, k_new, v_new, cu_tokens, table, 
     """One layer's new tokens: k_new and v_new [T][H_kv][128] appended to their slabs' pages (None: they are there), and
     the attention of q [T][H][128] -> out [T][H][128], all of q's type (bf16 or fp16). q, k_new and v_new may be slices of
     one projection; k_new and v_new have the same token stride."""
+    _device_of(q, "q")
     T, dtype = _torch(), q.dtype
     at, queue = _where(stream)
     half = dtype == T.torch.float16
@@ -688,7 +708,7 @@ def dkv_chunk_attn(pages: Pages, layer: int, q, k_new, v_new, cu_tokens, table, 
     pool = pages.num_pages * pages.page_rows * 128
     wp, wb = _work(workspace, at)
     _check(lib().dkv_chunk_attn(
-        pages.ref, layer, DKV_FP16 if half else DKV_BF16, tokens, qp, qs, kp, vp, ks,
+        pages.ref, int(layer), DKV_FP16 if half else DKV_BF16, tokens, qp, qs, kp, vp, ks,
         _on(cu_tokens, "cu_tokens", at, T.i32, pages.B + 1), _on(table, "table", at, T.i32, pages.slabs * pages.max_pages),
         _on(len, "len", at, T.i32, pages.slabs), _on(Kp, "Kp", at, one, pool), _on(Vp, "Vp", at, one, pool),
         1 if causal else 0, scale, _on(out, "out", at, one, tokens * pages.H * 128), wp, wb, _word(status, at),

@@ -211,3 +211,12 @@ def test_rows_of_another_type_are_not_packed(cuda):
     at = torch.from_numpy(cache.rows(0))
     assert n > 0 and int(s.status) == 0 and (Kp.cpu()[at].view(torch.float16) == 1).all()
     plan.close()
+
+
+def test_a_layer_of_numpy(cuda):
+    tokens = [1, 3]
+    cache = paged.Cache(lens_of(2, 2, 1, [30, 90], tokens, 1), 16, H=2)
+    cu, qkv = inputs(cache, tokens, 3)
+    c = Call(cache, np.int64(1), qkv, cu).run()
+    want, size, _, _ = paged.attention(cache, 1, *qkv, cu, True)
+    paged.assert_attention(c.out, want, size, cache.dtype)

@@ -39,3 +39,21 @@ def test_rows_of_another_type_are_not_packed(dkv, types):
 def test_rows_of_one_type_pass_that_check(dkv, types):
     """The next check refuses them, as they lie on the host."""
     refused(dkv, "CUDA tensor", dkv.dkv_page_compact, *compact_args(dkv, *types), stream=0)
+
+
+def test_what_is_no_tensor_is_refused(dkv):
+    """An address where a size, shape or type is needed, nothing, or an array of the host."""
+    import numpy as np
+    g, plan, K, V, table, ln, Kp, Vp = compact_args(dkv)
+    q = torch.zeros((1, 2, 128), dtype=BF)
+    for what in (1 << 20, None, np.zeros(1 << 16, np.uint8)):
+        name = type(what).__name__
+        refused(dkv, f"workspace .*{name}", dkv.dkv_page_release, g, A, A, A, A, A, A, A, what, stream=0)
+        refused(dkv, f"workspace .*{name}", dkv.dkv_page_tables, g, A, A, A, A, A, A, what, tokens=A, stream=0)
+        refused(dkv, f"K .*{name}", dkv.dkv_page_compact, g, plan, what, V, table, ln, Kp, Vp, stream=0)
+        refused(dkv, f"q .*{name}", dkv.dkv_chunk_attn, g, 0, what, None, None, A, A, A, A, A, A, None, stream=0)
+    refused(dkv, "K .*ndarray", dkv.dkv_page_compact, g, plan, np.zeros(1), V, table, ln, Kp, Vp, T_stride=40, stream=0)
+    refused(dkv, "q ", dkv.dkv_chunk_attn, g, 0, q, None, None, A, A, A, A, A, A, A, stream=0)
+
+
+A = 1 << 20  # an address that no check follows
