@@ -934,8 +934,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         fence_proxy_async_smem();
     }
     // The append kernel started only after every kernel before it had completed, and this one after
-    // that: what those wrote (lengths, tables, q, earlier rows) may be read now. The appended rows and the
-    // counters may not before pdl_wait().
+    // that: what those wrote (lengths, tables, q, earlier rows) is in L2 and may be read now. The fence drops
+    // what this SM's L1 holds from before, as lengths and tables are updated in place (0.1 us; loads past L1
+    // instead took 145 us for the queries' 126, since a tile's page numbers lie in a line of L1). The appended rows and the
+    // counters may not be read before pdl_wait().
+    asm volatile("fence.acq_rel.gpu;" ::: "memory");
     int64_t* before = reinterpret_cast<int64_t*>(sm + kOffRing);
     int group;
     tc_fence_before();
