@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(kAppThreads) chunk_append_kernel(const __grid_
     const int h = lo * a.Hkv + g;
     const int r = slab_len(a, h) - cu[lo + 1] + t;  // below the slab's length
     int page = -1;
-    if (r >= 0) page = a.table[(int64_t)h * a.max_pages + r / a.P];
+    if (r >= 0 && in_bounds(h < a.B * a.Hkv && r / a.P < a.max_pages, a.status)) page = a.table[(int64_t)h * a.max_pages + r / a.P];
     if (page < 0 || page >= a.num_pages) {
         if (sub == 0) report(a, DKV_DEV_PAGE_RANGE);
         return;
@@ -624,6 +624,7 @@ __device__ __forceinline__ float2 widen(uint32_t u)
 // Pool row of row r of the unit's slab, or -1.
 __device__ __forceinline__ int64_t pool_row(const ChunkArgs& a, int h, int r)
 {
+    if (!in_bounds(r >= 0 && r / a.P < a.max_pages, a.status)) return -1;
     const int page = a.table[(int64_t)h * a.max_pages + r / a.P];
     return page < 0 || page >= a.num_pages ? -1 : (int64_t)page * a.P + r % a.P;
 }
@@ -870,7 +871,8 @@ __device__ __forceinline__ void join_items(const ChunkArgs& a, const ChunkWork& 
 template <bool F16>
 __device__ __forceinline__ void join_pieces(const ChunkArgs& a, const ChunkWork& w, Waits& wait, float2* scale, int t0, int tokens, int g, int c0, int pieces)
 {
-    const int tid = threadIdx.x, rows = tokens * a.G, low = kTile / a.G * a.G;
+    const bool ok = in_bounds(t0 >= 0 && t0 + tokens <= a.T && tokens * a.G <= kPieceRows, a.status);
+    const int tid = threadIdx.x, rows = ok ? tokens * a.G : 0, low = kTile / a.G * a.G;
     const float c = a.qscale;
     // As many lanes a row as there are threads for (a power of 2), one for few pieces.
     int lanes = pieces <= kFew ? 1 : 32;
@@ -986,7 +988,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         Piece k;
         // Pages of tile j, and the lane's page number.
         auto pages_in = [&](int j) { return (min(max(k.kv - j * kTile, 0), kTile) + a.P - 1) / a.P; };
-        auto page_of = [&](int j) { return lane < pages_in(j) ? a.table[(int64_t)k.h * a.max_pages + j * ppt + lane] : 0; };
+        auto page_of = [&](int j) {
+            return lane < pages_in(j) && in_bounds(k.h >= 0 && k.h < a.B * a.Hkv && j >= 0 && j * ppt + lane < a.max_pages, a.status)
+                       ? a.table[(int64_t)k.h * a.max_pages + j * ppt + lane]
+                       : 0;
+        };
         auto load = [&](const CUtensorMap* map, int j, int page) {
             const int s = pos % kStages, np = pages_in(j);
             const bool good = page >= 0 && page < a.num_pages;
@@ -1150,7 +1156,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int steps = k.steps();
             const bool pair = k.pair(), whole = k.whole();
             const int tok = token + (pair ? p * TQ : 0);
-            const bool live = token < TQ && tok < k.tokens;
+            const bool live = token < TQ && tok < k.tokens && in_bounds(k.t0 >= 0 && k.t0 + tok < a.T && k.g * a.G + j < a.H, a.status);
             const int lim = !live ? 0x3fffffff : a.causal ? min(max(k.row0 + tok, 0), k.len) : k.len;
             const bool any = __any_sync(kFull, live);
             float m = -INFINITY, l = 0.f;
@@ -1180,6 +1186,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const volatile Piece* d = reinterpret_cast<const volatile Piece*>(sm + kOffPieces) + unit % kAhead;
                 c0 = d->c0;
                 pieces = d->pieces;
+                if (!in_bounds(c0 >= 0 && c0 <= c && pieces > c - c0 && c0 + pieces <= nctas, a.status)) c0 = c, pieces = 1;
                 few = pair && pieces <= kFew && min(k.kv, k.j1 * kTile) <= k.row0;
                 if (few) {
                     if (tid == 0) {

@@ -273,6 +273,13 @@ __device__ __forceinline__ bool pages_hold(const PageArgs& a, int (&page)[N])
     return false;
 }
 
+// Bounds-checked build: whether entries [e, e + n) are a slab's, and places [x, x + n) the free list's.
+__device__ __forceinline__ bool entries_hold(const PageArgs& a, int h, int e, int n)
+{
+    return in_bounds(h >= 0 && h < a.NH && e >= 0 && n <= a.max_pages - e, a.status);
+}
+__device__ __forceinline__ bool list_holds(const PageArgs& a, int x, int n) { return in_bounds(x >= 0 && n <= a.num_pages - x, a.status); }
+
 // For N values j[]: the last slab h in [lo, hi] with first[h] <= j, the one that page j belongs to.
 template <int N>
 __device__ __forceinline__ void slabs_of_pages(const int32_t* first, int lo, int hi, const int (&j)[N], int (&h)[N])
@@ -312,6 +319,13 @@ __device__ __forceinline__ void fill_pages(const PageArgs& a, const PageHead& he
     for (int i = 0; i < N; ++i) j[i] = min(end - 1, c0 + 32 * i + lane);
     slabs_of_pages(first, ha, hb, j, h);
 #pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int k = j[i] - first[h[i]];
+        if (!entries_hold(a, h[i], a.mode == kRelease ? k : pages_of(a, len[h[i]]) + k, 1) ||
+            !list_holds(a, a.mode == kRelease ? head.count + j[i] : head.count - 1 - j[i], 1))
+            return;
+    }
+#pragma unroll
     for (int i = 0; i < N; ++i)
         page[i] = a.mode == kRelease ? a.table[(int64_t)h[i] * a.max_pages + (j[i] - first[h[i]])] : a.free_pages[head.count - 1 - j[i]];
     pages_hold(a, page);
@@ -341,6 +355,9 @@ __device__ __forceinline__ void fill_chunks(const PageArgs& a, const PageHead& h
             fill_pages<kLong>(a, head, first, len, j0, end, ha, hb);
             continue;
         }
+        if (!entries_hold(a, ha, j0 - first[ha] + (a.mode == kRelease ? 0 : pages_of(a, len[ha])), end - j0) ||
+            !list_holds(a, a.mode == kRelease ? head.count + j0 : head.count - end, end - j0))
+            continue;
         const int32_t* from = a.mode == kRelease ? a.table + ((int64_t)ha * a.max_pages + (j0 - first[ha])) : a.free_pages + (head.count - 1 - j0);
         int32_t* to = a.mode == kRelease ? a.free_pages + head.count + j0 : a.table + ((int64_t)ha * a.max_pages + pages_of(a, len[ha]) + (j0 - first[ha]));
         const int step = a.mode == kRelease ? 1 : -1, n = end - j0;
@@ -413,7 +430,8 @@ __device__ __forceinline__ void fill_slots(const PageArgs& a, const PageHead& he
             for (int i = 0; i < V; ++i) {
                 const int r = shift[i] + t, p = r >> a.log_P;
                 const int32_t* from = p < had[i] ? table + ((int64_t)i * a.max_pages + p) : a.free_pages + (from_free[i] - p);
-                page[i] = *from;
+                const bool there = p < had[i] ? entries_hold(a, l * a.B * a.Hkv + g + i, p, 1) : list_holds(a, from_free[i] - p, 1);
+                page[i] = there ? *from : -1;
                 slot[i] = (int)((unsigned)page[i] << a.log_P) + (r & (a.P - 1));
             }
             if (!pages_hold(a, page))
@@ -421,7 +439,9 @@ __device__ __forceinline__ void fill_slots(const PageArgs& a, const PageHead& he
                 for (int i = 0; i < V; ++i)
                     if (page[i] < 0) slot[i] = -1;
             int32_t* to = a.slots + ((int64_t)l * a.max_tokens + t) * a.Hkv + g;
-            if (V == 4)
+            if (!in_bounds(l < a.L && t < a.max_tokens && g + V <= a.Hkv, a.status))
+                ;
+            else if (V == 4)
                 *reinterpret_cast<int4*>(to) = make_int4(slot[0], slot[1 % V], slot[2 % V], slot[3 % V]);
             else
                 to[0] = slot[0];
@@ -590,7 +610,7 @@ __global__ void __launch_bounds__(kPcWarps * 32, 1) page_compact_kernel(const __
                     while (a.plan.ioff[hr + 1] <= r);
                     n1 = a.plan.ioff[hr + 1];
                     const int lb = hr / a.plan.Hkv, l = lb / a.plan.B, i = lb - l * a.plan.B, b = a.seq ? a.seq[i] : i;
-                    slot_ok = b >= 0 && b < a.B;
+                    slot_ok = b >= 0 && b < a.B && in_bounds(hr < NH && l < a.plan.L, a.status);
                     const int64_t h = ((int64_t)l * a.B + (slot_ok ? b : 0)) * a.plan.Hkv + (hr - lb * a.plan.Hkv);
                     entries = h * a.max_pages;
                     shift = a.len[h] - n1;
