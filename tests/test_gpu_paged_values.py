@@ -220,3 +220,29 @@ def test_a_layer_of_numpy(cuda):
     c = Call(cache, np.int64(1), qkv, cu).run()
     want, size, _, _ = paged.attention(cache, 1, *qkv, cu, True)
     paged.assert_attention(c.out, want, size, cache.dtype)
+
+
+@pytest.mark.parametrize("name", ["page table", "page release", "paged compact", "chunk attention"])
+def test_an_injected_launch_failure_is_an_error(cuda, monkeypatch, name):
+    plan, _ = plan_of(1, 2, 1, [100])
+    cache = paged.Cache(np.zeros((1, 1, 1), int), 16, spare=9, wider=9, H=2)
+    s = State(cache)
+    K = torch.ones((1, 1, 1, 100, 128), dtype=torch.bfloat16, device="cuda")
+    Kp, Vp = cache.Kp.cuda(), cache.Vp.cuda()
+    cu, qkv = inputs(paged.Cache(np.full((1, 1, 1), 90), 16, H=2), [3], 1)
+    c = Call(paged.Cache(np.full((1, 1, 1), 90), 16, H=2), 0, qkv, cu)
+    call = {
+        "page table": lambda: s.tables(plan=plan),
+        "page release": lambda: s.release([1]),
+        "paged compact": lambda: dkv.dkv_page_compact(s.p, plan, K, K, s.table, s.len, Kp, Vp, status=s.status),
+        "chunk attention": c.run,
+    }[name]
+    call()
+    monkeypatch.setenv("DKV_FAULT", "launch")
+    with pytest.raises(dkv.DkvError, match=f"{name}.*injected launch failure") as e:
+        call()
+    assert e.value.status == dkv.DKV_ERR_CUDA
+    monkeypatch.delenv("DKV_FAULT")
+    call()
+    torch.cuda.synchronize()
+    plan.close()

@@ -57,3 +57,22 @@ def test_what_is_no_tensor_is_refused(dkv):
 
 
 A = 1 << 20  # an address that no check follows
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are none: a launch must not follow them")
+@pytest.mark.parametrize("name", ["page table", "page release", "chunk attention"])
+def test_an_injected_launch_failure_is_told_from_others(dkv, monkeypatch, name):
+    """Without a GPU every launch fails: only with the fault does the message say that it is the injected one."""
+    import ctypes
+    g, L = dkv.Pages(L=1, B=1, H=2, H_kv=1, page_rows=16, num_pages=4, max_pages=4), dkv.lib()
+    call = {
+        "page table": lambda: L.dkv_page_tables(g.ref, A, None, None, A, A, A, A, A, A, None, None, 0, A, 1 << 20, None, None),
+        "page release": lambda: L.dkv_page_release(g.ref, A, A, A, A, A, A, A, A, 1 << 20, None, None),
+        "chunk attention": lambda: L.dkv_chunk_attn(g.ref, 0, 0, 1, A, 256, None, None, 0, A, A, A, A, 2 * A, 1,
+                                                    ctypes.c_float(0), 3 * A, A, 1 << 40, None, None),
+    }[name]
+    for fault in (False, True):
+        monkeypatch.setenv("DKV_FAULT", "launch") if fault else monkeypatch.delenv("DKV_FAULT", raising=False)
+        assert call() == dkv.DKV_ERR_CUDA
+        said = L.dkv_last_error().decode()
+        assert name.split()[0] in said and ("injected launch failure" in said) == fault
