@@ -57,10 +57,10 @@ int64_t check_pages(const dkv_pages* g)
         return refuse("num_pages=%d of %d rows: need 1 to 2^31 - 17 rows", g->num_pages, g->page_rows), -1;
     if (g->max_pages < 1 || (int64_t)g->max_pages * g->page_rows > 0x7fffff00LL)
         return refuse("max_pages=%d of %d rows: need 1 to 2^31 - 256 rows", g->max_pages, g->page_rows), -1;
-    const int64_t NH = (int64_t)g->L * g->B * g->H_kv;
-    if (g->L > (1 << 20) || g->H_kv > (1 << 20) || NH > (1 << 26))
-        return refuse("L*B*H_kv=%lld slabs (more than 2^26)", (long long)NH), -1;
-    return NH;
+    // (The product of three large factors passes 64 bits.)
+    if (g->L > (1 << 20) || g->H_kv > (1 << 20) || (int64_t)g->L * g->B * g->H_kv > (1 << 26))
+        return refuse("L=%d B=%d H_kv=%d: more than 2^26 slabs", g->L, g->B, g->H_kv), -1;
+    return (int64_t)g->L * g->B * g->H_kv;
 }
 
 dkv_status check_plan(const dkv_pages* g, const dkv_plan* plan, const int32_t* seq, dkv::PlanView* v)

@@ -76,3 +76,11 @@ def test_an_injected_launch_failure_is_told_from_others(dkv, monkeypatch, name):
         assert call() == dkv.DKV_ERR_CUDA
         said = L.dkv_last_error().decode()
         assert name.split()[0] in said and ("injected launch failure" in said) == fault
+
+
+@pytest.mark.parametrize("kw", [dict(L=2**31 - 1, B=512, H=2**31 - 1, H_kv=2**31 - 1), dict(L=2**20, B=512, H=2**20, H_kv=2**20),
+                                dict(L=1, B=512, H=2**17 + 1, H_kv=2**17 + 1), dict(L=2**20 + 1, B=1, H=1, H_kv=1)])
+def test_a_geometry_of_too_many_slabs_is_named(dkv, kw):
+    """Factors whose product passes 64 bits among them."""
+    g = dkv.Pages(**kw, page_rows=16, num_pages=4, max_pages=4)
+    refused(dkv, f"L={kw['L']} B={kw['B']} H_kv={kw['H_kv']}", dkv.dkv_page_workspace_bytes, g)
