@@ -253,9 +253,11 @@ void dkv_vmm_free(dkv_vmm* buffer);
  * So n_appended and the context rows must not be written by a kernel that
  * signals early completion (griddepcontrol.launch_dependents) unless an ordinary
  * kernel or a copy lies between it and this call. Of this library the decode
- * calls and dkv_topk_mask signal early; they write neither, so calls of this
- * library may follow each other in any order (an append may be followed directly
- * by a call whose n_appended counts the appended row).
+ * calls, dkv_topk_mask and, where lengths and count are not updated in place,
+ * dkv_page_tables and dkv_page_release signal early; they write neither, so calls
+ * of this library may follow each other in any order (an append may be followed
+ * directly by a call whose n_appended counts the appended row), unless new_len or
+ * new_count of a page call is itself given to a decode call as n_appended or d_len.
  * Errors: DKV_ERR_INVALID_ARG (NULL/unaligned pointer, layer out of range,
  * only one of k_new/v_new), DKV_ERR_CUDA.
  */
@@ -423,7 +425,8 @@ dkv_status dkv_topk_mask(const float* P, int64_t n, int64_t K, uint8_t* M, void*
  *
  * status of every call: a device int32 that receives DKV_DEV_* bits, or NULL to
  * discard them. Values on the device (lengths, counts, page numbers, slots) are
- * checked there; what is out of range is never followed.
+ * checked there; what is out of range is never followed. (That a page is in two places at
+ * once is not seen.)
  * workspace: device scratch, 16-byte aligned, of at least the size named; nothing in
  * it need be kept or cleared. Calls that share one must be ordered, as must graphs
  * that were captured with the same one.
@@ -504,8 +507,10 @@ dkv_status dkv_page_release(const dkv_pages* pages, const int32_t* ended, const 
  * each slab, with len and table as they are after dkv_page_tables with this plan.
  * K, V       device 16-bit [L][plan B][H_kv][T_stride][128]. T_stride >= max ctx_len.
  * Bytes are copied exactly, so K, V, Kp and Vp are of one type; they are 16-byte aligned and
- * do not overlap. A row whose place is out of range is skipped (DKV_DEV_PAGE_RANGE). Dense
- * plans are rejected.
+ * do not overlap. A row whose place is out of range is skipped (DKV_DEV_PAGE_RANGE), so
+ * nothing is written to free slots after a dkv_page_tables that changed nothing. For a slot
+ * that already held rows, read the status word in between: its last rows would be overwritten.
+ * Dense plans are rejected.
  */
 dkv_status dkv_page_compact(const dkv_pages* pages, const dkv_plan* plan, const int32_t* seq, const void* K,
                             const void* V, int64_t T_stride, const int32_t* table, const int32_t* len, void* Kp,
@@ -519,7 +524,8 @@ dkv_status dkv_page_compact(const dkv_pages* pages, const dkv_plan* plan, const 
  * num_tokens  rows of q, k_new, v_new and out; num_tokens * H <= 2^30. Tokens cu_tokens[b] .. cu_tokens[b + 1] - 1
  *             are sequence b's; cu_tokens (device int32 [B + 1]) ascends from 0 to at most
  *             num_tokens (else nothing is written and DKV_DEV_PAGE_RANGE is set). Rows
- *             from cu_tokens[B] on are no token's: not read, and left as they are in out.
+ *             from cu_tokens[B] on are no token's: what they hold is not used, and they are
+ *             left as they are in out.
  * q           [num_tokens][H][128], token t at q + t * q_stride elements.
  * k_new,      [num_tokens][H_kv][128], token t at t * kv_stride elements, or both
  * v_new       NULL (the rows are in the pools already). When given they are first

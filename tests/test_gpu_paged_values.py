@@ -246,3 +246,57 @@ def test_an_injected_launch_failure_is_an_error(cuda, monkeypatch, name):
     call()
     torch.cuda.synchronize()
     plan.close()
+
+
+def test_rows_of_no_token_hold_anything(cuda):
+    """Rows behind the last sequence: what they hold in q, k_new and v_new is not used."""
+    for tokens in ([1, 3], [40, 1]):
+        cache = paged.Cache(lens_of(1, 2, 2, [200, 90], tokens, 1), 16, H=8)
+        cu, qkv = inputs(cache, tokens, 3, pad=30)
+        qkv = [x.clone() for x in qkv]
+        for x, fill in zip(qkv, (float("nan"), float("inf"), float("nan"))):
+            x[cu[-1]:] = fill
+        c = Call(cache, 0, qkv, cu).run()
+        want, size, Kp, Vp = paged.attention(cache, 0, *qkv, cu, True)
+        assert int(c.status) == 0
+        paged.assert_attention(c.out, want, size, cache.dtype)
+        for got, exp in ((c.Kp, Kp), (c.Vp, Vp)):
+            assert torch.equal(got.double().cpu().nan_to_num(99.0), exp.nan_to_num(99.0))
+
+
+def test_without_a_status_word(cuda):
+    """Values out of range with nowhere to report them."""
+    tokens = [2, 3]
+    cache = paged.Cache(lens_of(1, 2, 1, [98, 30], tokens, 1), 16, H=4)
+    cu, qkv = inputs(cache, tokens, 3, pad=7)
+    c = Call(cache, 0, qkv, [4, 6, 9])
+    c.status = None
+    before = bits(c.Kp), bits(c.Vp), bits(c.out)
+    c.run()
+    for got, old in zip((c.Kp, c.Vp, c.out), before):
+        assert torch.equal(bits(got), old)
+    s = State(cache)
+    s.status = None
+    s.len[0] = -4
+    s.tables(tokens=dev(tokens))
+    assert torch.equal(s.new_len, s.len) and torch.equal(s.new_count, s.count)
+    s = State(cache)
+    s.status = None
+    s.table[0, 0] = -7
+    s.release([1, 0])
+    assert int(s.free[cache.count]) == -1
+
+
+def test_a_prompt_that_found_no_pages_is_not_packed(cuda):
+    plan, _ = plan_of(2, 4, 2, [300, 200])
+    cache = paged.Cache(np.zeros((2, 3, 2), int), 16, spare=9, wider=30, H=4)
+    s = State(cache)
+    s.new_len, s.new_count = s.len, s.count
+    s.table.fill_(3)  # entries of sequences that are gone
+    K = torch.ones((2, 2, 2, 300, 128), dtype=torch.bfloat16, device="cuda")
+    Kp, Vp = cache.Kp.cuda(), cache.Vp.cuda()
+    s.tables(plan=plan, seq=dev([0, 2]))
+    dkv.dkv_page_compact(s.p, plan, K, K, s.table, s.len, Kp, Vp, seq=dev([0, 2]), status=s.status)
+    assert int(s.status) == dkv.DKV_DEV_PAGES_EXHAUSTED | dkv.DKV_DEV_PAGE_RANGE
+    assert torch.isnan(Kp).all() and torch.isnan(Vp).all()
+    plan.close()
