@@ -22,16 +22,23 @@
 //     warp 9          TMA: Q tiles, and K and V tiles page by page into one ring in the order of use.
 //     warp 10         walks the CTA's share and describes its units to the others (11 is idle).
 //
-// What bounds it. Next tokens stream the cache: 16 sequences of 3K-24K rows, 847 MB, in 129.6 us, 6.5
+// What bounds it. Next tokens stream the cache: 16 sequences of 3K-24K rows, 847 MB, in 131 us, 6.5
 // TB/s of the 6.8 of a plain copy. Turns and queries: a pair unit's tile (four products, 2,048 cycles
 // of the tensor pipe at its best) takes 1.52 us, 2,900 cycles. Q K^T reads both operands from shared
 // memory, 8 KB a 64-cycle instruction and so the 128 B a cycle that it gives, beside the copies into
 // the ring: about 630 cycles instead of 512, so the pipe is busy for 2,280. What bounds it is each
 // group's chain, as TMEM holds one S a group: 950 cycles from S to the first half of P, P V and the
-// next Q K^T behind it, and four hand-offs of 100 to 150 cycles. 200-777 queries over 5K-13K rows: 125.5 us, 1.27 PFLOP/s, 100 us of it in the loop;
-// 4K tokens over 45K rows: 1,700 us, 1.46 PFLOP/s, 0.86 of what the library's matrix product sustains
-// (1,531 us before the clocks fall under the power limit). One token over 1.8K rows: 14.5 us, all of
-// it latency: two launches, the count of the cost, one tile, the join.
+// next Q K^T behind it, and four hand-offs of 100 to 150 cycles. 200-777 queries over 5K-13K rows: 127.7 us, 1.24 PFLOP/s, 100 us of it in the loop;
+// 4K tokens over 45K rows: 1,730 us, 1.43 PFLOP/s, 0.85 of what the library's matrix product sustains
+// (1,531 us before the clocks fall under the power limit). One token over 1.8K rows: 15.1 us, all of
+// it latency: two launches, the count of the cost, one tile, the join (0.3 us of it the looks at offsets and
+// lengths, and the fence).
+//
+// Scores, their max and sum and O are fp32. The weights P are rounded to the inputs' type, as both operands of
+// the second product have it: half a step of each weight, of either sign, so that errors against 64 bits go from
+// the 0.0017 of the output's own rounding to 0.0019 (next tokens, queries) and 0.0021 (the turn) in bf16, from 0.00021 to
+// 0.00022 in fp16. P as a high and a low part would take another P V beside each, 1,024 more cycles for a pair
+// unit's 2,048.
 // Two MMA warps, a group each, took 173 us for the queries where one took 137 (their products alternate on
 // the pipe), four softmax warpgroups 152; stages freed by the softmax warps instead of by commits 136.
 //
@@ -127,8 +134,9 @@ __device__ __forceinline__ Unit make_unit(const ChunkArgs& a, int h, int t, int 
 }
 
 // What a cache tile costs: a pair unit's has twice the products, a split unit's waits for its rows.
-// Measured side by side 1.63 and 1.15 us (with one weight for both, the SMs with next tokens only were
-// done at 225 us of 320, in a step of two turns and ten next tokens).
+// In shares of one kind a pair unit's takes 1.52 us, a split unit's 1.14, so 4 : 3, but a step of two turns and ten
+// next tokens takes 308 us with 3 : 2 and 311 with 4 : 3 (queries 127.1 and 126.7, next tokens 130.4 and 130.0). With
+// one weight for both, the SMs with next tokens only were done at 225 us of 320.
 constexpr int kPairCost = 3, kSplitCost = 2;
 
 // The share of one CTA, unit by unit. Units lie end to end on a line of costs; a tile is the
@@ -747,7 +755,7 @@ struct RowSum {
 
 // Pieces that one thread adds up, in their order. A turn's units are cut in two or three, all but the last stored
 // long before; with that one stored and all read again as items of join_items the last CTAs took 9 to 17 us
-// longer (200-777 queries over 5K-13K rows: 137 us, 125.5 so).
+// longer (200-777 queries over 5K-13K rows: 137 us, and 125.5 so).
 constexpr int kFew = 3;
 
 // Where piece k of the unit that starts in CTA c0 lies.

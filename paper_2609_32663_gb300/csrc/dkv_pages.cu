@@ -20,8 +20,8 @@
 // and -1 (no page) moves in its place, so that no table, list or slot map ever leads out of the pools.
 //
 // What bounds it: the launch and the scan for a decode step (4.4 us of its 6.9); instructions more than bytes for
-// the large calls: 12.8 M pages given back, 103 MB, in 29.4 us, of which the scan takes 4 and whole runs of one slab go at
-// 6.2 TB/s; 256 K pages and 4.1 M slots, 17.7 MB, in 12.2 us.
+// the large calls: 12.8 M pages given back, 103 MB, in 29.3 us, of which launch and scan take 8.5 and chunks that hold
+// several slabs 4; 256 K pages and 4.1 M slots, 17.7 MB, in 12.2 us.
 #include "dkv_decode_common.cuh"
 #include "dkv_pages.cuh"
 #include "dkv_pool.cuh"
@@ -257,7 +257,7 @@ __device__ __forceinline__ int load_now(const int32_t* p)
 }
 
 // Whether all N page numbers that move are in range; if not, those that are none become -1 (reported). A
-// compare of the largest: 12.8 M pages given back take 29.4 us (28.6 without any look, 31.4 with one at each),
+// compare of the largest: 12.8 M pages given back take 29.3 us (28.6 without any look, 31.4 with one at each),
 // 4.1 M slots 12.2 (11.6, 14.7).
 template <int N>
 __device__ __forceinline__ bool pages_hold(const PageArgs& a, int (&page)[N])
@@ -379,7 +379,7 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b)
 
 // Slot map [L][t][Hkv], V neighbouring heads a lane. A warp takes a contiguous piece of the map, a unit of 32 / (Hkv / V)
 // tokens (of one token's 32 V heads, where it has more) after the other, and looks sequence, lengths and
-// scan up again only where they change (all of it for each entry: 14.3 us instead of 11.6 for 4.1 M
+// scan up again only where they change (all of it for each entry: 14.3 us instead of the 11.6 before pages were looked at, for 4.1 M
 // entries). Pages that this call takes are read from the free list: their table entries may not be
 // written yet.
 template <int V>
@@ -470,7 +470,7 @@ __device__ __forceinline__ void fill(const PageArgs& a, const PageHead& head, co
             fill_slots<1>(a, head, first, len, cu, w, warps);
     }
     // One page a lane while that is enough (latency counts). Chunks of neighbouring warps lie side by side:
-    // a contiguous piece a warp took 37 us where this takes 28.5, for the release of 12.8 M pages.
+    // a contiguous piece a warp took 37 us where this took 28.5, for the release of 12.8 M pages.
     if (head.pages > warps * 32)
         fill_chunks(a, head, first, len, (int64_t)warp * 32 * kLong, (int64_t)warps * 32 * kLong);
     else if (warp * 32 < head.pages)
