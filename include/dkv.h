@@ -62,7 +62,7 @@ typedef enum {
 #define DKV_DEV_TMA_TIMEOUT 0x2     /* a bulk copy did not complete within the wait bound */
 #define DKV_DEV_MERGE_TIMEOUT 0x4   /* a fused merge's partials were not all written within the wait bound: outputs of the plan's calls are not to be used until the word is cleared */
 #define DKV_DEV_PAGES_EXHAUSTED 0x10 /* dkv_page_tables: fewer free pages than the call needs; it changed nothing */
-#define DKV_DEV_PAGE_RANGE 0x20     /* paged cache: a length, token count, slot or page number on the device was out of its range; a table call changed nothing, another call skipped what it could not place */
+#define DKV_DEV_PAGE_RANGE 0x20     /* paged cache: a length, token count or offset, slot or page number on the device was out of its range; a table call changed nothing (or, for a page number, wrote -1 in its place), another call skipped what it could not place */
 #define DKV_DEV_BOUNDS 0x8          /* bounds-checked build only: an index or offset a kernel read was out of its range; the access was skipped */
 
 /* Pattern and model geometry (Sec. 3.2, Sec. 3.4). */
