@@ -14,7 +14,9 @@
  *   dkv_free          release a plan
  *
  * the same over a paged cache, whose sequences grow, come and go (dkv_page_tables,
- * dkv_page_release, dkv_page_compact, dkv_chunk_attn), and the step before them, the export of the pattern from learned retention
+ * dkv_page_release, dkv_page_compact, dkv_chunk_attn), in 16 or in 8 bits (dkv_quant_compact,
+ * dkv_quant_attn) with the rotary positions of what enters it (dkv_rope, dkv_rope_append), and
+ * the step before them, the export of the pattern from learned retention
  * probabilities with an exact budget (dkv_budget, dkv_topk_mask; Eq. 3).
  *
  * Conventions used by every entry point
@@ -555,6 +557,136 @@ dkv_status dkv_chunk_attn(const dkv_pages* pages, int32_t layer, int32_t dtype, 
                           const int32_t* cu_tokens, const int32_t* table, const int32_t* len, void* Kp, void* Vp,
                           int32_t causal, float scale, void* out, void* workspace, int64_t workspace_bytes,
                           int32_t* status, cudaStream_t stream);
+
+/*
+ * Rotary positions: pair i of the first rot_dim elements of a row, (a, b), becomes
+ * m (a cos x - b sin x, b cos x + a sin x) at position p, x = p f_i, with the pair's frequency
+ * f_i (radians a position) and one magnitude m; the elements behind are kept. A dkv_rotary holds
+ * the layout and frequencies; dkv_rotary_make and dkv_rotary_custom fill the caller's (host only).
+ *
+ * rot_dim     a multiple of 16, 16 to 128.
+ * interleaved 0: pair i is (i, i + rot_dim / 2); not 0: (2i, 2i + 1).
+ * theta       f_i = theta^(-2i / rot_dim), theta > 0; finite.
+ * scaling     positions past the trained context, with factor s >= 1 and context C >= 1 tokens:
+ *   DKV_ROPE_NONE    f_i.
+ *   DKV_ROPE_LINEAR  f_i / s.
+ *   DKV_ROPE_NTK     theta s^(rot_dim / (rot_dim - 2)) in place of theta.
+ *   DKV_ROPE_BANDS   f_i (k + (1 - k) / s), k = (C f_i / 2 pi - low) / (high - low) clamped to
+ *                    [0, 1]: pairs that turn less than `low` times within C tokens are scaled,
+ *                    those that turn more than `high` times are not. 0 < low < high.
+ *   DKV_ROPE_YARN    the same mix, k = 1 - clamp((i - i0) / max(i1 - i0, 0.001)), by the index of the pair,
+ *                    between the pairs that turn `high` and `low` times within C tokens, i(t) =
+ *                    rot_dim ln(C / (2 pi t)) / (2 ln theta): i0 = max(floor(i(high)), 0), i1 =
+ *                    min(ceil(i(low)), rot_dim - 1); m = 1 + 0.1 ln s. theta > 1.
+ *   What a scaling does not name is not read.
+ * dkv_rotary_custom takes the frequencies (host double [rot_dim / 2], |f| < 2^20) and the
+ * magnitude (finite) themselves.
+ * A frequency is held in 2^-64 of a turn, so that an angle is the low half of an integer product,
+ * exact for every position; cos and sin are fp32, and a turned element is rounded once.
+ * Errors: DKV_ERR_INVALID_ARG.
+ */
+typedef struct {
+    int32_t rot_dim;
+    int32_t interleaved;
+    float magnitude;
+    int32_t reserved;   /* 0 */
+    uint64_t turns[64]; /* pair i: turns a position, modulo 1, in units of 2^-64 */
+} dkv_rotary;
+
+#define DKV_ROPE_NONE 0
+#define DKV_ROPE_LINEAR 1
+#define DKV_ROPE_NTK 2
+#define DKV_ROPE_BANDS 3
+#define DKV_ROPE_YARN 4
+dkv_status dkv_rotary_make(dkv_rotary* rotary, int32_t rot_dim, int32_t interleaved, double theta, int32_t scaling,
+                           double factor, int32_t context, double low, double high);
+dkv_status dkv_rotary_custom(dkv_rotary* rotary, int32_t rot_dim, int32_t interleaved, const double* freq, double magnitude);
+
+/*
+ * Rows turned by their tokens' positions: what a prefill does to its q and K, before dense caches
+ * are pruned.
+ * dtype      DKV_BF16 or DKV_FP16: type of x and out.
+ * x, out     device [num_tokens][heads][128], token t at t * x_stride (out_stride) elements. out is
+ *            x, with its stride, or does not overlap it. num_tokens * heads <= 2^30.
+ *            Strides are multiples of 8, at least heads*128; 16-byte aligned.
+ * positions  device int32 [num_tokens], of any sign.
+ * rotary     host; read by the call, not kept.
+ * Asynchronous, allocates nothing, can be captured. Errors: DKV_ERR_INVALID_ARG, DKV_ERR_CUDA.
+ */
+dkv_status dkv_rope(const dkv_rotary* rotary, int32_t dtype, int32_t num_tokens, int32_t heads, const void* x, int64_t x_stride,
+                    const int32_t* positions, void* out, int64_t out_stride, cudaStream_t stream);
+
+/*
+ * The paged cache in 8 bits. Its pools hold a byte for each 16-bit element, and every row has a
+ * scale of its own:
+ *   Kp, Vp  uint8 [num_pages * page_rows][128]: e4m3 values (FP8, 4 exponent bits, no infinities)
+ *   Ks, Vs  uint8 [num_pages * page_rows]: byte u stands for the scale 2^(u - 127) (E8M0)
+ * all 16-byte aligned. Element i of a row is its value i times the row's scale. Geometry,
+ * tables, lengths, dkv_page_tables and dkv_page_release are the same as for 16-bit pools.
+ * The calls below write a row x with the least scale 2^e for which max |x| <= 448 2^e (e >=
+ * -126), and each x 2^-e rounded to the nearest e4m3 value, ties to even: an error of at most
+ * 2^-4 of an element, or 2^-10 of the scale where that is more. An element that is not finite is
+ * held as NaN (byte 0x7f), and the scale goes by the others. Scale bytes of 0 and above 247 are never
+ * written, and are not to be there for rows that are read.
+ */
+
+/*
+ * One layer's new tokens before their attention: q and k_new are turned by their positions, k_new
+ * and v_new written to the last rows of their slabs, in one launch.
+ *
+ * dtype        DKV_BF16 or DKV_FP16: type of q, q_out, k_new, v_new and 16-bit pools.
+ * rotary       host, or NULL: nothing is turned. positions (device int32 [num_tokens]) goes with it.
+ * num_tokens, cu_tokens, table, len  as for dkv_chunk_attn: len[h] counts the new tokens. Rows from
+ *              cu_tokens[B] on are no token's and are left as they are in q_out; token offsets out
+ *              of order set DKV_DEV_PAGE_RANGE and nothing is written; a row whose length, page
+ *              or place is out of range is skipped and sets the same bit.
+ * q, q_out     [num_tokens][H][128], token t at t * q_stride (q_out_stride) elements, or both NULL.
+ *              q_out is q, with its stride, or does not overlap it.
+ * k_new, v_new [num_tokens][H_kv][128], token t at t * kv_stride elements, or both NULL. They are
+ *              not changed, and must not overlap the pools or q_out.
+ * Kp, Vp       the pools: 16-bit of dtype where Ks and Vs are NULL, else 8-bit. A turned key is
+ *              rounded once, to what the pool holds. (NULL without k_new.)
+ * Strides are multiples of 8, at least H*128 (H_kv*128); all 16-byte aligned.
+ * After it, dkv_chunk_attn is called with k_new and v_new NULL; dkv_quant_attn as it is. It signals
+ * early completion: what it writes may not be given to a decode call as n_appended or context rows
+ * that directly follows it.
+ * Asynchronous, allocates nothing, can be captured. Errors: DKV_ERR_INVALID_ARG, DKV_ERR_CUDA.
+ */
+dkv_status dkv_rope_append(const dkv_pages* pages, int32_t layer, const dkv_rotary* rotary, int32_t dtype, int32_t num_tokens,
+                           const int32_t* positions, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                           const void* k_new, const void* v_new, int64_t kv_stride, const int32_t* cu_tokens,
+                           const int32_t* table, const int32_t* len, void* Kp, void* Vp, uint8_t* Ks, uint8_t* Vs,
+                           int32_t* status, cudaStream_t stream);
+
+/*
+ * Prune-and-pack into 8-bit pages: dkv_page_compact for such pools, whose rows are written as
+ * described above. dtype: DKV_BF16 or DKV_FP16, the type of K and V. Ks, Vs and the pools do not
+ * overlap one another or K and V.
+ */
+dkv_status dkv_quant_compact(const dkv_pages* pages, const dkv_plan* plan, const int32_t* seq, int32_t dtype, const void* K,
+                             const void* V, int64_t T_stride, const int32_t* table, const int32_t* len, void* Kp, void* Vp,
+                             uint8_t* Ks, uint8_t* Vs, int32_t* status, cudaStream_t stream);
+
+/*
+ * One layer's attention of a step's new tokens over 8-bit pages (dkv_chunk_attn over such pools;
+ * the rows of the new tokens are in them already, from dkv_rope_append or dkv_quant_compact).
+ *
+ * max_tokens  the most tokens that one sequence brings, or <= 0: num_tokens. A sequence that brings
+ *             more is skipped: its outputs are not written and DKV_DEV_PAGE_RANGE is set. Small
+ *             numbers save a launch.
+ * Kp, Vp, Ks, Vs  are read only.
+ * out         as for dkv_chunk_attn. Scores, softmax statistics and sums are fp32. The e4m3 values and q
+ *             (scaled by a power of two a row) enter the products as fp16, which holds them exactly but for
+ *             elements of q below 2^-28 of the row's largest; softmax weights, times V's scales, are rounded to
+ *             fp16, whose least step is at most 2^-30 of the largest such product of the row; the output is rounded once.
+ * workspace   dkv_quant_workspace_bytes(pages) bytes (-1: a bad geometry).
+ * Other arguments, what is promised and errors are those of dkv_chunk_attn.
+ */
+int64_t dkv_quant_workspace_bytes(const dkv_pages* pages);
+dkv_status dkv_quant_attn(const dkv_pages* pages, int32_t layer, int32_t dtype, int32_t num_tokens, int32_t max_tokens,
+                          const void* q, int64_t q_stride, const int32_t* cu_tokens, const int32_t* table, const int32_t* len,
+                          const void* Kp, const void* Vp, const uint8_t* Ks, const uint8_t* Vs, int32_t causal, float scale,
+                          void* out, void* workspace, int64_t workspace_bytes, int32_t* status, cudaStream_t stream);
 
 #ifdef __cplusplus
 }

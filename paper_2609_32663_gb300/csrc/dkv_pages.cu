@@ -23,7 +23,7 @@
 // the large calls: 12.8 M pages given back, 103 MB, in 29.3 us, of which launch and scan take 8.5 and chunks that hold
 // several slabs 4; 256 K pages and 4.1 M slots, 17.7 MB, in 12.2 us.
 #include "dkv_decode_common.cuh"
-#include "dkv_pages.cuh"
+#include "dkv_quant.cuh"
 #include "dkv_pool.cuh"
 
 #include <algorithm>
@@ -692,6 +692,7 @@ cudaError_t page_setup(int* sms)
     if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
     if ((e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
     if ((e = chunk_setup()) != cudaSuccess) return e;
+    if ((e = quant_setup()) != cudaSuccess) return e;
     if ((e = cudaFuncSetAttribute(page_fused_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFusedSlabs * 4)) != cudaSuccess) return e;
     if ((e = cudaFuncSetAttribute(page_compact_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPcSmem)) != cudaSuccess) return e;
     if (count < kMost) known[count++] = Known{id, *sms};

@@ -1,0 +1,104 @@
+// Rotary positions and the paged cache in 8 bits (dkv_rope.cu, dkv_quant.cu, dkv_quant_attn.cu):
+// declarations shared with the host side (dkv_pages_api.cu), and a row's scale and e4m3 values.
+#pragma once
+
+#include "dkv_pages.cuh"
+
+namespace dkv {
+
+struct RopeArgs {
+    const uint16_t* q;     // [T] rows of q_stride elements, H x 128 used, or null
+    uint16_t* q_out;
+    const uint16_t* k;     // [T] rows of kv_stride elements, Hkv x 128 used, or null
+    const uint16_t* v;
+    int64_t q_stride, out_stride, kv_stride;
+    const int32_t* positions;  // [T], or null where nothing is turned (rot = 0)
+    const int32_t* cu;     // [B + 1], or null: all T rows are tokens
+    const int32_t* table;  // the layer's slabs: [B * Hkv][max_pages]
+    const int32_t* len;    // [B * Hkv]
+    void* Kp;              // 16-bit or 8-bit pools
+    void* Vp;
+    uint8_t* Ks;           // null: 16-bit pools
+    uint8_t* Vs;
+    int32_t* status;
+    int T, B, H, Hkv, P, num_pages, max_pages;
+    int fp16, interleaved, rot;
+    float magnitude;
+    uint64_t turns[64];
+};
+cudaError_t launch_rope(const RopeArgs& a, cudaStream_t st);
+
+struct QuantCompactArgs {
+    PageCompactArgs c;     // (Kp and Vp are pools of bytes)
+    uint8_t* Ks;
+    uint8_t* Vs;
+    int fp16;
+};
+cudaError_t launch_quant_compact(const QuantCompactArgs& a, cudaStream_t st);
+
+struct QuantAttnArgs {
+    const uint16_t* q;      // [T] rows of q_stride elements, H x 128 used
+    int64_t q_stride;
+    const int32_t* cu;      // [B + 1]
+    const int32_t* table;   // the layer's slabs: [B * Hkv][max_pages]
+    const int32_t* len;     // [B * Hkv]
+    const uint8_t* Kp;
+    const uint8_t* Vp;
+    const uint8_t* Ks;
+    const uint8_t* Vs;
+    uint16_t* out;          // [T][H][128]
+    int32_t* status;
+    void* work;
+    int T, B, H, Hkv, G, P, num_pages, max_pages;
+    int most;               // tokens of a sequence, at most
+    int causal, fp16;
+    float qscale;           // softmax scale * log2(e)
+};
+int64_t quant_workspace_bytes();
+cudaError_t quant_setup();  // the kernels' attributes in the current context
+// short_boxes (fault injection): page copies deliver half the bytes that a stage expects, inside the
+// stage, so that every wait for them runs out.
+cudaError_t launch_quant_attn(const QuantAttnArgs& a, bool short_boxes, cudaStream_t st);
+
+#ifdef __CUDACC__
+namespace {
+
+// A value as it is held: what is not finite is NaN. `size`: |x|, or 0 for what is not finite.
+__device__ __forceinline__ float held(float x, float& size)
+{
+    const float y = fabsf(x);
+    const bool finite = y < INFINITY;
+    size = finite ? y : 0.f;
+    return finite ? x : __uint_as_float(0x7fffffffu);
+}
+
+// Scale byte u of a row whose largest element is `size`: the least e = u - 127 with size <= 448 2^e.
+// 448 = 1.75 2^8, so for size = 1.m 2^x it is x - 8, or one more where 1.m > 1.75.
+__device__ __forceinline__ uint32_t scale_byte(float size)
+{
+    const uint32_t bits = __float_as_uint(size);
+    const int u = (int)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return (uint32_t)max(u, 1);
+}
+
+// 2^(u - 127) and its inverse (u in [1, 253]).
+__device__ __forceinline__ float scale_of(uint32_t u) { return __uint_as_float(u << 23); }
+__device__ __forceinline__ float inverse_scale(uint32_t u) { return __uint_as_float((254u - u) << 23); }
+
+// Four e4m3 values, the first in the lowest byte.
+__device__ __forceinline__ uint32_t pack_e4m3(float x0, float x1, float x2, float x3)
+{
+    uint32_t v;
+    asm("{\n\t.reg .b16 lo, hi;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\t"
+        "mov.b32 %0, {lo, hi};\n\t}"
+        : "=r"(v)
+        : "f"(x0), "f"(x1), "f"(x2), "f"(x3));
+    return v;
+}
+
+}  // namespace
+#endif
+
+}  // namespace dkv

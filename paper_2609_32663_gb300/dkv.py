@@ -37,7 +37,9 @@ EXPORTS = ("dkv_last_error", "dkv_map_pattern", "dkv_plan_dense", "dkv_plan_quer
            "dkv_topk_mask", "dkv_decode_multi", "dkv_map_pattern_inplace", "dkv_compact_inplace",
            "dkv_vmm_alloc", "dkv_vmm_trim", "dkv_vmm_pages_to_keep", "dkv_vmm_mapped_bytes", "dkv_vmm_page_bytes",
            "dkv_vmm_free", "dkv_page_workspace_bytes", "dkv_page_tables", "dkv_page_release", "dkv_page_compact",
-           "dkv_chunk_workspace_bytes", "dkv_chunk_attn")
+           "dkv_chunk_workspace_bytes", "dkv_chunk_attn", "dkv_rotary_make", "dkv_rotary_custom", "dkv_rope", "dkv_rope_append",
+           "dkv_quant_compact", "dkv_quant_workspace_bytes", "dkv_quant_attn")
+DKV_ROPE_NONE, DKV_ROPE_LINEAR, DKV_ROPE_NTK, DKV_ROPE_BANDS, DKV_ROPE_YARN = range(5)
 
 
 class DkvError(RuntimeError):
@@ -101,6 +103,19 @@ class Pages:
     @cached_property
     def slabs(self):
         return self.L * self.B * self.H_kv
+
+
+class dkv_rotary(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float),
+                ("reserved", ctypes.c_int32), ("turns", ctypes.c_uint64 * 64)]
+
+
+class Rotary:
+    """Layout and frequencies of rotary positions (dkv_rotary), from dkv_rotary_make or dkv_rotary_custom."""
+
+    def __init__(self):
+        self.c = dkv_rotary()
+        self.ref = ctypes.byref(self.c)
 
 
 _lib = None
@@ -182,6 +197,21 @@ def lib(path: str | None = None):
     L.dkv_chunk_workspace_bytes.argtypes = [PG]
     L.dkv_chunk_attn.restype = ctypes.c_int
     L.dkv_chunk_attn.argtypes = [PG, I32, I32, I32, V, I64, V, V, I64, V, V, V, V, V, I32, ctypes.c_float, V, V, I64, V, V]
+    RT, F64 = ctypes.POINTER(dkv_rotary), ctypes.c_double
+    L.dkv_rotary_make.restype = ctypes.c_int
+    L.dkv_rotary_make.argtypes = [RT, I32, I32, F64, I32, F64, I32, F64, F64]
+    L.dkv_rotary_custom.restype = ctypes.c_int
+    L.dkv_rotary_custom.argtypes = [RT, I32, I32, V, F64]
+    L.dkv_rope.restype = ctypes.c_int
+    L.dkv_rope.argtypes = [RT, I32, I32, I32, V, I64, V, V, I64, V]
+    L.dkv_rope_append.restype = ctypes.c_int
+    L.dkv_rope_append.argtypes = [PG, I32, RT, I32, I32, V, V, I64, V, I64, V, V, I64, V, V, V, V, V, V, V, V, V]
+    L.dkv_quant_compact.restype = ctypes.c_int
+    L.dkv_quant_compact.argtypes = [PG, V, V, I32, V, V, I64, V, V, V, V, V, V, V, V]
+    L.dkv_quant_workspace_bytes.restype = I64
+    L.dkv_quant_workspace_bytes.argtypes = [PG]
+    L.dkv_quant_attn.restype = ctypes.c_int
+    L.dkv_quant_attn.argtypes = [PG, I32, I32, I32, I32, V, I64, V, V, V, V, V, V, V, I32, ctypes.c_float, V, V, I64, V, V]
     if path is None:
         _lib = L
     return L
@@ -238,6 +268,8 @@ class _Torch:
         self.i32 = (torch.int32,)
         self.f32 = (torch.float32,)
         self.u8 = (torch.uint8,)
+        self.e4m3 = (torch.uint8, torch.float8_e4m3fn)
+        self.e8m0 = (torch.uint8,) + ((torch.float8_e8m0fnu,) if hasattr(torch, "float8_e8m0fnu") else ())
         C = torch._C
         self.raw_stream = getattr(C, "_cuda_getCurrentRawStream", None)
         self.device = getattr(C, "_cuda_getDevice", None)
@@ -713,3 +745,148 @@ def dkv_chunk_attn(pages: Pages, layer: int, q, k_new, v_new, cu_tokens, table, 
         _on(len, "len", at, T.i32, pages.slabs), _on(Kp, "Kp", at, one, pool), _on(Vp, "Vp", at, one, pool),
         1 if causal else 0, scale, _on(out, "out", at, one, tokens * pages.H * 128), wp, wb, _word(status, at),
         queue), "dkv_chunk_attn")
+
+
+_SCALINGS = {"none": DKV_ROPE_NONE, "linear": DKV_ROPE_LINEAR, "ntk": DKV_ROPE_NTK, "bands": DKV_ROPE_BANDS, "yarn": DKV_ROPE_YARN}
+
+
+def dkv_rotary_make(rot_dim: int = 128, theta: float = 10000.0, interleaved: bool = False, scaling: str = "none",
+                    factor: float = 1.0, context: int = 0, low: float = 0.0, high: float = 0.0) -> Rotary:
+    """Rotary positions of the first rot_dim elements, f_i = theta^(-2i / rot_dim), scaled for a long context: "none",
+    "linear", "ntk", "bands" or "yarn"."""
+    if scaling not in _SCALINGS:
+        _bad(f"scaling is {scaling!r}, expected one of {sorted(_SCALINGS)}")
+    r = Rotary()
+    _check(lib().dkv_rotary_make(r.ref, int(rot_dim), 1 if interleaved else 0, float(theta), _SCALINGS[scaling], float(factor),
+                                 int(context), float(low), float(high)), "dkv_rotary_make")
+    return r
+
+
+def dkv_rotary_custom(freq, interleaved: bool = False, magnitude: float = 1.0) -> Rotary:
+    """Rotary positions with these frequencies (radians a position, one a pair)."""
+    f = np.ascontiguousarray(freq, dtype=np.float64).reshape(-1)
+    r = Rotary()
+    _check(lib().dkv_rotary_custom(r.ref, 2 * f.size, 1 if interleaved else 0, _ptr(f), float(magnitude)), "dkv_rotary_custom")
+    return r
+
+
+def _rows16(x, name):
+    """Whether x, of [tokens][heads][128] rows, is fp16; what is neither that nor bf16 is refused."""
+    _device_of(x, name)
+    T = _torch().torch
+    half = x.dtype == T.float16
+    if not (half or x.dtype == T.bfloat16) or x.dim() != 3:
+        _bad(f"{name} is {x.dtype} of {x.dim()} dimensions, expected bfloat16 or float16 [T][heads][128]")
+    return half
+
+
+def _rotary_ref(rotary):
+    if not isinstance(rotary, Rotary):
+        _bad(f"rotary must be a Rotary, not {type(rotary).__name__}")
+    return rotary.ref
+
+
+def dkv_rope(x, positions, rotary: Rotary, out, stream=None):
+    """Rows x [T][heads][128] turned by their positions (int32 [T]) -> out, of x's type and shape. Either may be a slice of a
+    projection; out may be x."""
+    half = _rows16(x, "x")
+    at, queue = _where(stream)
+    tokens, heads = x.shape[:2]
+    xp, xs = _token_rows(x, "x", at, x.dtype, tokens, heads)
+    op, os_ = _token_rows(out, "out", at, x.dtype, tokens, heads)
+    _check(lib().dkv_rope(_rotary_ref(rotary), DKV_FP16 if half else DKV_BF16, tokens, heads, xp, xs,
+                          _on(positions, "positions", at, _torch().i32, tokens), op, os_, queue), "dkv_rope")
+
+
+def _scales(pages, at, Ks, Vs):
+    n = pages.num_pages * pages.page_rows
+    return _on(Ks, "Ks", at, _torch().e8m0, n), _on(Vs, "Vs", at, _torch().e8m0, n)
+
+
+def dkv_rope_append(pages: Pages, layer: int, q, k_new, v_new, positions, cu_tokens, table, len, Kp, Vp, q_out, Ks=None, Vs=None,
+                    rotary: Rotary | None = None, status=None, stream=None):
+    """One layer's new tokens: q [T][H][128] turned by their positions (int32 [T]) -> q_out, k_new turned and with v_new
+    [T][H_kv][128] written to their slabs' pages, which are of their type, or 8-bit where the scales Ks and Vs are given. q and
+    q_out, or k_new and v_new, may be None; without a rotary nothing is turned (and positions is not used)."""
+    first, name = (q, "q") if q is not None else (k_new, "k_new (without q)")
+    half, T = _rows16(first, name), _torch()
+    at, queue = _where(stream)
+    tokens, dtype = first.shape[0], first.dtype
+    qp = op = kp = vp = None
+    qs = os_ = ks = 0
+    if (q is None) != (q_out is None):
+        _bad("q and q_out must both be given or both be None")
+    if q is not None:
+        qp, qs = _token_rows(q, "q", at, dtype, tokens, pages.H)
+        op, os_ = _token_rows(q_out, "q_out", at, dtype, tokens, pages.H)
+    if (k_new is None) != (v_new is None):
+        _bad("k_new and v_new must both be given or both be None")
+    if (Ks is None) != (Vs is None):
+        _bad("Ks and Vs must both be given or both be None")
+    if k_new is not None:
+        kp, ks = _token_rows(k_new, "k_new", at, dtype, tokens, pages.H_kv)
+        vp, vs = _token_rows(v_new, "v_new", at, dtype, tokens, pages.H_kv)
+        if ks != vs:
+            _bad(f"k_new and v_new have token strides {ks} and {vs}")
+    pool, types = pages.num_pages * pages.page_rows * 128, (dtype,) if Ks is None else T.e4m3
+    ksp, vsp = _scales(pages, at, Ks, Vs)
+    turn = rotary is not None
+    _check(lib().dkv_rope_append(
+        pages.ref, int(layer), _rotary_ref(rotary) if turn else None, DKV_FP16 if half else DKV_BF16, tokens,
+        _on(positions, "positions", at, T.i32, tokens) if turn else None, qp, qs, op, os_, kp, vp, ks,
+        _on(cu_tokens, "cu_tokens", at, T.i32, pages.B + 1), _on(table, "table", at, T.i32, pages.slabs * pages.max_pages),
+        _on(len, "len", at, T.i32, pages.slabs), _on(Kp, "Kp", at, types, pool), _on(Vp, "Vp", at, types, pool), ksp, vsp,
+        _word(status, at), queue), "dkv_rope_append")
+
+
+def dkv_quant_compact(pages: Pages, plan: Plan, K, V, table, len, Kp, Vp, Ks, Vs, seq=None, T_stride: int | None = None,
+                      status=None, stream=None):
+    """The kept rows of plan sequence i become the last rows of slot seq[i]'s slabs, in 8-bit pages with their scales. K and V
+    are bfloat16 or float16 [L][plan B][H_kv][T_stride][128]."""
+    T, sh = _torch(), plan.shape
+    for t, name in ((K, "K"), (V, "V")):
+        _device_of(t, name)
+        if t.dtype not in (T.torch.bfloat16, T.torch.float16):
+            _bad(f"{name} is {t.dtype}, expected bfloat16 or float16")
+    _one_type("K and V", K, V)
+    if T_stride is None:
+        T_stride = K.shape[-2]
+    at, queue = _where(stream)
+    handle = plan.address
+    dense = sh.L * plan.B * sh.H_kv * int(T_stride) * 128
+    pool = pages.num_pages * pages.page_rows * 128
+    for t, name in ((K, "K"), (V, "V")):
+        if t.numel() < dense:
+            _bad(f"{name} has {t.numel()} elements, needs at least {dense}")
+    ksp, vsp = _scales(pages, at, Ks, Vs)
+    _check(lib().dkv_quant_compact(
+        pages.ref, handle, _on(seq, "seq", at, T.i32, plan.B), DKV_FP16 if K.dtype == T.torch.float16 else DKV_BF16,
+        _on(K, "K", at, (K.dtype,)), _on(V, "V", at, (K.dtype,)), int(T_stride),
+        _on(table, "table", at, T.i32, pages.slabs * pages.max_pages), _on(len, "len", at, T.i32, pages.slabs),
+        _on(Kp, "Kp", at, T.e4m3, pool), _on(Vp, "Vp", at, T.e4m3, pool), ksp, vsp, _word(status, at), queue), "dkv_quant_compact")
+
+
+def dkv_quant_workspace_bytes(pages: Pages) -> int:
+    n = int(lib().dkv_quant_workspace_bytes(ctypes.byref(pages.c)))
+    if n < 0:
+        _check(DKV_ERR_INVALID_ARG, "dkv_quant_workspace_bytes")
+    return n
+
+
+def dkv_quant_attn(pages: Pages, layer: int, q, cu_tokens, table, len, Kp, Vp, Ks, Vs, out, workspace, causal: bool = True,
+                   scale: float = 0.0, max_tokens: int = 0, status=None, stream=None):
+    """One layer's attention of q [T][H][128] over 8-bit pages -> out [T][H][128], both bfloat16 or float16. max_tokens: the
+    most tokens that one sequence brings (0: not known)."""
+    half, T = _rows16(q, "q"), _torch()
+    at, queue = _where(stream)
+    tokens = q.shape[0]
+    qp, qs = _token_rows(q, "q", at, q.dtype, tokens, pages.H)
+    pool = pages.num_pages * pages.page_rows * 128
+    ksp, vsp = _scales(pages, at, Ks, Vs)
+    wp, wb = _work(workspace, at)
+    _check(lib().dkv_quant_attn(
+        pages.ref, int(layer), DKV_FP16 if half else DKV_BF16, tokens, int(max_tokens), qp, qs,
+        _on(cu_tokens, "cu_tokens", at, T.i32, pages.B + 1), _on(table, "table", at, T.i32, pages.slabs * pages.max_pages),
+        _on(len, "len", at, T.i32, pages.slabs), _on(Kp, "Kp", at, T.e4m3, pool), _on(Vp, "Vp", at, T.e4m3, pool), ksp, vsp,
+        1 if causal else 0, scale, _on(out, "out", at, (q.dtype,), tokens * pages.H * 128), wp, wb, _word(status, at), queue),
+        "dkv_quant_attn")
