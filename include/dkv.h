@@ -672,14 +672,17 @@ dkv_status dkv_quant_compact(const dkv_pages* pages, const dkv_plan* plan, const
  * the rows of the new tokens are in them already, from dkv_rope_append or dkv_quant_compact).
  *
  * max_tokens  the most tokens that one sequence brings, or <= 0: num_tokens. A sequence that brings
- *             more is skipped: its outputs are not written and DKV_DEV_PAGE_RANGE is set. Small
- *             numbers save a launch.
+ *             more is skipped: its outputs are not written and DKV_DEV_PAGE_RANGE is set. With
+ *             max_tokens * H / H_kv <= 16 a launch is saved.
  * Kp, Vp, Ks, Vs  are read only.
- * out         as for dkv_chunk_attn. Scores, softmax statistics and sums are fp32. The e4m3 values and q
- *             (scaled by a power of two a row) enter the products as fp16, which holds them exactly but for
- *             elements of q below 2^-28 of the row's largest; softmax weights, times V's scales, are rounded to
- *             fp16, whose least step is at most 2^-30 of the largest such product of the row; the output is rounded once.
- * workspace   dkv_quant_workspace_bytes(pages) bytes (-1: a bad geometry).
+ * out         as for dkv_chunk_attn. Scores, softmax statistics and sums are fp32, the output is rounded
+ *             once. Sequences of at most 16 tokens x H / H_kv: q (scaled by a power of two a row) enters the
+ *             products as fp16, exactly but for elements below 2^-28 of the row's largest; weights,
+ *             times their rows' V scales, are rounded to fp16, with a least step of 2^-30 of the largest such
+ *             product. Others: each row of K and V enters the products in dtype, which holds a
+ *             bf16 one exactly, an fp16 one to 2^-24 (scale bytes up to 135, 2^8, as rows of fp16
+ *             values have them; larger elements than 2^17 are infinite); weights are rounded to dtype.
+ * workspace   dkv_quant_workspace_bytes(pages) bytes (-1: a bad geometry), about 46 MB.
  * Other arguments, what is promised and errors are those of dkv_chunk_attn.
  */
 int64_t dkv_quant_workspace_bytes(const dkv_pages* pages);

@@ -45,7 +45,7 @@
 // Every wait is bounded (polls and 2 s), and so are the softmax warps' meetings (Waits::meet); one
 // that runs out sets DKV_DEV_TMA_TIMEOUT, the roles leave, copies and products in flight are
 // drained, and the outputs of the CTA's unfinished units stay unwritten.
-#include "dkv_pages.cuh"
+#include "dkv_quant.cuh"
 #include "dkv_tcgen05.cuh"
 
 #include <cuda_bf16.h>
@@ -60,26 +60,38 @@ namespace {
 constexpr int kTile = 128;                 // query rows and cache rows of a tile
 constexpr int kHalf = kTile * 128;         // one 64-dim half of a tile (16 KB)
 constexpr int kOperand = 2 * kHalf;        // a tile: dims 0-63, then 64-127
-constexpr int kStages = 5;                 // ring of K and V tiles
-constexpr int kThreads = 384;
-constexpr int kRegsSoft = 216, kRegsRest = 72;  // a thread's registers after the split; launched with 168
-static_assert(2 * kRegsSoft + kRegsRest <= 3 * 168, "three warpgroups share what they were launched with");
 constexpr int kSoft = 256;                 // threads of the softmax groups
-constexpr int kMaxCtas = 160;              // CTAs of the largest grid (the workspace's size)
+constexpr int kMaxCtas = kChunkCounters;    // CTAs of the largest grid (the workspace's size)
 constexpr int kPieceRows = 2 * kTile;      // rows of a piece in the workspace
 constexpr int kTmemCols = 512;             // S of group p at 128 p (P over its first half), O at 256 + 128 p
 
-// Shared memory, from its 1024-byte aligned start (there is no room to align it by hand).
-constexpr int kOffQ = 0;
-constexpr int kOffRing = kOffQ + 2 * kOperand;
-constexpr int kOffBars = kOffRing + kStages * kOperand;
 constexpr int kAhead = 4;                  // ring of unit descriptors
-constexpr int kNumBars = 2 * kStages + 3 * kAhead + 11;  // full[], empty[], said[], q_full[], late[], q_empty[2], s_full[2], p_half[2], p_full[2], o_done[2], fin
-constexpr int kOffMisc = kOffBars + (kNumBars + 1) / 2 * 16;  // int[4]: TMEM address, abort, last
-constexpr int kOffPieces = kOffMisc + 16;                      // Piece[kAhead]
-constexpr int kOffMl = kOffPieces + kAhead * 64;                           // float2[128]: group 1's (m, l), then group 0's
-constexpr int kSmemBytes = kOffMl + 2 * kTile * 8;
-static_assert(kSmemBytes <= 227 * 1024, "fits one CTA");
+constexpr int kPieceBytes = 48;
+
+// Shared memory, from its 1024-byte aligned start (there is no room to align it by hand), and threads. Q8: pools of
+// 8 bits, whose rows land in a ring of their own, `raw`, with their scale bytes; a warpgroup more turns them into the
+// 16-bit tiles of the ring that the products read.
+template <bool Q8>
+struct Lay {
+    static constexpr int kStages = Q8 ? 3 : 5;       // ring of K and V tiles
+    static constexpr int kRaw = Q8 ? 4 : 0;
+    static constexpr int kThreads = Q8 ? 512 : 384;
+    // A thread's registers after the split; launched with 128 or 168.
+    static constexpr int kRegsSoft = Q8 ? 208 : 216, kRegsRest = Q8 ? 48 : 72, kRegsConvert = Q8 ? 48 : 0;
+    static_assert(2 * kRegsSoft + kRegsRest + kRegsConvert <= (Q8 ? 4 * 128 : 3 * 168), "the warpgroups share what they were launched with");
+    static constexpr int kOffQ = 0;
+    static constexpr int kOffRing = kOffQ + 2 * kOperand;
+    static constexpr int kOffRaw = kOffRing + kStages * kOperand;
+    static constexpr int kOffScales = kOffRaw + kRaw * kHalf;
+    static constexpr int kOffBars = kOffScales + kRaw * kTile;
+    static constexpr int kNumBars = 2 * kStages + 2 * kRaw + 3 * kAhead + 11;  // full[], empty[], raw_full[], raw_empty[], said[], q_full[], late[], q_empty[2], s_full[2], p_half[2], p_full[2], o_done[2], fin
+    static constexpr int kOffMisc = kOffBars + (kNumBars + 1) / 2 * 16;       // int[4]: TMEM address, abort, last
+    static constexpr int kOffPieces = kOffMisc + 16;                           // Piece[kAhead]
+    static constexpr int kOffMl = kOffPieces + kAhead * kPieceBytes;           // float2[128]: group 1's (m, l), then group 0's
+    static constexpr int kSmemBytes = kOffMl + 2 * kTile * 8;
+    static constexpr int kMaxGroups = kStages * kOperand / 8;                  // prefix sums in the ring before its first use
+    static_assert(kSmemBytes <= 227 * 1024, "fits one CTA");
+};
 
 // Workspace.
 struct ChunkWork {
@@ -96,6 +108,14 @@ struct ChunkMaps {
 };
 
 __device__ __forceinline__ int cu_at(const ChunkArgs& a, int b) { return min(max(a.cu[b], 0), a.T); }
+
+// Tokens of sequence b that the kernel deals with.
+template <bool Q8>
+__device__ __forceinline__ int tokens_at(const ChunkArgs& a, int b)
+{
+    const int n = cu_at(a, b + 1) - cu_at(a, b);
+    return Q8 && (n < a.least || n > a.most) ? 0 : n;
+}
 
 // ---------------------------------------------------------------- units
 struct Unit {
@@ -141,6 +161,7 @@ constexpr int kPairCost = 3, kSplitCost = 2;
 
 // The share of one CTA, unit by unit. Units lie end to end on a line of costs; a tile is the
 // CTA's in whose part of the line it starts.
+template <bool Q8>
 struct Walk {
     int b, g, i, t, n, j0, j1, tiles;
     int64_t start, end;  // of the unit, of the share
@@ -169,9 +190,9 @@ struct Walk {
             if (++g == a.Hkv) {
                 g = 0;
                 do ++b;
-                while (b < a.B - 1 && cu_at(a, b + 1) <= cu_at(a, b));
+                while (b < a.B - 1 && tokens_at<Q8>(a, b) <= 0);
                 t = cu_at(a, b);
-                n = cu_at(a, b + 1) - t;
+                n = tokens_at<Q8>(a, b);
             }
         }
         enter(a, slab_len(a, b * a.Hkv + g), 0);
@@ -181,23 +202,24 @@ struct Walk {
 
 // What the other roles need of a CTA's part of a unit, described by the walking warp.
 struct alignas(16) Piece {
-    int t0, tokens, row0, len;  // as in Unit
-    int kv, h, g, j0;
-    int j1, flags, fresh, pad0;
-    int c0, pieces, pad1, pad2;  // CTAs c0 .. c0 + pieces - 1 hold the unit (written after the rest: `late`)
-    static constexpr int kPair = 1, kWhole = 2, kMore = 4;
+    int t0, row0, len, kv;  // as in Unit
+    int h, g, j0, j1;
+    int flags, fresh;       // flags: kPair, kWhole, kMore, and the tokens above kTokens
+    int c0, pieces;         // CTAs c0 .. c0 + pieces - 1 hold the unit (written after the rest: `late`)
+    static constexpr int kPair = 1, kWhole = 2, kMore = 4, kTokens = 8;
     __device__ __forceinline__ bool pair() const { return flags & kPair; }
     __device__ __forceinline__ bool whole() const { return flags & kWhole; }
     __device__ __forceinline__ bool more() const { return flags & kMore; }  // the CTA has a unit after this
+    __device__ __forceinline__ int tokens() const { return flags >> kTokens; }
     __device__ __forceinline__ int steps() const { return pair() ? 2 * (j1 - j0) : j1 - j0; }
     __device__ __forceinline__ int tile(int s) const { return j0 + (pair() ? s >> 1 : s); }
 };
-static_assert(sizeof(Piece) == 64, "four 16-byte words, of which read_piece reads three");
+static_assert(sizeof(Piece) == kPieceBytes, "three 16-byte words");
 
 __device__ __forceinline__ Piece read_piece(const unsigned char* at)
 {
     union {
-        uint4 u[4];
+        uint4 u[3];
         Piece p;
     } x;
 #pragma unroll
@@ -294,13 +316,12 @@ __global__ void __launch_bounds__(kAppThreads) chunk_append_kernel(const __grid_
 }
 
 // ---------------------------------------------------------------- schedule
-constexpr int kMaxGroups = kStages * kOperand / 8;  // prefix sums in the ring before its first use
-
 // Cost of a unit, and of slab h. any_pair is set if there is a pair unit.
 __device__ __forceinline__ int unit_cost(const Unit& u) { return u.tiles() * (kSplitCost + (int)u.pair); }
+template <bool Q8>
 __device__ __forceinline__ int64_t slab_cost(const ChunkArgs& a, int h, int& any_pair)
 {
-    const int b = h / a.Hkv, t = cu_at(a, b), n = cu_at(a, b + 1) - t, len = slab_len(a, h), TQ = kTile / a.G;
+    const int b = h / a.Hkv, t = cu_at(a, b), n = tokens_at<Q8>(a, b), len = slab_len(a, h), TQ = kTile / a.G;
     any_pair |= n > TQ;
     int64_t sum = 0;
 #pragma unroll 1
@@ -311,8 +332,10 @@ __device__ __forceinline__ int64_t slab_cost(const ChunkArgs& a, int h, int& any
 // All threads of the CTA: the cost of every slab (or group of slabs, where there are more than
 // fit), summed into `before`. Every CTA does it for itself, beside the append: as a kernel's
 // job in front of this one it was 2 us on the way of a small call.
+template <bool Q8>
 __device__ __forceinline__ Extent count_cost(const ChunkArgs& a, int64_t* before, int64_t* sums, int nctas, int& group)
 {
+    constexpr int kThreads = Lay<Q8>::kThreads, kMaxGroups = Lay<Q8>::kMaxGroups;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, slabs = a.B * a.Hkv;
     group = (slabs + kMaxGroups - 1) / kMaxGroups;
     const int groups = (slabs + group - 1) / group, per = (groups + kThreads - 1) / kThreads;
@@ -323,7 +346,7 @@ __device__ __forceinline__ Extent count_cost(const ChunkArgs& a, int64_t* before
     for (int x = g0; x < g1; ++x) {
         before[x] = mine;
 #pragma unroll 1
-        for (int h = x * group; h < min(slabs, (x + 1) * group); ++h) mine += slab_cost(a, h, any_pair);
+        for (int h = x * group; h < min(slabs, (x + 1) * group); ++h) mine += slab_cost<Q8>(a, h, any_pair);
     }
     int64_t up = mine;
 #pragma unroll
@@ -334,8 +357,8 @@ __device__ __forceinline__ Extent count_cost(const ChunkArgs& a, int64_t* before
     // Whether there is a pair unit, and whether the offsets are bad, goes along in the sums' upper bits (a
     // barrier that votes, instead, cost the whole kernel 5 %). The cost itself is below 2^52: at most 2^26
     // slabs' last units and 2^23 full ones, 2^24 tiles each.
-    constexpr int kFlag = 52, kBad = kFlag + 4;
-    static_assert(kThreads / 32 < 16, "a field of 4 bits counts the warps");
+    constexpr int kFlag = 52, kBad = kFlag + 5;
+    static_assert(kThreads / 32 < 32, "a field of 5 bits counts the warps");
     bool bad = false;
 #pragma unroll 1
     for (int b = tid; b < a.B; b += kThreads) bad |= bad_offsets(a, b);
@@ -349,7 +372,7 @@ __device__ __forceinline__ Extent count_cost(const ChunkArgs& a, int64_t* before
         total += sums[k];
     }
     const bool skip = total >> kBad;
-    const int dearest = (total >> kFlag) & 15 ? kPairCost : kSplitCost;
+    const int dearest = (total >> kFlag) & 31 ? kPairCost : kSplitCost;
     total &= ((int64_t)1 << kFlag) - 1;
 #pragma unroll 1
     for (int x = g0; x < g1; ++x) before[x] += base;
@@ -361,7 +384,8 @@ __device__ __forceinline__ Extent count_cost(const ChunkArgs& a, int64_t* before
 }
 
 // Where the share of CTA c (which has one) starts.
-__device__ __forceinline__ void seek(const ChunkArgs& a, const Extent& e, const int64_t* before, int group, int c, Walk& k)
+template <bool Q8>
+__device__ __forceinline__ void seek(const ChunkArgs& a, const Extent& e, const int64_t* before, int group, int c, Walk<Q8>& k)
 {
     const int64_t pos = share_start(e, c);
     k.end = share_start(e, c + 1);
@@ -376,11 +400,11 @@ __device__ __forceinline__ void seek(const ChunkArgs& a, const Extent& e, const 
     int64_t off = pos - before[lo];
     int h = lo * group, any = 0;
     if (group > 1)
-        for (int64_t x; off >= (x = slab_cost(a, h, any)); ++h) off -= x;
+        for (int64_t x; off >= (x = slab_cost<Q8>(a, h, any)); ++h) off -= x;
     k.b = h / a.Hkv;
     k.g = h - k.b * a.Hkv;
     k.t = cu_at(a, k.b);
-    k.n = cu_at(a, k.b + 1) - k.t;
+    k.n = tokens_at<Q8>(a, k.b);
     const int len = slab_len(a, h);
     k.i = 0;
 #pragma unroll 1
@@ -451,6 +475,18 @@ struct Waits {
     }
 };
 
+// Both 16-bit values of x times those of f.
+template <bool F16>
+__device__ __forceinline__ uint32_t scale2(uint32_t x, uint32_t f)
+{
+    uint32_t y;
+    if (F16)
+        asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(y) : "r"(x), "r"(f));
+    else
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(x), "r"(f));
+    return y;
+}
+
 template <bool F16>
 __device__ __forceinline__ uint32_t pack16(float lo, float hi)
 {
@@ -459,6 +495,111 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi)
         return *reinterpret_cast<const uint32_t*>(&x);
     }
     return pack_bf16(lo, hi);
+}
+
+// Row r of an 8-bit tile as a row of a 16-bit one, both as the copies' swizzle lays them out: value times 2^(u - 127) (half of
+// that in fp16, see kHalved). Every such value is one of the type, but for fp16 below 2^-23. bf16: the
+// exponent and fraction of a code, moved to their places, are the value times 2^-120, subnormal ones too; NaN codes are
+// looked for and written apart.
+template <bool F16>
+__device__ __forceinline__ void widen_row(const unsigned char* raw, uint32_t u, bool none, unsigned char* tile, int r)
+{
+    const int swz = r & 7;
+    // 2^(u - 128) or 2^(u - 7), as a product of two where one would pass the type's range.
+    uint32_t f1, f2;
+    bool two;
+    if (F16) {
+        const int e = (int)u - 113;  // biased by 15
+        const int e1 = min(max(e, 1), 30), e2 = min(e - e1 + 15, 30);
+        f1 = (uint32_t)e1 << 10;
+        f2 = e2 > 0 ? (uint32_t)e2 << 10 : e2 > -10 ? 1u << (9 + e2) : 0u;  // (subnormal, or none)
+        two = e1 != e;
+    } else {
+        const int e = (int)u + 120;  // biased by 127
+        const int e1 = min(e, 254), e2 = e - e1 + 127;
+        f1 = (uint32_t)e1 << 7;
+        f2 = (uint32_t)e2 << 7;
+        two = e1 != e;
+    }
+    f1 |= f1 << 16;
+    f2 |= f2 << 16;
+    two = __any_sync(kFull, two);
+    uint32_t nan = 0;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        uint4 x;
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
+                     : "r"(smem_u32(raw) + r * 128 + ((c ^ swz) << 4))
+                     : "memory");
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        uint32_t y[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (F16) {
+                widen_e4m3(w[i], y[2 * i], y[2 * i + 1]);
+            } else {
+                nan |= (w[i] & 0x7f7f7f7fu) + 0x01010101u;
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    const uint32_t p = __byte_perm(w[i], 0u, z ? 0x4342 : 0x4140);  // a code in the low byte of each half
+                    y[2 * i + z] = (p & 0x00800080u) * 240u + (p << 4);              // 0x80 16 + 0x80 240 = 0x8000
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            y[i] = scale2<F16>(y[i], f1);
+            if (two) y[i] = scale2<F16>(y[i], f2);
+            if (none) y[i] = 0;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            *reinterpret_cast<uint4*>(tile + (c >> 2) * kHalf + r * 128 + (((2 * (c & 3) + i) ^ swz) << 4)) =
+                make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+    }
+    if (!F16 && (nan & 0x80808080u) && !none) {
+#pragma unroll 1
+        for (int d = 0; d < kHeadDim; ++d)
+            if ((raw[r * 128 + (((d >> 4) ^ swz) << 4) + (d & 15)] & 0x7f) == 0x7f)
+                *reinterpret_cast<uint16_t*>(tile + (d >> 6) * kHalf + r * 128 + ((((d >> 3) & 7) ^ swz) << 4) + (d & 7) * 2) = 0x7fff;
+    }
+}
+
+// The converting warpgroup: thread r has row r of each tile, in the order of the copies.
+template <bool F16>
+__device__ __forceinline__ void convert(unsigned char* sm, uint64_t* full, uint64_t* empty, uint64_t* raw_full, uint64_t* raw_empty, uint64_t* said,
+                                        Waits& wait)
+{
+    using Y = Lay<true>;
+    const int r = threadIdx.x & 127, lane = threadIdx.x & 31;
+    int pos = 0, unit = 0;
+    Piece k;
+    do {
+        if (!wait(&said[unit % kAhead], (unit / kAhead) & 1)) break;
+        k = read_piece(sm + Y::kOffPieces + unit % kAhead * sizeof(Piece));
+        ++unit;
+        const int steps = k.steps();
+#pragma unroll 1
+        for (int x = -2; x < 2 * steps && wait.ok; ++x) {
+            const int s = x == -2 ? 0 : (x >> 1) + 2 * (x & 1);  // K(0), K(1), then V(s), K(s + 2)
+            if (s >= steps || (k.pair() && (s & 1))) continue;
+            const bool value = x >= 0 && !(x & 1);
+            const int from = pos % Y::kRaw, to = pos % Y::kStages;
+            if (!wait(&raw_full[from], (pos / Y::kRaw) & 1)) break;
+            if (pos >= Y::kStages && !wait(&empty[to], (pos / Y::kStages - 1) & 1)) break;
+            ++pos;
+            // Rows past the unit's last are zero in V's tiles: 0 NaN is NaN.
+            const bool none = value && r >= k.kv - k.tile(s) * kTile;
+            widen_row<F16>(sm + Y::kOffRaw + from * kHalf, sm[Y::kOffScales + from * kTile + r], none, sm + Y::kOffRing + to * kOperand, r);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(smem_u32(&raw_empty[from]));
+                mbar_arrive(smem_u32(&full[to]));
+            }
+        }
+    } while (wait.ok && k.more());
 }
 
 // Zeroes rows [first, 128) of a V tile (one warp).
@@ -619,8 +760,14 @@ __device__ __forceinline__ void store_piece(float4* at, const float (&v)[32])
     for (int k = 0; k < 8; ++k) __stcg(at + k * kPieceRows, make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]));
 }
 
-// 1 / l; a sum of 0 (no rows) gives 0, NaN stays.
-__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
+// 8-bit rows enter fp16 products at half their value, as fp16 ends at 2^16 and e4m3 values times the scale of a row of fp16
+// values at 448 2^8. (The scores' factor 2 is the host's.)
+template <bool F16, bool Q8>
+constexpr float kHalved = F16 && Q8 ? 0.5f : 1.f;
+
+// 1 / l, and what undoes kHalved in O; a sum of 0 (no rows) gives 0, NaN stays.
+template <bool F16, bool Q8>
+__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : (F16 && Q8 ? 2.f : 1.f) / l; }
 
 template <bool F16>
 __device__ __forceinline__ float2 widen(uint32_t u)
@@ -637,12 +784,40 @@ __device__ __forceinline__ int64_t pool_row(const ChunkArgs& a, int h, int r)
     return page < 0 || page >= a.num_pages ? -1 : (int64_t)page * a.P + r % a.P;
 }
 
+// Elements dim .. dim + 15 of a pool's row.
+template <bool F16, bool Q8>
+__device__ __forceinline__ void pool_values(const uint16_t* pool, const uint8_t* scales, int64_t row, int dim, float (&v)[16])
+{
+    if constexpr (Q8) {
+        const uint4 x = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(pool) + row * kHeadDim + dim);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        const float z = scale_of(scales[row]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t lo, hi;
+            widen_e4m3(w[e], lo, hi);
+            const float2 y0 = __half22float2(*reinterpret_cast<const __half2*>(&lo)), y1 = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+            v[4 * e] = y0.x * z;
+            v[4 * e + 1] = y0.y * z;
+            v[4 * e + 2] = y1.x * z;
+            v[4 * e + 3] = y1.y * z;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float2 y = widen<F16>(reinterpret_cast<const uint32_t*>(pool + row * kHeadDim + dim)[e]);
+            v[2 * e] = y.x;
+            v[2 * e + 1] = y.y;
+        }
+    }
+}
+
 // A value of V that is not finite, in a later token's row, spoils the rows of the same tile
 // that do not see it (0 NaN is NaN). Rows whose result is not finite (`odd`) and that have
 // such a value in a masked place, rows [lim, end), are computed again without the tensor cores:
 // o = sum over rows [first, lim) of 2^(s - mc) v, dims [d0, d0 + nd). Slow and rare: 4 rows at
 // once, 8 lanes and 16 dims a lane each.
-template <bool F16>
+template <bool F16, bool Q8>
 __device__ __forceinline__ void mend_rows(const ChunkArgs& a, int h, bool odd, int first, int lim, int end, float mc, float z,
                                           const uint16_t* q, uint16_t* out, float4* piece, int d0, int nd)
 {
@@ -665,11 +840,10 @@ __device__ __forceinline__ void mend_rows(const ChunkArgs& a, int h, bool odd, i
         for (int r = max(L, first) + (lane >> 3); r < end; r += 4) {
             const int64_t row = pool_row(a, h, r);
             if (row < 0 || !mine) continue;
+            float v[16];
+            pool_values<F16, Q8>(a.Vp, a.Vs, row, dim, v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float2 v = widen<F16>(reinterpret_cast<const uint32_t*>(a.Vp + row * kHeadDim + dim)[e]);
-                spoilt += 0.f * v.x + 0.f * v.y;
-            }
+            for (int e = 0; e < 16; ++e) spoilt += 0.f * v[e];
         }
         if (!__any_sync(kFull, spoilt != spoilt)) continue;
         float o[16];
@@ -681,23 +855,23 @@ __device__ __forceinline__ void mend_rows(const ChunkArgs& a, int h, bool odd, i
             const int r = r0 + (lane >> 3);
             const int64_t row = r < last ? pool_row(a, h, r) : -1;
             float s = 0.f;
-            if (row >= 0)
+            if (row >= 0) {
+                float k[16];
+                pool_values<F16, Q8>(a.Kp, a.Ks, row, dim, k);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float2 x = widen<F16>(reinterpret_cast<const uint32_t*>(q1 + dim)[e]);
-                    const float2 k = widen<F16>(reinterpret_cast<const uint32_t*>(a.Kp + row * kHeadDim + dim)[e]);
-                    s = fmaf(x.x, k.x, fmaf(x.y, k.y, s));
+                    s = fmaf(x.x, k[2 * e], fmaf(x.y, k[2 * e + 1], s));
                 }
+            }
 #pragma unroll
             for (int x = 4; x >= 1; x >>= 1) s += __shfl_xor_sync(kFull, s, x);
             if (row >= 0) {
-                const float p = ex2(fmaf(s, a.qscale, -m1));
+                const float p = ex2(fmaf(s * kHalved<F16, Q8>, a.qscale, -m1)) * kHalved<F16, Q8>;
+                float v[16];
+                pool_values<F16, Q8>(a.Vp, a.Vs, row, dim, v);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float2 v = widen<F16>(reinterpret_cast<const uint32_t*>(a.Vp + row * kHeadDim + dim)[e]);
-                    o[2 * e] = fmaf(p, v.x, o[2 * e]);
-                    o[2 * e + 1] = fmaf(p, v.y, o[2 * e + 1]);
-                }
+                for (int e = 0; e < 16; ++e) o[e] = fmaf(p, v[e], o[e]);
             }
         }
 #pragma unroll
@@ -763,7 +937,7 @@ __device__ __forceinline__ int64_t piece_at(int c0, int k) { return (int64_t)(c0
 
 // Joining a pair unit's few pieces, this CTA's (`own`) still in TMEM: the thread of each row adds the
 // others to it. The sums are those of join_items.
-template <bool F16>
+template <bool F16, bool Q8>
 __device__ __forceinline__ void join_own(const ChunkArgs& a, const ChunkWork& w, int c0, int pieces, int own, int prow, bool live, float2 mine,
                                          uint32_t o_at, uint16_t* out)
 {
@@ -777,7 +951,7 @@ __device__ __forceinline__ void join_own(const ChunkArgs& a, const ChunkWork& w,
     RowSum sum{-INFINITY, 0.f};
 #pragma unroll
     for (int k = 0; k < kFew; ++k) sum.add(ml[k], c);
-    const float z = inverse(sum.L);
+    const float z = inverse<F16, Q8>(sum.L);
 #pragma unroll 1
     for (int e = 0; e < kHeadDim / 32; ++e) {
         float acc[32];
@@ -876,7 +1050,7 @@ __device__ __forceinline__ void join_items(const ChunkArgs& a, const ChunkWork& 
 }
 
 // The last piece's CTA joins the pieces. `scale` (shared): each row's max and 1 / sum over them.
-template <bool F16>
+template <bool F16, bool Q8>
 __device__ __forceinline__ void join_pieces(const ChunkArgs& a, const ChunkWork& w, Waits& wait, float2* scale, int t0, int tokens, int g, int c0, int pieces)
 {
     const bool ok = in_bounds(t0 >= 0 && t0 + tokens <= a.T && tokens * a.G <= kPieceRows, a.status);
@@ -898,7 +1072,7 @@ __device__ __forceinline__ void join_pieces(const ChunkArgs& a, const ChunkWork&
         L = (L == 0.f ? 0.f : L * ex2((M - M1) * c)) + (L0 == 0.f ? 0.f : L0 * ex2((M0 - M1) * c));
         M = M1;
     }
-    if (x < rows && first == 0) scale[x] = make_float2(M, inverse(L));
+    if (x < rows && first == 0) scale[x] = make_float2(M, inverse<F16, Q8>(L));
     if (!wait.meet()) return;
     if (pieces <= 2)
         join_items<F16, 4, 2>(a, w, scale, t0, rows, g, c0, pieces);
@@ -908,8 +1082,8 @@ __device__ __forceinline__ void join_pieces(const ChunkArgs& a, const ChunkWork&
         join_items<F16, 1, 8>(a, w, scale, t0, rows, g, c0, pieces);
 }
 
-template <bool F16>
-__global__ void __launch_bounds__(kThreads, 1)
+template <bool F16, bool Q8>
+__global__ void __launch_bounds__(Lay<Q8>::kThreads, 1)
     chunk_attn_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkMaps maps, const __grid_constant__ ChunkWork w, int nctas)
 {
     extern __shared__ __align__(1024) unsigned char sm[];
@@ -917,9 +1091,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (threadIdx.x == 0) report(a, DKV_DEV_TMA_TIMEOUT);
         return;
     }
-    uint64_t* full = reinterpret_cast<uint64_t*>(sm + kOffBars);  // [kStages] the stage's rows landed
+    using Y = Lay<Q8>;
+    constexpr int kStages = Y::kStages, kOffQ = Y::kOffQ, kOffRing = Y::kOffRing, kOffPieces = Y::kOffPieces;
+    uint64_t* full = reinterpret_cast<uint64_t*>(sm + Y::kOffBars);  // [kStages] the stage's rows landed (Q8: are converted)
     uint64_t* empty = full + kStages;                              // [kStages] its products are done
-    uint64_t* said = empty + kStages;                              // [kAhead] the unit is described
+    uint64_t* raw_full = empty + kStages;                          // [kRaw] 8-bit rows and their scales landed
+    uint64_t* raw_empty = raw_full + Y::kRaw;                      // [kRaw] they are converted
+    uint64_t* said = raw_empty + Y::kRaw;                          // [kAhead] the unit is described
     uint64_t* q_full = said + kAhead;                              // [kAhead] its Q landed
     uint64_t* late = q_full + kAhead;                              // [kAhead] the unit's CTAs are described
     uint64_t* q_empty = late + kAhead;                             // [2] the unit's score products are done
@@ -928,18 +1106,21 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint64_t* p_full = p_half + 2;                                 // [2] all of it
     uint64_t* o_done = p_full + 2;                                 // [2] the group's last product of the unit is done
     uint64_t* fin = o_done + 2;                                    // drain after a timeout
-    volatile int* misc = reinterpret_cast<volatile int*>(sm + kOffMisc);
-    float2* sh_ml = reinterpret_cast<float2*>(sm + kOffMl);        // [2][128]
+    volatile int* misc = reinterpret_cast<volatile int*>(sm + Y::kOffMisc);
+    float2* sh_ml = reinterpret_cast<float2*>(sm + Y::kOffMl);        // [2][128]
 
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31, c = blockIdx.x;
     if (warp == 8) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(sm + kOffMisc)),
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(sm + Y::kOffMisc)),
                      "r"(kTmemCols));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     if (tid == 0) {
         misc[1] = 0;
-        for (int i = 0; i < kNumBars; ++i) mbar_init(smem_u32(full + i), full + i >= p_half && full + i < p_full + 2 ? 4 : 1);
+        for (int i = 0; i < Y::kNumBars; ++i) {
+            const bool by_warps = (full + i >= p_half && full + i < p_full + 2) || (Q8 && (i < kStages || (full + i >= raw_empty && full + i < said)));
+            mbar_init(smem_u32(full + i), by_warps ? 4 : 1);  // (a warpgroup's warps each arrive)
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_proxy_async_smem();
     }
@@ -949,20 +1130,27 @@ __global__ void __launch_bounds__(kThreads, 1)
     // instead took 145 us for the queries' 126, since a tile's page numbers lie in a line of L1). The appended rows and the
     // counters may not be read before pdl_wait().
     asm volatile("fence.acq_rel.gpu;" ::: "memory");
+    if (Q8) pdl_launch_dependents();  // to the kernel of the sequences with few tokens, which takes the SMs that are done
     int64_t* before = reinterpret_cast<int64_t*>(sm + kOffRing);
     int group;
     tc_fence_before();
-    const Extent head = count_cost(a, before, reinterpret_cast<int64_t*>(sm + kOffMl), nctas, group);
+    const Extent head = count_cost<Q8>(a, before, reinterpret_cast<int64_t*>(sm + Y::kOffMl), nctas, group);
     tc_fence_after();
     const uint32_t tmem = (uint32_t)uniform(misc[0]);
     const bool work = c < head.parts;
     Waits wait{misc + 1, a.status, true, false};
     const int TQ = kTile / a.G;
-    if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
+    if (Q8 && warp >= 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Y::kRegsConvert));
+    if (work) {
+        if constexpr (Q8)
+            convert<F16>(sm, full, empty, raw_full, raw_empty, said, wait);
+    }
+    } else if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Y::kRegsRest));
     if (work && warp == 10) {
         // ---------------------------------------------------------------- walk
-        Walk k;
+        Walk<Q8> k;
         seek(a, head, before, group, c, k);
         fence_proxy_async_smem();  // `before` lies in the ring, which the copies write next
         __syncwarp();
@@ -973,10 +1161,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             const bool whole = k.whole(), more = k.more();
             Piece* d = reinterpret_cast<Piece*>(sm + kOffPieces) + unit % kAhead;
             if (lane == 0) {
-                *reinterpret_cast<int4*>(&d->t0) = make_int4(k.u.t0, k.u.tokens, k.u.row0, k.u.len);
-                *reinterpret_cast<int4*>(&d->kv) = make_int4(k.u.kv, k.u.h, k.g, k.j0);
-                *reinterpret_cast<int4*>(&d->j1) = make_int4(
-                    k.j1, (k.u.pair ? Piece::kPair : 0) | (whole ? Piece::kWhole : 0) | (more ? Piece::kMore : 0), k.u.fresh, 0);
+                *reinterpret_cast<int4*>(&d->t0) = make_int4(k.u.t0, k.u.row0, k.u.len, k.u.kv);
+                *reinterpret_cast<int4*>(&d->h) = make_int4(k.u.h, k.g, k.j0, k.j1);
+                *reinterpret_cast<int2*>(&d->flags) = make_int2(
+                    (k.u.pair ? Piece::kPair : 0) | (whole ? Piece::kWhole : 0) | (more ? Piece::kMore : 0) | k.u.tokens << Piece::kTokens, k.u.fresh);
                 mbar_arrive(smem_u32(&said[unit % kAhead]));
             }
             const int c0 = whole ? c : cta_of(head, k.start), last = whole ? c : cta_of(head, k.start + (k.tiles - 1) * k.cost());
@@ -1002,10 +1190,30 @@ __global__ void __launch_bounds__(kThreads, 1)
                        : 0;
         };
         auto load = [&](const CUtensorMap* map, int j, int page) {
-            const int s = pos % kStages, np = pages_in(j);
+            constexpr int kRing = Q8 ? Y::kRaw : kStages;
+            const int s = pos % kRing, np = pages_in(j);
             const bool good = page >= 0 && page < a.num_pages;
             if (!good) report(a, DKV_DEV_PAGE_RANGE);
             const int y = (good ? page : a.num_pages) * a.P;  // behind the pool: zeros
+            if constexpr (Q8) {
+                if (pos >= kRing && !wait(&raw_empty[s], (pos / kRing - 1) & 1)) return;
+                const uint32_t bar = smem_u32(&raw_full[s]), dst = smem_u32(sm + Y::kOffRaw + s * kHalf), sc = smem_u32(sm + Y::kOffScales + s * kTile);
+                const int scaled = __popc(__ballot_sync(kFull, lane < np && good));  // (rows of zeros need no scale)
+                if (lane == 0) mbar_arrive_expect_tx(bar, np * a.P * kHeadDim + scaled * a.P);
+                __syncwarp();
+                uint64_t pol;
+                if (k.pair())
+                    asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol));
+                else
+                    pol = evict_first_policy();
+                if (lane < np) {
+                    tma_box(dst + lane * a.P * kHeadDim, map, 0, y, bar, pol);
+                    if (good) bulk_g2s(sc + lane * a.P, (map == &maps.cache.k ? a.Ks : a.Vs) + y, a.P, bar, pol);
+                }
+                __syncwarp();
+                ++pos;
+                return;
+            }
             if (!appended && (j + 1) * kTile > k.len - k.fresh) {
                 pdl_wait();
                 asm volatile("fence.proxy.async.global;" ::: "memory");  // the rows were written by ordinary stores
@@ -1060,7 +1268,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         } while (wait.ok && k.more());
         if (!wait.ok) {
             // Copies in flight land (or run out of time) before the CTA exits.
-            for (int x = max(0, pos - kStages); x < pos; ++x) land(&full[x % kStages], (x / kStages) & 1);
+            constexpr int kRing = Q8 ? Y::kRaw : kStages;
+            for (int x = max(0, pos - kRing); x < pos; ++x) land((Q8 ? raw_full : full) + x % kRing, (x / kRing) & 1);
             for (int x = max(0, unit - 2); x < unit; ++x) land(&q_full[x % kAhead], (x / kAhead) & 1);
         }
     } else if (work && warp == 8) {
@@ -1093,7 +1302,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         ++pos;
                         // Rows past the unit's last (another token's, or never written) are zeroed: 0 NaN is NaN.
                         const int valid = max(k.kv - k.tile(x) * kTile, 0);
-                        if (valid < kTile) zero_rows(sm + kOffRing + curV * kOperand, valid, lane);
+                        if (!Q8 && valid < kTile) zero_rows(sm + kOffRing + curV * kOperand, valid, lane);
                     }
                     if (!wait(&p_half[p], (phases >> p) & 1)) break;
                     tc_fence_after();
@@ -1147,7 +1356,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
     }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoft));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Y::kRegsSoft));
         if (work) {
         // ---------------------------------------------------------------- softmax groups
         const int p = warp >> 2, r = tid & 127;
@@ -1164,7 +1373,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int steps = k.steps();
             const bool pair = k.pair(), whole = k.whole();
             const int tok = token + (pair ? p * TQ : 0);
-            const bool live = token < TQ && tok < k.tokens && in_bounds(k.t0 >= 0 && k.t0 + tok < a.T && k.g * a.G + j < a.H, a.status);
+            const bool live = token < TQ && tok < k.tokens() && in_bounds(k.t0 >= 0 && k.t0 + tok < a.T && k.g * a.G + j < a.H, a.status);
             const int lim = !live ? 0x3fffffff : a.causal ? min(max(k.row0 + tok, 0), k.len) : k.len;
             const bool any = __any_sync(kFull, live);
             float m = -INFINITY, l = 0.f;
@@ -1216,7 +1425,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             float odd = 0.f;  // NaN if a result is not finite
             if (pair) {
                 if (any && !last) {
-                    const float z = inverse(l);
+                    const float z = inverse<F16, Q8>(l);
 #pragma unroll 1
                     for (int e = 0; e < 4; ++e) {
                         float v[32];
@@ -1227,7 +1436,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (live && !whole) store_piece(o_piece + 8 * e * kPieceRows, v);
                     }
                     if (__any_sync(kFull, hidden && odd != odd))
-                        mend_rows<F16>(a, k.h, hidden && odd != odd, first, lim, end, origin<F16>(m, cs), z, q, out, o_piece, 0, kHeadDim);
+                        mend_rows<F16, Q8>(a, k.h, hidden && odd != odd, first, lim, end, origin<F16>(m, cs), z, q, out, o_piece, 0, kHeadDim);
                     if (live && !whole) __stcg(w.ml + slot * kPieceRows + prow, make_float2(m, l));
                 }
             } else {
@@ -1239,7 +1448,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const float2 x = sh_ml[r], y = sh_ml[kTile + r];
                 const float M = fmaxf(x.x, y.x);
                 const float fx = x.x == -INFINITY ? 0.f : ex2((x.x - M) * cs), fy = y.x == -INFINITY ? 0.f : ex2((y.x - M) * cs);
-                const float L = x.y * fx + y.y * fy, z = inverse(L);
+                const float L = x.y * fx + y.y * fy, z = inverse<F16, Q8>(L);
                 const bool two = steps > 1;
                 if (any) {
 #pragma unroll 1
@@ -1256,7 +1465,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (live && !whole) store_piece(o_piece + 8 * e * kPieceRows, v);
                     }
                     if (__any_sync(kFull, hidden && odd != odd))
-                        mend_rows<F16>(a, k.h, hidden && odd != odd, first, lim, end, origin<F16>(M, cs), z, q, out, o_piece, 64 * p, 64);
+                        mend_rows<F16, Q8>(a, k.h, hidden && odd != odd, first, lim, end, origin<F16>(M, cs), z, q, out, o_piece, 64 * p, 64);
                     if (live && !whole && p == 0) __stcg(w.ml + slot * kPieceRows + prow, make_float2(M, L));
                 }
             }
@@ -1270,9 +1479,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!wait.meet()) break;
                 last = misc[2];
                 if (last) __threadfence();
-                if (last && !few) join_pieces<F16>(a, w, wait, sh_ml, k.t0, k.tokens, k.g, c0, pieces);
+                if (last && !few) join_pieces<F16, Q8>(a, w, wait, sh_ml, k.t0, k.tokens(), k.g, c0, pieces);
             }
-            if (few && last && any) join_own<F16>(a, w, c0, pieces, c - c0, prow, live, make_float2(m, l), o_at + p * kTile, out);
+            if (few && last && any) join_own<F16, Q8>(a, w, c0, pieces, c - c0, prow, live, make_float2(m, l), o_at + p * kTile, out);
             if (!pair || !whole) {
                 tc_fence_before();
                 if (!wait.meet()) break;  // O of the other group, sh_ml and misc[2] are read
@@ -1321,10 +1530,41 @@ cudaError_t make_q_map(const ChunkArgs& a, CUtensorMap* map)
                : cudaErrorInvalidValue;
 }
 
-template <bool F16>
+// 8-bit pools: a box is a page of rows of 128 bytes.
+cudaError_t make_byte_map(const ChunkArgs& a, const void* pool, bool short_boxes, CUtensorMap* map)
+{
+    PFN_cuTensorMapEncodeTiled_v12000 enc = encode_tiled();
+    if (!enc) return cudaErrorNotSupported;
+    const cuuint64_t dim[2] = {(cuuint64_t)kHeadDim, (cuuint64_t)a.num_pages * a.P};
+    const cuuint64_t stride[1] = {(cuuint64_t)kHeadDim};
+    const cuuint32_t box[2] = {(cuuint32_t)kHeadDim, (cuuint32_t)(short_boxes ? a.P / 2 : a.P)};
+    const cuuint32_t elem[2] = {1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(pool), dim, stride, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? cudaSuccess
+               : cudaErrorInvalidValue;
+}
+
+template <bool F16, bool Q8>
 cudaError_t launch_attn(const ChunkArgs& a, const ChunkMaps& maps, const ChunkWork& w, int nctas, cudaStream_t st)
 {
-    return launch_pdl(chunk_attn_kernel<F16>, nctas, kThreads, kSmemBytes, st, a, maps, w, nctas);
+    return launch_pdl(chunk_attn_kernel<F16, Q8>, nctas, Lay<Q8>::kThreads, Lay<Q8>::kSmemBytes, st, a, maps, w, nctas);
+}
+
+template <bool F16, bool Q8>
+cudaError_t setup_attn()
+{
+    return cudaFuncSetAttribute(chunk_attn_kernel<F16, Q8>, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay<Q8>::kSmemBytes);
+}
+
+ChunkWork carve(void* work)
+{
+    unsigned char* base = static_cast<unsigned char*>(work);
+    ChunkWork w;
+    w.done = reinterpret_cast<int32_t*>(base);
+    w.ml = reinterpret_cast<float2*>(base + kOffPieceMl);
+    w.o = reinterpret_cast<float4*>(base + kOffPieceO);
+    return w;
 }
 
 }  // namespace
@@ -1333,8 +1573,10 @@ int64_t chunk_workspace_bytes() { return kWorkBytes; }
 
 cudaError_t chunk_setup()
 {
-    cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(chunk_attn_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    cudaError_t e = setup_attn<false, false>();
+    if (e == cudaSuccess) e = setup_attn<true, false>();
+    if (e == cudaSuccess) e = setup_attn<false, true>();
+    if (e == cudaSuccess) e = setup_attn<true, true>();
     return e;
 }
 
@@ -1347,15 +1589,22 @@ cudaError_t launch_chunk(const ChunkArgs& a, bool short_boxes, cudaStream_t st)
     ChunkMaps maps;
     if ((e = make_cache_maps(a.Kp, a.Vp, (int64_t)a.num_pages * a.P, &maps.cache, short_boxes, a.P, false)) != cudaSuccess) return e;
     if ((e = make_q_map(a, &maps.q)) != cudaSuccess) return e;
-    unsigned char* base = static_cast<unsigned char*>(a.work);
-    ChunkWork w;
-    w.done = reinterpret_cast<int32_t*>(base);
-    w.ml = reinterpret_cast<float2*>(base + kOffPieceMl);
-    w.o = reinterpret_cast<float4*>(base + kOffPieceO);
+    const ChunkWork w = carve(a.work);
     const int64_t rows = a.k_new ? (int64_t)a.T * a.Hkv : 0;
     const int blocks = 1 + (int)((rows + kAppThreads / 16 - 1) / (kAppThreads / 16));
     if ((e = launch_pdl(chunk_append_kernel, blocks, kAppThreads, 0, st, a, w)) != cudaSuccess) return e;
-    return a.fp16 ? launch_attn<true>(a, maps, w, nctas, st) : launch_attn<false>(a, maps, w, nctas, st);
+    return a.fp16 ? launch_attn<true, false>(a, maps, w, nctas, st) : launch_attn<false, false>(a, maps, w, nctas, st);
+}
+
+cudaError_t launch_chunk8(const ChunkArgs& a, int nctas, bool short_boxes, cudaStream_t st)
+{
+    cudaError_t e;
+    ChunkMaps maps;
+    if ((e = make_byte_map(a, a.Kp, short_boxes, &maps.cache.k)) != cudaSuccess) return e;
+    if ((e = make_byte_map(a, a.Vp, short_boxes, &maps.cache.v)) != cudaSuccess) return e;
+    if ((e = make_q_map(a, &maps.q)) != cudaSuccess) return e;
+    const ChunkWork w = carve(a.work);
+    return a.fp16 ? launch_attn<true, true>(a, maps, w, nctas, st) : launch_attn<false, true>(a, maps, w, nctas, st);
 }
 
 }  // namespace dkv

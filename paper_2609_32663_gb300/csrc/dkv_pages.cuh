@@ -93,8 +93,13 @@ struct ChunkArgs {
     int T, B, H, Hkv, G, P, num_pages, max_pages;
     int causal, fp16;
     float qscale;           // softmax scale * log2(e)
+    // 8-bit pools (launch_chunk8; Kp and Vp are bytes then, k_new and v_new null):
+    const uint8_t* Ks;
+    const uint8_t* Vs;
+    int least, most;        // a sequence with fewer or more tokens is left out
 };
 int64_t chunk_workspace_bytes();
+constexpr int kChunkCounters = 160;  // int32 words at the start of its workspace
 cudaError_t chunk_setup();  // the kernels' attributes in the current context
 // SMs of the current device; the kernels' attributes are set once a context (a lock and a
 // look-up, where the runtime calls take microseconds).
@@ -102,5 +107,7 @@ cudaError_t page_setup(int* sms);
 // short_boxes (fault injection): page copies deliver half the bytes that a stage expects,
 // inside the stage, so that every wait for them runs out.
 cudaError_t launch_chunk(const ChunkArgs& a, bool short_boxes, cudaStream_t st);
+// The same over 8-bit pools, after a kernel that signals early and clears the counters.
+cudaError_t launch_chunk8(const ChunkArgs& a, int nctas, bool short_boxes, cudaStream_t st);
 
 }  // namespace dkv

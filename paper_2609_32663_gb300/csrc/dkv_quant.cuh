@@ -50,7 +50,7 @@ struct QuantAttnArgs {
     int32_t* status;
     void* work;
     int T, B, H, Hkv, G, P, num_pages, max_pages;
-    int most;               // tokens of a sequence, at most
+    int most, few;          // tokens of a sequence, at most; of one that quant_attn_kernel deals with
     int causal, fp16;
     float qscale;           // softmax scale * log2(e)
 };
@@ -96,6 +96,17 @@ __device__ __forceinline__ uint32_t pack_e4m3(float x0, float x1, float x2, floa
         : "=r"(v)
         : "f"(x0), "f"(x1), "f"(x2), "f"(x3));
     return v;
+}
+
+// The four e4m3 values of a word as fp16 pairs.
+__device__ __forceinline__ void widen_e4m3(uint32_t w, uint32_t& lo, uint32_t& hi)
+{
+    asm("{\n\t.reg .b16 l, h;\n\t"
+        "mov.b32 {l, h}, %2;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %0, l;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+        : "=r"(lo), "=r"(hi)
+        : "r"(w));
 }
 
 }  // namespace

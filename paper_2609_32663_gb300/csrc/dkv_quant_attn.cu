@@ -62,9 +62,11 @@ struct QuantWork {
     int32_t* done;  // [kMaxCtas] finished pieces of the unit that starts in CTA c and ends in a later one
     State* state;   // [kMaxCtas][2][16]
     float4* o;      // [kMaxCtas][2][16][32]
+    int32_t* chunk; // the workspace of the kernel of many tokens, its counters first
 };
 constexpr int64_t kOffState = (kMaxCtas * 4 + 255) / 256 * 256, kOffO = kOffState + (int64_t)kMaxCtas * 2 * kCols * sizeof(State),
                   kWorkBytes = kOffO + (int64_t)kMaxCtas * 2 * kCols * kHeadDim * 4;
+static_assert(kWorkBytes % 256 == 0, "the other kernel's workspace lies behind it");
 
 __device__ __forceinline__ void report(const QuantAttnArgs& a, int bits)
 {
@@ -79,11 +81,11 @@ __device__ __forceinline__ bool bad_offsets(const QuantAttnArgs& a, int b)
     return t1 < t0 || t1 > a.T || (b == 0 && t0 != 0);
 }
 
-// Tokens of sequence b that this call deals with.
+// Tokens of sequence b that quant_attn_kernel deals with.
 __device__ __forceinline__ int tokens_of(const QuantAttnArgs& a, int b)
 {
     const int n = cu_at(a, b + 1) - cu_at(a, b);
-    return n > a.most ? 0 : n;
+    return n > a.few ? 0 : n;
 }
 
 // Rows of slab h; none if its length is out of range.
@@ -111,10 +113,13 @@ __global__ void __launch_bounds__(512) quant_begin_kernel(const __grid_constant_
     pdl_wait();
     pdl_launch_dependents();
     if (tid < kMaxCtas) w.done[tid] = 0;
-    static_assert(kMaxSlots <= 512, "a thread each");
+    if (tid < kChunkCounters) w.chunk[tid] = 0;
+    static_assert(kMaxSlots <= 512 && kChunkCounters <= 512, "a thread each");
     if (tid < a.B && (bad_offsets(a, tid) || cu_at(a, tid + 1) - cu_at(a, tid) > a.most)) report(a, DKV_DEV_PAGE_RANGE);
-    for (int h = tid; h < a.B * a.Hkv; h += 512)
-        if (tokens_of(a, h / a.Hkv) > 0 && a.len[h] != slab_len(a, h)) report(a, DKV_DEV_PAGE_RANGE);
+    for (int h = tid; h < a.B * a.Hkv; h += 512) {
+        const int b = h / a.Hkv;
+        if (cu_at(a, b + 1) > cu_at(a, b) && a.len[h] != slab_len(a, h)) report(a, DKV_DEV_PAGE_RANGE);
+    }
 }
 
 // ---------------------------------------------------------------- schedule
@@ -245,17 +250,6 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&x)[4], uint3
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(y0), "r"(y1));
-}
-
-// The four e4m3 values of a word as fp16 pairs.
-__device__ __forceinline__ void widen_e4m3(uint32_t w, uint32_t& lo, uint32_t& hi)
-{
-    asm("{\n\t.reg .b16 l, h;\n\t"
-        "mov.b32 {l, h}, %2;\n\t"
-        "cvt.rn.f16x2.e4m3x2 %0, l;\n\t"
-        "cvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
-        : "=r"(lo), "=r"(hi)
-        : "r"(w));
 }
 
 __device__ __forceinline__ uint32_t half2_of(float x, float y)
@@ -723,7 +717,7 @@ cudaError_t make_pool_map(const QuantAttnArgs& a, const uint8_t* pool, bool shor
 
 }  // namespace
 
-int64_t quant_workspace_bytes() { return kWorkBytes; }
+int64_t quant_workspace_bytes() { return kWorkBytes + chunk_workspace_bytes(); }
 
 cudaError_t quant_setup()
 {
@@ -746,9 +740,41 @@ cudaError_t launch_quant_attn(const QuantAttnArgs& a, bool short_boxes, cudaStre
     w.done = reinterpret_cast<int32_t*>(base);
     w.state = reinterpret_cast<State*>(base + kOffState);
     w.o = reinterpret_cast<float4*>(base + kOffO);
-    if ((e = launch_pdl(quant_begin_kernel, 1, 512, 0, st, a, w)) != cudaSuccess) return e;
-    return a.fp16 ? launch_pdl(quant_attn_kernel<true>, nctas, kThreads, kSmemBytes, st, a, maps, w, nctas)
-                  : launch_pdl(quant_attn_kernel<false>, nctas, kThreads, kSmemBytes, st, a, maps, w, nctas);
+    w.chunk = reinterpret_cast<int32_t*>(base + kWorkBytes);
+    QuantAttnArgs few = a;
+    few.few = std::min(a.most, kCols / a.G);
+    if ((e = launch_pdl(quant_begin_kernel, 1, 512, 0, st, few, w)) != cudaSuccess) return e;
+    if (a.most > few.few) {
+        ChunkArgs c{};
+        c.q = a.q;
+        c.q_stride = a.q_stride;
+        c.cu = a.cu;
+        c.table = a.table;
+        c.len = a.len;
+        c.Kp = reinterpret_cast<uint16_t*>(const_cast<uint8_t*>(a.Kp));
+        c.Vp = reinterpret_cast<uint16_t*>(const_cast<uint8_t*>(a.Vp));
+        c.out = a.out;
+        c.status = a.status;
+        c.work = w.chunk;
+        c.T = a.T;
+        c.B = a.B;
+        c.H = a.H;
+        c.Hkv = a.Hkv;
+        c.G = a.G;
+        c.P = a.P;
+        c.num_pages = a.num_pages;
+        c.max_pages = a.max_pages;
+        c.causal = a.causal;
+        c.fp16 = a.fp16;
+        c.qscale = a.fp16 ? 2 * a.qscale : a.qscale;  // (fp16 keys enter at half their value)
+        c.Ks = a.Ks;
+        c.Vs = a.Vs;
+        c.least = few.few + 1;
+        c.most = a.most;
+        if ((e = launch_chunk8(c, nctas, short_boxes, st)) != cudaSuccess) return e;
+    }
+    return a.fp16 ? launch_pdl(quant_attn_kernel<true>, nctas, kThreads, kSmemBytes, st, few, maps, w, nctas)
+                  : launch_pdl(quant_attn_kernel<false>, nctas, kThreads, kSmemBytes, st, few, maps, w, nctas);
 }
 
 }  // namespace dkv

@@ -92,14 +92,23 @@ def attention(c8, layer, q, cu, causal=True, scale=None):
     return out, size
 
 
-def assert_attention(got, want, size, dtype, what=""):
-    """Each output is rounded once, u |o|; each weight, times its row's V scale, to fp16: 2^-11 sum w|v|, or half of its least
-    step, 2^-31 of the largest such product (below 1e-6 of sum w|v| for the inputs here). Scores are 32-bit sums of 128
-    products, |error| <= 128 2^-24 sum|q k| scale < 2e-4 for the standard normal inputs here (sum |q k| scale < 25), which
-    moves a weight by twice that."""
+def weight_rounding(tokens, G, dtype, rows):
+    """Half a step of a softmax weight, relative, for each of `rows` tokens: 2^-11 (fp16) where a sequence's tokens x G are at most
+    16, else that of the call's type."""
+    few = np.repeat([n * G <= 16 for n in tokens], tokens)
+    u = np.full(rows, torch.finfo(dtype).eps / 2)
+    u[:few.size][few] = 2.0 ** -11
+    return torch.from_numpy(u)[:, None, None]
+
+
+def assert_attention(got, want, size, dtype, what="", weights=None):
+    """Each output is rounded once, u |o|, and so is each weight (`weights`, relative; a sequence of few tokens has them
+    times their rows' V scales, in fp16): weights sum w|v|, or half of fp16's least step, 2^-31 of the largest such product (below
+    1e-6 of sum w|v| for the inputs here). Scores are 32-bit sums of 128 products, |error| <= 128 2^-24 sum|q k| scale < 2e-4 for
+    the standard normal inputs here (sum |q k| scale < 25), which moves a weight by twice that."""
     u = torch.finfo(dtype).eps / 2
     got = got.double().cpu()
-    bound = u * want.abs() * (1 + 1e-3) + (2.0 ** -11 + 4e-4) * size + 1e-30
+    bound = u * want.abs() * (1 + 1e-3) + ((u if weights is None else weights) + 4e-4) * size + 1e-30
     finite = torch.isfinite(want)
     assert torch.equal(torch.isnan(got), torch.isnan(want)), f"{what}: NaN in other places"
     assert torch.equal(got[~finite & ~torch.isnan(want)], want[~finite & ~torch.isnan(want)]), what
