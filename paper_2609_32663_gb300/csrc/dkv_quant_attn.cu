@@ -33,28 +33,41 @@
 namespace dkv {
 namespace {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = 32 * kWarps;
-constexpr int kCols = 16;                  // columns of a unit
+#ifndef QW
+#define QW 12
+#endif
+#ifndef QLEAST
+#define QLEAST 8
+#endif
+constexpr int kMostCols = 16;              // columns of a unit, at most
 constexpr int kRows = 32;                  // cache rows of a tile
 constexpr int kTileBytes = kRows * kHeadDim;
-constexpr int kStages = 3;                 // ring of a warp
+constexpr int kStageBytes = 2 * kTileBytes;  // K, then V
 constexpr int kMaxCtas = 160;              // CTAs of the largest grid (the workspace's size)
 constexpr float kShift = 7.f;              // weights for the second product are 2^7 larger: fp16 has 2^15 above the slack
 
-// Shared memory, from its 1024-byte aligned start.
-constexpr int kStageBytes = 2 * kTileBytes;                            // K, then V
-constexpr int kOffSum = kWarps * kStages * kStageBytes;                // float[kWarps][16][64], before that State[kWarps][16]
-constexpr int kOffScales = kOffSum + kWarps * kCols * 64 * 4;          // a stage's scale bytes: of K, of V
-constexpr int kOffBars = kOffScales + kWarps * kStages * 2 * kRows;
-constexpr int kOffMisc = kOffBars + kWarps * kStages * 8;              // int[4]: abort, last
-constexpr int kSmemBytes = kOffMisc + 16;
-static_assert(kSmemBytes <= 227 * 1024, "fits one CTA");
-constexpr int kMaxGroups = kOffSum / 8;    // prefix sums in the rings before their first use
+// Z: 8-column halves of a unit's columns. One half takes half of the registers, so a CTA has more warps.
+template <int Z>
+struct Cfg {
+    static constexpr int kCols = 8 * Z;
+    static constexpr int kWarps = Z == 1 ? QW : 8;
+    static constexpr int kThreads = 32 * kWarps;
+    static constexpr int kStages = Z == 1 && QW > 8 ? 2 : 3;  // ring of a warp
+    // Shared memory, from its 1024-byte aligned start.
+    static constexpr int kOffSum = kWarps * kStages * kStageBytes;            // float[kWarps][kCols][64], before that State[kWarps][kCols]
+    static constexpr int kOffScales = kOffSum + kWarps * kCols * 64 * 4;      // a stage's scale bytes: of K, of V
+    static constexpr int kOffFactors = kOffScales + kWarps * kStages * 2 * kRows;  // uint32[kWarps][kRows]: a tile's scales
+    static constexpr int kOffBars = kOffFactors + kWarps * kRows * 4;
+    static constexpr int kOffMisc = kOffBars + kWarps * kStages * 8;          // int[4]: abort, last
+    static constexpr int kSmemBytes = kOffMisc + 16;
+    static constexpr int kMaxGroups = kOffSum / 8;                            // prefix sums in the rings before their first use
+    static_assert(kSmemBytes <= 227 * 1024, "fits one CTA");
+    static_assert(kOffBars % 8 == 0 && kOffScales % 16 == 0, "aligned");
+};
 
-// A column's softmax over some rows: max of x + ev, max of x, sum of 2^(x - top).
+// A column's softmax over some rows: max of x, sum of 2^(x - top), and the V scale (its exponent) that O goes by.
 struct State {
-    float reach, top, sum, pad;
+    float top, sum, scale, pad;
 };
 
 // Workspace.
@@ -64,8 +77,8 @@ struct QuantWork {
     float4* o;      // [kMaxCtas][2][16][32]
     int32_t* chunk; // the workspace of the kernel of many tokens, its counters first
 };
-constexpr int64_t kOffState = (kMaxCtas * 4 + 255) / 256 * 256, kOffO = kOffState + (int64_t)kMaxCtas * 2 * kCols * sizeof(State),
-                  kWorkBytes = kOffO + (int64_t)kMaxCtas * 2 * kCols * kHeadDim * 4;
+constexpr int64_t kOffState = (kMaxCtas * 4 + 255) / 256 * 256, kOffO = kOffState + (int64_t)kMaxCtas * 2 * kMostCols * sizeof(State),
+                  kWorkBytes = kOffO + (int64_t)kMaxCtas * 2 * kMostCols * kHeadDim * 4;
 static_assert(kWorkBytes % 256 == 0, "the other kernel's workspace lies behind it");
 
 __device__ __forceinline__ void report(const QuantAttnArgs& a, int bits)
@@ -98,12 +111,14 @@ __device__ __forceinline__ int slab_len(const QuantAttnArgs& a, int h)
 // Rows that token i of n sees.
 __device__ __forceinline__ int sees(const QuantAttnArgs& a, int len, int n, int i) { return a.causal ? min(max(len - n + i + 1, 0), len) : len; }
 
-__device__ __forceinline__ int blocks_of(const QuantAttnArgs& a, int n) { return (int)(((int64_t)n * a.G + kCols - 1) / kCols); }
+template <int Z>
+__device__ __forceinline__ int blocks_of(const QuantAttnArgs& a, int n) { return (int)(((int64_t)n * a.G + 8 * Z - 1) / (8 * Z)); }
 
 // Cache rows, and tiles, of block i of n tokens over a slab of len rows.
+template <int Z>
 __device__ __forceinline__ int block_rows(const QuantAttnArgs& a, int len, int n, int i)
 {
-    return sees(a, len, n, min(n, (int)((i * (int64_t)kCols + kCols - 1) / a.G + 1)) - 1);
+    return sees(a, len, n, min(n, (int)((i * (int64_t)(8 * Z) + 8 * Z - 1) / a.G + 1)) - 1);
 }
 __device__ __forceinline__ int tiles_of(int rows) { return max(1, (int)(((unsigned)rows + kRows - 1) / kRows)); }
 
@@ -123,15 +138,17 @@ __global__ void __launch_bounds__(512) quant_begin_kernel(const __grid_constant_
 }
 
 // ---------------------------------------------------------------- schedule
+template <int Z>
 __device__ __forceinline__ int64_t slab_tiles(const QuantAttnArgs& a, int h)
 {
     const int n = tokens_of(a, h / a.Hkv), len = slab_len(a, h);
     int64_t sum = 0;
 #pragma unroll 1
-    for (int i = 0, nb = blocks_of(a, n); i < nb; ++i) sum += tiles_of(block_rows(a, len, n, i));
+    for (int i = 0, nb = blocks_of<Z>(a, n); i < nb; ++i) sum += tiles_of(block_rows<Z>(a, len, n, i));
     return sum;
 }
 
+constexpr int kLeast = QLEAST;  // tiles of a share, where there are so many: its warps take them side by side
 struct Extent {
     int64_t tiles;
     int parts;
@@ -144,8 +161,10 @@ __device__ __forceinline__ int64_t share_start(const Extent& e, int c) { return 
 __device__ __forceinline__ int cta_of(const Extent& e, int64_t x) { return (int)divide((x + 1) * e.parts - 1, e.tiles); }
 
 // All threads of the CTA: the tiles before every slab (or group of slabs, where there are more than fit), into `before`.
+template <int Z>
 __device__ __forceinline__ Extent count_tiles(const QuantAttnArgs& a, int64_t* before, int64_t* sums, int nctas, int& group)
 {
+    constexpr int kMaxGroups = Cfg<Z>::kMaxGroups, kThreads = Cfg<Z>::kThreads, kWarps = Cfg<Z>::kWarps;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, slabs = a.B * a.Hkv;
     group = (slabs + kMaxGroups - 1) / kMaxGroups;
     const int groups = (slabs + group - 1) / group, per = (groups + kThreads - 1) / kThreads;
@@ -155,7 +174,7 @@ __device__ __forceinline__ Extent count_tiles(const QuantAttnArgs& a, int64_t* b
     for (int x = g0; x < g1; ++x) {
         before[x] = mine;
 #pragma unroll 1
-        for (int h = x * group; h < min(slabs, (x + 1) * group); ++h) mine += slab_tiles(a, h);
+        for (int h = x * group; h < min(slabs, (x + 1) * group); ++h) mine += slab_tiles<Z>(a, h);
     }
     int64_t up = mine;
 #pragma unroll
@@ -177,17 +196,18 @@ __device__ __forceinline__ Extent count_tiles(const QuantAttnArgs& a, int64_t* b
 #pragma unroll 1
     for (int x = g0; x < g1; ++x) before[x] += base;
     __syncthreads();
-    return bad ? Extent{0, 0} : Extent{total, (int)min((int64_t)nctas, total)};
+    return bad ? Extent{0, 0} : Extent{total, (int)min((int64_t)nctas, (total + kLeast - 1) / kLeast)};
 }
 
 // The share of one CTA, unit by unit.
+template <int Z>
 struct Walk {
     int b, g, i, t, n, len;    // sequence, head, block; the sequence's first token, its tokens, the slab's rows
     int rows, tiles, j0, j1;   // of the unit; the CTA's tiles of it
     int64_t start, end;        // of the unit, of the share
     __device__ __forceinline__ void enter(const QuantAttnArgs& a, int64_t off)
     {
-        rows = block_rows(a, len, n, i);
+        rows = block_rows<Z>(a, len, n, i);
         tiles = tiles_of(rows);
         j0 = (int)off;
         j1 = (int)min((int64_t)tiles, end - start);
@@ -201,7 +221,7 @@ struct Walk {
     __device__ __forceinline__ void next(const QuantAttnArgs& a)
     {
         start += tiles;
-        if (++i >= blocks_of(a, n)) {
+        if (++i >= blocks_of<Z>(a, n)) {
             i = 0;
             if (++g == a.Hkv) {
                 g = 0;
@@ -216,7 +236,8 @@ struct Walk {
     __device__ __forceinline__ bool whole() const { return j0 == 0 && j1 == tiles; }
 };
 
-__device__ __forceinline__ void seek(const QuantAttnArgs& a, const Extent& e, const int64_t* before, int group, int c, Walk& k)
+template <int Z>
+__device__ __forceinline__ void seek(const QuantAttnArgs& a, const Extent& e, const int64_t* before, int group, int c, Walk<Z>& k)
 {
     const int64_t pos = share_start(e, c);
     k.end = share_start(e, c + 1);
@@ -231,14 +252,14 @@ __device__ __forceinline__ void seek(const QuantAttnArgs& a, const Extent& e, co
     int64_t off = pos - before[lo];
     int h = lo * group;
     if (group > 1)
-        for (int64_t x; off >= (x = slab_tiles(a, h)); ++h) off -= x;
+        for (int64_t x; off >= (x = slab_tiles<Z>(a, h)); ++h) off -= x;
     k.b = h / a.Hkv;
     k.g = h - k.b * a.Hkv;
     k.sequence(a);
     k.len = slab_len(a, h);
     k.i = 0;
 #pragma unroll 1
-    for (int x; off >= (x = tiles_of(block_rows(a, k.len, k.n, k.i))); ++k.i) off -= x;
+    for (int x; off >= (x = tiles_of(block_rows<Z>(a, k.len, k.n, k.i))); ++k.i) off -= x;
     k.start = pos - off;
     k.enter(a, off);
 }
@@ -257,6 +278,9 @@ __device__ __forceinline__ uint32_t half2_of(float x, float y)
     const __half2 v = __floats2half2_rn(x, y);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
+
+// 2^x, 0 below 2^-126; x <= 127.
+__device__ __forceinline__ float exp2i(int x) { return __uint_as_float((uint32_t)max(x + 127, 0) << 23); }
 
 // Bytes of a word that are NaN, as 0xff.
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return __vcmpeq4(w & 0x7f7f7f7fu, 0x7f7f7f7fu); }
@@ -300,99 +324,143 @@ __device__ __forceinline__ void load_column(const uint16_t* src, bool live, uint
     for (int i = 0; i < 16; ++i) q[i] = half2_of(f[2 * i] * scale, f[2 * i + 1] * scale);
 }
 
-// What a lane has of its warp's columns lane / 4 and lane / 4 + 8.
+// An 8 x 8 matrix of 16-bit values, row lane / 4, columns 2 (lane % 4) and the next: transposed.
+__device__ __forceinline__ uint32_t transposed(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+// What a lane (g = lane / 4, t = lane % 4) has of its warp's columns 8 z + 2 t + e.
+template <int Z>
 struct Acc {
-    float o[16][4];               // dims 32 t + i and 32 t + 16 + i of the one column, then of the other (t = lane % 4)
-    float reach[2], top[2], l[2]; // l: of the lane's rows
+    float o[8][Z][4];         // dims 16 g + 2 i of columns e = 0, 1, then dims 16 g + 2 i + 1
+    float top[Z][2], l[Z][2]; // in units of 1 / cs; l: of the lane's rows
+    int scale;                // byte of the largest V scale so far, which O goes by
 };
 
 // One tile: scores, softmax, O += P V. lim: the tile's rows that the columns see; rows: those of the unit; `shown`: rows
 // that all columns see.
-__device__ __forceinline__ void tile_step(Acc& c, const uint32_t (&q)[2][16], const float (&cs)[2], const unsigned char* k, const unsigned char* v,
-                                          const unsigned char* scales, const int (&lim)[2], int shown, int rows)
+template <int Z>
+__device__ __forceinline__ void tile_step(Acc<Z>& c, const uint32_t (&q)[Z][16], const float (&cs)[Z][2], const unsigned char* k, const unsigned char* v,
+                                          const unsigned char* scales, uint32_t* factors, const int (&lim)[Z][2], int shown, int rows)
 {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    float s[4][4];
+    // A row a lane: its scales as factors. O goes by the largest V scale so far; where a larger one comes, it is
+    // brought to that.
+    {
+        const int ku = scales[lane], vu = lane < rows ? scales[kRows + lane] : 0;
+        if (__any_sync(kFull, vu > c.scale)) {
+            const int most = max(__reduce_max_sync(kFull, vu), c.scale);
+            const float down = exp2i(c.scale - most);
+            c.scale = most;
 #pragma unroll
-    for (int nt = 0; nt < 4; ++nt) {
+            for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
-        const unsigned char* row = k + (8 * nt + g) * kHeadDim;
+                for (int z = 0; z < Z; ++z)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint4 x = lds128(row + (((2 * t + i) ^ g) << 4));
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                    for (int e = 0; e < 4; ++e) c.o[i][z][e] *= down;
+        }
+        // (powers of two: the upper half of each has all of it)
+        factors[lane] = __float_as_uint(scale_of(ku)) | __float_as_uint(exp2i(vu - c.scale + (int)kShift)) >> 16;
+    }
+    // Rows 16 m + g and 16 m + g + 8 of columns 2 t and 2 t + 1.
+    float s[2][Z][4];
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                const int ks = 4 * i + y;  // dims 32 t + 4 ks .. + 3 of every t
-                uint32_t b0, b1;
-                widen_e4m3(w[y], b0, b1);
-                const uint32_t A[4] = {q[0][2 * ks], q[1][2 * ks], q[0][2 * ks + 1], q[1][2 * ks + 1]};
-                mma(s[nt], A, b0, b1);
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int z = 0; z < Z; ++z)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[m][z][e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint32_t w[4][4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const uint4 u = lds128(k + (8 * x + g) * kHeadDim + (((2 * t + i) ^ g) << 4));
+            w[x][0] = u.x;
+            w[x][1] = u.y;
+            w[x][2] = u.z;
+            w[x][3] = u.w;
+        }
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            const int ks = 4 * i + y;  // dims 32 t + 4 ks .. + 3 of every t
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                uint32_t A[4];
+                widen_e4m3(w[2 * m][y], A[0], A[2]);
+                widen_e4m3(w[2 * m + 1][y], A[1], A[3]);
+#pragma unroll
+                for (int z = 0; z < Z; ++z) mma(s[m][z], A, q[z][2 * ks], q[z][2 * ks + 1]);
             }
         }
     }
-    // Scores in units of the base-2 softmax, and with V's exponents.
-    float r[4][4];
+    const bool edge = shown < kRows;
+    __syncwarp();  // the factors are there
+    // Scores by their rows' scales; f: the rows' factors of their weights.
+    float f[4];
 #pragma unroll
-    for (int nt = 0; nt < 4; ++nt) {
-        const uint32_t ku = *reinterpret_cast<const uint16_t*>(scales + 8 * nt + 2 * t), vu = *reinterpret_cast<const uint16_t*>(scales + kRows + 8 * nt + 2 * t);
-        const float k0 = scale_of(ku & 255u), k1 = scale_of(ku >> 8);
-        const float v0 = (float)(vu & 255u) - 127.f, v1 = (float)(vu >> 8) - 127.f;
+    for (int x = 0; x < 4; ++x) {
+        const uint32_t u = factors[8 * x + g];
+        f[x] = __uint_as_float(u << 16);
+        const float kf = __uint_as_float(u & 0xffff0000u);
 #pragma unroll
-        for (int z = 0; z < 2; ++z) {
-            s[nt][2 * z] *= cs[z] * k0;
-            s[nt][2 * z + 1] *= cs[z] * k1;
-            r[nt][2 * z] = s[nt][2 * z] + v0;
-            r[nt][2 * z + 1] = s[nt][2 * z + 1] + v1;
+        for (int z = 0; z < Z; ++z)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) s[x >> 1][z][2 * (x & 1) + e] *= kf;
+    }
+    if (edge) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int z = 0; z < Z; ++z)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (8 * x + g >= lim[z][e]) s[x >> 1][z][2 * (x & 1) + e] = -INFINITY;  // also over NaN
+    }
+    // The maxima move only when a score tops them by 2^kSlack (they are then found over the lanes of a column).
+    float mx[Z][2];
+    bool any = false;
+#pragma unroll
+    for (int z = 0; z < Z; ++z)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            mx[z][e] = fmaxf(fmaxf(s[0][z][e], s[0][z][2 + e]), fmaxf(s[1][z][e], s[1][z][2 + e]));
+            any |= (mx[z][e] - c.top[z][e]) * cs[z][e] > kSlack;
+        }
+    if (__any_sync(kFull, any)) {
+#pragma unroll
+        for (int z = 0; z < Z; ++z) {
+            float alpha[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) mx[z][e] = fmaxf(mx[z][e], __shfl_xor_sync(kFull, mx[z][e], o));
+                const bool up = mx[z][e] > c.top[z][e];
+                alpha[e] = up ? ex2((c.top[z][e] - mx[z][e]) * cs[z][e]) : 1.f;
+                if (up) c.top[z][e] = mx[z][e];
+                c.l[z][e] *= alpha[e];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) c.o[i][z][e] *= alpha[e & 1];
         }
     }
-    if (shown < kRows) {
+    uint32_t p[4][Z];
 #pragma unroll
-        for (int nt = 0; nt < 4; ++nt)
+    for (int z = 0; z < Z; ++z) {
+        float top[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (8 * nt + 2 * t + (e & 1) >= lim[e >> 1]) s[nt][e] = r[nt][e] = -INFINITY;  // also over NaN
-    }
-    float mx[2], mr[2];
+        for (int e = 0; e < 2; ++e) top[e] = c.top[z][e] == -INFINITY ? 0.f : c.top[z][e] * cs[z][e];
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
-        mx[z] = mr[z] = -INFINITY;
-#pragma unroll
-        for (int nt = 0; nt < 4; ++nt) {
-            mx[z] = fmaxf(mx[z], fmaxf(s[nt][2 * z], s[nt][2 * z + 1]));
-            mr[z] = fmaxf(mr[z], fmaxf(r[nt][2 * z], r[nt][2 * z + 1]));
-        }
-#pragma unroll
-        for (int o = 1; o < 4; o <<= 1) {
-            mx[z] = fmaxf(mx[z], __shfl_xor_sync(kFull, mx[z], o));
-            mr[z] = fmaxf(mr[z], __shfl_xor_sync(kFull, mr[z], o));
-        }
-    }
-    // The maxima move only when a score tops them by 2^kSlack.
-    const bool up0 = mx[0] - c.top[0] > kSlack, up1 = mx[1] - c.top[1] > kSlack, out0 = mr[0] - c.reach[0] > kSlack, out1 = mr[1] - c.reach[1] > kSlack;
-    if (__any_sync(kFull, up0 || up1 || out0 || out1)) {
-        if (up0) c.l[0] *= ex2(c.top[0] - mx[0]), c.top[0] = mx[0];
-        if (up1) c.l[1] *= ex2(c.top[1] - mx[1]), c.top[1] = mx[1];
-        const float a0 = out0 ? ex2(c.reach[0] - mr[0]) : 1.f, a1 = out1 ? ex2(c.reach[1] - mr[1]) : 1.f;
-        if (out0) c.reach[0] = mr[0];
-        if (out1) c.reach[1] = mr[1];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            c.o[i][0] *= a0;
-            c.o[i][1] *= a0;
-            c.o[i][2] *= a1;
-            c.o[i][3] *= a1;
-        }
-    }
-    uint32_t p[2][4];
-#pragma unroll
-    for (int z = 0; z < 2; ++z) {
-        const float top = c.top[z] == -INFINITY ? 0.f : c.top[z], reach = (c.reach[z] == -INFINITY ? 0.f : c.reach[z]) - kShift;
-#pragma unroll
-        for (int nt = 0; nt < 4; ++nt) {
-            c.l[z] += ex2(s[nt][2 * z] - top) + ex2(s[nt][2 * z + 1] - top);
-            p[nt >> 1][2 * (nt & 1) + z] = half2_of(ex2(r[nt][2 * z] - reach), ex2(r[nt][2 * z + 1] - reach));
+        for (int x = 0; x < 4; ++x) {
+            const float w0 = ex2(fmaf(s[x >> 1][z][2 * (x & 1)], cs[z][0], -top[0])), w1 = ex2(fmaf(s[x >> 1][z][2 * (x & 1) + 1], cs[z][1], -top[1]));
+            c.l[z][0] += w0;
+            c.l[z][1] += w1;
+            p[x][z] = transposed(half2_of(w0 * f[x], w1 * f[x]));
         }
     }
     bool odd = false;  // NaN in a row of V that not all columns see
@@ -407,7 +475,7 @@ __device__ __forceinline__ void tile_step(Acc& c, const uint32_t (&q)[2][16], co
             w[x][1] = u.y;
             w[x][2] = u.z;
             w[x][3] = u.w;
-            if (shown < kRows && row >= shown) {  // 0 NaN is NaN
+            if (edge && row >= shown) {  // 0 NaN is NaN
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
                     const uint32_t bad = nan_bytes(w[x][y]);
@@ -417,36 +485,39 @@ __device__ __forceinline__ void tile_step(Acc& c, const uint32_t (&q)[2][16], co
             }
         }
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-            uint32_t b[4], d[4];
-            widen_e4m3(__byte_perm(w[0][y], w[1][y], 0x5140), b[0], b[1]);
-            widen_e4m3(__byte_perm(w[0][y], w[1][y], 0x7362), b[2], b[3]);
-            widen_e4m3(__byte_perm(w[2][y], w[3][y], 0x5140), d[0], d[1]);
-            widen_e4m3(__byte_perm(w[2][y], w[3][y], 0x7362), d[2], d[3]);
+        for (int y = 0; y < 4; ++y)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mma(c.o[4 * y + i], p[kb], b[i], d[i]);
-        }
+            for (int x = 0; x < 2; ++x) {  // dims 16 g + 4 y + 2 x and the next
+                uint32_t A[4];
+                widen_e4m3(__byte_perm(w[0][y], w[1][y], x ? 0x7362 : 0x5140), A[0], A[1]);
+                widen_e4m3(__byte_perm(w[2][y], w[3][y], x ? 0x7362 : 0x5140), A[2], A[3]);
+#pragma unroll
+                for (int z = 0; z < Z; ++z) mma(c.o[2 * y + x][z], A, p[2 * kb][z], p[2 * kb + 1][z]);
+            }
     }
-    if (shown < kRows && __any_sync(kFull, odd)) {
+    if (edge && __any_sync(kFull, odd)) {
         // The columns that do see such a row are NaN in its dims.
 #pragma unroll 1
         for (int row = max(shown, 0); row < min(rows, kRows); ++row)
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                const uint32_t code = v[row * kHeadDim + (((2 * t + (i >> 4)) ^ (row & 7)) << 4) + (i & 15)];
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t code = v[row * kHeadDim + ((g ^ (row & 7)) << 4) + i];
                 if ((code & 0x7fu) == 0x7fu) {
-                    if (row < lim[0]) c.o[i & 15][i >> 4] = __uint_as_float(0x7fffffffu);
-                    if (row < lim[1]) c.o[i & 15][2 + (i >> 4)] = __uint_as_float(0x7fffffffu);
+#pragma unroll
+                    for (int z = 0; z < Z; ++z)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            if (row < lim[z][e]) c.o[i >> 1][z][2 * (i & 1) + e] = __uint_as_float(0x7fffffffu);
                 }
             }
     }
 }
 
-// Factors that join states: that of O, 2^(reach - R), and that of the sum, 2^(top - M).
+// Factor that joins a state to others of this maximum; of its O besides 2^(scale - the largest scale).
 __device__ __forceinline__ float factor(float x, float most) { return x == -INFINITY ? 0.f : ex2(x - most); }
 
-// What turns O (relative to reach) into the output: 2^(reach - kShift - top) / sum; 0 for no rows.
-__device__ __forceinline__ float final_scale(float reach, float top, float sum) { return sum == 0.f ? 0.f : ex2(reach - kShift - top) / sum; }
+// What turns O into the output: 2^(scale - 127 - kShift) / sum; 0 for no rows. (A sum is at most 2^39 and the scale 2^120.)
+__device__ __forceinline__ float final_scale(float scale, float sum) { return sum == 0.f ? 0.f : ex2(scale - (127.f + kShift)) / sum; }
 
 template <bool F16>
 __device__ __forceinline__ uint2 pack4(float4 x, float z)
@@ -455,25 +526,30 @@ __device__ __forceinline__ uint2 pack4(float4 x, float z)
     return make_uint2(pack_bf16(x.x * z, x.y * z), pack_bf16(x.z * z, x.w * z));
 }
 
+__device__ __forceinline__ int bank_of(int t) { return (t & 1) | (t & 2) << 1; }
+
 // Where piece k of the unit that starts in CTA c0 lies.
 __device__ __forceinline__ int64_t piece_at(int c0, int k) { return (int64_t)(c0 + k) * 2 + (k == 0); }
 
-template <bool F16>
-__global__ void __launch_bounds__(kThreads, 1)
+template <bool F16, int Z>
+__global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
     quant_attn_kernel(const __grid_constant__ QuantAttnArgs a, const __grid_constant__ CacheMaps maps, const __grid_constant__ QuantWork w, int nctas)
 {
+    using C = Cfg<Z>;
+    constexpr int kWarps = C::kWarps, kStages = C::kStages, kCols = C::kCols;
     extern __shared__ __align__(1024) unsigned char sm[];
     if (smem_u32(sm) & 1023) {  // never: the swizzled tiles need it
         if (threadIdx.x == 0) report(a, DKV_DEV_TMA_TIMEOUT);
         return;
     }
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31, c = blockIdx.x, g = lane >> 2, t = lane & 3;
-    uint64_t* full = reinterpret_cast<uint64_t*>(sm + kOffBars) + warp * kStages;
-    volatile int* misc = reinterpret_cast<volatile int*>(sm + kOffMisc);
-    float* sums = reinterpret_cast<float*>(sm + kOffSum);
-    State* states = reinterpret_cast<State*>(sm + kOffSum);
+    uint64_t* full = reinterpret_cast<uint64_t*>(sm + C::kOffBars) + warp * kStages;
+    volatile int* misc = reinterpret_cast<volatile int*>(sm + C::kOffMisc);
+    float* sums = reinterpret_cast<float*>(sm + C::kOffSum);
+    State* states = reinterpret_cast<State*>(sm + C::kOffSum);
     unsigned char* ring = sm + warp * kStages * kStageBytes;
-    unsigned char* scales = sm + kOffScales + warp * kStages * 2 * kRows;
+    unsigned char* scales = sm + C::kOffScales + warp * kStages * 2 * kRows;
+    uint32_t* factors = reinterpret_cast<uint32_t*>(sm + C::kOffFactors) + warp * kRows;
     if (lane == 0)
         for (int s = 0; s < kStages; ++s) mbar_init(smem_u32(full + s), 1);
     if (tid == 0) misc[0] = 0;
@@ -481,165 +557,198 @@ __global__ void __launch_bounds__(kThreads, 1)
     // What the kernels before the begin kernel wrote may be read (it started after they had completed, and
     // this one after that); the fence drops what this SM's L1 holds from before. The counters may not, before pdl_wait().
     asm volatile("fence.acq_rel.gpu;" ::: "memory");
+    pdl_launch_dependents();
     int group;
-    const Extent head = count_tiles(a, reinterpret_cast<int64_t*>(sm), reinterpret_cast<int64_t*>(sm + kOffSum), nctas, group);
+    const Extent head = count_tiles<Z>(a, reinterpret_cast<int64_t*>(sm), reinterpret_cast<int64_t*>(sm + C::kOffSum), nctas, group);
     if (c < head.parts) {
-        Walk k;
+        Walk<Z> k;
         seek(a, head, reinterpret_cast<const int64_t*>(sm), group, c, k);
         fence_proxy_async_smem();  // the sums of tiles lie in the rings, which the copies write next
         __syncthreads();
-        Walk f = k;                 // ahead of k by the ring's stages
-        int fj = f.j0 + warp, fetched = 0, used = 0, page0 = 0, page1 = 0, ahead = 0;  // ahead: tiles of f since its pages were read
+        Walk<Z> f = k;              // ahead of k by the ring's stages
+        int fj = f.j0 + warp, stage = 0, used = 0, fetched = 0, rows0 = 0, rows1 = 0, ahead = 0;  // ahead: tiles of f since its pages were read
         bool left = true, ok = true;
         const uint64_t pol = evict_first_policy();
+        const int log_P = 31 - __clz(a.P), box = min(a.P, kRows);
+        // The next tile on its way. Each lane knows the pool rows of one of the next 32 tiles (of its two halves, where pages have
+        // 16 rows); a bad page's are behind the pool, from where zeros come.
         auto fetch = [&] {
-            while (left && fj >= f.j1) {
-                left = f.more();
-                if (left) {
-                    f.next(a);
-                    fj = f.j0 + warp;
-                    ahead = 0;
-                }
-            }
             if (!left) return;
-            const int h = f.b * a.Hkv + f.g;
+            while (fj >= f.j1) {
+                left = f.more();
+                if (!left) return;
+                f.next(a);
+                fj = f.j0 + warp;
+                ahead = 0;
+            }
             if ((ahead & 31) == 0) {
+                const int h = f.b * a.Hkv + f.g;
                 const int64_t row = ((int64_t)fj + (int64_t)kWarps * lane) * kRows;
                 const bool mine = row < f.rows && in_bounds(h >= 0 && h < a.B * a.Hkv && row / a.P < a.max_pages, a.status);
-                const int32_t* at = a.table + (int64_t)h * a.max_pages + (mine ? (int)row / a.P : 0);
-                page0 = mine ? at[0] : 0;
-                page1 = mine && a.P < kRows && row + a.P < f.rows ? at[1] : 0;
+                const bool second = mine && a.P < kRows && row + a.P < f.rows;
+                const int32_t* at = a.table + (int64_t)h * a.max_pages + (mine ? (int)row >> log_P : 0);
+                const int p0 = mine ? at[0] : 0, p1 = second ? at[1] : 0;
+                const bool bad0 = p0 < 0 || p0 >= a.num_pages, bad1 = p1 < 0 || p1 >= a.num_pages;
+                if (bad0 || bad1) report(a, DKV_DEV_PAGE_RANGE);
+                rows0 = bad0 ? -1 : (p0 << log_P) + ((int)row & (a.P - 1));
+                rows1 = bad1 ? -1 : p1 << log_P;
             }
-            const int p0 = __shfl_sync(kFull, page0, ahead & 31), p1 = __shfl_sync(kFull, page1, ahead & 31);
+            const int r0 = __shfl_sync(kFull, rows0, ahead & 31), r1 = __shfl_sync(kFull, rows1, ahead & 31);
             ++ahead;
-            const int s = fetched % kStages, rows = f.rows - fj * kRows, box = min(a.P, kRows);
+            const int rows = f.rows - fj * kRows, boxes = rows <= 0 ? 0 : a.P < kRows && rows > a.P ? 2 : 1;
+            fj += kWarps;
             ++fetched;
-            const int boxes = rows <= 0 ? 0 : a.P < kRows && rows > a.P ? 2 : 1;
-            __syncwarp();
             if (lane == 0) {
-                const uint32_t bar = smem_u32(full + s), dst = smem_u32(ring + s * kStageBytes);
-                unsigned char* sc = scales + s * 2 * kRows;
-                const bool good0 = p0 >= 0 && p0 < a.num_pages, good1 = p1 >= 0 && p1 < a.num_pages;
-                mbar_arrive_expect_tx(bar, boxes * 2 * box * kHeadDim + ((boxes > 0 && good0) + (boxes > 1 && good1)) * 2 * box);
+                const uint32_t bar = smem_u32(full + stage), dst = smem_u32(ring + stage * kStageBytes);
+                unsigned char* sc = scales + stage * 2 * kRows;
+                mbar_arrive_expect_tx(bar, boxes * 2 * box * kHeadDim + ((boxes > 0 && r0 >= 0) + (boxes > 1 && r1 >= 0)) * 2 * box);
+#pragma unroll 1
                 for (int x = 0; x < boxes; ++x) {
-                    const bool good = x ? good1 : good0;
-                    const int y = good ? (x ? p1 : p0) * a.P + (x ? 0 : fj * kRows % a.P) : a.num_pages * a.P;  // behind the pool: zeros
+                    const int r = x ? r1 : r0, y = r < 0 ? a.num_pages * a.P : r;
                     tma_box(dst + x * box * kHeadDim, &maps.k, 0, y, bar, pol);
                     tma_box(dst + kTileBytes + x * box * kHeadDim, &maps.v, 0, y, bar, pol);
-                    if (good) {
+                    if (r >= 0) {
                         bulk_g2s(smem_u32(sc) + x * box, a.Ks + y, box, bar, pol);
                         bulk_g2s(smem_u32(sc) + kRows + x * box, a.Vs + y, box, bar, pol);
                     } else {
-                        report(a, DKV_DEV_PAGE_RANGE);
-                        for (int i = 0; i < box; ++i) sc[x * box + i] = sc[kRows + x * box + i] = 127;
+                        for (int i = 0; i < box; ++i) sc[x * box + i] = sc[kRows + x * box + i] = 1;
                     }
                 }
             }
-            fj += kWarps;
+            stage = stage + 1 == kStages ? 0 : stage + 1;
             __syncwarp();
         };
         for (int s = 0; s < kStages; ++s) fetch();
+        int at_stage = 0;
+        uint32_t phases = 0;  // bit s: the parity of stage s's next tile
 #pragma unroll 1
         for (;;) {
             // The unit's columns of this lane.
             const int col0 = k.i * kCols, cols = min((int64_t)kCols, (int64_t)k.n * a.G - col0);
-            Acc acc;
-            uint32_t q[2][16];
-            float cs[2];
-            int lim[2];
+            Acc<Z> acc;
+            uint32_t q[Z][16];
+            float cs[Z][2];
+            int lim[Z][2];
+            acc.scale = 0;
 #pragma unroll
-            for (int z = 0; z < 2; ++z) {
-                const int x = g + 8 * z, token = (col0 + x) / a.G, j = col0 + x - token * a.G;
+            for (int z = 0; z < Z; ++z) {
+                const int x = 8 * z + g, token = (col0 + x) / a.G, j = col0 + x - token * a.G;
                 const bool live = x < cols && in_bounds(k.t + token < a.T && k.g * a.G + j < a.H, a.status);
-                load_column<F16>(a.q + (int64_t)(k.t + token) * a.q_stride + (k.g * a.G + j) * kHeadDim + 32 * t, live, q[z], cs[z]);
-                cs[z] *= a.qscale;
-                lim[z] = live ? sees(a, k.len, k.n, token) : k.rows;
-                acc.reach[z] = acc.top[z] = -INFINITY;
-                acc.l[z] = 0.f;
+                float back;  // (of column g)
+                load_column<F16>(a.q + (int64_t)(k.t + token) * a.q_stride + (k.g * a.G + j) * kHeadDim + 32 * t, live, q[z], back);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int y = 8 * z + 2 * t + e;
+                    cs[z][e] = __shfl_sync(kFull, back, 8 * t + 4 * e) * a.qscale;
+                    lim[z][e] = y < cols ? sees(a, k.len, k.n, (col0 + y) / a.G) : k.rows;
+                    acc.top[z][e] = -INFINITY;
+                    acc.l[z][e] = 0.f;
+                }
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
+            for (int i = 0; i < 8; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc.o[i][e] = 0.f;
+                for (int z = 0; z < Z; ++z)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc.o[i][z][e] = 0.f;
             const int shown = sees(a, k.len, k.n, col0 / a.G);
 #pragma unroll 1
             for (int j = k.j0 + warp; j < k.j1; j += kWarps) {
-                const int s = used % kStages;
-                if (ok && !__all_sync(kFull, mbar_wait(smem_u32(full + s), (used / kStages) & 1))) {
+                if (ok && !__all_sync(kFull, mbar_wait(smem_u32(full + at_stage), (phases >> at_stage) & 1))) {
                     ok = false;
                     misc[0] = 1;
                     if (lane == 0) report(a, DKV_DEV_TMA_TIMEOUT);
                 }
                 if (!ok) break;
                 ++used;
-                const int r0 = j * kRows, tl[2] = {lim[0] - r0, lim[1] - r0};
-                const unsigned char* tile = ring + s * kStageBytes;
-                tile_step(acc, q, cs, tile, tile + kTileBytes, scales + s * 2 * kRows, tl, shown - r0, k.rows - r0);
+                phases ^= 1u << at_stage;
+                const int r0 = j * kRows;
+                int tl[Z][2];
+#pragma unroll
+                for (int z = 0; z < Z; ++z)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) tl[z][e] = lim[z][e] - r0;
+                const unsigned char* tile = ring + at_stage * kStageBytes;
+                tile_step<Z>(acc, q, cs, tile, tile + kTileBytes, scales + at_stage * 2 * kRows, factors, tl, shown - r0, k.rows - r0);
+                at_stage = at_stage + 1 == kStages ? 0 : at_stage + 1;
                 __syncwarp();
                 fetch();
             }
             // The warps' states: joined in the order of the warps, 64 dims at a time.
             const int active = min(kWarps, k.j1 - k.j0);
 #pragma unroll
-            for (int z = 0; z < 2; ++z) {
-                acc.l[z] += __shfl_xor_sync(kFull, acc.l[z], 1);
-                acc.l[z] += __shfl_xor_sync(kFull, acc.l[z], 2);
-                if (t == 0) states[warp * kCols + g + 8 * z] = State{acc.reach[z], acc.top[z], acc.l[z], 0.f};
-            }
+            for (int z = 0; z < Z; ++z)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                    for (int o = 4; o < 32; o <<= 1) acc.l[z][e] += __shfl_xor_sync(kFull, acc.l[z][e], o);
+                    if (g == 0) states[warp * kCols + 8 * z + 2 * t + e] = State{acc.top[z][e] * cs[z][e], acc.l[z][e], (float)acc.scale, 0.f};
+                }
             __syncthreads();
             const bool aborted = misc[0];
-            const int mine = tid >> 4, chunk = tid & 15;  // this thread sums 4 dims of column `mine`: chunk 4 t + i of lane t's 16
-            State total{-INFINITY, -INFINITY, 0.f, 0.f};
-            float f0 = -INFINITY, f1 = -INFINITY;
+            const int mine = tid >> 4, chunk = tid & 15;  // this thread sums 4 dims of column `mine`: chunk 2 g + i of lane g's 8
+            State total{-INFINITY, 0.f, 0.f, 0.f};
+            float f0[Z][2];
+#pragma unroll
+            for (int z = 0; z < Z; ++z) f0[z][0] = f0[z][1] = -INFINITY;
+#pragma unroll 4
             for (int x = 0; x < active; ++x) {
-                const State y = states[x * kCols + mine];
-                total.reach = fmaxf(total.reach, y.reach);
-                total.top = fmaxf(total.top, y.top);
-                f0 = fmaxf(f0, states[x * kCols + g].reach);
-                f1 = fmaxf(f1, states[x * kCols + g + 8].reach);
+                if (mine < kCols) total.top = fmaxf(total.top, states[x * kCols + mine].top);
+                total.scale = fmaxf(total.scale, states[x * kCols].scale);
+#pragma unroll
+                for (int z = 0; z < Z; ++z)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) f0[z][e] = fmaxf(f0[z][e], states[x * kCols + 8 * z + 2 * t + e].top);
             }
-            for (int x = 0; x < active; ++x) {
-                const State y = states[x * kCols + mine];
-                total.sum += y.sum * factor(y.top, total.top);
-            }
-            f0 = factor(acc.reach[0], f0);
-            f1 = factor(acc.reach[1], f1);
+            if (mine < kCols)
+#pragma unroll 4
+                for (int x = 0; x < active; ++x) {
+                    const State y = states[x * kCols + mine];
+                    total.sum += y.sum * factor(y.top, total.top);
+                }
+#pragma unroll
+            for (int z = 0; z < Z; ++z)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) f0[z][e] = factor(acc.top[z][e] * cs[z][e], f0[z][e]) * ex2((float)acc.scale - total.scale);
             const bool whole = k.whole(), live = mine < cols && !aborted;
             const int token = (col0 + mine) / a.G, head_j = col0 + mine - token * a.G;
             uint16_t* out = a.out + ((int64_t)(k.t + token) * a.H + k.g * a.G + head_j) * kHeadDim;
             const int64_t slot = (int64_t)c * 2 + (k.j0 == 0);
-            const float z = final_scale(total.reach, total.top, total.sum);
+            const float z = final_scale(total.scale, total.sum);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 __syncthreads();
                 if (warp < active) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        // (chunks are permuted so that a quarter-warp's eight lie in different banks)
-                        const int at = (4 * t + i) ^ (t >> 1) ^ (2 * (g & 1));
-                        float4* to = reinterpret_cast<float4*>(sums + (warp * kCols + g) * 64) + at;
-                        to[0] = make_float4(acc.o[4 * i][half] * f0, acc.o[4 * i + 1][half] * f0, acc.o[4 * i + 2][half] * f0, acc.o[4 * i + 3][half] * f0);
-                        to[8 * 16] = make_float4(acc.o[4 * i][2 + half] * f1, acc.o[4 * i + 1][2 + half] * f1, acc.o[4 * i + 2][2 + half] * f1,
-                                                 acc.o[4 * i + 3][2 + half] * f1);
-                    }
+                    for (int z = 0; z < Z; ++z)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                // (chunks are permuted so that a quarter-warp's eight lie in different banks)
+                                const float f1 = f0[z][e], *x = acc.o[4 * half + 2 * i][z], *y = acc.o[4 * half + 2 * i + 1][z];
+                                reinterpret_cast<float4*>(sums + (warp * kCols + 8 * z + 2 * t + e) * 64)[(2 * g + i) ^ bank_of(t)] =
+                                    make_float4(x[e] * f1, x[2 + e] * f1, y[e] * f1, y[2 + e] * f1);
+                            }
                 }
                 __syncthreads();
                 if (live) {
-                    const int at = chunk ^ (chunk >> 3) ^ (2 * (mine & 1));
+                    const int at = chunk ^ bank_of((mine >> 1) & 3);
                     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
                     for (int x = 0; x < active; ++x) {
                         const float4 y = reinterpret_cast<const float4*>(sums + (x * kCols + mine) * 64)[at];
                         v = make_float4(v.x + y.x, v.y + y.y, v.z + y.z, v.w + y.w);
                     }
-                    const int dim = 32 * (chunk >> 2) + 16 * half + 4 * (chunk & 3);
+                    const int dim = 16 * (chunk >> 1) + 8 * half + 4 * (chunk & 1);
                     if (whole)
                         *reinterpret_cast<uint2*>(out + dim) = pack4<F16>(v, z);
                     else
-                        __stcg(w.o + (slot * kCols + mine) * (kHeadDim / 4) + dim / 4, v);
+                        __stcg(w.o + (slot * kMostCols + mine) * (kHeadDim / 4) + dim / 4, v);
                 }
             }
             if (!whole) {
-                if (live && chunk == 0) __stcg(reinterpret_cast<float4*>(w.state + slot * kCols + mine), make_float4(total.reach, total.top, total.sum, 0.f));
+                if (live && chunk == 0) __stcg(reinterpret_cast<float4*>(w.state + slot * kMostCols + mine), make_float4(total.top, total.sum, total.scale, 0.f));
                 const int c0 = cta_of(head, k.start), pieces = cta_of(head, k.start + k.tiles - 1) - c0 + 1;
                 __threadfence();
                 __syncthreads();
@@ -649,28 +758,44 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 __syncthreads();
                 if (misc[1] && mine < cols && in_bounds(c0 >= 0 && c0 + pieces <= nctas, a.status)) {
+                    // kJoin pieces on the way at once, in the order of the CTAs.
                     __threadfence();
-                    State all{-INFINITY, -INFINITY, 0.f, 0.f};
-#pragma unroll 4
-                    for (int x = 0; x < pieces; ++x) {
-                        const float4 y = __ldcg(reinterpret_cast<const float4*>(w.state + piece_at(c0, x) * kCols + mine));
-                        all.reach = fmaxf(all.reach, y.x);
-                        all.top = fmaxf(all.top, y.y);
-                    }
+                    constexpr int kJoin = Z == 1 ? 4 : 8;
+                    State all{-INFINITY, 0.f, 0.f, 0.f};
                     float4 v[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-#pragma unroll 4
-                    for (int x = 0; x < pieces; ++x) {
-                        const int64_t piece = piece_at(c0, x) * kCols + mine;
-                        const float4 y = __ldcg(reinterpret_cast<const float4*>(w.state + piece));
-                        const float fo = factor(y.x, all.reach);
-                        all.sum += y.z * factor(y.y, all.top);
+#pragma unroll 1
+                    for (int x0 = 0; x0 < pieces; x0 += kJoin) {
+                        float4 y[kJoin], u[kJoin][2];
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const float4 u = __ldcg(w.o + piece * (kHeadDim / 4) + 2 * chunk + i);
-                            v[i] = make_float4(fmaf(u.x, fo, v[i].x), fmaf(u.y, fo, v[i].y), fmaf(u.z, fo, v[i].z), fmaf(u.w, fo, v[i].w));
+                        for (int x = 0; x < kJoin; ++x) {
+                            const int64_t piece = piece_at(c0, min(x0 + x, pieces - 1)) * kMostCols + mine;
+                            y[x] = __ldcg(reinterpret_cast<const float4*>(w.state + piece));
+                            u[x][0] = __ldcg(w.o + piece * (kHeadDim / 4) + 2 * chunk);
+                            u[x][1] = __ldcg(w.o + piece * (kHeadDim / 4) + 2 * chunk + 1);
                         }
+                        State now = all;
+#pragma unroll
+                        for (int x = 0; x < kJoin; ++x) {
+                            now.top = fmaxf(now.top, y[x].x);
+                            now.scale = fmaxf(now.scale, y[x].z);
+                        }
+                        const float old = factor(all.top, now.top), old_o = old * ex2(all.scale - now.scale);
+                        now.sum *= old;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) v[i] = make_float4(v[i].x * old_o, v[i].y * old_o, v[i].z * old_o, v[i].w * old_o);
+#pragma unroll
+                        for (int x = 0; x < kJoin; ++x) {
+                            if (x0 + x >= pieces) break;
+                            const float fl = factor(y[x].x, now.top), fo = fl * ex2(y[x].z - now.scale);
+                            now.sum += y[x].y * fl;
+#pragma unroll
+                            for (int i = 0; i < 2; ++i)
+                                v[i] = make_float4(fmaf(u[x][i].x, fo, v[i].x), fmaf(u[x][i].y, fo, v[i].y), fmaf(u[x][i].z, fo, v[i].z),
+                                                   fmaf(u[x][i].w, fo, v[i].w));
+                        }
+                        all = now;
                     }
-                    const float y = final_scale(all.reach, all.top, all.sum);
+                    const float y = final_scale(all.scale, all.sum);
                     const uint2 lo = pack4<F16>(v[0], y), hi = pack4<F16>(v[1], y);
                     *reinterpret_cast<uint4*>(out + 8 * chunk) = make_uint4(lo.x, lo.y, hi.x, hi.y);
                 }
@@ -680,7 +805,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             k.next(a);
         }
         // Copies in flight land (or run out of time) before the CTA exits.
-        for (; used < fetched; ++used) mbar_wait(smem_u32(full + used % kStages), (used / kStages) & 1);
+        for (; used < fetched; ++used) {
+            mbar_wait(smem_u32(full + at_stage), (phases >> at_stage) & 1);
+            phases ^= 1u << at_stage;
+            at_stage = at_stage + 1 == kStages ? 0 : at_stage + 1;
+        }
     }
     pdl_wait();  // the call is not over before its begin kernel
 }
@@ -715,14 +844,30 @@ cudaError_t make_pool_map(const QuantAttnArgs& a, const uint8_t* pool, bool shor
                : cudaErrorInvalidValue;
 }
 
+template <bool F16, int Z>
+cudaError_t setup_few()
+{
+    return cudaFuncSetAttribute(quant_attn_kernel<F16, Z>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<Z>::kSmemBytes);
+}
+
+template <bool F16>
+cudaError_t launch_few(const QuantAttnArgs& a, const CacheMaps& maps, const QuantWork& w, int nctas, cudaStream_t st)
+{
+    if (a.few * a.G <= Cfg<1>::kCols)
+        return launch_pdl(quant_attn_kernel<F16, 1>, nctas, Cfg<1>::kThreads, Cfg<1>::kSmemBytes, st, a, maps, w, nctas);
+    return launch_pdl(quant_attn_kernel<F16, 2>, nctas, Cfg<2>::kThreads, Cfg<2>::kSmemBytes, st, a, maps, w, nctas);
+}
+
 }  // namespace
 
 int64_t quant_workspace_bytes() { return kWorkBytes + chunk_workspace_bytes(); }
 
 cudaError_t quant_setup()
 {
-    cudaError_t e = cudaFuncSetAttribute(quant_attn_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(quant_attn_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    cudaError_t e = setup_few<false, 1>();
+    if (e == cudaSuccess) e = setup_few<true, 1>();
+    if (e == cudaSuccess) e = setup_few<false, 2>();
+    if (e == cudaSuccess) e = setup_few<true, 2>();
     return e;
 }
 
@@ -742,7 +887,7 @@ cudaError_t launch_quant_attn(const QuantAttnArgs& a, bool short_boxes, cudaStre
     w.o = reinterpret_cast<float4*>(base + kOffO);
     w.chunk = reinterpret_cast<int32_t*>(base + kWorkBytes);
     QuantAttnArgs few = a;
-    few.few = std::min(a.most, kCols / a.G);
+    few.few = std::min(a.most, kMostCols / a.G);
     if ((e = launch_pdl(quant_begin_kernel, 1, 512, 0, st, few, w)) != cudaSuccess) return e;
     if (a.most > few.few) {
         ChunkArgs c{};
@@ -773,8 +918,7 @@ cudaError_t launch_quant_attn(const QuantAttnArgs& a, bool short_boxes, cudaStre
         c.most = a.most;
         if ((e = launch_chunk8(c, nctas, short_boxes, st)) != cudaSuccess) return e;
     }
-    return a.fp16 ? launch_pdl(quant_attn_kernel<true>, nctas, kThreads, kSmemBytes, st, few, maps, w, nctas)
-                  : launch_pdl(quant_attn_kernel<false>, nctas, kThreads, kSmemBytes, st, few, maps, w, nctas);
+    return a.fp16 ? launch_few<true>(few, maps, w, nctas, st) : launch_few<false>(few, maps, w, nctas, st);
 }
 
 }  // namespace dkv
