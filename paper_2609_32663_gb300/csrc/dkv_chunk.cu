@@ -497,6 +497,56 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi)
     return pack_bf16(lo, hi);
 }
 
+__device__ __forceinline__ void store_shared(uint32_t at, uint4 x)
+{
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+}
+
+// The row's eight chunks of 16 codes, times f1 (and f2).
+template <bool F16, bool TWO>
+__device__ __forceinline__ void widen_chunks(uint32_t src, uint32_t dst, int swz, uint32_t f1, uint32_t f2)
+{
+    uint32_t nan = 0;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        uint4 x;
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(src + ((c ^ swz) << 4)) : "memory");
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        uint32_t y[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (F16) {
+                widen_e4m3(w[i], y[2 * i], y[2 * i + 1]);
+            } else {
+                nan |= (w[i] & 0x7f7f7f7fu) + 0x01010101u;
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    const uint32_t p = __byte_perm(w[i], 0u, z ? 0x4342 : 0x4140);  // a code in the low byte of each half
+                    y[2 * i + z] = (p & 0x00800080u) * 240u + p * 16u;               // 0x80 16 + 0x80 240 = 0x8000
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            y[i] = scale2<F16>(y[i], f1);
+            if (TWO) y[i] = scale2<F16>(y[i], f2);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            store_shared(dst + (c >> 2) * kHalf + (((2 * (c & 3) + i) ^ swz) << 4), make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]));
+    }
+    if (!F16 && (nan & 0x80808080u)) {
+#pragma unroll 1
+        for (int d = 0; d < kHeadDim; ++d) {
+            uint32_t code;
+            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(code) : "r"(src + (((d >> 4) ^ swz) << 4) + (d & 15)) : "memory");
+            if ((code & 0x7fu) == 0x7fu)
+                asm volatile("st.shared.u16 [%0], %1;" ::"r"(dst + (d >> 6) * kHalf + ((((d >> 3) & 7) ^ swz) << 4) + (d & 7) * 2), "h"((uint16_t)0x7fff)
+                             : "memory");
+        }
+    }
+}
+
 // Row r of an 8-bit tile as a row of a 16-bit one, both as the copies' swizzle lays them out: value times 2^(u - 127) (half of
 // that in fp16, see kHalved). Every such value is one of the type, but for fp16 below 2^-23. bf16: the
 // exponent and fraction of a code, moved to their places, are the value times 2^-120, subnormal ones too; NaN codes are
@@ -523,46 +573,14 @@ __device__ __forceinline__ void widen_row(const unsigned char* raw, uint32_t u, 
     }
     f1 |= f1 << 16;
     f2 |= f2 << 16;
-    two = __any_sync(kFull, two);
-    uint32_t nan = 0;
+    const uint32_t src = smem_u32(raw) + r * 128, dst = smem_u32(tile) + r * 128;
+    if (none) {
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        uint4 x;
-        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
-                     : "r"(smem_u32(raw) + r * 128 + ((c ^ swz) << 4))
-                     : "memory");
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-        uint32_t y[8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (F16) {
-                widen_e4m3(w[i], y[2 * i], y[2 * i + 1]);
-            } else {
-                nan |= (w[i] & 0x7f7f7f7fu) + 0x01010101u;
-#pragma unroll
-                for (int z = 0; z < 2; ++z) {
-                    const uint32_t p = __byte_perm(w[i], 0u, z ? 0x4342 : 0x4140);  // a code in the low byte of each half
-                    y[2 * i + z] = (p & 0x00800080u) * 240u + (p << 4);              // 0x80 16 + 0x80 240 = 0x8000
-                }
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            y[i] = scale2<F16>(y[i], f1);
-            if (two) y[i] = scale2<F16>(y[i], f2);
-            if (none) y[i] = 0;
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            *reinterpret_cast<uint4*>(tile + (c >> 2) * kHalf + r * 128 + (((2 * (c & 3) + i) ^ swz) << 4)) =
-                make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
-    }
-    if (!F16 && (nan & 0x80808080u) && !none) {
-#pragma unroll 1
-        for (int d = 0; d < kHeadDim; ++d)
-            if ((raw[r * 128 + (((d >> 4) ^ swz) << 4) + (d & 15)] & 0x7f) == 0x7f)
-                *reinterpret_cast<uint16_t*>(tile + (d >> 6) * kHalf + r * 128 + ((((d >> 3) & 7) ^ swz) << 4) + (d & 7) * 2) = 0x7fff;
+        for (int c = 0; c < 16; ++c) store_shared(dst + (c >> 3) * kHalf + ((c & 7) << 4), make_uint4(0u, 0u, 0u, 0u));
+    } else if (!two) {
+        widen_chunks<F16, false>(src, dst, swz, f1, f2);
+    } else {
+        widen_chunks<F16, true>(src, dst, swz, f1, f2);
     }
 }
 
