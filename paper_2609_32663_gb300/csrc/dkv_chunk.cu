@@ -502,23 +502,34 @@ __device__ __forceinline__ void store_shared(uint32_t at, uint4 x)
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
 }
 
-// The row's eight chunks of 16 codes, times f1 (and f2).
+__device__ __forceinline__ uint4 load_shared(uint32_t at)
+{
+    uint4 x;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(at) : "memory");
+    return x;
+}
+
+// The row's eight chunks of 16 codes, times f1 (and f2). kEarly chunks are on their way before the first is used: one
+// warp a scheduler does this, which has nothing else to do while a load is.
 template <bool F16, bool TWO>
 __device__ __forceinline__ void widen_chunks(uint32_t src, uint32_t dst, int swz, uint32_t f1, uint32_t f2)
 {
+    constexpr int kEarly = 3;
     uint32_t nan = 0;
+    uint4 x[8];
+#pragma unroll
+    for (int c = 0; c < kEarly; ++c) x[c] = load_shared(src + ((c ^ swz) << 4));
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
-        uint4 x;
-        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(src + ((c ^ swz) << 4)) : "memory");
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        if (c + kEarly < 8) x[c + kEarly] = load_shared(src + (((c + kEarly) ^ swz) << 4));
+        const uint32_t w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
         uint32_t y[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (F16) {
                 widen_e4m3(w[i], y[2 * i], y[2 * i + 1]);
             } else {
-                nan |= (w[i] & 0x7f7f7f7fu) + 0x01010101u;
+                nan |= w[i] ^ (w[i] + 0x01010101u);  // bit 7 of a byte: its lower bits are all ones (or a lower byte is a NaN)
 #pragma unroll
                 for (int z = 0; z < 2; ++z) {
                     const uint32_t p = __byte_perm(w[i], 0u, z ? 0x4342 : 0x4140);  // a code in the low byte of each half
