@@ -9,9 +9,6 @@
 
 #include "dkv_decode_common.cuh"
 
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
 #include <algorithm>
 
 namespace dkv {
@@ -39,32 +36,10 @@ template <bool F16>
 __device__ __forceinline__ void hold_row(const uint4 (&x)[2], uint8_t* pool, uint8_t* scales, int64_t at, int sub)
 {
     const uint32_t w[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
-    float f[16], most = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (F16) {
-            const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-            f[2 * i] = v.x;
-            f[2 * i + 1] = v.y;
-        } else {
-            f[2 * i] = __uint_as_float(w[i] << 16);
-            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        float size;
-        f[i] = held(f[i], size);
-        most = fmaxf(most, size);
-    }
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) most = fmaxf(most, __shfl_xor_sync(kFull, most, o));
+    uint32_t u;
+    const uint4 v = hold_lane<F16>(w, u);
     if (at < 0) return;
-    const uint32_t u = scale_byte(most);
-    const float z = inverse_scale(u);
-    reinterpret_cast<uint4*>(pool + at * kHeadDim)[sub] =
-        make_uint4(pack_e4m3(f[0] * z, f[1] * z, f[2] * z, f[3] * z), pack_e4m3(f[4] * z, f[5] * z, f[6] * z, f[7] * z),
-                   pack_e4m3(f[8] * z, f[9] * z, f[10] * z, f[11] * z), pack_e4m3(f[12] * z, f[13] * z, f[14] * z, f[15] * z));
+    reinterpret_cast<uint4*>(pool + at * kHeadDim)[sub] = v;
     if (sub == 0) scales[at] = (uint8_t)u;
 }
 
@@ -118,6 +93,7 @@ __global__ void __launch_bounds__(kQcThreads) quant_compact_kernel(const __grid_
                 const int x = x0 + 4 * y + (lane >> 3);
                 const int64_t src = __shfl_sync(kFull, from, x);
                 at[y] = __shfl_sync(kFull, to, x);
+                K[y][0] = K[y][1] = V[y][0] = V[y][1] = make_uint4(0u, 0u, 0u, 0u);
                 if (src >= 0) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {

@@ -61,6 +61,11 @@ cudaError_t quant_setup();  // the kernels' attributes in the current context
 cudaError_t launch_quant_attn(const QuantAttnArgs& a, bool short_boxes, cudaStream_t st);
 
 #ifdef __CUDACC__
+}  // namespace dkv
+
+#include <cuda_fp16.h>
+
+namespace dkv {
 namespace {
 
 // A value as it is held: what is not finite is NaN. `size`: |x|, or 0 for what is not finite.
@@ -85,6 +90,11 @@ __device__ __forceinline__ uint32_t scale_byte(float size)
 __device__ __forceinline__ float scale_of(uint32_t u) { return __uint_as_float(u << 23); }
 __device__ __forceinline__ float inverse_scale(uint32_t u) { return __uint_as_float((254u - u) << 23); }
 
+// Rows of 16-bit values, 8 lanes a row (in groups of 8 neighbours): the lane's 16 elements w as 16 e4m3 values, and the row's
+// scale byte. All lanes of the warp.
+template <bool F16>
+__device__ __forceinline__ uint4 hold_lane(const uint32_t (&w)[8], uint32_t& u);
+
 // Four e4m3 values, the first in the lowest byte.
 __device__ __forceinline__ uint32_t pack_e4m3(float x0, float x1, float x2, float x3)
 {
@@ -96,6 +106,71 @@ __device__ __forceinline__ uint32_t pack_e4m3(float x0, float x1, float x2, floa
         : "=r"(v)
         : "f"(x0), "f"(x1), "f"(x2), "f"(x3));
     return v;
+}
+
+// Two e4m3 values of a pair of fp16 values.
+__device__ __forceinline__ uint32_t pack_e4m3_f16(uint32_t x)
+{
+    uint32_t v;
+    asm("{\n\t.reg .b16 y;\n\tcvt.rn.satfinite.e4m3x2.f16x2 y, %1;\n\tmov.b32 %0, {y, 0};\n\t}" : "=r"(v) : "r"(x));
+    return v;
+}
+
+template <bool F16>
+__device__ __forceinline__ uint4 hold_lane(const uint32_t (&w)[8], uint32_t& u)
+{
+    // The largest element as its 15 bits, which order as the sizes do; infinities and NaN come after all others.
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
+    m = max(m & 0xffffu, m >> 16);
+    const float size = F16 ? __half2float(__ushort_as_half((uint16_t)m)) : __uint_as_float(m << 16);
+    u = scale_byte(size);
+    // fp16: the factor 2^(127 - u) has to be one, and what it takes below 2^-14 is below a half of the least step, 2^-10.
+    const bool plain = m < (F16 ? 0x7c00u : 0x7f80u) && (!F16 || (u >= 112u && u <= 141u));
+    uint32_t y[8];
+    if (__all_sync(0xffffffffu, plain)) {
+        const uint32_t f = F16 ? (142u - u) << 10 : (254u - u) << 7, f2 = f | f << 16;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t z;
+            if (F16) {
+                asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(z) : "r"(w[i]), "r"(f2));
+                y[i] = pack_e4m3_f16(z);
+            } else {
+                asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(z) : "r"(w[i]), "r"(f2));
+                y[i] = z;
+            }
+        }
+        uint4 v;
+        uint32_t* x = &v.x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            x[i] = F16 ? __byte_perm(y[2 * i], y[2 * i + 1], 0x5410)
+                       : pack_e4m3(__uint_as_float(y[2 * i] << 16), __uint_as_float(y[2 * i] & 0xffff0000u), __uint_as_float(y[2 * i + 1] << 16),
+                                   __uint_as_float(y[2 * i + 1] & 0xffff0000u));
+        return v;
+    }
+    float f[16], most = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        f[2 * i] = F16 ? __half2float(__ushort_as_half((uint16_t)w[i])) : __uint_as_float(w[i] << 16);
+        f[2 * i + 1] = F16 ? __half2float(__ushort_as_half((uint16_t)(w[i] >> 16))) : __uint_as_float(w[i] & 0xffff0000u);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float s;
+        f[i] = held(f[i], s);
+        most = fmaxf(most, s);
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    u = scale_byte(most);
+    const float z = inverse_scale(u);
+    return make_uint4(pack_e4m3(f[0] * z, f[1] * z, f[2] * z, f[3] * z), pack_e4m3(f[4] * z, f[5] * z, f[6] * z, f[7] * z),
+                      pack_e4m3(f[8] * z, f[9] * z, f[10] * z, f[11] * z), pack_e4m3(f[12] * z, f[13] * z, f[14] * z, f[15] * z));
 }
 
 // The four e4m3 values of a word as fp16 pairs.

@@ -70,8 +70,30 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
     __shared__ int32_t cu[kMaxSlots + 1];
     const int tid = threadIdx.x, per = kRopeThreads / tokens, mine = tid / per, t = blockIdx.x * tokens + mine;
     const int sub = tid & 7, group = (tid - mine * per) >> 3, groups = per >> 3, pairs = a.rot >> 1;
+    const int heads = a.q ? a.H : 0, all = POOL ? heads + 2 * a.Hkv : heads;
+    const bool turned = sub < a.rot >> 4;
+    // The lane's two chunks of 8 elements.
+    const int chunk0 = turned ? (INTER ? 2 * sub : sub) : 2 * sub, chunk1 = turned && !INTER ? sub + (a.rot >> 4) : chunk0 + 1;
+    uint4 x[kBatch][2];
+    auto load = [&](int h0) {
+#pragma unroll
+        for (int y = 0; y < kBatch; ++y) {
+            const int h = h0 + y * groups + group;
+            if (h < all && t < a.T) {
+                const uint16_t* src = h < heads ? a.q + t * a.q_stride + (int64_t)h * kHeadDim
+                                                : (h < heads + a.Hkv ? a.k + (int64_t)(h - heads) * kHeadDim
+                                                                     : a.v + (int64_t)(h - heads - a.Hkv) * kHeadDim) +
+                                                      t * a.kv_stride;
+                x[y][0] = __ldcs(reinterpret_cast<const uint4*>(src) + chunk0);
+                x[y][1] = __ldcs(reinterpret_cast<const uint4*>(src) + chunk1);
+            } else {
+                x[y][0] = x[y][1] = make_uint4(0u, 0u, 0u, 0u);
+            }
+        }
+    };
     pdl_wait();
     pdl_launch_dependents();
+    load(0);  // on their way while cos and sin are found
     for (int i = tid; i < tokens * pairs; i += kRopeThreads) {
         const int x = i / pairs, pair = i - x * pairs, at = blockIdx.x * tokens + x;
         if (at < a.T) reinterpret_cast<float2*>(cs[x])[pair] = turn(a.turns[pair] * (uint64_t)(int64_t)a.positions[at], a.magnitude);
@@ -93,7 +115,6 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
     }
     if (t >= (a.cu ? cu[a.B] : a.T)) return;  // (whole warps)
     float c[8], s[8];
-    const bool turned = sub < a.rot >> 4;
     if (turned) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -104,8 +125,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
             s[2 * i + 1] = x.w;
         }
     }
-    // The lane's two chunks of 8 elements.
-    const int chunk0 = turned ? (INTER ? 2 * sub : sub) : 2 * sub, chunk1 = turned && !INTER ? sub + (a.rot >> 4) : chunk0 + 1;
+    const int log_P = 31 - __clz(max(a.P, 1));
     int b = 0, back = 0;  // the token's sequence, and how far from the end of its slabs the token's row lies
     if (POOL) {
         int hi = a.B - 1;  // the last sequence that starts at t or before
@@ -118,30 +138,21 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
         }
         back = cu[b + 1] - t;
     }
-    const int heads = a.q ? a.H : 0, all = POOL ? heads + 2 * a.Hkv : heads;
 #pragma unroll 1
     for (int h0 = 0; h0 < all; h0 += kBatch * groups) {
-        uint4 x[kBatch][2];
+        if (h0) load(h0);
         int page[kBatch], row[kBatch];  // of k and v: the page, and the row in it
 #pragma unroll
         for (int y = 0; y < kBatch; ++y) {
             const int h = h0 + y * groups + group;
             page[y] = -1;
             row[y] = 0;
-            if (h < all) {
-                const uint16_t* src = h < heads ? a.q + t * a.q_stride + (int64_t)h * kHeadDim
-                                                : (h < heads + a.Hkv ? a.k + (int64_t)(h - heads) * kHeadDim
-                                                                     : a.v + (int64_t)(h - heads - a.Hkv) * kHeadDim) +
-                                                      t * a.kv_stride;
-                x[y][0] = __ldcs(reinterpret_cast<const uint4*>(src) + chunk0);
-                x[y][1] = __ldcs(reinterpret_cast<const uint4*>(src) + chunk1);
-                if (POOL && h >= heads) {
-                    const int64_t slab = (int64_t)b * a.Hkv + (h - heads < a.Hkv ? h - heads : h - heads - a.Hkv);
-                    const int n = a.len[slab], r = n - back;
-                    if (r >= 0 && n <= a.max_pages * a.P) {  // (the product is below 2^31)
-                        page[y] = a.table[slab * a.max_pages + r / a.P];
-                        row[y] = r % a.P;
-                    }
+            if (POOL && h >= heads && h < all) {
+                const int64_t slab = (int64_t)b * a.Hkv + (h - heads < a.Hkv ? h - heads : h - heads - a.Hkv);
+                const int n = a.len[slab], r = n - back;
+                if (r >= 0 && n <= a.max_pages * a.P) {  // (the product is below 2^31)
+                    page[y] = a.table[slab * a.max_pages + (r >> log_P)];
+                    row[y] = r & (a.P - 1);
                 }
             }
         }
@@ -223,8 +234,11 @@ cudaError_t launch_rope(const RopeArgs& a, cudaStream_t st)
     int sms = 0;
     const cudaError_t e = page_setup(&sms);
     if (e != cudaSuccess) return e;
-    // Few tokens are spread over the SMs; of many, a CTA has some, so that its threads' pairs are all used.
-    const int tokens = a.T >= 16 * sms ? 4 : 1, grid = (a.T + tokens - 1) / tokens;
+    // A CTA has so many tokens that a thread has its rows in one batch; fewer, where the SMs would not all have a CTA.
+    const int heads = (a.q ? a.H : 0) + (a.k ? 2 * a.Hkv : 0);
+    int tokens = kRopeTokens;
+    while (tokens > 1 && (tokens * heads > kBatch * kRopeThreads / 8 || a.T < 2 * sms * tokens)) tokens >>= 1;
+    const int grid = (a.T + tokens - 1) / tokens;
     if (a.fp16) return a.interleaved ? launch_pool<true, true>(a, grid, tokens, st) : launch_pool<true, false>(a, grid, tokens, st);
     return a.interleaved ? launch_pool<false, true>(a, grid, tokens, st) : launch_pool<false, false>(a, grid, tokens, st);
 }
