@@ -611,10 +611,11 @@ dkv_status dkv_rotary_custom(dkv_rotary* rotary, int32_t rot_dim, int32_t interl
  *            Strides are multiples of 8, at least heads*128; 16-byte aligned.
  * positions  device int32 [num_tokens], of any sign.
  * rotary     host; read by the call, not kept.
+ * status     as for the paged cache's calls: a device int32, or NULL.
  * Asynchronous, allocates nothing, can be captured. Errors: DKV_ERR_INVALID_ARG, DKV_ERR_CUDA.
  */
 dkv_status dkv_rope(const dkv_rotary* rotary, int32_t dtype, int32_t num_tokens, int32_t heads, const void* x, int64_t x_stride,
-                    const int32_t* positions, void* out, int64_t out_stride, cudaStream_t stream);
+                    const int32_t* positions, void* out, int64_t out_stride, int32_t* status, cudaStream_t stream);
 
 /*
  * The paged cache in 8 bits. Its pools hold a byte for each 16-bit element, and every row has a

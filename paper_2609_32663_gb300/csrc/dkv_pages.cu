@@ -693,6 +693,7 @@ cudaError_t page_setup(int* sms)
     if ((e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
     if ((e = chunk_setup()) != cudaSuccess) return e;
     if ((e = quant_setup()) != cudaSuccess) return e;
+    if ((e = rope_setup()) != cudaSuccess) return e;
     if ((e = cudaFuncSetAttribute(page_fused_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFusedSlabs * 4)) != cudaSuccess) return e;
     if ((e = cudaFuncSetAttribute(page_compact_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPcSmem)) != cudaSuccess) return e;
     if (count < kMost) known[count++] = Known{id, *sms};

@@ -388,7 +388,7 @@ dkv_status dkv_rotary_make(dkv_rotary* rotary, int32_t rot_dim, int32_t interlea
 }
 
 dkv_status dkv_rope(const dkv_rotary* rotary, int32_t dtype, int32_t num_tokens, int32_t heads, const void* x, int64_t x_stride,
-                    const int32_t* positions, void* out, int64_t out_stride, cudaStream_t stream)
+                    const int32_t* positions, void* out, int64_t out_stride, int32_t* status, cudaStream_t stream)
 {
     dkv::RopeArgs a{};
     if (!rotary) return refuse("rotary is NULL");
@@ -398,6 +398,7 @@ dkv_status dkv_rope(const dkv_rotary* rotary, int32_t dtype, int32_t num_tokens,
     if (num_tokens == 0) return dkv::set_error(DKV_OK, "");
     if (!rotary_ok(rotary, positions, &a)) return DKV_ERR_INVALID_ARG;
     if (!x || !out || !aligned(x, 16) || !aligned(out, 16)) return refuse("x/out is NULL or not 16-byte aligned");
+    if (!aligned(status, 4)) return refuse("status must be 4-byte aligned");
     if (!stride_ok("x_stride", x_stride, heads) || !stride_ok("out_stride", out_stride, heads)) return DKV_ERR_INVALID_ARG;
     if (!apart(x, x_stride, out, out_stride, num_tokens, heads)) return refuse("out overlaps x: it is x, with its stride, or apart from it");
     a.q = static_cast<const uint16_t*>(x);
@@ -406,6 +407,7 @@ dkv_status dkv_rope(const dkv_rotary* rotary, int32_t dtype, int32_t num_tokens,
     a.out_stride = out_stride;
     a.T = num_tokens;
     a.H = heads;
+    a.status = status;
     a.fp16 = dtype == DKV_FP16;
     return launched(dkv::launch_rope(a, stream), "rope kernel");
 }

@@ -26,6 +26,7 @@ struct RopeArgs {
     float magnitude;
     uint64_t turns[64];
 };
+cudaError_t rope_setup();  // the kernels' attributes in the current context
 cudaError_t launch_rope(const RopeArgs& a, cudaStream_t st);
 
 struct QuantCompactArgs {

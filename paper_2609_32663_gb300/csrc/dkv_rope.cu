@@ -5,11 +5,12 @@
 // p; its nearest quarter turn is taken off in integers, which leaves at most an eighth of a turn
 // with 29 bits, and cos and sin are taken of that in fp32.
 //
-//   rope_kernel  a CTA has some tokens; its threads first compute their pairs' cos and sin into shared
-//                memory, one pair a thread, which serve all heads of a token. Then 8 lanes have a row: lane s
-//                turns pairs 8s .. 8s + 7, which lie in two 16-byte chunks in either layout, or copies two chunks
-//                behind rot_dim. k and v rows go to their pages, 16-bit or (after the row's largest
-//                element is found over the 8 lanes) as e4m3 values with a scale byte.
+//   rope_kernel  one CTA an SM. An item is some heads of a token; a warp takes every n-th item, whose rows
+//                land in a ring of its own by bulk copies (the heads of a token lie together), and finds the token's
+//                cos and sin, two pairs a lane. Then 8 lanes have a row: lane s turns pairs 8s .. 8s + 7, which lie in two
+//                16-byte chunks in either layout, or copies two chunks behind rot_dim. k and v rows go to their
+//                pages, 16-bit or (after the row's largest element is found over the 8 lanes) as e4m3 values with a
+//                scale byte.
 //
 // What bounds it: memory, each row in and out once.
 #include "dkv_quant.cuh"
@@ -19,12 +20,20 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
+
 namespace dkv {
 namespace {
 
-constexpr int kRopeThreads = 256;
-constexpr int kRopeTokens = 8;  // tokens of a CTA, at most
-constexpr int kBatch = 4;       // rows of 8 lanes on the way at once
+constexpr int kRopeWarps = 16;
+constexpr int kRopeThreads = 32 * kRopeWarps;
+constexpr int kMostHeads = 24;      // rows of an item, at most
+constexpr int kMostStages = 8;      // of a warp's ring
+constexpr int kRopeRing = 192 * 1024;
+// Shared memory: the rings, then a warp's (cos, sin) of its item's pairs, its barriers, and the token offsets.
+constexpr int kOffTurns = kRopeRing, kOffRopeBars = kOffTurns + kRopeWarps * 64 * 8, kOffCu = kOffRopeBars + kRopeWarps * kMostStages * 8,
+              kRopeSmem = kOffCu + (kMaxSlots + 1) * 4;
+static_assert(kRopeSmem <= 227 * 1024 && kRopeWarps * 2 * kMostHeads * kRowBytes <= kRopeRing, "fits one CTA, two stages a warp");
 
 template <bool F16>
 __device__ __forceinline__ float2 widen16(uint32_t u)
@@ -62,44 +71,34 @@ __device__ __forceinline__ void report(const RopeArgs& a, int bits)
     if (a.status) atomicOr(a.status, bits);
 }
 
+// How a call is cut: a token's `all` heads (of q, k and v) in `parts` items of up to `heads` rows, rings of `stages`.
+struct RopeCut {
+    int all, parts, heads, stages;
+};
+
 // POOL: bits of an element of the pools; 0: no k and v.
 template <bool F16, bool INTER, int POOL>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeArgs a, int tokens)
+__global__ void __launch_bounds__(kRopeThreads, 1) rope_kernel(const __grid_constant__ RopeArgs a, const RopeCut cut)
 {
-    __shared__ float4 cs[kRopeTokens][32];  // a pair's (cos, sin), two pairs
-    __shared__ int32_t cu[kMaxSlots + 1];
-    const int tid = threadIdx.x, per = kRopeThreads / tokens, mine = tid / per, t = blockIdx.x * tokens + mine;
-    const int sub = tid & 7, group = (tid - mine * per) >> 3, groups = per >> 3, pairs = a.rot >> 1;
-    const int heads = a.q ? a.H : 0, all = POOL ? heads + 2 * a.Hkv : heads;
+    extern __shared__ __align__(128) unsigned char sm[];
+    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31, sub = lane & 7, pairs = a.rot >> 1;
+    unsigned char* ring = sm + warp * (kRopeRing / kRopeWarps);
+    float2* cs = reinterpret_cast<float2*>(sm + kOffTurns) + warp * 64;
+    uint64_t* full = reinterpret_cast<uint64_t*>(sm + kOffRopeBars) + warp * kMostStages;
+    int32_t* cu = reinterpret_cast<int32_t*>(sm + kOffCu);
+    if (lane < cut.stages) mbar_init(smem_u32(full + lane), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_proxy_async_smem();
+    const int qheads = a.q ? a.H : 0;
     const bool turned = sub < a.rot >> 4;
     // The lane's two chunks of 8 elements.
     const int chunk0 = turned ? (INTER ? 2 * sub : sub) : 2 * sub, chunk1 = turned && !INTER ? sub + (a.rot >> 4) : chunk0 + 1;
-    uint4 x[kBatch][2];
-    auto load = [&](int h0) {
-#pragma unroll
-        for (int y = 0; y < kBatch; ++y) {
-            const int h = h0 + y * groups + group;
-            if (h < all && t < a.T) {
-                const uint16_t* src = h < heads ? a.q + t * a.q_stride + (int64_t)h * kHeadDim
-                                                : (h < heads + a.Hkv ? a.k + (int64_t)(h - heads) * kHeadDim
-                                                                     : a.v + (int64_t)(h - heads - a.Hkv) * kHeadDim) +
-                                                      t * a.kv_stride;
-                x[y][0] = __ldcs(reinterpret_cast<const uint4*>(src) + chunk0);
-                x[y][1] = __ldcs(reinterpret_cast<const uint4*>(src) + chunk1);
-            } else {
-                x[y][0] = x[y][1] = make_uint4(0u, 0u, 0u, 0u);
-            }
-        }
-    };
+    const int log_P = 31 - __clz(max(a.P, 1));
     pdl_wait();
     pdl_launch_dependents();
-    load(0);  // on their way while cos and sin are found
-    for (int i = tid; i < tokens * pairs; i += kRopeThreads) {
-        const int x = i / pairs, pair = i - x * pairs, at = blockIdx.x * tokens + x;
-        if (at < a.T) reinterpret_cast<float2*>(cs[x])[pair] = turn(a.turns[pair] * (uint64_t)(int64_t)a.positions[at], a.magnitude);
-    }
-    bool bad = false;
+    int tokens = a.T;
     if (a.cu) {
+        bool bad = false;
         for (int b = tid; b <= a.B; b += kRopeThreads) {
             const int c0 = a.cu[b];
             cu[b] = c0;
@@ -108,27 +107,50 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
                 bad |= c1 < c0 || c1 > a.T || (b == 0 && c0 != 0);
             }
         }
-    }
-    if (__syncthreads_or(bad)) {
-        if (blockIdx.x == 0 && tid == 0) report(a, DKV_DEV_PAGE_RANGE);
-        return;
-    }
-    if (t >= (a.cu ? cu[a.B] : a.T)) return;  // (whole warps)
-    float c[8], s[8];
-    if (turned) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float4 x = cs[mine][4 * sub + i];
-            c[2 * i] = x.x;
-            s[2 * i] = x.y;
-            c[2 * i + 1] = x.z;
-            s[2 * i + 1] = x.w;
+        if (__syncthreads_or(bad)) {
+            if (blockIdx.x == 0 && tid == 0) report(a, DKV_DEV_PAGE_RANGE);
+            return;
         }
+        tokens = cu[a.B];
     }
-    const int log_P = 31 - __clz(max(a.P, 1));
-    int b = 0, back = 0;  // the token's sequence, and how far from the end of its slabs the token's row lies
-    if (POOL) {
-        int hi = a.B - 1;  // the last sequence that starts at t or before
+    const int64_t items = (int64_t)tokens * cut.parts, stride = (int64_t)gridDim.x * kRopeWarps;
+    const int64_t first = (int64_t)blockIdx.x + (int64_t)gridDim.x * warp;  // a few items lie in as many SMs
+    if (first >= items) return;
+    const int stage_bytes = cut.heads * kRowBytes;
+    const uint64_t pol = evict_first_policy();
+    // Rows [h0, h1) of token t, heads of q, then of k, then of v.
+    auto split = [&](int64_t item, int& t, int& h0, int& h1) {
+        t = cut.parts == 1 ? (int)item : (int)(item / cut.parts);
+        h0 = (int)(item - (int64_t)t * cut.parts) * cut.heads;
+        h1 = min(h0 + cut.heads, cut.all);
+    };
+    auto fetch = [&](int64_t item, int stage) {
+        if (item >= items) return;
+        int t, h0, h1;
+        split(item, t, h0, h1);
+        if (lane == 0) {
+            const uint32_t bar = smem_u32(full + stage), dst = smem_u32(ring) + stage * stage_bytes;
+            mbar_arrive_expect_tx(bar, (h1 - h0) * kRowBytes);
+            const int q1 = min(h1, qheads);
+            if (q1 > h0) bulk_g2s(dst, a.q + t * a.q_stride + h0 * kHeadDim, (q1 - h0) * kRowBytes, bar, pol);
+            if (POOL) {
+                const int k0 = max(h0, qheads), k1 = min(h1, qheads + a.Hkv), v0 = max(h0, qheads + a.Hkv);
+                const int64_t row = t * a.kv_stride;
+                if (k1 > k0) bulk_g2s(dst + (k0 - h0) * kRowBytes, a.k + row + (k0 - qheads) * kHeadDim, (k1 - k0) * kRowBytes, bar, pol);
+                if (h1 > v0) bulk_g2s(dst + (v0 - h0) * kRowBytes, a.v + row + (v0 - qheads - a.Hkv) * kHeadDim, (h1 - v0) * kRowBytes, bar, pol);
+            }
+        }
+        __syncwarp();
+    };
+    // Lane x: the place in its slab of row x of an item, if that is one of k or v (-1: none).
+    auto place = [&](int64_t item, int64_t& entry) {
+        entry = 0;
+        if (!POOL || item >= items) return -1;
+        int t, h0, h1;
+        split(item, t, h0, h1);
+        const int h = h0 + lane;
+        if (h < qheads || h >= h1) return -1;
+        int b = 0, hi = a.B - 1;  // the last sequence that starts at t or before
         while (b < hi) {
             const int mid = (b + hi + 1) >> 1;
             if (cu[mid] <= t)
@@ -136,40 +158,75 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
             else
                 hi = mid - 1;
         }
-        back = cu[b + 1] - t;
-    }
+        const int64_t slab = (int64_t)b * a.Hkv + (h - qheads < a.Hkv ? h - qheads : h - qheads - a.Hkv);
+        const int n = a.len[slab], r = n - (cu[b + 1] - t);
+        if (r < 0 || n > a.max_pages * a.P) {  // (the product is below 2^31)
+            report(a, DKV_DEV_PAGE_RANGE);
+            return -1;
+        }
+        entry = slab * a.max_pages;
+        return r;
+    };
+    static_assert(kMostHeads <= 32, "a lane each");
+    for (int s = 0; s < cut.stages; ++s) fetch(first + s * stride, s);
+    int64_t entry;
+    int pos = pairs ? a.positions[cut.parts == 1 ? first : first / cut.parts] : 0, row = place(first, entry), stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
 #pragma unroll 1
-    for (int h0 = 0; h0 < all; h0 += kBatch * groups) {
-        if (h0) load(h0);
-        int page[kBatch], row[kBatch];  // of k and v: the page, and the row in it
+    for (int64_t item = first; item < items; item += stride) {
+        int t, h0, h1;
+        split(item, t, h0, h1);
+        int page = -1;
+        if (POOL && row >= 0) {
+            page = in_bounds(row >> log_P < a.max_pages, a.status) ? a.table[entry + (row >> log_P)] : -1;
+            row &= a.P - 1;
+        }
+        for (int i = lane; i < pairs; i += 32) cs[i] = turn(a.turns[i] * (uint64_t)(int64_t)pos, a.magnitude);
+        const int64_t next = item + stride;
+        const int place0 = row;
+        if (pairs && next < items) pos = a.positions[cut.parts == 1 ? next : next / cut.parts];
+        row = place(next, entry);
+        int64_t at = -1;  // the pool row
+        if (POOL && h0 + lane >= qheads && h0 + lane < h1) {
+            if (page >= 0 && page < a.num_pages)
+                at = (int64_t)page * a.P + place0;
+            else
+                report(a, DKV_DEV_PAGE_RANGE);
+        }
+        __syncwarp();
+        float c[8], s[8];
+        if (turned) {
 #pragma unroll
-        for (int y = 0; y < kBatch; ++y) {
-            const int h = h0 + y * groups + group;
-            page[y] = -1;
-            row[y] = 0;
-            if (POOL && h >= heads && h < all) {
-                const int64_t slab = (int64_t)b * a.Hkv + (h - heads < a.Hkv ? h - heads : h - heads - a.Hkv);
-                const int n = a.len[slab], r = n - back;
-                if (r >= 0 && n <= a.max_pages * a.P) {  // (the product is below 2^31)
-                    page[y] = a.table[slab * a.max_pages + (r >> log_P)];
-                    row[y] = r & (a.P - 1);
-                }
+            for (int i = 0; i < 4; ++i) {
+                const float4 x = *reinterpret_cast<const float4*>(cs + 8 * sub + 2 * i);
+                c[2 * i] = x.x;
+                s[2 * i] = x.y;
+                c[2 * i + 1] = x.z;
+                s[2 * i + 1] = x.w;
             }
         }
-#pragma unroll
-        for (int y = 0; y < kBatch; ++y) {
-            const int h = h0 + y * groups + group;
-            const bool pooled = POOL && h >= heads && h < all, key = h < heads + a.Hkv;
-            if (POOL != 8 && h >= all) continue;
-            uint32_t w[8] = {x[y][0].x, x[y][0].y, x[y][0].z, x[y][0].w, x[y][1].x, x[y][1].y, x[y][1].z, x[y][1].w};
+        if (!__all_sync(kFull, mbar_wait(smem_u32(full + stage), phase))) {
+            ok = false;
+            break;
+        }
+        const unsigned char* rows = ring + stage * stage_bytes;
+        uint16_t* out = a.q_out + t * a.out_stride;
+#pragma unroll 2
+        for (int x0 = 0; x0 < h1 - h0; x0 += 4) {
+            const int x = x0 + (lane >> 3), h = h0 + x;
+            const bool some = h < h1, pooled = POOL && some && h >= qheads, key = h < qheads + a.Hkv;
+            const uint4 lo = *reinterpret_cast<const uint4*>(rows + min(x, cut.heads - 1) * kRowBytes + chunk0 * 16),
+                        hi = *reinterpret_cast<const uint4*>(rows + min(x, cut.heads - 1) * kRowBytes + chunk1 * 16);
+            uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
             float f[16];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float2 v = widen16<F16>(w[i]);
-                f[2 * i] = v.x;
-                f[2 * i + 1] = v.y;
-            }
             if (turned && key) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float2 v = widen16<F16>(w[i]);
+                    f[2 * i] = v.x;
+                    f[2 * i + 1] = v.y;
+                }
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int p = INTER ? 2 * i : i, q = INTER ? 2 * i + 1 : i + 8;
@@ -177,70 +234,118 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
                     f[p] = fmaf(u, c[i], -v * s[i]);
                     f[q] = fmaf(v, c[i], u * s[i]);
                 }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) w[i] = narrow16<F16>(f[2 * i], f[2 * i + 1]);
             }
-            if (!pooled && h < all) {
-                uint4* dst = reinterpret_cast<uint4*>(a.q_out + t * a.out_stride + (int64_t)h * kHeadDim);
+            if (POOL != 8 || !pooled) {
+                if (turned && key) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i] = narrow16<F16>(f[2 * i], f[2 * i + 1]);
+                }
+            }
+            if (some && !pooled) {
+                uint4* dst = reinterpret_cast<uint4*>(out + (int64_t)h * kHeadDim);
                 dst[chunk0] = make_uint4(w[0], w[1], w[2], w[3]);
                 dst[chunk1] = make_uint4(w[4], w[5], w[6], w[7]);
             }
-            if (POOL == 0) continue;
-            const bool placed = pooled && page[y] >= 0 && page[y] < a.num_pages;
-            if (pooled && !placed && sub == 0) report(a, DKV_DEV_PAGE_RANGE);
-            const int64_t at = (int64_t)page[y] * a.P + row[y];
+            if (POOL == 0 || !__any_sync(kFull, pooled)) continue;
+            const int64_t to = __shfl_sync(kFull, at, min(x, 31));
             if (POOL == 16) {
-                if (placed) {
-                    uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(key ? a.Kp : a.Vp) + at * kHeadDim);
+                if (pooled && to >= 0) {
+                    uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(key ? a.Kp : a.Vp) + to * kHeadDim);
                     dst[chunk0] = make_uint4(w[0], w[1], w[2], w[3]);
                     dst[chunk1] = make_uint4(w[4], w[5], w[6], w[7]);
                 }
-            } else if (__any_sync(kFull, pooled)) {
-                float most = 0.f;
+                continue;
+            }
+            if (!(turned && key)) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float size;
-                    f[i] = held(f[i], size);
-                    most = fmaxf(most, size);
-                }
-#pragma unroll
-                for (int o = 1; o < 8; o <<= 1) most = fmaxf(most, __shfl_xor_sync(kFull, most, o));
-                const uint32_t u = scale_byte(most);
-                const float z = inverse_scale(u);
-                if (placed) {
-                    uint2* dst = reinterpret_cast<uint2*>(static_cast<uint8_t*>(key ? a.Kp : a.Vp) + at * kHeadDim);
-                    dst[chunk0] = make_uint2(pack_e4m3(f[0] * z, f[1] * z, f[2] * z, f[3] * z), pack_e4m3(f[4] * z, f[5] * z, f[6] * z, f[7] * z));
-                    dst[chunk1] = make_uint2(pack_e4m3(f[8] * z, f[9] * z, f[10] * z, f[11] * z),
-                                             pack_e4m3(f[12] * z, f[13] * z, f[14] * z, f[15] * z));
-                    if (sub == 0) (key ? a.Ks : a.Vs)[at] = (uint8_t)u;
+                for (int i = 0; i < 8; ++i) {
+                    const float2 v = widen16<F16>(w[i]);
+                    f[2 * i] = v.x;
+                    f[2 * i + 1] = v.y;
                 }
             }
+            float most = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float size;
+                f[i] = held(f[i], size);
+                most = fmaxf(most, size);
+            }
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) most = fmaxf(most, __shfl_xor_sync(kFull, most, o));
+            const uint32_t u = scale_byte(most);
+            const float z = inverse_scale(u);
+            if (pooled && to >= 0) {
+                uint2* dst = reinterpret_cast<uint2*>(static_cast<uint8_t*>(key ? a.Kp : a.Vp) + to * kHeadDim);
+                dst[chunk0] = make_uint2(pack_e4m3(f[0] * z, f[1] * z, f[2] * z, f[3] * z), pack_e4m3(f[4] * z, f[5] * z, f[6] * z, f[7] * z));
+                dst[chunk1] = make_uint2(pack_e4m3(f[8] * z, f[9] * z, f[10] * z, f[11] * z), pack_e4m3(f[12] * z, f[13] * z, f[14] * z, f[15] * z));
+                if (sub == 0) (key ? a.Ks : a.Vs)[to] = (uint8_t)u;
+            }
         }
+        __syncwarp();  // the stage, and cos and sin, are read
+        fetch(item + cut.stages * stride, stage);
+        if (++stage == cut.stages) {
+            stage = 0;
+            phase ^= 1;
+        }
+    }
+    if (!ok) {
+        if (lane == 0) report(a, DKV_DEV_TMA_TIMEOUT);
+        for (int s = 0; s < cut.stages; ++s)  // copies in flight land, or run out of time, before the CTA exits
+            for (int parity = 0; parity < 2; ++parity) mbar_wait(smem_u32(full + s), parity);
     }
 }
 
-template <bool F16, bool INTER>
-cudaError_t launch_pool(const RopeArgs& a, int grid, int tokens, cudaStream_t st)
+template <bool F16, bool INTER, int POOL>
+cudaError_t launch_one(const RopeArgs& a, const RopeCut& cut, int grid, cudaStream_t st)
 {
-    if (!a.k) return launch_pdl(rope_kernel<F16, INTER, 0>, grid, kRopeThreads, 0, st, a, tokens);
-    return a.Ks ? launch_pdl(rope_kernel<F16, INTER, 8>, grid, kRopeThreads, 0, st, a, tokens)
-                : launch_pdl(rope_kernel<F16, INTER, 16>, grid, kRopeThreads, 0, st, a, tokens);
+    return launch_pdl(rope_kernel<F16, INTER, POOL>, grid, kRopeThreads, kRopeSmem, st, a, cut);
+}
+
+template <bool F16, bool INTER>
+cudaError_t launch_pool(const RopeArgs& a, const RopeCut& cut, int grid, cudaStream_t st)
+{
+    if (!a.k) return launch_one<F16, INTER, 0>(a, cut, grid, st);
+    return a.Ks ? launch_one<F16, INTER, 8>(a, cut, grid, st) : launch_one<F16, INTER, 16>(a, cut, grid, st);
+}
+
+template <bool F16, bool INTER>
+cudaError_t setup_pools()
+{
+    const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+    cudaError_t e = cudaFuncSetAttribute(rope_kernel<F16, INTER, 0>, attr, kRopeSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(rope_kernel<F16, INTER, 8>, attr, kRopeSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(rope_kernel<F16, INTER, 16>, attr, kRopeSmem);
+    return e;
 }
 
 }  // namespace
+
+cudaError_t rope_setup()
+{
+    cudaError_t e = setup_pools<false, false>();
+    if (e == cudaSuccess) e = setup_pools<false, true>();
+    if (e == cudaSuccess) e = setup_pools<true, false>();
+    if (e == cudaSuccess) e = setup_pools<true, true>();
+    return e;
+}
 
 cudaError_t launch_rope(const RopeArgs& a, cudaStream_t st)
 {
     int sms = 0;
     const cudaError_t e = page_setup(&sms);
     if (e != cudaSuccess) return e;
-    // A CTA has so many tokens that a thread has its rows in one batch; fewer, where the SMs would not all have a CTA.
-    const int heads = (a.q ? a.H : 0) + (a.k ? 2 * a.Hkv : 0);
-    int tokens = kRopeTokens;
-    while (tokens > 1 && (tokens * heads > kBatch * kRopeThreads / 8 || a.T < 2 * sms * tokens)) tokens >>= 1;
-    const int grid = (a.T + tokens - 1) / tokens;
-    if (a.fp16) return a.interleaved ? launch_pool<true, true>(a, grid, tokens, st) : launch_pool<true, false>(a, grid, tokens, st);
-    return a.interleaved ? launch_pool<false, true>(a, grid, tokens, st) : launch_pool<false, false>(a, grid, tokens, st);
+    RopeCut cut;
+    cut.all = (a.q ? a.H : 0) + (a.k ? 2 * a.Hkv : 0);
+    // Items of as many rows as a ring takes, or of fewer (four are the lanes of a warp), where the warps would not all have one.
+    const int64_t warps = (int64_t)sms * kRopeWarps, wanted = (warps + a.T - 1) / a.T;
+    const int most = (int)std::min<int64_t>((cut.all + 3) / 4, std::max<int64_t>(wanted, (cut.all + kMostHeads - 1) / kMostHeads));
+    cut.heads = ((cut.all + most - 1) / most + 3) / 4 * 4;
+    cut.parts = (cut.all + cut.heads - 1) / cut.heads;
+    cut.stages = std::min(kMostStages, kRopeRing / kRopeWarps / (cut.heads * kRowBytes));
+    const int grid = (int)std::min<int64_t>(sms, (int64_t)a.T * cut.parts);
+    if (a.fp16) return a.interleaved ? launch_pool<true, true>(a, cut, grid, st) : launch_pool<true, false>(a, cut, grid, st);
+    return a.interleaved ? launch_pool<false, true>(a, cut, grid, st) : launch_pool<false, false>(a, cut, grid, st);
 }
 
 }  // namespace dkv

@@ -203,7 +203,7 @@ def lib(path: str | None = None):
     L.dkv_rotary_custom.restype = ctypes.c_int
     L.dkv_rotary_custom.argtypes = [RT, I32, I32, V, F64]
     L.dkv_rope.restype = ctypes.c_int
-    L.dkv_rope.argtypes = [RT, I32, I32, I32, V, I64, V, V, I64, V]
+    L.dkv_rope.argtypes = [RT, I32, I32, I32, V, I64, V, V, I64, V, V]
     L.dkv_rope_append.restype = ctypes.c_int
     L.dkv_rope_append.argtypes = [PG, I32, RT, I32, I32, V, V, I64, V, I64, V, V, I64, V, V, V, V, V, V, V, V, V]
     L.dkv_quant_compact.restype = ctypes.c_int
@@ -786,7 +786,7 @@ def _rotary_ref(rotary):
     return rotary.ref
 
 
-def dkv_rope(x, positions, rotary: Rotary, out, stream=None):
+def dkv_rope(x, positions, rotary: Rotary, out, status=None, stream=None):
     """Rows x [T][heads][128] turned by their positions (int32 [T]) -> out, of x's type and shape. Either may be a slice of a
     projection; out may be x."""
     half = _rows16(x, "x")
@@ -795,7 +795,7 @@ def dkv_rope(x, positions, rotary: Rotary, out, stream=None):
     xp, xs = _token_rows(x, "x", at, x.dtype, tokens, heads)
     op, os_ = _token_rows(out, "out", at, x.dtype, tokens, heads)
     _check(lib().dkv_rope(_rotary_ref(rotary), DKV_FP16 if half else DKV_BF16, tokens, heads, xp, xs,
-                          _on(positions, "positions", at, _torch().i32, tokens), op, os_, queue), "dkv_rope")
+                          _on(positions, "positions", at, _torch().i32, tokens), op, os_, _word(status, at), queue), "dkv_rope")
 
 
 def _scales(pages, at, Ks, Vs):

@@ -102,11 +102,12 @@ def test_bad_frequencies(dkv):
 
 def rope(dkv, rotary=None, **kw):
     r = rotary or dkv.dkv_rotary_make()
-    a = dict(dtype=0, T=4, heads=2, x=A, xs=256, pos=A, out=2 * A, os=256) | kw
-    return dkv.lib().dkv_rope(r.ref if r else None, a["dtype"], a["T"], a["heads"], a["x"], a["xs"], a["pos"], a["out"], a["os"], None)
+    a = dict(dtype=0, T=4, heads=2, x=A, xs=256, pos=A, out=2 * A, os=256, status=None) | kw
+    return dkv.lib().dkv_rope(r.ref if r else None, a["dtype"], a["T"], a["heads"], a["x"], a["xs"], a["pos"], a["out"], a["os"],
+                              a["status"], None)
 
 
-@pytest.mark.parametrize("kw", [dict(dtype=2), dict(T=-1), dict(heads=0), dict(T=1 << 30, heads=2), dict(x=None), dict(x=A + 8), dict(out=None),
+@pytest.mark.parametrize("kw", [dict(dtype=2), dict(T=-1), dict(heads=0), dict(status=A + 2), dict(T=1 << 30, heads=2), dict(x=None), dict(x=A + 8), dict(out=None),
                                 dict(pos=None), dict(pos=A + 2), dict(xs=128), dict(xs=260), dict(os=128), dict(xs=1 << 40),
                                 dict(out=A, os=512), dict(out=A + 256), dict(out=A - 256)])
 def test_rope_refuses(dkv, kw):
