@@ -69,15 +69,6 @@ cudaError_t launch_quant_attn(const QuantAttnArgs& a, bool short_boxes, cudaStre
 namespace dkv {
 namespace {
 
-// A value as it is held: what is not finite is NaN. `size`: |x|, or 0 for what is not finite.
-__device__ __forceinline__ float held(float x, float& size)
-{
-    const float y = fabsf(x);
-    const bool finite = y < INFINITY;
-    size = finite ? y : 0.f;
-    return finite ? x : __uint_as_float(0x7fffffffu);
-}
-
 // Scale byte u of a row whose largest element is `size`: the least e = u - 127 with size <= 448 2^e.
 // 448 = 1.75 2^8, so for size = 1.m 2^x it is x - 8, or one more where 1.m > 1.75.
 __device__ __forceinline__ uint32_t scale_byte(float size)
@@ -95,6 +86,7 @@ __device__ __forceinline__ float inverse_scale(uint32_t u) { return __uint_as_fl
 // scale byte. All lanes of the warp.
 template <bool F16>
 __device__ __forceinline__ uint4 hold_lane(const uint32_t (&w)[8], uint32_t& u);
+__device__ __forceinline__ uint4 hold_lane(const float (&x)[16], uint32_t& u);  // the same of 32-bit values
 
 // Four e4m3 values, the first in the lowest byte.
 __device__ __forceinline__ uint32_t pack_e4m3(float x0, float x1, float x2, float x3)
@@ -154,17 +146,32 @@ __device__ __forceinline__ uint4 hold_lane(const uint32_t (&w)[8], uint32_t& u)
                                    __uint_as_float(y[2 * i + 1] & 0xffff0000u));
         return v;
     }
-    float f[16], most = 0.f;
+    float f[16];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         f[2 * i] = F16 ? __half2float(__ushort_as_half((uint16_t)w[i])) : __uint_as_float(w[i] << 16);
         f[2 * i + 1] = F16 ? __half2float(__ushort_as_half((uint16_t)(w[i] >> 16))) : __uint_as_float(w[i] & 0xffff0000u);
     }
+    return hold_lane(f, u);
+}
+
+__device__ __forceinline__ uint4 hold_lane(const float (&x)[16], uint32_t& u)
+{
+    float f[16], most = 0.f, odd = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        float s;
-        f[i] = held(f[i], s);
-        most = fmaxf(most, s);
+        f[i] = x[i];
+        most = fmaxf(most, fabsf(x[i]));
+        odd = fmaf(x[i], 0.f, odd);  // NaN if any is not finite
+    }
+    if (__any_sync(0xffffffffu, odd != odd)) {  // those are NaN, and the scale goes by the others
+        most = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const bool finite = fabsf(x[i]) < INFINITY;
+            most = fmaxf(most, finite ? fabsf(x[i]) : 0.f);
+            if (!finite) f[i] = __uint_as_float(0x7fffffffu);
+        }
     }
 #pragma unroll
     for (int o = 1; o < 8; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));

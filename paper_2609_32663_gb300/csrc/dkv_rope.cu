@@ -76,6 +76,20 @@ struct RopeCut {
     int all, parts, heads, stages;
 };
 
+// Part `part` of token t. Items lie part after part, so that a warp has some of every part (those of k and v cost more).
+struct Item {
+    int t, part;
+    __device__ __forceinline__ void advance(int by_t, int by_part, int tokens)
+    {
+        t += by_t;
+        part += by_part;
+        if (t >= tokens) {
+            t -= tokens;
+            ++part;
+        }
+    }
+};
+
 // POOL: bits of an element of the pools; 0: no k and v.
 template <bool F16, bool INTER, int POOL>
 __global__ void __launch_bounds__(kRopeThreads, 1) rope_kernel(const __grid_constant__ RopeArgs a, const RopeCut cut)
@@ -113,21 +127,17 @@ __global__ void __launch_bounds__(kRopeThreads, 1) rope_kernel(const __grid_cons
         }
         tokens = cu[a.B];
     }
-    const int64_t items = (int64_t)tokens * cut.parts, stride = (int64_t)gridDim.x * kRopeWarps;
-    const int64_t first = (int64_t)blockIdx.x + (int64_t)gridDim.x * warp;  // a few items lie in as many SMs
-    if (first >= items) return;
+    if (tokens <= 0) return;
+    // Every n-th item from the first on; a few lie in as many SMs. (There are fewer than 2^31, see tokens_ok.)
+    const int first = blockIdx.x + gridDim.x * warp, stride = gridDim.x * kRopeWarps, by_part = stride / tokens, by_t = stride - by_part * tokens;
+    Item now{first % tokens, first / tokens};
+    if (now.part >= cut.parts) return;
     const int stage_bytes = cut.heads * kRowBytes;
     const uint64_t pol = evict_first_policy();
-    // Rows [h0, h1) of token t, heads of q, then of k, then of v.
-    auto split = [&](int64_t item, int& t, int& h0, int& h1) {
-        t = cut.parts == 1 ? (int)item : (int)(item / cut.parts);
-        h0 = (int)(item - (int64_t)t * cut.parts) * cut.heads;
-        h1 = min(h0 + cut.heads, cut.all);
-    };
-    auto fetch = [&](int64_t item, int stage) {
-        if (item >= items) return;
-        int t, h0, h1;
-        split(item, t, h0, h1);
+    // Rows [h0, h1) of an item: heads of q, then of k, then of v.
+    auto fetch = [&](const Item& x, int stage) {
+        if (x.part >= cut.parts) return;
+        const int t = x.t, h0 = x.part * cut.heads, h1 = min(h0 + cut.heads, cut.all);
         if (lane == 0) {
             const uint32_t bar = smem_u32(full + stage), dst = smem_u32(ring) + stage * stage_bytes;
             mbar_arrive_expect_tx(bar, (h1 - h0) * kRowBytes);
@@ -143,13 +153,11 @@ __global__ void __launch_bounds__(kRopeThreads, 1) rope_kernel(const __grid_cons
         __syncwarp();
     };
     // Lane x: the place in its slab of row x of an item, if that is one of k or v (-1: none).
-    auto place = [&](int64_t item, int64_t& entry) {
+    auto place = [&](const Item& x, int64_t& entry) {
         entry = 0;
-        if (!POOL || item >= items) return -1;
-        int t, h0, h1;
-        split(item, t, h0, h1);
-        const int h = h0 + lane;
-        if (h < qheads || h >= h1) return -1;
+        if (!POOL || x.part >= cut.parts) return -1;
+        const int t = x.t, h = x.part * cut.heads + lane;
+        if (h < qheads || h >= min((x.part + 1) * cut.heads, cut.all)) return -1;
         int b = 0, hi = a.B - 1;  // the last sequence that starts at t or before
         while (b < hi) {
             const int mid = (b + hi + 1) >> 1;
@@ -168,25 +176,28 @@ __global__ void __launch_bounds__(kRopeThreads, 1) rope_kernel(const __grid_cons
         return r;
     };
     static_assert(kMostHeads <= 32, "a lane each");
-    for (int s = 0; s < cut.stages; ++s) fetch(first + s * stride, s);
+    Item ahead = now;
+    for (int s = 0; s < cut.stages; ++s) {
+        fetch(ahead, s);
+        ahead.advance(by_t, by_part, tokens);
+    }
     int64_t entry;
-    int pos = pairs ? a.positions[cut.parts == 1 ? first : first / cut.parts] : 0, row = place(first, entry), stage = 0;
+    int pos = pairs ? a.positions[now.t] : 0, row = place(now, entry), stage = 0;
     uint32_t phase = 0;
     bool ok = true;
 #pragma unroll 1
-    for (int64_t item = first; item < items; item += stride) {
-        int t, h0, h1;
-        split(item, t, h0, h1);
+    while (now.part < cut.parts) {
+        const int t = now.t, h0 = now.part * cut.heads, h1 = min(h0 + cut.heads, cut.all);
         int page = -1;
         if (POOL && row >= 0) {
             page = in_bounds(row >> log_P < a.max_pages, a.status) ? a.table[entry + (row >> log_P)] : -1;
             row &= a.P - 1;
         }
         for (int i = lane; i < pairs; i += 32) cs[i] = turn(a.turns[i] * (uint64_t)(int64_t)pos, a.magnitude);
-        const int64_t next = item + stride;
         const int place0 = row;
-        if (pairs && next < items) pos = a.positions[cut.parts == 1 ? next : next / cut.parts];
-        row = place(next, entry);
+        now.advance(by_t, by_part, tokens);
+        if (pairs && now.part < cut.parts) pos = a.positions[now.t];
+        row = place(now, entry);
         int64_t at = -1;  // the pool row
         if (POOL && h0 + lane >= qheads && h0 + lane < h1) {
             if (page >= 0 && page < a.num_pages)
@@ -219,71 +230,64 @@ __global__ void __launch_bounds__(kRopeThreads, 1) rope_kernel(const __grid_cons
             const uint4 lo = *reinterpret_cast<const uint4*>(rows + min(x, cut.heads - 1) * kRowBytes + chunk0 * 16),
                         hi = *reinterpret_cast<const uint4*>(rows + min(x, cut.heads - 1) * kRowBytes + chunk1 * 16);
             uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+            const int64_t to = POOL ? __shfl_sync(kFull, at, min(x, 31)) : -1;
+            const bool turns = __any_sync(kFull, some && key && turned);
             float f[16];
-            if (turned && key) {
+            if (turns) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float2 v = widen16<F16>(w[i]);
                     f[2 * i] = v.x;
                     f[2 * i + 1] = v.y;
                 }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int p = INTER ? 2 * i : i, q = INTER ? 2 * i + 1 : i + 8;
-                    const float u = f[p], v = f[q];
-                    f[p] = fmaf(u, c[i], -v * s[i]);
-                    f[q] = fmaf(v, c[i], u * s[i]);
-                }
-            }
-            if (POOL != 8 || !pooled) {
                 if (turned && key) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i] = narrow16<F16>(f[2 * i], f[2 * i + 1]);
+                    for (int i = 0; i < 8; ++i) {
+                        const int p = INTER ? 2 * i : i, q = INTER ? 2 * i + 1 : i + 8;
+                        const float u = f[p], v = f[q];
+                        f[p] = fmaf(u, c[i], -v * s[i]);
+                        f[q] = fmaf(v, c[i], u * s[i]);
+                    }
+                    if (POOL != 8 || !pooled) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) w[i] = narrow16<F16>(f[2 * i], f[2 * i + 1]);
+                    }
                 }
             }
-            if (some && !pooled) {
+            if (some && !(POOL && pooled)) {
                 uint4* dst = reinterpret_cast<uint4*>(out + (int64_t)h * kHeadDim);
                 dst[chunk0] = make_uint4(w[0], w[1], w[2], w[3]);
                 dst[chunk1] = make_uint4(w[4], w[5], w[6], w[7]);
             }
-            if (POOL == 0 || !__any_sync(kFull, pooled)) continue;
-            const int64_t to = __shfl_sync(kFull, at, min(x, 31));
-            if (POOL == 16) {
+            if (POOL == 16 && pooled && to >= 0) {
+                uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(key ? a.Kp : a.Vp) + to * kHeadDim);
+                dst[chunk0] = make_uint4(w[0], w[1], w[2], w[3]);
+                dst[chunk1] = make_uint4(w[4], w[5], w[6], w[7]);
+            }
+            if (POOL == 8 && __any_sync(kFull, pooled)) {
+                uint4 v;
+                uint32_t u;
+                if (!__any_sync(kFull, pooled && !(key && turns))) {
+                    v = hold_lane(f, u);
+                } else {
+                    v = hold_lane<F16>(w, u);
+                    if (turns) {  // rows of both kinds
+                        uint32_t u1;
+                        const uint4 v1 = hold_lane(f, u1);
+                        if (key) v = v1, u = u1;
+                    }
+                }
                 if (pooled && to >= 0) {
-                    uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(key ? a.Kp : a.Vp) + to * kHeadDim);
-                    dst[chunk0] = make_uint4(w[0], w[1], w[2], w[3]);
-                    dst[chunk1] = make_uint4(w[4], w[5], w[6], w[7]);
+                    uint2* dst = reinterpret_cast<uint2*>(static_cast<uint8_t*>(key ? a.Kp : a.Vp) + to * kHeadDim);
+                    dst[chunk0] = make_uint2(v.x, v.y);
+                    dst[chunk1] = make_uint2(v.z, v.w);
+                    if (sub == 0) (key ? a.Ks : a.Vs)[to] = (uint8_t)u;
                 }
-                continue;
-            }
-            if (!(turned && key)) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float2 v = widen16<F16>(w[i]);
-                    f[2 * i] = v.x;
-                    f[2 * i + 1] = v.y;
-                }
-            }
-            float most = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float size;
-                f[i] = held(f[i], size);
-                most = fmaxf(most, size);
-            }
-#pragma unroll
-            for (int o = 1; o < 8; o <<= 1) most = fmaxf(most, __shfl_xor_sync(kFull, most, o));
-            const uint32_t u = scale_byte(most);
-            const float z = inverse_scale(u);
-            if (pooled && to >= 0) {
-                uint2* dst = reinterpret_cast<uint2*>(static_cast<uint8_t*>(key ? a.Kp : a.Vp) + to * kHeadDim);
-                dst[chunk0] = make_uint2(pack_e4m3(f[0] * z, f[1] * z, f[2] * z, f[3] * z), pack_e4m3(f[4] * z, f[5] * z, f[6] * z, f[7] * z));
-                dst[chunk1] = make_uint2(pack_e4m3(f[8] * z, f[9] * z, f[10] * z, f[11] * z), pack_e4m3(f[12] * z, f[13] * z, f[14] * z, f[15] * z));
-                if (sub == 0) (key ? a.Ks : a.Vs)[to] = (uint8_t)u;
             }
         }
         __syncwarp();  // the stage, and cos and sin, are read
-        fetch(item + cut.stages * stride, stage);
+        fetch(ahead, stage);
+        ahead.advance(by_t, by_part, tokens);
         if (++stage == cut.stages) {
             stage = 0;
             phase ^= 1;
