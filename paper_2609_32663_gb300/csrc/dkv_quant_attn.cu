@@ -2,9 +2,9 @@
 // per query head, to the first len - n + i + 1 rows of its slab (causal) or to all len rows,
 //   o = sum_r softmax_r(scale 2^ek_r q.k_r) 2^ev_r v_r,   k_r, v_r e4m3 values, 2^ek_r, 2^ev_r their rows' scales.
 //
-// Unit of work: 16 columns (token x head of the group, column = token G + head) of one sequence and KV
+// Unit of work: the columns (token x head of the group, column = token G + head; at most 8, or 16) of one sequence and KV
 // head, against the cache rows that its last token sees, in tiles of 32 rows. All (unit, tile) pairs,
-// unit after unit, are cut into contiguous equal shares, one a CTA, one CTA an SM; a CTA's 8 warps take the tiles
+// unit after unit, are cut into contiguous equal shares, one a CTA, one CTA an SM; a CTA's warps take the tiles
 // of its part of a unit in turn, each through a ring of its own, and are joined at its end. A unit that
 // lies in several CTAs is joined by the one that finishes last.
 //
@@ -33,12 +33,6 @@
 namespace dkv {
 namespace {
 
-#ifndef QW
-#define QW 12
-#endif
-#ifndef QLEAST
-#define QLEAST 8
-#endif
 constexpr int kMostCols = 16;              // columns of a unit, at most
 constexpr int kRows = 32;                  // cache rows of a tile
 constexpr int kTileBytes = kRows * kHeadDim;
@@ -50,9 +44,9 @@ constexpr float kShift = 7.f;              // weights for the second product are
 template <int Z>
 struct Cfg {
     static constexpr int kCols = 8 * Z;
-    static constexpr int kWarps = Z == 1 ? QW : 8;
+    static constexpr int kWarps = Z == 1 ? 12 : 8;
     static constexpr int kThreads = 32 * kWarps;
-    static constexpr int kStages = Z == 1 && QW > 8 ? 2 : 3;  // ring of a warp
+    static constexpr int kStages = Z == 1 ? 2 : 3;  // ring of a warp
     // Shared memory, from its 1024-byte aligned start.
     static constexpr int kOffSum = kWarps * kStages * kStageBytes;            // float[kWarps][kCols][64], before that State[kWarps][kCols]
     static constexpr int kOffScales = kOffSum + kWarps * kCols * 64 * 4;      // a stage's scale bytes: of K, of V
@@ -111,44 +105,39 @@ __device__ __forceinline__ int slab_len(const QuantAttnArgs& a, int h)
 // Rows that token i of n sees.
 __device__ __forceinline__ int sees(const QuantAttnArgs& a, int len, int n, int i) { return a.causal ? min(max(len - n + i + 1, 0), len) : len; }
 
-template <int Z>
-__device__ __forceinline__ int blocks_of(const QuantAttnArgs& a, int n) { return (int)(((int64_t)n * a.G + 8 * Z - 1) / (8 * Z)); }
-
-// Cache rows, and tiles, of block i of n tokens over a slab of len rows.
-template <int Z>
-__device__ __forceinline__ int block_rows(const QuantAttnArgs& a, int len, int n, int i)
-{
-    return sees(a, len, n, min(n, (int)((i * (int64_t)(8 * Z) + 8 * Z - 1) / a.G + 1)) - 1);
-}
 __device__ __forceinline__ int tiles_of(int rows) { return max(1, (int)(((unsigned)rows + kRows - 1) / kRows)); }
 
-__global__ void __launch_bounds__(512) quant_begin_kernel(const __grid_constant__ QuantAttnArgs a, const __grid_constant__ QuantWork w)
+// Tiles of slab h's unit.
+__device__ __forceinline__ int slab_tiles(const QuantAttnArgs& a, int h)
 {
-    const int tid = threadIdx.x;
+    const int n = tokens_of(a, h / a.Hkv);
+    return n == 0 ? 0 : tiles_of(sees(a, slab_len(a, h), n, n - 1));
+}
+
+// Clears the counters of both kernels. `early`: the next kernel waits for this one before it reads anything; else it
+// does only for the counters, and starts once every kernel before this one has completed.
+__global__ void __launch_bounds__(256) quant_begin_kernel(const __grid_constant__ QuantWork w, int early)
+{
+    if (early) pdl_launch_dependents();
     pdl_wait();
-    pdl_launch_dependents();
-    if (tid < kMaxCtas) w.done[tid] = 0;
-    if (tid < kChunkCounters) w.chunk[tid] = 0;
-    static_assert(kMaxSlots <= 512 && kChunkCounters <= 512, "a thread each");
-    if (tid < a.B && (bad_offsets(a, tid) || cu_at(a, tid + 1) - cu_at(a, tid) > a.most)) report(a, DKV_DEV_PAGE_RANGE);
-    for (int h = tid; h < a.B * a.Hkv; h += 512) {
+    if (!early) pdl_launch_dependents();
+    for (int i = threadIdx.x; i < kMaxCtas; i += 256) w.done[i] = 0;
+    for (int i = threadIdx.x; i < kChunkCounters; i += 256) w.chunk[i] = 0;
+}
+
+// Reports what lives on the device and is out of range (one CTA).
+__device__ __forceinline__ void check(const QuantAttnArgs& a)
+{
+    for (int b = threadIdx.x; b < a.B; b += blockDim.x)
+        if (bad_offsets(a, b) || cu_at(a, b + 1) - cu_at(a, b) > a.most) report(a, DKV_DEV_PAGE_RANGE);
+    for (int h = threadIdx.x; h < a.B * a.Hkv; h += blockDim.x) {
         const int b = h / a.Hkv;
         if (cu_at(a, b + 1) > cu_at(a, b) && a.len[h] != slab_len(a, h)) report(a, DKV_DEV_PAGE_RANGE);
     }
 }
 
 // ---------------------------------------------------------------- schedule
-template <int Z>
-__device__ __forceinline__ int64_t slab_tiles(const QuantAttnArgs& a, int h)
-{
-    const int n = tokens_of(a, h / a.Hkv), len = slab_len(a, h);
-    int64_t sum = 0;
-#pragma unroll 1
-    for (int i = 0, nb = blocks_of<Z>(a, n); i < nb; ++i) sum += tiles_of(block_rows<Z>(a, len, n, i));
-    return sum;
-}
-
-constexpr int kLeast = QLEAST;  // tiles of a share, where there are so many: its warps take them side by side
+constexpr int kLeast = 8;  // tiles of a share, where there are so many: its warps take them side by side
 struct Extent {
     int64_t tiles;
     int parts;
@@ -174,7 +163,7 @@ __device__ __forceinline__ Extent count_tiles(const QuantAttnArgs& a, int64_t* b
     for (int x = g0; x < g1; ++x) {
         before[x] = mine;
 #pragma unroll 1
-        for (int h = x * group; h < min(slabs, (x + 1) * group); ++h) mine += slab_tiles<Z>(a, h);
+        for (int h = x * group; h < min(slabs, (x + 1) * group); ++h) mine += slab_tiles(a, h);
     }
     int64_t up = mine;
 #pragma unroll
@@ -200,14 +189,14 @@ __device__ __forceinline__ Extent count_tiles(const QuantAttnArgs& a, int64_t* b
 }
 
 // The share of one CTA, unit by unit.
-template <int Z>
 struct Walk {
-    int b, g, i, t, n, len;    // sequence, head, block; the sequence's first token, its tokens, the slab's rows
+    int b, g, t, n, len;       // sequence, head; the sequence's first token, its tokens, the slab's rows
     int rows, tiles, j0, j1;   // of the unit; the CTA's tiles of it
     int64_t start, end;        // of the unit, of the share
     __device__ __forceinline__ void enter(const QuantAttnArgs& a, int64_t off)
     {
-        rows = block_rows<Z>(a, len, n, i);
+        len = slab_len(a, b * a.Hkv + g);
+        rows = sees(a, len, n, n - 1);
         tiles = tiles_of(rows);
         j0 = (int)off;
         j1 = (int)min((int64_t)tiles, end - start);
@@ -221,23 +210,18 @@ struct Walk {
     __device__ __forceinline__ void next(const QuantAttnArgs& a)
     {
         start += tiles;
-        if (++i >= blocks_of<Z>(a, n)) {
-            i = 0;
-            if (++g == a.Hkv) {
-                g = 0;
-                do ++b;
-                while (b < a.B - 1 && tokens_of(a, b) == 0);
-                sequence(a);
-            }
-            len = slab_len(a, b * a.Hkv + g);
+        if (++g == a.Hkv) {
+            g = 0;
+            do ++b;
+            while (b < a.B - 1 && tokens_of(a, b) == 0);
+            sequence(a);
         }
         enter(a, 0);
     }
     __device__ __forceinline__ bool whole() const { return j0 == 0 && j1 == tiles; }
 };
 
-template <int Z>
-__device__ __forceinline__ void seek(const QuantAttnArgs& a, const Extent& e, const int64_t* before, int group, int c, Walk<Z>& k)
+__device__ __forceinline__ void seek(const QuantAttnArgs& a, const Extent& e, const int64_t* before, int group, int c, Walk& k)
 {
     const int64_t pos = share_start(e, c);
     k.end = share_start(e, c + 1);
@@ -252,14 +236,10 @@ __device__ __forceinline__ void seek(const QuantAttnArgs& a, const Extent& e, co
     int64_t off = pos - before[lo];
     int h = lo * group;
     if (group > 1)
-        for (int64_t x; off >= (x = slab_tiles<Z>(a, h)); ++h) off -= x;
+        for (int x; off >= (x = slab_tiles(a, h)); ++h) off -= x;
     k.b = h / a.Hkv;
     k.g = h - k.b * a.Hkv;
     k.sequence(a);
-    k.len = slab_len(a, h);
-    k.i = 0;
-#pragma unroll 1
-    for (int x; off >= (x = tiles_of(block_rows<Z>(a, k.len, k.n, k.i))); ++k.i) off -= x;
     k.start = pos - off;
     k.enter(a, off);
 }
@@ -292,14 +272,18 @@ __device__ __forceinline__ uint4 lds128(const unsigned char* p)
     return v;
 }
 
-// A lane's half of a column of q (elements 32 t .. 32 t + 31 of 128) as fp16 pairs, scaled by a power of two that
-// takes the column's largest element to 2^14 .. 2^15; `back`: its inverse.
-template <bool F16>
-__device__ __forceinline__ void load_column(const uint16_t* src, bool live, uint32_t (&q)[16], float& back)
+// A lane's quarter of a column of q (elements 32 t .. 32 t + 31 of 128), zeros if there is none.
+__device__ __forceinline__ void load_column(const uint16_t* src, bool live, uint4 (&x)[4])
 {
-    uint4 x[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = live ? ld_prev(reinterpret_cast<const uint4*>(src) + i) : make_uint4(0u, 0u, 0u, 0u);
+}
+
+// The same as fp16 pairs, scaled by a power of two that takes the column's largest element to 2^14 .. 2^15; `back`: its
+// inverse.
+template <bool F16>
+__device__ __forceinline__ void scale_column(const uint4 (&x)[4], uint32_t (&q)[16], float& back)
+{
     float f[32], most = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -533,7 +517,8 @@ __device__ __forceinline__ int64_t piece_at(int c0, int k) { return (int64_t)(c0
 
 template <bool F16, int Z>
 __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
-    quant_attn_kernel(const __grid_constant__ QuantAttnArgs a, const __grid_constant__ CacheMaps maps, const __grid_constant__ QuantWork w, int nctas)
+    quant_attn_kernel(const __grid_constant__ QuantAttnArgs a, const __grid_constant__ CacheMaps maps, const __grid_constant__ QuantWork w, int nctas,
+                      int alone)
 {
     using C = Cfg<Z>;
     constexpr int kWarps = C::kWarps, kStages = C::kStages, kCols = C::kCols;
@@ -554,22 +539,35 @@ __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
         for (int s = 0; s < kStages; ++s) mbar_init(smem_u32(full + s), 1);
     if (tid == 0) misc[0] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    // What the kernels before the begin kernel wrote may be read (it started after they had completed, and
-    // this one after that); the fence drops what this SM's L1 holds from before. The counters may not, before pdl_wait().
+    // alone: this kernel was started before the ones before it had completed, and waits for them (and the begin
+    // kernel). Else it follows the kernel of many tokens, which started after the ones before the call had: what they
+    // wrote may be read, and the wait is for the counters. The fence drops what this SM's L1 holds from before.
+    if (alone) pdl_wait();
     asm volatile("fence.acq_rel.gpu;" ::: "memory");
     pdl_launch_dependents();
+    if (c == nctas - 1) check(a);
     int group;
     const Extent head = count_tiles<Z>(a, reinterpret_cast<int64_t*>(sm), reinterpret_cast<int64_t*>(sm + C::kOffSum), nctas, group);
     if (c < head.parts) {
-        Walk<Z> k;
+        Walk k;
         seek(a, head, reinterpret_cast<const int64_t*>(sm), group, c, k);
         fence_proxy_async_smem();  // the sums of tiles lie in the rings, which the copies write next
         __syncthreads();
-        Walk<Z> f = k;              // ahead of k by the ring's stages
+        Walk f = k;              // ahead of k by the ring's stages
         int fj = f.j0 + warp, stage = 0, used = 0, fetched = 0, rows0 = 0, rows1 = 0, ahead = 0;  // ahead: tiles of f since its pages were read
         bool left = true, ok = true;
         const uint64_t pol = evict_first_policy();
         const int log_P = 31 - __clz(a.P), box = min(a.P, kRows);
+        uint4 qx[Z][4];  // the unit's columns as they lie in memory
+        auto load_q = [&] {
+#pragma unroll
+            for (int z = 0; z < Z; ++z) {
+                const int x = 8 * z + g, token = x / a.G, j = x - token * a.G;
+                const bool live = token < k.n && in_bounds(k.t + token < a.T && k.g * a.G + j < a.H, a.status);
+                load_column(a.q + (int64_t)(k.t + token) * a.q_stride + (k.g * a.G + j) * kHeadDim + 32 * t, live, qx[z]);
+            }
+        };
+        load_q();
         // The next tile on its way. Each lane knows the pool rows of one of the next 32 tiles (of its two halves, where pages have
         // 16 rows); a bad page's are behind the pool, from where zeros come.
         auto fetch = [&] {
@@ -623,8 +621,7 @@ __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
         uint32_t phases = 0;  // bit s: the parity of stage s's next tile
 #pragma unroll 1
         for (;;) {
-            // The unit's columns of this lane.
-            const int col0 = k.i * kCols, cols = min((int64_t)kCols, (int64_t)k.n * a.G - col0);
+            const int cols = k.n * a.G;
             Acc<Z> acc;
             uint32_t q[Z][16];
             float cs[Z][2];
@@ -632,15 +629,13 @@ __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
             acc.scale = 0;
 #pragma unroll
             for (int z = 0; z < Z; ++z) {
-                const int x = 8 * z + g, token = (col0 + x) / a.G, j = col0 + x - token * a.G;
-                const bool live = x < cols && in_bounds(k.t + token < a.T && k.g * a.G + j < a.H, a.status);
                 float back;  // (of column g)
-                load_column<F16>(a.q + (int64_t)(k.t + token) * a.q_stride + (k.g * a.G + j) * kHeadDim + 32 * t, live, q[z], back);
+                scale_column<F16>(qx[z], q[z], back);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int y = 8 * z + 2 * t + e;
                     cs[z][e] = __shfl_sync(kFull, back, 8 * t + 4 * e) * a.qscale;
-                    lim[z][e] = y < cols ? sees(a, k.len, k.n, (col0 + y) / a.G) : k.rows;
+                    lim[z][e] = y < cols ? sees(a, k.len, k.n, y / a.G) : k.rows;
                     acc.top[z][e] = -INFINITY;
                     acc.l[z][e] = 0.f;
                 }
@@ -651,7 +646,7 @@ __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
                 for (int z = 0; z < Z; ++z)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc.o[i][z][e] = 0.f;
-            const int shown = sees(a, k.len, k.n, col0 / a.G);
+            const int shown = sees(a, k.len, k.n, 0);
 #pragma unroll 1
             for (int j = k.j0 + warp; j < k.j1; j += kWarps) {
                 if (ok && !__all_sync(kFull, mbar_wait(smem_u32(full + at_stage), (phases >> at_stage) & 1))) {
@@ -711,7 +706,7 @@ __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) f0[z][e] = factor(acc.top[z][e] * cs[z][e], f0[z][e]) * ex2((float)acc.scale - total.scale);
             const bool whole = k.whole(), live = mine < cols && !aborted;
-            const int token = (col0 + mine) / a.G, head_j = col0 + mine - token * a.G;
+            const int token = mine / a.G, head_j = mine - token * a.G;
             uint16_t* out = a.out + ((int64_t)(k.t + token) * a.H + k.g * a.G + head_j) * kHeadDim;
             const int64_t slot = (int64_t)c * 2 + (k.j0 == 0);
             const float z = final_scale(total.scale, total.sum);
@@ -760,7 +755,7 @@ __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
                 if (misc[1] && mine < cols && in_bounds(c0 >= 0 && c0 + pieces <= nctas, a.status)) {
                     // kJoin pieces on the way at once, in the order of the CTAs.
                     __threadfence();
-                    constexpr int kJoin = Z == 1 ? 4 : 8;
+                    constexpr int kJoin = 8;
                     State all{-INFINITY, 0.f, 0.f, 0.f};
                     float4 v[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
 #pragma unroll 1
@@ -803,6 +798,7 @@ __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
             __syncthreads();  // sums and misc[1] are read
             if (!k.more()) break;
             k.next(a);
+            load_q();
         }
         // Copies in flight land (or run out of time) before the CTA exits.
         for (; used < fetched; ++used) {
@@ -851,11 +847,11 @@ cudaError_t setup_few()
 }
 
 template <bool F16>
-cudaError_t launch_few(const QuantAttnArgs& a, const CacheMaps& maps, const QuantWork& w, int nctas, cudaStream_t st)
+cudaError_t launch_few(const QuantAttnArgs& a, const CacheMaps& maps, const QuantWork& w, int nctas, int alone, cudaStream_t st)
 {
     if (a.few * a.G <= Cfg<1>::kCols)
-        return launch_pdl(quant_attn_kernel<F16, 1>, nctas, Cfg<1>::kThreads, Cfg<1>::kSmemBytes, st, a, maps, w, nctas);
-    return launch_pdl(quant_attn_kernel<F16, 2>, nctas, Cfg<2>::kThreads, Cfg<2>::kSmemBytes, st, a, maps, w, nctas);
+        return launch_pdl(quant_attn_kernel<F16, 1>, nctas, Cfg<1>::kThreads, Cfg<1>::kSmemBytes, st, a, maps, w, nctas, alone);
+    return launch_pdl(quant_attn_kernel<F16, 2>, nctas, Cfg<2>::kThreads, Cfg<2>::kSmemBytes, st, a, maps, w, nctas, alone);
 }
 
 }  // namespace
@@ -888,8 +884,9 @@ cudaError_t launch_quant_attn(const QuantAttnArgs& a, bool short_boxes, cudaStre
     w.chunk = reinterpret_cast<int32_t*>(base + kWorkBytes);
     QuantAttnArgs few = a;
     few.few = std::min(a.most, kMostCols / a.G);
-    if ((e = launch_pdl(quant_begin_kernel, 1, 512, 0, st, few, w)) != cudaSuccess) return e;
-    if (a.most > few.few) {
+    const int alone = a.most <= few.few;
+    if ((e = launch_pdl(quant_begin_kernel, 1, 256, 0, st, w, alone)) != cudaSuccess) return e;
+    if (!alone) {
         ChunkArgs c{};
         c.q = a.q;
         c.q_stride = a.q_stride;
@@ -918,7 +915,7 @@ cudaError_t launch_quant_attn(const QuantAttnArgs& a, bool short_boxes, cudaStre
         c.most = a.most;
         if ((e = launch_chunk8(c, nctas, short_boxes, st)) != cudaSuccess) return e;
     }
-    return a.fp16 ? launch_few<true>(few, maps, w, nctas, st) : launch_few<false>(few, maps, w, nctas, st);
+    return a.fp16 ? launch_few<true>(few, maps, w, nctas, alone, st) : launch_few<false>(few, maps, w, nctas, alone, st);
 }
 
 }  // namespace dkv

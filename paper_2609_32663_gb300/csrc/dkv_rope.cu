@@ -33,6 +33,7 @@ constexpr int kRopeRing = 192 * 1024;
 // Shared memory: the rings, then a warp's (cos, sin) of its item's pairs, its barriers, and the token offsets.
 constexpr int kOffTurns = kRopeRing, kOffRopeBars = kOffTurns + kRopeWarps * 64 * 8, kOffCu = kOffRopeBars + kRopeWarps * kMostStages * 8,
               kRopeSmem = kOffCu + (kMaxSlots + 1) * 4;
+static_assert(kRopeRing % (kRopeWarps * kRowBytes) == 0, "a warp's ring starts on a row's alignment");
 static_assert(kRopeSmem <= 227 * 1024 && kRopeWarps * 2 * kMostHeads * kRowBytes <= kRopeRing, "fits one CTA, two stages a warp");
 
 template <bool F16>
