@@ -107,11 +107,13 @@ __device__ __forceinline__ int sees(const QuantAttnArgs& a, int len, int n, int 
 
 __device__ __forceinline__ int tiles_of(int rows) { return max(1, (int)(((unsigned)rows + kRows - 1) / kRows)); }
 
-// Tiles of slab h's unit.
-__device__ __forceinline__ int slab_tiles(const QuantAttnArgs& a, int h)
+// What slab h's unit costs: its tiles, and as much as kStart of them for its start (the join of the warps, a fence, a count:
+// 3 us, in which a CTA has its share of 16 tiles from memory).
+constexpr int kStart = 16;
+__device__ __forceinline__ int slab_cost(const QuantAttnArgs& a, int h)
 {
-    const int n = tokens_of(a, h / a.Hkv);
-    return n == 0 ? 0 : tiles_of(sees(a, slab_len(a, h), n, n - 1));
+    const int n = tokens_of(a, h / a.Hkv), len = slab_len(a, h);  // (both loads at once)
+    return n == 0 ? 0 : kStart + tiles_of(sees(a, len, n, n - 1));
 }
 
 // Clears the counters of both kernels. `early`: the next kernel waits for this one before it reads anything; else it
@@ -137,21 +139,23 @@ __device__ __forceinline__ void check(const QuantAttnArgs& a)
 }
 
 // ---------------------------------------------------------------- schedule
-constexpr int kLeast = 8;  // tiles of a share, where there are so many: its warps take them side by side
+// Units lie end to end on a line of costs, kStart before the tiles of each; a tile is the CTA's in whose part of the line it
+// lies. Shares are not shorter than kLeast, where a CTA's warps would not all have a tile.
+constexpr int kLeast = 8;
 struct Extent {
-    int64_t tiles;
+    int64_t cost;
     int parts;
 };
 __device__ __forceinline__ int64_t divide(int64_t x, int64_t y)
 {
     return x <= UINT32_MAX && y <= UINT32_MAX ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
 }
-__device__ __forceinline__ int64_t share_start(const Extent& e, int c) { return divide(e.tiles * c, e.parts); }
-__device__ __forceinline__ int cta_of(const Extent& e, int64_t x) { return (int)divide((x + 1) * e.parts - 1, e.tiles); }
+__device__ __forceinline__ int64_t share_start(const Extent& e, int c) { return divide(e.cost * c, e.parts); }
+__device__ __forceinline__ int cta_of(const Extent& e, int64_t x) { return (int)divide((x + 1) * e.parts - 1, e.cost); }
 
-// All threads of the CTA: the tiles before every slab (or group of slabs, where there are more than fit), into `before`.
+// All threads of the CTA: the cost before every slab (or group of slabs, where there are more than fit), into `before`.
 template <int Z>
-__device__ __forceinline__ Extent count_tiles(const QuantAttnArgs& a, int64_t* before, int64_t* sums, int nctas, int& group)
+__device__ __forceinline__ Extent count_cost(const QuantAttnArgs& a, int64_t* before, int64_t* sums, int nctas, int& group)
 {
     constexpr int kMaxGroups = Cfg<Z>::kMaxGroups, kThreads = Cfg<Z>::kThreads, kWarps = Cfg<Z>::kWarps;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, slabs = a.B * a.Hkv;
@@ -163,7 +167,7 @@ __device__ __forceinline__ Extent count_tiles(const QuantAttnArgs& a, int64_t* b
     for (int x = g0; x < g1; ++x) {
         before[x] = mine;
 #pragma unroll 1
-        for (int h = x * group; h < min(slabs, (x + 1) * group); ++h) mine += slab_tiles(a, h);
+        for (int h = x * group; h < min(slabs, (x + 1) * group); ++h) mine += slab_cost(a, h);
     }
     int64_t up = mine;
 #pragma unroll
@@ -192,24 +196,25 @@ __device__ __forceinline__ Extent count_tiles(const QuantAttnArgs& a, int64_t* b
 struct Walk {
     int b, g, t, n, len;       // sequence, head; the sequence's first token, its tokens, the slab's rows
     int rows, tiles, j0, j1;   // of the unit; the CTA's tiles of it
-    int64_t start, end;        // of the unit, of the share
-    __device__ __forceinline__ void enter(const QuantAttnArgs& a, int64_t off)
-    {
-        len = slab_len(a, b * a.Hkv + g);
-        rows = sees(a, len, n, n - 1);
-        tiles = tiles_of(rows);
-        j0 = (int)off;
-        j1 = (int)min((int64_t)tiles, end - start);
-    }
-    __device__ __forceinline__ bool more() const { return start + tiles < end; }
+    int64_t start, end;        // where the unit's tiles start, where the share ends
     __device__ __forceinline__ void sequence(const QuantAttnArgs& a)
     {
         t = cu_at(a, b);
         n = tokens_of(a, b);
     }
+    // The unit (b, g), from its tile j on; `start` is set.
+    __device__ __forceinline__ void enter(const QuantAttnArgs& a, int j)
+    {
+        len = slab_len(a, b * a.Hkv + g);
+        rows = sees(a, len, n, n - 1);
+        tiles = tiles_of(rows);
+        j0 = j;
+        j1 = (int)min((int64_t)tiles, end - start);
+    }
+    __device__ __forceinline__ bool more() const { return start + tiles + kStart < end; }
     __device__ __forceinline__ void next(const QuantAttnArgs& a)
     {
-        start += tiles;
+        start += tiles + kStart;
         if (++g == a.Hkv) {
             g = 0;
             do ++b;
@@ -221,8 +226,10 @@ struct Walk {
     __device__ __forceinline__ bool whole() const { return j0 == 0 && j1 == tiles; }
 };
 
-__device__ __forceinline__ void seek(const QuantAttnArgs& a, const Extent& e, const int64_t* before, int group, int c, Walk& k)
+// Where the share of CTA c starts; false if no tile lies in it.
+__device__ __forceinline__ bool seek(const QuantAttnArgs& a, const Extent& e, const int64_t* before, int group, int c, Walk& k)
 {
+    if (c >= e.parts) return false;
     const int64_t pos = share_start(e, c);
     k.end = share_start(e, c + 1);
     int lo = 0, hi = (a.B * a.Hkv + group - 1) / group - 1;  // the last group that starts at `pos` or before (it has units)
@@ -236,12 +243,14 @@ __device__ __forceinline__ void seek(const QuantAttnArgs& a, const Extent& e, co
     int64_t off = pos - before[lo];
     int h = lo * group;
     if (group > 1)
-        for (int x; off >= (x = slab_tiles(a, h)); ++h) off -= x;
+        for (int x; off >= (x = slab_cost(a, h)); ++h) off -= x;
+    k.start = pos - off + kStart;
+    if (k.start >= k.end) return false;
     k.b = h / a.Hkv;
     k.g = h - k.b * a.Hkv;
     k.sequence(a);
-    k.start = pos - off;
-    k.enter(a, off);
+    k.enter(a, (int)max(off - kStart, (int64_t)0));
+    return true;
 }
 
 // ---------------------------------------------------------------- products
@@ -547,10 +556,9 @@ __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
     pdl_launch_dependents();
     if (c == nctas - 1) check(a);
     int group;
-    const Extent head = count_tiles<Z>(a, reinterpret_cast<int64_t*>(sm), reinterpret_cast<int64_t*>(sm + C::kOffSum), nctas, group);
-    if (c < head.parts) {
-        Walk k;
-        seek(a, head, reinterpret_cast<const int64_t*>(sm), group, c, k);
+    const Extent head = count_cost<Z>(a, reinterpret_cast<int64_t*>(sm), reinterpret_cast<int64_t*>(sm + C::kOffSum), nctas, group);
+    Walk k;
+    if (seek(a, head, reinterpret_cast<const int64_t*>(sm), group, c, k)) {
         fence_proxy_async_smem();  // the sums of tiles lie in the rings, which the copies write next
         __syncthreads();
         Walk f = k;              // ahead of k by the ring's stages
