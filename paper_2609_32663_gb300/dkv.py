@@ -610,6 +610,11 @@ def _work(workspace, at):
 def _word(status, at):
     if status is None or isinstance(status, int):
         return status
+    try:
+        if status.get_device() == at and status.dtype is _T.torch.int32 and status.numel() == 1:
+            return status.data_ptr()
+    except AttributeError:
+        pass
     _device_of(status, "status")
     if status.numel() < 1:
         _bad("status has no element")
@@ -705,6 +710,13 @@ def dkv_chunk_workspace_bytes(pages: Pages) -> int:
 def _token_rows(t, name, at, dtype, tokens, heads):
     """Address and token stride (elements) of a [tokens][heads][128] tensor whose tokens may lie apart (a slice of a
     projection); heads and elements are contiguous."""
+    try:  # (what is right is found so; what is not is named below)
+        if t.get_device() == at and t.dtype is dtype and t.shape == (tokens, heads, 128):
+            stride = t.stride()
+            if stride[2] == 1 and stride[1] == 128 and tokens > 1:
+                return t.data_ptr(), stride[0]
+    except AttributeError:
+        pass
     if _device_of(t, name) != at:
         _bad(f"{name} must be a CUDA tensor on cuda:{at}")
     if t.dtype != dtype or t.shape != (tokens, heads, 128):
@@ -772,10 +784,11 @@ def dkv_rotary_custom(freq, interleaved: bool = False, magnitude: float = 1.0) -
 
 def _rows16(x, name):
     """Whether x, of [tokens][heads][128] rows, is fp16; what is neither that nor bf16 is refused."""
-    _device_of(x, name)
     T = _torch().torch
-    half = x.dtype == T.float16
-    if not (half or x.dtype == T.bfloat16) or x.dim() != 3:
+    _device_of(x, name)
+    dtype = x.dtype
+    half = dtype is T.float16
+    if not (half or dtype is T.bfloat16) or x.dim() != 3:
         _bad(f"{name} is {x.dtype} of {x.dim()} dimensions, expected bfloat16 or float16 [T][heads][128]")
     return half
 
