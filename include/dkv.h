@@ -677,7 +677,8 @@ dkv_status dkv_quant_compact(const dkv_pages* pages, const dkv_plan* plan, const
  *             max_tokens * H / H_kv <= 16 a launch is saved.
  * Kp, Vp, Ks, Vs  are read only.
  * out         as for dkv_chunk_attn. Scores, softmax statistics and sums are fp32, the output is rounded
- *             once. Sequences of at most 16 tokens x H / H_kv: q (scaled by a power of two a row) enters the
+ *             once. Calls of max_tokens * H / H_kv <= 16, and sequences of n tokens, n * H / H_kv <= 8, in
+ *             others: q (scaled by a power of two a row) enters the
  *             products as fp16, exactly but for elements below 2^-28 of the row's largest; weights,
  *             times their rows' V scales, are rounded to fp16, with a least step of 2^-30 of the largest such
  *             product. Others: each row of K and V enters the products in dtype, which holds a

@@ -77,7 +77,7 @@ struct Lay {
     static constexpr int kRaw = Q8 ? 4 : 0;
     static constexpr int kThreads = Q8 ? 512 : 384;
     // A thread's registers after the split; launched with 128 or 168.
-    static constexpr int kRegsSoft = Q8 ? 208 : 216, kRegsRest = Q8 ? 48 : 72, kRegsConvert = Q8 ? 48 : 0;
+    static constexpr int kRegsSoft = Q8 ? 208 : 216, kRegsRest = Q8 ? 24 : 72, kRegsConvert = Q8 ? 72 : 0;
     static_assert(2 * kRegsSoft + kRegsRest + kRegsConvert <= (Q8 ? 4 * 128 : 3 * 168), "the warpgroups share what they were launched with");
     static constexpr int kOffQ = 0;
     static constexpr int kOffRing = kOffQ + 2 * kOperand;
@@ -1144,12 +1144,11 @@ __global__ void __launch_bounds__(Lay<Q8>::kThreads, 1)
                      "r"(kTmemCols));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
-    if (tid == 0) {
-        misc[1] = 0;
-        for (int i = 0; i < Y::kNumBars; ++i) {
-            const bool by_warps = (full + i >= p_half && full + i < p_full + 2) || (Q8 && (i < kStages || (full + i >= raw_empty && full + i < said)));
-            mbar_init(smem_u32(full + i), by_warps ? 4 : 1);  // (a warpgroup's warps each arrive)
-        }
+    if (tid == 0) misc[1] = 0;
+    if (tid < Y::kNumBars) {
+        const uint64_t* bar = full + tid;
+        const bool by_warps = (bar >= p_half && bar < p_full + 2) || (Q8 && (bar < empty || (bar >= raw_empty && bar < said)));
+        mbar_init(smem_u32(bar), by_warps ? 4 : 1);  // (a warpgroup's warps each arrive)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_proxy_async_smem();
     }

@@ -713,8 +713,8 @@ def _token_rows(t, name, at, dtype, tokens, heads):
     try:  # (what is right is found so; what is not is named below)
         if t.get_device() == at and t.dtype is dtype and t.shape == (tokens, heads, 128):
             stride = t.stride()
-            if stride[2] == 1 and stride[1] == 128 and tokens > 1:
-                return t.data_ptr(), stride[0]
+            if stride[2] == 1 and (stride[1] == 128 or heads == 1):
+                return t.data_ptr(), stride[0] if tokens > 1 else heads * 128
     except AttributeError:
         pass
     if _device_of(t, name) != at:

@@ -92,10 +92,11 @@ def attention(c8, layer, q, cu, causal=True, scale=None):
     return out, size
 
 
-def weight_rounding(tokens, G, dtype, rows):
+def weight_rounding(tokens, G, dtype, rows, most=0):
     """Half a step of a softmax weight, relative, for each of `rows` tokens: 2^-11 (fp16) where a sequence's tokens x G are at most
-    16, else that of the call's type."""
-    few = np.repeat([n * G <= 16 for n in tokens], tokens)
+    8, or at most 16 if no sequence of the call may have more, else that of the call's type."""
+    few = 16 if (most if 0 < most < rows else rows) * G <= 16 else 8
+    few = np.repeat([n * G <= few for n in tokens], tokens)
     u = np.full(rows, torch.finfo(dtype).eps / 2)
     u[:few.size][few] = 2.0 ** -11
     return torch.from_numpy(u)[:, None, None]

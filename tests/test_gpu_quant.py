@@ -41,7 +41,7 @@ def check(c8, layer, tokens, causal=True, pad=0, seed=1, scale=0.0, most=0, q=No
     c = Call(c8, layer, q, cu, causal, scale, most).run()
     want, size = quant.attention(c8, layer, q, cu, causal, scale or None)
     assert int(c.status) == 0
-    weights = quant.weight_rounding(tokens, c8.cache.H // c8.cache.Hkv, q.dtype, q.shape[0])
+    weights = quant.weight_rounding(tokens, c8.cache.H // c8.cache.Hkv, q.dtype, q.shape[0], most)
     quant.assert_attention(c.out, want, size, q.dtype, f"tokens {tokens}", weights)
     return c
 
