@@ -255,11 +255,13 @@ void dkv_vmm_free(dkv_vmm* buffer);
  * So n_appended and the context rows must not be written by a kernel that
  * signals early completion (griddepcontrol.launch_dependents) unless an ordinary
  * kernel or a copy lies between it and this call. Of this library the decode
- * calls, dkv_topk_mask and, where lengths and count are not updated in place,
+ * calls, dkv_topk_mask, dkv_rope, dkv_rope_append, dkv_quant_attn and, where lengths
+ * and count are not updated in place,
  * dkv_page_tables and dkv_page_release signal early; they write neither, so calls
  * of this library may follow each other in any order (an append may be followed
  * directly by a call whose n_appended counts the appended row), unless new_len or
- * new_count of a page call is itself given to a decode call as n_appended or d_len.
+ * new_count of a page call is itself given to a decode call as n_appended or d_len, or
+ * what the other three write as its context rows.
  * Errors: DKV_ERR_INVALID_ARG (NULL/unaligned pointer, layer out of range,
  * only one of k_new/v_new), DKV_ERR_CUDA.
  */
@@ -648,9 +650,7 @@ dkv_status dkv_rope(const dkv_rotary* rotary, int32_t dtype, int32_t num_tokens,
  * Kp, Vp       the pools: 16-bit of dtype where Ks and Vs are NULL, else 8-bit. A turned key is
  *              rounded once, to what the pool holds. (NULL without k_new.)
  * Strides are multiples of 8, at least H*128 (H_kv*128); all 16-byte aligned.
- * After it, dkv_chunk_attn is called with k_new and v_new NULL; dkv_quant_attn as it is. It signals
- * early completion: what it writes may not be given to a decode call as n_appended or context rows
- * that directly follows it.
+ * After it, dkv_chunk_attn is called with k_new and v_new NULL; dkv_quant_attn as it is.
  * Asynchronous, allocates nothing, can be captured. Errors: DKV_ERR_INVALID_ARG, DKV_ERR_CUDA.
  */
 dkv_status dkv_rope_append(const dkv_pages* pages, int32_t layer, const dkv_rotary* rotary, int32_t dtype, int32_t num_tokens,
@@ -680,8 +680,8 @@ dkv_status dkv_quant_compact(const dkv_pages* pages, const dkv_plan* plan, const
  *             once. Calls of max_tokens * H / H_kv <= 16, and sequences of n tokens, n * H / H_kv <= 8, in
  *             others: q (scaled by a power of two a row) enters the
  *             products as fp16, exactly but for elements below 2^-28 of the row's largest; weights,
- *             times their rows' V scales, are rounded to fp16, with a least step of 2^-30 of the largest such
- *             product. Others: each row of K and V enters the products in dtype, which holds a
+ *             times their rows' V scales, are rounded to fp16, whose least step is at most 2^-31 of the largest
+ *             weight times the largest V scale (of the rows that the token sees). Others: each row of K and V enters the products in dtype, which holds a
  *             bf16 one exactly, an fp16 one to 2^-24 (scale bytes up to 135, 2^8, as rows of fp16
  *             values have them; larger elements than 2^17 are infinite); weights are rounded to dtype.
  * workspace   dkv_quant_workspace_bytes(pages) bytes (-1: a bad geometry), about 46 MB.

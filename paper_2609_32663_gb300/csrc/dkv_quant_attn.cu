@@ -17,8 +17,8 @@
 // pairs of rows after a byte permutation. Tiles lie in shared memory as TMA's 128-byte swizzle puts them, which makes
 // these 16-byte reads free of conflicts.
 //
-// A row's V scale goes into its weight's exponent, x_r + ev_r, so O has a running maximum of its own beside that of the
-// scores x_r, which the sum of weights goes by.
+// A row's V scale goes into its weight's exponent: O goes by 2^(top + scale), the running maxima of the scores and of the V
+// scales that the column has seen (of those alone: a later token's row may hold anything), the sum of weights by 2^top.
 #include "dkv_quant.cuh"
 
 #include "dkv_tcgen05.cuh"
@@ -330,7 +330,7 @@ template <int Z>
 struct Acc {
     float o[8][Z][4];         // dims 16 g + 2 i of columns e = 0, 1, then dims 16 g + 2 i + 1
     float top[Z][2], l[Z][2]; // in units of 1 / cs; l: of the lane's rows
-    int scale;                // byte of the largest V scale so far, which O goes by
+    int scale[Z][2];          // byte of the largest V scale that the column has seen, which its O goes by
 };
 
 // One tile: scores, softmax, O += P V. lim: the tile's rows that the columns see; rows: those of the unit; `shown`: rows
@@ -340,23 +340,46 @@ __device__ __forceinline__ void tile_step(Acc<Z>& c, const uint32_t (&q)[Z][16],
                                           const unsigned char* scales, uint32_t* factors, const int (&lim)[Z][2], int shown, int rows)
 {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    // A row a lane: its scales as factors. O goes by the largest V scale so far; where a larger one comes, it is
-    // brought to that.
+    const bool edge = shown < kRows;
+    // A row a lane: K's scale as a factor, V's as an exponent. A column's O goes by the largest V scale that it has seen so far;
+    // where a larger one comes, it is brought to that.
     {
-        const int ku = scales[lane], vu = lane < rows ? scales[kRows + lane] : 0;
-        if (__any_sync(kFull, vu > c.scale)) {
-            const int most = max(__reduce_max_sync(kFull, vu), c.scale);
-            const float down = exp2i(c.scale - most);
-            c.scale = most;
+        const int ku = scales[lane], vu = scales[kRows + lane];
+        // (a power of two, and a whole number below 256: the upper half of each has all of it)
+        factors[lane] = __float_as_uint(scale_of(ku)) | __float_as_uint((float)(vu - 127)) >> 16;
+        int most = lane < shown ? vu : 0;
+        bool more = false;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+        for (int z = 0; z < Z; ++z) more |= most > min(c.scale[z][0], c.scale[z][1]);
+        if (edge || __any_sync(kFull, more)) {
+            most = __reduce_max_sync(kFull, most);
+            int own[Z][2];
 #pragma unroll
-                for (int z = 0; z < Z; ++z)
+            for (int z = 0; z < Z; ++z) own[z][0] = own[z][1] = most;
+            if (edge) {  // rows that not all columns see: the lane's columns' own
+                for (int row = max(shown, 0); row < min(rows, kRows); ++row) {
+                    const int u = scales[kRows + row];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) c.o[i][z][e] *= down;
+                    for (int z = 0; z < Z; ++z)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            if (row < lim[z][e]) own[z][e] = max(own[z][e], u);
+                }
+            }
+#pragma unroll
+            for (int z = 0; z < Z; ++z)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int to = max(own[z][e], c.scale[z][e]);
+                    const float down = exp2i(c.scale[z][e] - to);
+                    c.scale[z][e] = to;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        c.o[i][z][e] *= down;
+                        c.o[i][z][2 + e] *= down;
+                    }
+                }
         }
-        // (powers of two: the upper half of each has all of it)
-        factors[lane] = __float_as_uint(scale_of(ku)) | __float_as_uint(exp2i(vu - c.scale + (int)kShift)) >> 16;
     }
     // Rows 16 m + g and 16 m + g + 8 of columns 2 t and 2 t + 1.
     float s[2][Z][4];
@@ -390,9 +413,8 @@ __device__ __forceinline__ void tile_step(Acc<Z>& c, const uint32_t (&q)[Z][16],
             }
         }
     }
-    const bool edge = shown < kRows;
     __syncwarp();  // the factors are there
-    // Scores by their rows' scales; f: the rows' factors of their weights.
+    // Scores by their rows' scales; f: the exponents of the rows' V scales.
     float f[4];
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
@@ -431,7 +453,7 @@ __device__ __forceinline__ void tile_step(Acc<Z>& c, const uint32_t (&q)[Z][16],
             for (int e = 0; e < 2; ++e) {
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) mx[z][e] = fmaxf(mx[z][e], __shfl_xor_sync(kFull, mx[z][e], o));
-                const bool up = mx[z][e] > c.top[z][e];
+                const bool up = (mx[z][e] - c.top[z][e]) * cs[z][e] > kSlack;  // (a column's own, whatever the others hold)
                 alpha[e] = up ? ex2((c.top[z][e] - mx[z][e]) * cs[z][e]) : 1.f;
                 if (up) c.top[z][e] = mx[z][e];
                 c.l[z][e] *= alpha[e];
@@ -445,15 +467,18 @@ __device__ __forceinline__ void tile_step(Acc<Z>& c, const uint32_t (&q)[Z][16],
     uint32_t p[4][Z];
 #pragma unroll
     for (int z = 0; z < Z; ++z) {
-        float top[2];
+        float top[2], ref[2];  // origins of the weights, and of the weights times V's scales
 #pragma unroll
-        for (int e = 0; e < 2; ++e) top[e] = c.top[z][e] == -INFINITY ? 0.f : c.top[z][e] * cs[z][e];
+        for (int e = 0; e < 2; ++e) {
+            top[e] = c.top[z][e] == -INFINITY ? 0.f : c.top[z][e] * cs[z][e];
+            ref[e] = top[e] + ((float)(c.scale[z][e] - 127) - kShift);
+        }
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-            const float w0 = ex2(fmaf(s[x >> 1][z][2 * (x & 1)], cs[z][0], -top[0])), w1 = ex2(fmaf(s[x >> 1][z][2 * (x & 1) + 1], cs[z][1], -top[1]));
-            c.l[z][0] += w0;
-            c.l[z][1] += w1;
-            p[x][z] = transposed(half2_of(w0 * f[x], w1 * f[x]));
+            const float x0 = s[x >> 1][z][2 * (x & 1)], x1 = s[x >> 1][z][2 * (x & 1) + 1];
+            c.l[z][0] += ex2(fmaf(x0, cs[z][0], -top[0]));
+            c.l[z][1] += ex2(fmaf(x1, cs[z][1], -top[1]));
+            p[x][z] = transposed(half2_of(ex2(fmaf(x0, cs[z][0], f[x] - ref[0])), ex2(fmaf(x1, cs[z][1], f[x] - ref[1]))));
         }
     }
     bool odd = false;  // NaN in a row of V that not all columns see
@@ -634,7 +659,6 @@ __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
             uint32_t q[Z][16];
             float cs[Z][2];
             int lim[Z][2];
-            acc.scale = 0;
 #pragma unroll
             for (int z = 0; z < Z; ++z) {
                 float back;  // (of column g)
@@ -645,6 +669,7 @@ __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
                     cs[z][e] = __shfl_sync(kFull, back, 8 * t + 4 * e) * a.qscale;
                     lim[z][e] = y < cols ? sees(a, k.len, k.n, y / a.G) : k.rows;
                     acc.top[z][e] = -INFINITY;
+                    acc.scale[z][e] = 0;
                     acc.l[z][e] = 0.f;
                 }
             }
@@ -685,23 +710,29 @@ __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
                 for (int e = 0; e < 2; ++e) {
 #pragma unroll
                     for (int o = 4; o < 32; o <<= 1) acc.l[z][e] += __shfl_xor_sync(kFull, acc.l[z][e], o);
-                    if (g == 0) states[warp * kCols + 8 * z + 2 * t + e] = State{acc.top[z][e] * cs[z][e], acc.l[z][e], (float)acc.scale, 0.f};
+                    if (g == 0) states[warp * kCols + 8 * z + 2 * t + e] = State{acc.top[z][e] * cs[z][e], acc.l[z][e], (float)acc.scale[z][e], 0.f};
                 }
             __syncthreads();
             const bool aborted = misc[0];
             const int mine = tid >> 4, chunk = tid & 15;  // this thread sums 4 dims of column `mine`: chunk 2 g + i of lane g's 8
             State total{-INFINITY, 0.f, 0.f, 0.f};
-            float f0[Z][2];
+            float f0[Z][2], up[Z][2];  // of this lane's columns: what joins its O; the largest scale
 #pragma unroll
-            for (int z = 0; z < Z; ++z) f0[z][0] = f0[z][1] = -INFINITY;
+            for (int z = 0; z < Z; ++z) f0[z][0] = f0[z][1] = -INFINITY, up[z][0] = up[z][1] = 0.f;
 #pragma unroll 4
             for (int x = 0; x < active; ++x) {
-                if (mine < kCols) total.top = fmaxf(total.top, states[x * kCols + mine].top);
-                total.scale = fmaxf(total.scale, states[x * kCols].scale);
+                if (mine < kCols) {
+                    total.top = fmaxf(total.top, states[x * kCols + mine].top);
+                    total.scale = fmaxf(total.scale, states[x * kCols + mine].scale);
+                }
 #pragma unroll
                 for (int z = 0; z < Z; ++z)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) f0[z][e] = fmaxf(f0[z][e], states[x * kCols + 8 * z + 2 * t + e].top);
+                    for (int e = 0; e < 2; ++e) {
+                        const State y = states[x * kCols + 8 * z + 2 * t + e];
+                        f0[z][e] = fmaxf(f0[z][e], y.top);
+                        up[z][e] = fmaxf(up[z][e], y.scale);
+                    }
             }
             if (mine < kCols)
 #pragma unroll 4
@@ -712,7 +743,7 @@ __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
 #pragma unroll
             for (int z = 0; z < Z; ++z)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) f0[z][e] = factor(acc.top[z][e] * cs[z][e], f0[z][e]) * ex2((float)acc.scale - total.scale);
+                for (int e = 0; e < 2; ++e) f0[z][e] = factor(acc.top[z][e] * cs[z][e], f0[z][e]) * ex2((float)acc.scale[z][e] - up[z][e]);
             const bool whole = k.whole(), live = mine < cols && !aborted;
             const int token = mine / a.G, head_j = mine - token * a.G;
             uint16_t* out = a.out + ((int64_t)(k.t + token) * a.H + k.g * a.G + head_j) * kHeadDim;

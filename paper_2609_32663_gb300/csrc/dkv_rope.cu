@@ -104,6 +104,7 @@ __global__ void __launch_bounds__(kRopeThreads, 1) rope_kernel(const __grid_cons
     if (lane < cut.stages) mbar_init(smem_u32(full + lane), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async_smem();
+    __syncwarp();
     const int qheads = a.q ? a.H : 0;
     const bool turned = sub < a.rot >> 4;
     // The lane's two chunks of 8 elements.

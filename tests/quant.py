@@ -104,8 +104,8 @@ def weight_rounding(tokens, G, dtype, rows, most=0):
 
 def assert_attention(got, want, size, dtype, what="", weights=None):
     """Each output is rounded once, u |o|, and so is each weight (`weights`, relative; a sequence of few tokens has them
-    times their rows' V scales, in fp16): weights sum w|v|, or half of fp16's least step, 2^-31 of the largest such product (below
-    1e-6 of sum w|v| for the inputs here). Scores are 32-bit sums of 128 products, |error| <= 128 2^-24 sum|q k| scale < 2e-4 for
+    times their rows' V scales, in fp16): weights sum w|v|, or half of fp16's least step, 2^-32 of the largest weight times the
+    largest scale (below 1e-6 of sum w|v| for the inputs here). Scores are 32-bit sums of 128 products, |error| <= 128 2^-24 sum|q k| scale < 2e-4 for
     the standard normal inputs here (sum |q k| scale < 25), which moves a weight by twice that."""
     u = torch.finfo(dtype).eps / 2
     got = got.double().cpu()

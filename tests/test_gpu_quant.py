@@ -66,6 +66,26 @@ def test_group_sizes(cuda, G, Hkv, dtype):
     check(quant.Cache8(lens, 32, H=G * Hkv, seed=G, dtype=dtype), 0, tokens)
 
 
+@pytest.mark.parametrize("G", [1, 2, 3, 4, 5, 7, 8])
+@pytest.mark.parametrize("cols", [8, 16])
+@pytest.mark.parametrize("causal", [True, False])
+def test_few_tokens_a_sequence(cuda, G, cols, causal):
+    """As many columns as the kernels of 8 and of 16 take, sequences of fewer beside them, rows that only the last ones see."""
+    n = max(cols // G, 1)
+    tokens = [n, 1, 0, n, max(n - 1, 1), n]
+    for page, ctx in ((16, [0, 40, 3, 33, 500, 14]), (128, [1300, 0, 9, 255, 31, 4000])):
+        check(quant.Cache8(lens_of(1, 6, 2, ctx, tokens, G), page, H=2 * G, seed=G), 0, tokens, causal=causal, most=n)
+
+
+def test_no_token_at_all(cuda):
+    """Sequences that bring nothing: nothing is written."""
+    c8 = quant.Cache8(np.array([[[40], [0]]]), 16, H=4)
+    _, q = inputs(c8, [0, 0], 1, pad=70)
+    for most in (0, 1, 70):
+        c = Call(c8, 0, q, [0, 0, 0], most=most).run()
+        assert int(c.status) == 0 and torch.isnan(c.out.float()).all()
+
+
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("pad", [0, 5])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
@@ -153,7 +173,7 @@ def test_queries_of_any_size(cuda, size, dtype):
     check(c8, 0, tokens, q=q, scale=128 ** -0.5 / size)
 
 
-@pytest.mark.parametrize("tokens", [[70, 4], [3, 4]])
+@pytest.mark.parametrize("tokens", [[70, 4], [3, 4], [4, 4]])
 def test_later_tokens_hold_anything(cuda, tokens):
     """NaN in K and V of a later token changes no earlier token's output, and is NaN for those that see it."""
     for dtype in (torch.bfloat16, torch.float16):
@@ -167,12 +187,40 @@ def test_later_tokens_hold_anything(cuda, tokens):
         c8.V8[last[2][3], 9] = 0x7f
         c8.sync()
         cu, q = inputs(c8, tokens, 2)
-        x = Call(c8, 0, q, cu).run()
+        x = Call(c8, 0, q, cu, most=max(tokens)).run()
         want, size = quant.attention(c8, 0, q, cu)
         # (the definition's sums over what a token sees alone)
         quant.assert_attention(x.out, want, size, dtype)
         assert torch.isnan(want[k1, :4]).all() and torch.isnan(want[n + 3, :4, 9]).all() and torch.isfinite(want[0]).all()
         assert torch.isfinite(x.out[n:n + 3].float()).all()
+
+
+@pytest.mark.parametrize("tokens", [[70, 4], [3, 4], [4, 4], [2, 2]])
+@pytest.mark.parametrize("most", [0, 1])
+@pytest.mark.parametrize("dtype,byte", [(torch.bfloat16, 240), (torch.bfloat16, 150), (torch.float16, 135)])
+def test_later_tokens_may_be_far_larger(cuda, tokens, most, dtype, byte):
+    """A later token's K and V of 448 2^113 (or of the largest that fp16 rows have) change no earlier token's output, and are most
+    of the outputs that see them."""
+    c8 = quant.Cache8(lens_of(1, 2, 2, [90, 128], tokens, 5), 16, H=8, dtype=dtype)
+    c, n = c8.cache, tokens[0]
+    last = [c.rows(h)[-tokens[h // 2]:] for h in range(4)]  # the new rows of each slab
+    cu, q = inputs(c8, tokens, 2)
+    first = Call(c8, 0, q, cu, most=max(tokens) if most else 0).run()  # (all rows as they were)
+    for h in range(4):
+        r = last[h][tokens[h // 2] - 1]
+        c8.V8[r], c8.Vs[r] = 0x7e, byte
+    c8.Ks[last[0][n - 1]] = min(byte, 140)
+    c8.sync()
+    x = Call(c8, 0, q, cu, most=max(tokens) if most else 0).run()
+    want, size = quant.attention(c8, 0, q, cu)
+    ends = [n - 1, sum(tokens) - 1]
+    others = [i for i in range(sum(tokens)) if i not in ends]
+    assert torch.equal(x.out[others], first.out[others])
+    finite = want.abs() <= torch.finfo(dtype).max
+    for t in ends:
+        got, w, sz = x.out[t:t + 1, 4:].double().cpu(), want[t:t + 1, 4:], size[t:t + 1, 4:]
+        ok = finite[t:t + 1, 4:]
+        quant.assert_attention(torch.where(ok, got, w), w, sz, dtype)
 
 
 @pytest.mark.parametrize("tokens,ctx", [([1], 300), ([40], 200), ([1, 5], 0)])

@@ -304,6 +304,72 @@ def test_bad_offsets_write_nothing(cuda):
         assert torch.isnan(a.out.float()).all() and all((p == 0x7f).all() for p in a.pools) and all((s == 255).all() for s in a.scales)
 
 
+@pytest.mark.parametrize("H,Hkv,tokens", [(100, 100, [3, 1]), (64, 8, [700, 0, 5]), (8, 1, [1]), (3, 3, [2500, 1])])
+def test_many_and_few_heads(cuda, H, Hkv, tokens):
+    """Tokens cut into several items, and whole."""
+    for bits in (8, 16):
+        a = Append(lens_of(1, len(tokens), Hkv, [20] * len(tokens), tokens, H), 32, tokens, H=H, bits=bits, rot=128, pad=1, seed=H)
+        a.run(0).check(0)
+        assert int(a.status) == 0
+
+
+def test_no_token_at_all(cuda):
+    a = Append(lens_of(1, 2, 1, [20, 0], [0, 0], 1), 16, [0, 0], H=2, pad=40)
+    a.run(0)
+    assert int(a.status) == 0 and torch.isnan(a.out.float()).all() and all((p == 0x7f).all() for p in a.pools)
+
+
+def test_two_streams_at_once(cuda):
+    calls = [(Append(lens_of(1, 2, 2, [200, 10], [5 + 600 * i, 1], i), 16, [5 + 600 * i, 1], H=8, seed=i), torch.cuda.Stream()) for i in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for a, s in calls:
+            dkv.dkv_rope_append(a.c.pages, 0, a.q, a.k, a.v, a.positions, a.cu, a.table, a.len, *a.pools, a.out, *a.scales, rotary=a.rotary,
+                                status=a.status, stream=s)
+    torch.cuda.synchronize()
+    for a, _ in calls:
+        a.check(0)
+        assert int(a.status) == 0
+
+
+def test_captured_append(cuda):
+    """A graph reads offsets, lengths, tables and positions when it runs; rows behind fewer tokens stay."""
+    a = Append(lens_of(1, 2, 1, [20, 9], [4, 30], 1), 16, [4, 30], H=2)
+    a.run(0)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        dkv.dkv_rope_append(a.c.pages, 0, a.q, a.k, a.v, a.positions, a.cu, a.table, a.len, *a.pools, a.out, *a.scales, rotary=a.rotary,
+                            status=a.status)
+    for x, v in ((a.out, NAN), (a.pools[0], 0x7f), (a.pools[1], 0x7f), (a.scales[0], 255), (a.scales[1], 255)):
+        x.fill_(v)
+    a.pos = a.pos[::-1].copy() + 5
+    a.positions.copy_(dev(a.pos))
+    g.replay()
+    torch.cuda.synchronize()
+    a.check(0)
+    a.out.fill_(NAN)
+    a.cu.copy_(dev([0, 4, 4]))
+    a.len.copy_(dev(np.array([a.c.lens[0], a.c.lens[1] - 30])))
+    g.replay()
+    torch.cuda.synchronize()
+    assert int(a.status) == 0 and torch.isfinite(a.out[:4].float()).all() and torch.isnan(a.out[4:].float()).all()
+
+
+def test_pool_places_past_32_bits(cuda):
+    """8-bit pools of more than 4 GB: pages at their end."""
+    page, num, tokens = 128, 340_000, [3, 70]
+    a = Append(lens_of(1, 2, 1, [300, 100], tokens, 1), page, tokens, H=2)
+    small = a.c.pages.num_pages
+    wide = [torch.full((num * page, *x.shape[1:]), int(x.flatten()[0]), dtype=torch.uint8, device="cuda") for x in a.pools + a.scales]
+    table = torch.where(a.table < small, a.table + (num - small), a.table)
+    g = dkv.Pages(L=1, B=2, H=2, H_kv=1, page_rows=page, num_pages=num, max_pages=a.table.shape[1])
+    dkv.dkv_rope_append(g, 0, a.q, a.k, a.v, a.positions, a.cu, table, a.len, *wide[:2], a.out, *wide[2:], rotary=a.rotary, status=a.status)
+    torch.cuda.synchronize()
+    a.pools, a.scales = [x[-small * page:] for x in wide[:2]], [x[-small * page:] for x in wide[2:]]
+    a.check(0)
+    assert int(a.status) == 0 and all((x[:1 << 20] == x[0]).all() for x in wide[:2])
+
+
 def test_more_sequences_than_threads(cuda):
     tokens = [b % 3 for b in range(512)]
     a = Append(lens_of(1, 512, 1, [b % 40 for b in range(512)], tokens, 1), 16, tokens, H=2)
