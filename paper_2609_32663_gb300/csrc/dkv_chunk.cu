@@ -21,6 +21,9 @@
 //                     that the tensor pipe itself keeps S(s + 2) behind the PV(s) whose P it overwrites.
 //     warp 9          TMA: Q tiles, and K and V tiles page by page into one ring in the order of use.
 //     warp 10         walks the CTA's share and describes its units to the others (11 is idle).
+//   Over 8-bit pools (Q8; sequences of more columns than quant_attn_kernel takes, dkv_quant_attn.cu) the rows land in a ring
+//   of their own, and warps 12-15 turn them into the 16-bit tiles, a row a thread, with its scale: exactly in
+//   bf16, at half their value in fp16. Counters are cleared, and rows were appended, by kernels before.
 //
 // What bounds it. Next tokens stream the cache: 16 sequences of 3K-24K rows, 847 MB, in 131 us, 6.5
 // TB/s of the 6.8 of a plain copy. Turns and queries: a pair unit's tile (four products, 2,048 cycles
@@ -33,6 +36,11 @@
 // (1,531 us before the clocks fall under the power limit). One token over 1.8K rows: 15.1 us, all of
 // it latency: two launches, the count of the cost, one tile, the join (0.3 us of it the looks at offsets and
 // lengths, and the fence).
+//
+// Over 8-bit pools the turn takes 1,720 us (bf16): a tile's two conversions are 1,300 cycles each of its 3,500, beside the softmax
+// warps on the same schedulers. A row's loads three ahead of their use: 2,012 us to 1,849; the registers split 208, 24 (one-warp
+// roles), 72 (conversion) instead of 208, 48, 48: to 1,720 (208, 40, 56: 1,807; 216, 40, 40: 1,905; 200, 56, 56: 1,970).
+// Drafts of four sequences, 63 MB, take 48 us: 64 KB of rows on the way an SM are too few for their latency.
 //
 // Scores, their max and sum and O are fp32. The weights P are rounded to the inputs' type, as both operands of
 // the second product have it: half a step of each weight, of either sign, so that errors against 64 bits go from

@@ -12,7 +12,10 @@
 //                pages, 16-bit or (after the row's largest element is found over the 8 lanes) as e4m3 values with a
 //                scale byte.
 //
-// What bounds it: memory, each row in and out once.
+// What bounds it: memory, each row in and out once: 30,001 tokens of 28 heads, 430 MB, take 75 us, where a plain copy of as much
+// takes 70; 16K tokens of 8 heads in a wider projection 18.7 us (67 MB: 14.4), a turn of 4K tokens to 8-bit pages 22 (92 MB: 17):
+// a launch, the first rows' latency and three to seven items a warp. As a grid of short CTAs that kept rows in registers these
+// took 69, 22 and 30 us; two CTAs an SM of half the warps, 24 warps, or no unrolling change nothing or cost up to 5 us.
 #include "dkv_quant.cuh"
 
 #include "dkv_tcgen05.cuh"
