@@ -849,7 +849,7 @@ __device__ __forceinline__ void pool_values(const uint16_t* pool, const uint8_t*
     }
 }
 
-// A value of V that is not finite, in a later token's row, spoils the rows of the same tile
+// A value of V that is not finite (as it enters the products), in a later token's row, spoils the rows of the same tile
 // that do not see it (0 NaN is NaN). Rows whose result is not finite (`odd`) and that have
 // such a value in a masked place, rows [lim, end), are computed again without the tensor cores:
 // o = sum over rows [first, lim) of 2^(s - mc) v, dims [d0, d0 + nd). Slow and rare: 4 rows at
@@ -880,7 +880,7 @@ __device__ __forceinline__ void mend_rows(const ChunkArgs& a, int h, bool odd, i
             float v[16];
             pool_values<F16, Q8>(a.Vp, a.Vs, row, dim, v);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) spoilt += 0.f * v[e];
+            for (int e = 0; e < 16; ++e) spoilt += 0.f * (F16 && Q8 ? __half2float(__float2half_rn(v[e] * kHalved<F16, Q8>)) : v[e]);
         }
         if (!__any_sync(kFull, spoilt != spoilt)) continue;
         float o[16];

@@ -223,6 +223,25 @@ def test_later_tokens_may_be_far_larger(cuda, tokens, most, dtype, byte):
         quant.assert_attention(torch.where(ok, got, w), w, sz, dtype)
 
 
+@pytest.mark.parametrize("tokens", [[70, 4], [33, 40]])
+@pytest.mark.parametrize("byte", [136, 140, 200, 247])
+def test_later_rows_past_fp16_spoil_no_earlier_output(cuda, tokens, byte):
+    """fp16 products over a row of V that fp16 does not hold: tokens that do not see it are as without it. (Their outputs may be
+    computed another way then, so they are held to the definition.)"""
+    c8 = quant.Cache8(lens_of(1, 2, 2, [90, 128], tokens, 5), 16, H=8, dtype=torch.float16)
+    c, n = c8.cache, tokens[0]
+    cu, q = inputs(c8, tokens, 2)
+    want, size = quant.attention(c8, 0, q, cu)
+    for h in range(4):
+        r = c.rows(h)[-1]
+        c8.V8[r, ::3], c8.Vs[r] = 0x7e, byte
+        c8.Ks[r] = 140
+    c8.sync()
+    x = Call(c8, 0, q, cu).run()
+    others = [i for i in range(sum(tokens)) if i not in (n - 1, sum(tokens) - 1)]
+    quant.assert_attention(x.out[others], want[others], size[others], torch.float16)
+
+
 @pytest.mark.parametrize("tokens,ctx", [([1], 300), ([40], 200), ([1, 5], 0)])
 def test_scores_of_minus_infinity_alone_give_zeros(cuda, tokens, ctx):
     c8 = quant.Cache8(lens_of(1, len(tokens), 2, [ctx] * len(tokens), tokens, 2), 16, H=8)
