@@ -679,7 +679,8 @@ dkv_status dkv_quant_compact(const dkv_pages* pages, const dkv_plan* plan, const
  * out         as for dkv_chunk_attn. Scores, softmax statistics and sums are fp32, the output is rounded
  *             once. Calls of max_tokens * H / H_kv <= 16, and sequences of n tokens, n * H / H_kv <= 8, in
  *             others: q (scaled by a power of two a row) enters the
- *             products as fp16, exactly but for elements below 2^-28 of the row's largest; weights,
+ *             products as fp16, exactly but for elements below 2^-28 of the row's largest (and scores may
+ *             pass the range of fp32 where K has elements above 2^106); weights,
  *             times their rows' V scales, are rounded to fp16, whose least step is at most 2^-31 of the largest
  *             weight times the largest V scale (of the rows that the token sees). Others: each row of K and V enters the products in dtype, which holds a
  *             bf16 one exactly, an fp16 one to 2^-24 (scale bytes up to 135, 2^8, as rows of fp16

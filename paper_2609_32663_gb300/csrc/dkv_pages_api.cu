@@ -499,6 +499,7 @@ dkv_status dkv_quant_attn(const dkv_pages* g, int32_t layer, int32_t dtype, int3
     if (!dtype_ok(dtype) || !tokens_ok(num_tokens, g->H, "H")) return DKV_ERR_INVALID_ARG;
     float qscale;
     if (!scale_ok(scale, &qscale)) return DKV_ERR_INVALID_ARG;
+    if (dtype == DKV_FP16 && !std::isfinite(2 * qscale)) return refuse("scale=%g is too large", scale);  // (fp16 keys enter at half their value)
     if (num_tokens == 0) return dkv::set_error(DKV_OK, "");
     if (!q || !cu_tokens || !table || !len || !Kp || !Vp || !Ks || !Vs || !out) return refuse("NULL q/cu_tokens/table/len/Kp/Vp/Ks/Vs/out");
     if (!aligned(q, 16) || !aligned(Kp, 16) || !aligned(Vp, 16) || !aligned(Ks, 16) || !aligned(Vs, 16) || !aligned(out, 16))

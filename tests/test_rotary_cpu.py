@@ -167,7 +167,8 @@ def attn(dkv, **kw):
 @pytest.mark.parametrize("kw", [dict(layer=2), dict(dtype=2), dict(T=-1), dict(T=1 << 28), dict(q=None), dict(q=A + 8), dict(qs=1016), dict(qs=1025),
                                 dict(cu=None), dict(cu=A + 1), dict(table=None), dict(len=None), dict(Kp=None), dict(Vp=A + 8), dict(Ks=None),
                                 dict(Vs=A + 1), dict(out=None), dict(out=A + 4), dict(work=None), dict(work=A + 8), dict(bytes=100),
-                                dict(status=A + 2), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=3e38)])
+                                dict(status=A + 2), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=3e38),
+                                dict(dtype=1, scale=2e38)])
 def test_attention_refuses(dkv, kw):
     assert attn(dkv, **kw) == dkv.DKV_ERR_INVALID_ARG
     assert dkv.lib().dkv_last_error()
