@@ -40,7 +40,8 @@
 // Over 8-bit pools the turn takes 1,720 us (bf16): a tile's two conversions are 1,300 cycles each of its 3,500, beside the softmax
 // warps on the same schedulers. A row's loads three ahead of their use: 2,012 us to 1,849; the registers split 208, 24 (one-warp
 // roles), 72 (conversion) instead of 208, 48, 48: to 1,720 (208, 40, 56: 1,807; 216, 40, 40: 1,905; 200, 56, 56: 1,970).
-// Drafts of four sequences, 63 MB, take 48 us: 64 KB of rows on the way an SM are too few for their latency.
+// Drafts of four sequences, 63 MB, take 37 us: 7 to the first tile, 13 tiles a CTA at 1.24 (the conversion), 4 for the pieces' stores, and
+// the join of up to 17 of them a unit, which the kernel behind this one does on all SMs (by the last CTA of a unit: 50 us).
 //
 // Scores, their max and sum and O are fp32. The weights P are rounded to the inputs' type, as both operands of
 // the second product have it: half a step of each weight, of either sign, so that errors against 64 bits go from
@@ -70,7 +71,7 @@ constexpr int kHalf = kTile * 128;         // one 64-dim half of a tile (16 KB)
 constexpr int kOperand = 2 * kHalf;        // a tile: dims 0-63, then 64-127
 constexpr int kSoft = 256;                 // threads of the softmax groups
 constexpr int kMaxCtas = kChunkCounters;    // CTAs of the largest grid (the workspace's size)
-constexpr int kPieceRows = 2 * kTile;      // rows of a piece in the workspace
+constexpr int kPieceRows = kChunkRows;     // rows of a piece in the workspace
 constexpr int kTmemCols = 512;             // S of group p at 128 p (P over its first half), O at 256 + 128 p
 
 constexpr int kAhead = 4;                  // ring of unit descriptors
@@ -1111,7 +1112,9 @@ __device__ __forceinline__ void join_pieces(const ChunkArgs& a, const ChunkWork&
     }
     if (x < rows && first == 0) scale[x] = make_float2(M, inverse<F16, Q8>(L));
     if (!wait.meet()) return;
-    if (pieces <= 2)
+    if (Q8)  // (a few)
+        join_items<F16, 2, 4>(a, w, scale, t0, rows, g, c0, pieces);
+    else if (pieces <= 2)
         join_items<F16, 4, 2>(a, w, scale, t0, rows, g, c0, pieces);
     else if (rows > 16)
         join_items<F16, 2, 4>(a, w, scale, t0, rows, g, c0, pieces);
@@ -1505,7 +1508,17 @@ __global__ void __launch_bounds__(Lay<Q8>::kThreads, 1)
                     if (live && !whole && p == 0) __stcg(w.ml + slot * kPieceRows + prow, make_float2(M, L));
                 }
             }
-            if (!whole && !last) {
+            if (Q8 && pieces > kFew) {
+                // The next kernel joins many pieces, all its CTAs a few rows each: it starts that with all of them there. (The last CTA
+                // to finish took 17 us for drafts' units of 17 pieces. With the turn's units of two or three pieces left to it
+                // as well the turn took 1,787 us for 1,718.)
+                if (!wait.meet()) break;
+                if (tid == 0) {
+                    pdl_wait();  // the counters are cleared
+                    if (k.j0 == 0) a.jobs[c0] = make_int4(k.t0, k.tokens(), k.g, pieces);
+                    atomicAdd(w.done + c0, k.j0 == 0 ? 1 + kJobStarts : 1);
+                }
+            } else if (!whole && !last) {
                 __threadfence();
                 if (!wait.meet()) break;
                 if (tid == 0) {
@@ -1630,6 +1643,12 @@ cudaError_t launch_chunk(const ChunkArgs& a, bool short_boxes, cudaStream_t st)
     const int blocks = 1 + (int)((rows + kAppThreads / 16 - 1) / (kAppThreads / 16));
     if ((e = launch_pdl(chunk_append_kernel, blocks, kAppThreads, 0, st, a, w)) != cudaSuccess) return e;
     return a.fp16 ? launch_attn<true, false>(a, maps, w, nctas, st) : launch_attn<false, false>(a, maps, w, nctas, st);
+}
+
+ChunkJobs chunk_jobs(const ChunkArgs& a)
+{
+    const ChunkWork w = carve(a.work);
+    return ChunkJobs{a.jobs, w.done, w.ml, w.o, a.qscale, a.fp16 ? 1 / kHalved<true, true> : 1.f};
 }
 
 cudaError_t launch_chunk8(const ChunkArgs& a, int nctas, bool short_boxes, cudaStream_t st)

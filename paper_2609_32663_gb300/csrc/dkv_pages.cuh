@@ -97,7 +97,19 @@ struct ChunkArgs {
     const uint8_t* Ks;
     const uint8_t* Vs;
     int least, most;        // a sequence with fewer or more tokens is left out
+    int4* jobs;             // [kChunkCounters] units that the next kernel joins, at the CTA that has their first piece
 };
+// What the kernel behind launch_chunk8's joins: unit c is jobs[c] = (first token, tokens, KV head, pieces), if done[c] is its
+// pieces + kJobStarts. Row x of a unit (token G + head of the group) lies at x, or, from a tile's whole tokens on, in the
+// second tile of each piece (chunk_attn_kernel's layout).
+struct ChunkJobs {
+    const int4* jobs;
+    const int32_t* done;
+    const float2* ml;       // [piece][kChunkRows] max (in units of 1 / qscale) and sum
+    const float4* o;        // [piece][32][kChunkRows]
+    float qscale, back;     // back: what O is to be multiplied by besides 1 / sum
+};
+constexpr int kChunkTile = 128, kChunkRows = 2 * kChunkTile, kJobStarts = 1 << 16;
 int64_t chunk_workspace_bytes();
 constexpr int kChunkCounters = 160;  // int32 words at the start of its workspace
 cudaError_t chunk_setup();  // the kernels' attributes in the current context
@@ -107,7 +119,9 @@ cudaError_t page_setup(int* sms);
 // short_boxes (fault injection): page copies deliver half the bytes that a stage expects,
 // inside the stage, so that every wait for them runs out.
 cudaError_t launch_chunk(const ChunkArgs& a, bool short_boxes, cudaStream_t st);
-// The same over 8-bit pools, after a kernel that signals early and clears the counters.
+// The same over 8-bit pools, after a kernel that signals early and clears the counters. Units in more than
+// a few pieces are left to the next kernel (chunk_jobs).
 cudaError_t launch_chunk8(const ChunkArgs& a, int nctas, bool short_boxes, cudaStream_t st);
+ChunkJobs chunk_jobs(const ChunkArgs& a);
 
 }  // namespace dkv

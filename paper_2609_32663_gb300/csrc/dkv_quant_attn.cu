@@ -65,6 +65,7 @@ struct Cfg {
     static constexpr int kSmemBytes = kOffMisc + 16;
     static constexpr int kMaxGroups = kOffSum / 8;                            // prefix sums in the rings before their first use
     static_assert(kSmemBytes <= 227 * 1024, "fits one CTA");
+    static_assert(kChunkCounters * 20 + 20 <= kOffScales - kOffSum && kOffSum % 16 == 0, "join_chunks's units fit");
     static_assert(kOffBars % 8 == 0 && kOffScales % 16 == 0, "aligned");
 };
 
@@ -78,9 +79,10 @@ struct QuantWork {
     int32_t* done;  // [kMaxCtas] finished pieces of the unit that starts in CTA c and ends in a later one
     State* state;   // [kMaxCtas][2][16]
     float4* o;      // [kMaxCtas][2][16][32]
-    int32_t* chunk; // the workspace of the kernel of many tokens, its counters first
+    int4* jobs;     // [kChunkCounters] what the kernel of many tokens leaves to this one
+    int32_t* chunk; // that kernel's workspace, its counters first
 };
-constexpr int64_t kOffState = (kMaxCtas * 4 + 255) / 256 * 256, kOffO = kOffState + (int64_t)kMaxCtas * 2 * kMostCols * sizeof(State),
+constexpr int64_t kOffJobs = (kMaxCtas * 4 + 255) / 256 * 256, kOffState = kOffJobs + (kChunkCounters * 16 + 255) / 256 * 256, kOffO = kOffState + (int64_t)kMaxCtas * 2 * kMostCols * sizeof(State),
                   kWorkBytes = kOffO + (int64_t)kMaxCtas * 2 * kMostCols * kHeadDim * 4;
 static_assert(kWorkBytes % 256 == 0, "the other kernel's workspace lies behind it");
 
@@ -558,10 +560,97 @@ __device__ __forceinline__ int bank_of(int t) { return (t & 1) | (t & 2) << 1; }
 // Where piece k of the unit that starts in CTA c0 lies.
 __device__ __forceinline__ int64_t piece_at(int c0, int k) { return (int64_t)(c0 + k) * 2 + (k == 0); }
 
+// The cut units of the kernel of many tokens, after it (all threads of all CTAs): a warp has 8 rows and 16 dims of a unit at
+// once, a lane 4 dims of a row; kJoin pieces on the way at once, in their order. `units`: shared.
+template <bool F16, int kThreads>
+__device__ __forceinline__ void join_chunks(const QuantAttnArgs& a, const ChunkJobs& x, int nctas, int4* units)
+{
+    constexpr int kUnits = kChunkCounters, kJoin = 8, kWarps = kThreads / 32;
+    static_assert(kUnits % 32 == 0 && kUnits <= kThreads, "a thread a unit");
+    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
+    int* ends = reinterpret_cast<int*>(units + kUnits);  // [kUnits] the tasks up to a unit's last; then its warps' sums
+    int* sums = ends + kUnits;
+    int tasks = 0;
+    if (tid < kUnits) {
+        const int n = tid < nctas ? __ldcg(x.done + tid) : 0;
+        int4 u = make_int4(0, 0, 0, 0);
+        if (n >= kJobStarts) u = __ldcg(x.jobs + tid);
+        if (n >= kJobStarts && n == u.w + kJobStarts &&
+            in_bounds(u.x >= 0 && u.x + u.y <= a.T && u.y * a.G <= kChunkRows && u.z < a.Hkv && tid + u.w <= nctas, a.status))
+            tasks = (u.y * a.G + 7) / 8 * 8;
+        units[tid] = u;
+        int up = tasks;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(kFull, up, o);
+            if (lane >= o) up += y;
+        }
+        ends[tid] = up;
+        if (lane == 31) sums[warp] = up;
+    }
+    __syncthreads();
+    int before = 0, total = 0;
+#pragma unroll
+    for (int i = 0; i < kUnits / 32; ++i) {
+        before += i < warp ? sums[i] : 0;
+        total += sums[i];
+    }
+    if (total == 0) return;
+    __syncthreads();
+    if (tid < kUnits) ends[tid] += before;
+    __syncthreads();
+    const int low = kChunkTile / a.G * a.G;
+#pragma unroll 1
+    for (int task = warp * nctas + blockIdx.x; task < total; task += kWarps * nctas) {
+        int c0 = 0, hi = kUnits - 1;  // the first unit that ends after the task
+        while (c0 < hi) {
+            const int mid = (c0 + hi) >> 1;
+            if (ends[mid] > task)
+                hi = mid;
+            else
+                c0 = mid + 1;
+        }
+        const int4 u = units[c0];
+        const int rows = u.y * a.G, i = task - (ends[c0] - (rows + 7) / 8 * 8), row = (i >> 3) * 8 + (lane & 7), dim4 = (i & 7) * 4 + (lane >> 3);
+        if (row >= rows) continue;
+        const int at = row < low ? row : row - low + kChunkTile;
+        float top = -INFINITY, sum = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int k0 = 0; k0 < u.w; k0 += kJoin) {
+            float2 ml[kJoin];
+            float4 o[kJoin];
+#pragma unroll
+            for (int k = 0; k < kJoin; ++k) {
+                const int64_t piece = piece_at(c0, min(k0 + k, u.w - 1));
+                ml[k] = __ldcg(x.ml + piece * kChunkRows + at);
+                o[k] = __ldcg(x.o + (piece * (kHeadDim / 4) + dim4) * kChunkRows + at);
+            }
+            float now = top;
+#pragma unroll
+            for (int k = 0; k < kJoin; ++k) now = fmaxf(now, ml[k].x);
+            const float old = top == -INFINITY ? 0.f : ex2((top - now) * x.qscale);
+            sum *= old;
+            v = make_float4(v.x * old, v.y * old, v.z * old, v.w * old);
+#pragma unroll
+            for (int k = 0; k < kJoin; ++k) {
+                if (k0 + k >= u.w || (ml[k].x == -INFINITY && ml[k].y == 0.f)) continue;  // a piece that the row does not see
+                const float f = ml[k].x == -INFINITY ? 0.f : ex2((ml[k].x - now) * x.qscale);
+                sum = fmaf(ml[k].y, f, sum);
+                v = make_float4(fmaf(o[k].x, f, v.x), fmaf(o[k].y, f, v.y), fmaf(o[k].z, f, v.z), fmaf(o[k].w, f, v.w));
+            }
+            top = now;
+        }
+        const int token = row / a.G;
+        const int64_t to = ((int64_t)(u.x + token) * a.H + u.z * a.G + (row - token * a.G)) * kHeadDim + 4 * dim4;
+        *reinterpret_cast<uint2*>(a.out + to) = pack4<F16>(v, sum == 0.f ? 0.f : x.back / sum);
+    }
+}
+
 template <bool F16, int Z>
 __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
     quant_attn_kernel(const __grid_constant__ QuantAttnArgs a, const __grid_constant__ CacheMaps maps, const __grid_constant__ QuantWork w, int nctas,
-                      int alone)
+                      int alone, const __grid_constant__ ChunkJobs chunks)
 {
     using C = Cfg<Z>;
     constexpr int kWarps = C::kWarps, kStages = C::kStages, kCols = C::kCols;
@@ -855,7 +944,11 @@ __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
             at_stage = at_stage + 1 == kStages ? 0 : at_stage + 1;
         }
     }
-    pdl_wait();  // the call is not over before its begin kernel
+    pdl_wait();  // the call is not over before its begin kernel, and the one of many tokens
+    if (!alone) {
+        __syncthreads();
+        join_chunks<F16, C::kThreads>(a, chunks, nctas, reinterpret_cast<int4*>(sm + C::kOffSum));  // (where no copy writes)
+    }
 }
 
 PFN_cuTensorMapEncodeTiled_v12000 encode_tiled()
@@ -895,11 +988,12 @@ cudaError_t setup_few()
 }
 
 template <bool F16>
-cudaError_t launch_few(const QuantAttnArgs& a, const CacheMaps& maps, const QuantWork& w, int nctas, int alone, cudaStream_t st)
+cudaError_t launch_few(const QuantAttnArgs& a, const CacheMaps& maps, const QuantWork& w, int nctas, int alone,
+                       const ChunkJobs& chunks, cudaStream_t st)
 {
     if (a.few * a.G <= Cfg<1>::kCols)
-        return launch_pdl(quant_attn_kernel<F16, 1>, nctas, Cfg<1>::kThreads, Cfg<1>::kSmemBytes, st, a, maps, w, nctas, alone);
-    return launch_pdl(quant_attn_kernel<F16, 2>, nctas, Cfg<2>::kThreads, Cfg<2>::kSmemBytes, st, a, maps, w, nctas, alone);
+        return launch_pdl(quant_attn_kernel<F16, 1>, nctas, Cfg<1>::kThreads, Cfg<1>::kSmemBytes, st, a, maps, w, nctas, alone, chunks);
+    return launch_pdl(quant_attn_kernel<F16, 2>, nctas, Cfg<2>::kThreads, Cfg<2>::kSmemBytes, st, a, maps, w, nctas, alone, chunks);
 }
 
 }  // namespace
@@ -927,6 +1021,7 @@ cudaError_t launch_quant_attn(const QuantAttnArgs& a, bool short_boxes, cudaStre
     unsigned char* base = static_cast<unsigned char*>(a.work);
     QuantWork w;
     w.done = reinterpret_cast<int32_t*>(base);
+    w.jobs = reinterpret_cast<int4*>(base + kOffJobs);
     w.state = reinterpret_cast<State*>(base + kOffState);
     w.o = reinterpret_cast<float4*>(base + kOffO);
     w.chunk = reinterpret_cast<int32_t*>(base + kWorkBytes);
@@ -936,6 +1031,7 @@ cudaError_t launch_quant_attn(const QuantAttnArgs& a, bool short_boxes, cudaStre
     few.few = std::min(a.most, (a.most * a.G <= kMostCols ? kMostCols : Cfg<1>::kCols) / a.G);
     const int alone = a.most <= few.few;
     if ((e = launch_pdl(quant_begin_kernel, 1, 256, 0, st, w, alone)) != cudaSuccess) return e;
+    ChunkJobs chunks{};
     if (!alone) {
         ChunkArgs c{};
         c.q = a.q;
@@ -963,9 +1059,11 @@ cudaError_t launch_quant_attn(const QuantAttnArgs& a, bool short_boxes, cudaStre
         c.Vs = a.Vs;
         c.least = few.few + 1;
         c.most = a.most;
+        c.jobs = w.jobs;
+        chunks = chunk_jobs(c);
         if ((e = launch_chunk8(c, nctas, short_boxes, st)) != cudaSuccess) return e;
     }
-    return a.fp16 ? launch_few<true>(few, maps, w, nctas, alone, st) : launch_few<false>(few, maps, w, nctas, alone, st);
+    return a.fp16 ? launch_few<true>(few, maps, w, nctas, alone, chunks, st) : launch_few<false>(few, maps, w, nctas, alone, chunks, st);
 }
 
 }  // namespace dkv

@@ -130,6 +130,20 @@ def test_one_long_sequence(cuda, dtype):
     check(quant.Cache8(np.array([[[9000, 5]]]), 16, H=16, dtype=dtype), 0, [3])
 
 
+@pytest.mark.parametrize("G,tokens", [(7, [5]), (8, [16, 1]), (3, [50]), (4, [64, 2, 9]), (1, [200])])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("causal", [True, False])
+def test_drafts_in_many_pieces(cuda, G, tokens, dtype, causal):
+    """Units of up to 256 rows that many CTAs have a part of, joined in the same order each time."""
+    ctx = [12003, 5, 2500][:len(tokens)]
+    c8 = quant.Cache8(lens_of(1, len(tokens), 1, ctx, tokens, G), 32, H=G, dtype=dtype)
+    c = check(c8, 0, tokens, causal, pad=3)
+    assert torch.isnan(c.out[sum(tokens):].float()).all()
+    before = c.out.clone()
+    c.out.fill_(NAN)
+    assert torch.equal(c.run().out[:sum(tokens)], before[:sum(tokens)])
+
+
 def test_scales_far_apart(cuda):
     """Rows of V up to 2^40 apart, of K up to 2^6, and many rows of V that are all zero (their scale byte is 1) with weight."""
     r = np.random.default_rng(1)
