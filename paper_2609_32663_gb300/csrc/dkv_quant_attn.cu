@@ -7,7 +7,9 @@
 // Unit of work: a slab, its columns against the cache rows that its last token sees, in tiles of 32 rows. Units lie end to
 // end on a line of costs, a tile each and kStart for a unit's start, that is cut into equal shares, one a CTA, one CTA an SM;
 // a CTA's warps take the tiles of its part of a unit in turn, each through a ring of its own, and are joined at its end. A unit
-// that lies in several CTAs is joined by the one that finishes last, in the order of the CTAs.
+// that lies in several CTAs is joined by the one that finishes last, in the order of the CTAs. Behind chunk_attn_kernel this one also
+// joins what that left in many pieces, a warp 8 rows and 16 dims (join_chunks; it waits for that kernel's end anyway): 3 us for
+// the drafts of four sequences, 17 where a unit's last CTA did it.
 //
 //   quant_begin_kernel  clears the counters.
 //   quant_attn_kernel   the rest.
