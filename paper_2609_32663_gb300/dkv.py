@@ -101,6 +101,10 @@ class Pages:
         return ctypes.byref(self.c)
 
     @cached_property
+    def at(self):
+        return ctypes.addressof(self.c)
+
+    @cached_property
     def slabs(self):
         return self.L * self.B * self.H_kv
 
@@ -116,9 +120,11 @@ class Rotary:
     def __init__(self):
         self.c = dkv_rotary()
         self.ref = ctypes.byref(self.c)
+        self.at = ctypes.addressof(self.c)
 
 
 _lib = None
+_entry = {}  # addresses of the loaded library's entry points that csrc/dkv_torch.cpp calls
 
 
 def lib(path: str | None = None):
@@ -214,7 +220,14 @@ def lib(path: str | None = None):
     L.dkv_quant_attn.argtypes = [PG, I32, I32, I32, I32, V, I64, V, V, V, V, V, V, V, I32, ctypes.c_float, V, V, I64, V, V]
     if path is None:
         _lib = L
+        _entry.update({n: ctypes.cast(getattr(L, n), V).value for n in ("dkv_rope", "dkv_rope_append", "dkv_quant_compact", "dkv_quant_attn")})
     return L
+
+
+def _address(name):
+    """Address of an entry point."""
+    lib()
+    return _entry[name]
 
 
 def _check(status, func):
@@ -273,6 +286,24 @@ class _Torch:
         C = torch._C
         self.raw_stream = getattr(C, "_cuda_getCurrentRawStream", None)
         self.device = getattr(C, "_cuda_getDevice", None)
+        self.calls = _torch_calls()
+
+
+def _torch_calls():
+    """The module of csrc/dkv_torch.cpp, which looks at a call's tensors and makes it (None where it was not built: the
+    functions below do the same themselves)."""
+    path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "dkv_torch.so")
+    if not os.path.exists(path):
+        return None
+    from importlib.machinery import ExtensionFileLoader
+    from importlib.util import module_from_spec, spec_from_file_location
+    try:
+        spec = spec_from_file_location("dkv_torch", path, loader=ExtensionFileLoader("dkv_torch", path))
+        module = module_from_spec(spec)
+        spec.loader.exec_module(module)
+    except ImportError:  # (built against another torch)
+        return None
+    return module
 
 
 def _torch():
@@ -802,8 +833,12 @@ def _rotary_ref(rotary):
 def dkv_rope(x, positions, rotary: Rotary, out, status=None, stream=None):
     """Rows x [T][heads][128] turned by their positions (int32 [T]) -> out, of x's type and shape. Either may be a slice of a
     projection; out may be x."""
-    half = _rows16(x, "x")
     at, queue = _where(stream)
+    if _T.calls is not None and isinstance(rotary, Rotary):
+        done = _T.calls.rope(_entry.get("dkv_rope") or _address("dkv_rope"), at, queue, rotary.at, x, positions, out, status)
+        if done is not None:
+            return _check(done, "dkv_rope")
+    half = _rows16(x, "x")
     tokens, heads = x.shape[:2]
     xp, xs = _token_rows(x, "x", at, x.dtype, tokens, heads)
     op, os_ = _token_rows(out, "out", at, x.dtype, tokens, heads)
@@ -821,9 +856,15 @@ def dkv_rope_append(pages: Pages, layer: int, q, k_new, v_new, positions, cu_tok
     """One layer's new tokens: q [T][H][128] turned by their positions (int32 [T]) -> q_out, k_new turned and with v_new
     [T][H_kv][128] written to their slabs' pages, which are of their type, or 8-bit where the scales Ks and Vs are given. q and
     q_out, or k_new and v_new, may be None; without a rotary nothing is turned (and positions is not used)."""
+    at, queue = _where(stream)
+    if _T.calls is not None and (rotary is None or isinstance(rotary, Rotary)):
+        done = _T.calls.rope_append(
+            _entry.get("dkv_rope_append") or _address("dkv_rope_append"), at, queue, pages.at, layer, None if rotary is None else rotary.at, q,
+            k_new, v_new, positions, cu_tokens, table, len, Kp, Vp, q_out, Ks, Vs, status)
+        if done is not None:
+            return _check(done, "dkv_rope_append")
     first, name = (q, "q") if q is not None else (k_new, "k_new (without q)")
     half, T = _rows16(first, name), _torch()
-    at, queue = _where(stream)
     tokens, dtype = first.shape[0], first.dtype
     qp = op = kp = vp = None
     qs = os_ = ks = 0
@@ -857,6 +898,12 @@ def dkv_quant_compact(pages: Pages, plan: Plan, K, V, table, len, Kp, Vp, Ks, Vs
     """The kept rows of plan sequence i become the last rows of slot seq[i]'s slabs, in 8-bit pages with their scales. K and V
     are bfloat16 or float16 [L][plan B][H_kv][T_stride][128]."""
     T, sh = _torch(), plan.shape
+    if T.calls is not None:
+        at, queue = _where(stream)
+        done = T.calls.quant_compact(_entry.get("dkv_quant_compact") or _address("dkv_quant_compact"), at, queue, pages.at, plan.address, seq, sh.L,
+                                     plan.B, sh.H_kv, K, V, T_stride, table, len, Kp, Vp, Ks, Vs, status)
+        if done is not None:
+            return _check(done, "dkv_quant_compact")
     for t, name in ((K, "K"), (V, "V")):
         _device_of(t, name)
         if t.dtype not in (T.torch.bfloat16, T.torch.float16):
@@ -890,8 +937,13 @@ def dkv_quant_attn(pages: Pages, layer: int, q, cu_tokens, table, len, Kp, Vp, K
                    scale: float = 0.0, max_tokens: int = 0, status=None, stream=None):
     """One layer's attention of q [T][H][128] over 8-bit pages -> out [T][H][128], both bfloat16 or float16. max_tokens: the
     most tokens that one sequence brings (0: not known)."""
-    half, T = _rows16(q, "q"), _torch()
     at, queue = _where(stream)
+    if _T.calls is not None:
+        done = _T.calls.quant_attn(_entry.get("dkv_quant_attn") or _address("dkv_quant_attn"), at, queue, pages.at, layer, q, cu_tokens, table,
+                                   len, Kp, Vp, Ks, Vs, out, workspace, causal, scale, max_tokens, status)
+        if done is not None:
+            return _check(done, "dkv_quant_attn")
+    half, T = _rows16(q, "q"), _torch()
     tokens = q.shape[0]
     qp, qs = _token_rows(q, "q", at, q.dtype, tokens, pages.H)
     pool = pages.num_pages * pages.page_rows * 128
