@@ -20,7 +20,6 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libdkv.so")
 OBJDIR = os.path.join(PKG, "_build")
-TORCH_CALLS = os.path.join(PKG, "dkv_torch.so")  # csrc/dkv_torch.cpp, a Python module
 LIB_DEBUG = os.path.join(PKG, "libdkv_debug.so")
 OBJDIR_DEBUG = os.path.join(PKG, "_build_debug")
 
@@ -95,17 +94,21 @@ def _build_locked(verbose, extra_flags, lib, objdir):
     return lib
 
 
+def torch_calls(version):
+    """The Python module of csrc/dkv_torch.cpp for this version of torch (its tensors are that version's)."""
+    return os.path.join(PKG, f"dkv_torch-{version}.so")
+
+
 def build_torch_calls(force=False):
     """Compile csrc/dkv_torch.cpp against the installed torch. Returns its path, or None where the headers of Python or torch
     are not installed (dkv.py then looks at tensors in Python)."""
     import sysconfig
-    from importlib.util import find_spec
-
-    src = os.path.join(CSRC, "dkv_torch.cpp")
-    python, spec = sysconfig.get_paths()["include"], find_spec("torch")
-    if spec is None:
+    try:
+        import torch as installed
+    except ImportError:
         return None
-    torch = os.path.dirname(spec.origin)
+    src, lib = os.path.join(CSRC, "dkv_torch.cpp"), torch_calls(installed.__version__)
+    python, torch = sysconfig.get_paths()["include"], os.path.dirname(installed.__file__)
     cuda = os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")
     headers = [os.path.join(python, "Python.h"), os.path.join(torch, "include", "torch", "csrc", "autograd", "python_variable.h")]
     if not all(os.path.exists(h) for h in headers):
@@ -114,17 +117,17 @@ def build_torch_calls(force=False):
     with open(os.path.join(OBJDIR, ".lock_torch"), "w") as lock:
         fcntl.flock(lock, fcntl.LOCK_EX)
         deps = [src, os.path.join(INCLUDE, "dkv.h"), __file__, *headers]
-        if not force and os.path.exists(TORCH_CALLS) and all(os.path.getmtime(p) <= os.path.getmtime(TORCH_CALLS) for p in deps):
-            return TORCH_CALLS
-        tmp = TORCH_CALLS + ".tmp"
+        if not force and os.path.exists(lib) and all(os.path.getmtime(p) <= os.path.getmtime(lib) for p in deps):
+            return lib
+        tmp = lib + ".tmp"
         cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", src, "-o", tmp, "-I" + INCLUDE, "-I" + python, "-I" + cuda,
                "-I" + os.path.join(torch, "include"), "-I" + os.path.join(torch, "include", "torch", "csrc", "api", "include"),
                "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError(f"g++ failed on {src}:\n{r.stdout}\n{r.stderr}")
-        os.replace(tmp, TORCH_CALLS)
-    return TORCH_CALLS
+        os.replace(tmp, lib)
+    return lib
 
 
 if __name__ == "__main__":

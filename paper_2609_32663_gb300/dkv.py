@@ -286,23 +286,21 @@ class _Torch:
         C = torch._C
         self.raw_stream = getattr(C, "_cuda_getCurrentRawStream", None)
         self.device = getattr(C, "_cuda_getDevice", None)
-        self.calls = _torch_calls()
+        self.calls = _torch_calls(torch.__version__)
 
 
-def _torch_calls():
+def _torch_calls(version):
     """The module of csrc/dkv_torch.cpp, which looks at a call's tensors and makes it (None where it was not built: the
     functions below do the same themselves)."""
-    path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "dkv_torch.so")
+    from .build import torch_calls
+    path = torch_calls(version)
     if not os.path.exists(path):
         return None
     from importlib.machinery import ExtensionFileLoader
     from importlib.util import module_from_spec, spec_from_file_location
-    try:
-        spec = spec_from_file_location("dkv_torch", path, loader=ExtensionFileLoader("dkv_torch", path))
-        module = module_from_spec(spec)
-        spec.loader.exec_module(module)
-    except ImportError:  # (built against another torch)
-        return None
+    spec = spec_from_file_location("dkv_torch", path, loader=ExtensionFileLoader("dkv_torch", path))
+    module = module_from_spec(spec)
+    spec.loader.exec_module(module)
     return module
 
 

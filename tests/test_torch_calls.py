@@ -16,7 +16,7 @@ def calls():
     build.build_library()
     if build.build_torch_calls() is None:
         pytest.skip("no headers of Python or torch")
-    module = dkv._torch_calls()
+    module = dkv._torch_calls(torch.__version__)
     assert module is not None
     return module
 
