@@ -172,13 +172,14 @@ __global__ void __launch_bounds__(kRopeThreads, 1) rope_kernel(const __grid_cons
                 hi = mid - 1;
         }
         const int64_t slab = (int64_t)b * a.Hkv + (h - qheads < a.Hkv ? h - qheads : h - qheads - a.Hkv);
-        const int n = a.len[slab], r = n - (cu[b + 1] - t);
-        if (r < 0 || n > a.max_pages * a.P) {  // (the product is below 2^31)
+        // (Both ends of n are looked at before the place is formed: a length near -2^31 would wrap to one that passes.)
+        const int n = a.len[slab], behind = cu[b + 1] - t;  // behind: 1 .. T
+        if (n < behind || n > a.max_pages * a.P) {          // (the product is below 2^31)
             report(a, DKV_DEV_PAGE_RANGE);
             return -1;
         }
         entry = slab * a.max_pages;
-        return r;
+        return n - behind;
     };
     static_assert(kMostHeads <= 32, "a lane each");
     Item ahead = now;
