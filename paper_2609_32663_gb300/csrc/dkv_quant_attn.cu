@@ -547,8 +547,21 @@ __device__ __forceinline__ void tile_step(Acc<Z>& c, const uint32_t (&q)[Z][16],
 // Factor that joins a state to others of this maximum; of its O besides 2^(scale - the largest scale).
 __device__ __forceinline__ float factor(float x, float most) { return x == -INFINITY ? 0.f : ex2(x - most); }
 
-// What turns O into the output: 2^(scale - 127 - kShift) / sum; 0 for no rows. (A sum is at most 2^39 and the scale 2^120.)
-__device__ __forceinline__ float final_scale(float scale, float sum) { return sum == 0.f ? 0.f : ex2(scale - (127.f + kShift)) / sum; }
+// What turns O into the output: 1 / sum times 2^(scale - 127 - kShift), 0 for no rows. That power may be 2^-133, below the
+// least normal number, where O / sum times it is a normal bf16 value: it is two factors of about its root, and O is multiplied by
+// `first` and then by `last`. (A sum is 1 to 2^39, so both are normal.)
+struct Final {
+    float first, last;
+};
+__device__ __forceinline__ Final final_scale(float scale, float sum)
+{
+    const int e = (int)scale - 127 - (int)kShift, half = e / 2;
+    return Final{sum == 0.f ? 0.f : exp2i(half) / sum, exp2i(e - half)};
+}
+__device__ __forceinline__ float4 final4(float4 x, Final z)
+{
+    return make_float4(x.x * z.first * z.last, x.y * z.first * z.last, x.z * z.first * z.last, x.w * z.first * z.last);
+}
 
 template <bool F16>
 __device__ __forceinline__ uint2 pack4(float4 x, float z)
@@ -848,7 +861,7 @@ __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
             const int token = mine / a.G, head_j = mine - token * a.G;
             uint16_t* out = a.out + ((int64_t)(k.t + token) * a.H + k.g * a.G + head_j) * kHeadDim;
             const int64_t slot = (int64_t)c * 2 + (k.j0 == 0);
-            const float z = final_scale(total.scale, total.sum);
+            const Final z = final_scale(total.scale, total.sum);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 __syncthreads();
@@ -876,7 +889,7 @@ __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
                     }
                     const int dim = 16 * (chunk >> 1) + 8 * half + 4 * (chunk & 1);
                     if (whole)
-                        *reinterpret_cast<uint2*>(out + dim) = pack4<F16>(v, z);
+                        *reinterpret_cast<uint2*>(out + dim) = pack4<F16>(final4(v, z), 1.f);
                     else
                         __stcg(w.o + (slot * kMostCols + mine) * (kHeadDim / 4) + dim / 4, v);
                 }
@@ -929,8 +942,8 @@ __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
                         }
                         all = now;
                     }
-                    const float y = final_scale(all.scale, all.sum);
-                    const uint2 lo = pack4<F16>(v[0], y), hi = pack4<F16>(v[1], y);
+                    const Final y = final_scale(all.scale, all.sum);
+                    const uint2 lo = pack4<F16>(final4(v[0], y), 1.f), hi = pack4<F16>(final4(v[1], y), 1.f);
                     *reinterpret_cast<uint4*>(out + 8 * chunk) = make_uint4(lo.x, lo.y, hi.x, hi.y);
                 }
             }
