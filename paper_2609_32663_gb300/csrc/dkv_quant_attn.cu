@@ -779,7 +779,10 @@ __global__ void __launch_bounds__(Cfg<Z>::kThreads, 1)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int y = 8 * z + 2 * t + e;
-                    cs[z][e] = __shfl_sync(kFull, back, 8 * t + 4 * e) * a.qscale;
+                    // Positive and finite, whatever q's size and the scale are (their product may pass fp32's range while the
+                    // scores do not, as those of a q or K of zeros): 0 or infinity times an infinite or a zero score were NaN. At the least
+                    // number, 2^-149, scores are below 2^-21, as they should be; at the largest those above the others have all weight.
+                    cs[z][e] = fminf(fmaxf(__shfl_sync(kFull, back, 8 * t + 4 * e) * a.qscale, 0x1p-149f), 0x1.fffffep127f);
                     lim[z][e] = y < cols ? sees(a, k.len, k.n, y / a.G) : k.rows;
                     acc.top[z][e] = -INFINITY;
                     acc.scale[z][e] = 0;

@@ -1,10 +1,11 @@
-"""dkv_quant_attn at the ends of its ranges: V of the least scales."""
+"""dkv_quant_attn at the ends of its ranges: V of the least scales, and products of q and the softmax scale that pass fp32's range
+by themselves."""
 import pytest
 import torch
 
 import quant
 from test_gpu_chunk import lens_of
-from test_gpu_quant import Call, inputs
+from test_gpu_quant import Call, check, inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +35,34 @@ def test_values_of_the_least_scales(cuda, byte, tokens, ctx):
     assert int(c.status) == 0
     err = ((got - want).abs() / bound).max()
     assert float(err) <= 1, f"{float(err):.3g} times the bound"
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("tokens", TOKENS)
+@pytest.mark.parametrize("size,scale", [(0.0, 2.0 ** -30), (0.0, 1e-38), (0.0, 1e-45), (2.0 ** -14, 1e-45), (1.0, 1e-45), (2.0 ** -120, 2.0 ** -40)])
+def test_scores_that_vanish(cuda, dtype, tokens, size, scale):
+    """Scores of nearly 0: the output is the mean of the rows of V that are seen."""
+    c8 = cache(tokens, 70, dtype=dtype)
+    _, q = inputs(c8, tokens, 2)
+    check(c8, 0, tokens, most=max(tokens), scale=scale, q=(q.double() * size).to(dtype))
+
+
+@pytest.mark.parametrize("tokens", TOKENS)
+def test_some_queries_of_zeros(cuda, tokens):
+    """Beside others in the same call, with a small scale."""
+    c8 = cache(tokens, 70)
+    _, q = inputs(c8, tokens, 2)
+    q[0, ::2] = 0
+    q[-1, 1::3] = 0
+    check(c8, 0, tokens, most=max(tokens), scale=2.0 ** -26, q=q)
+
+
+@pytest.mark.parametrize("tokens", TOKENS)
+def test_large_queries_and_scale(cuda, tokens):
+    """Their product passes fp32's range; K is 0 in all rows, and so are the scores."""
+    c8 = cache(tokens, 70)
+    held = c8.Ks != 255
+    c8.K8[held], c8.Ks[held] = 0, 1
+    c8.sync()
+    _, q = inputs(c8, tokens, 2)
+    check(c8, 0, tokens, most=max(tokens), scale=2.0 ** 20, q=(q.double().sign() * 2.0 ** 127).to(q.dtype))
