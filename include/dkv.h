@@ -609,7 +609,9 @@ dkv_status dkv_rotary_custom(dkv_rotary* rotary, int32_t rot_dim, int32_t interl
  * are pruned.
  * dtype      DKV_BF16 or DKV_FP16: type of x and out.
  * x, out     device [num_tokens][heads][128], token t at t * x_stride (out_stride) elements. out is
- *            x, with its stride, or does not overlap it. num_tokens * heads <= 2^30.
+ *            x, with its stride, or its rows do not overlap x's: with the same stride they may lie
+ *            between those (other heads of the same projection), with another one the two lie one
+ *            behind the other. num_tokens * heads <= 2^30.
  *            Strides are multiples of 8, at least heads*128; 16-byte aligned.
  * positions  device int32 [num_tokens], of any sign.
  * rotary     host; read by the call, not kept.
@@ -644,7 +646,7 @@ dkv_status dkv_rope(const dkv_rotary* rotary, int32_t dtype, int32_t num_tokens,
  *              of order set DKV_DEV_PAGE_RANGE and nothing is written; a row whose length, page
  *              or place is out of range is skipped and sets the same bit.
  * q, q_out     [num_tokens][H][128], token t at t * q_stride (q_out_stride) elements, or both NULL.
- *              q_out is q, with its stride, or does not overlap it.
+ *              q_out is q, with its stride, or its rows do not overlap q's, as out and x of dkv_rope.
  * k_new, v_new [num_tokens][H_kv][128], token t at t * kv_stride elements, or both NULL. They are
  *              not changed, and must not overlap the pools or q_out.
  * Kp, Vp       the pools: 16-bit of dtype where Ks and Vs are NULL, else 8-bit. A turned key is

@@ -114,13 +114,18 @@ bool rotary_ok(const dkv_rotary* r, const int32_t* positions, dkv::RopeArgs* a)
     return true;
 }
 
-// Rows of q that are written elsewhere or in place: [out, out + bytes) is [q, q + bytes) or apart from it.
+// Rows of q that are written elsewhere or in place: y is x, with its stride, or no row of one is a part of one of the other. With
+// one stride for both that is looked at row by row (x and y may be other heads of the same tokens); with two, their spans
+// have to lie apart.
 bool apart(const void* x, int64_t x_stride, const void* y, int64_t y_stride, int64_t tokens, int64_t heads)
 {
     if (x == y && x_stride == y_stride) return true;
-    const uintptr_t x0 = reinterpret_cast<uintptr_t>(x), y0 = reinterpret_cast<uintptr_t>(y);
-    const uintptr_t nx = (uintptr_t)((tokens - 1) * x_stride + heads * dkv::kHeadDim) * 2, ny = (uintptr_t)((tokens - 1) * y_stride + heads * dkv::kHeadDim) * 2;
-    return x0 + nx <= y0 || y0 + ny <= x0;
+    const uintptr_t x0 = reinterpret_cast<uintptr_t>(x), y0 = reinterpret_cast<uintptr_t>(y), row = (uintptr_t)heads * dkv::kHeadDim * 2;
+    const uintptr_t nx = (uintptr_t)(tokens - 1) * x_stride * 2 + row, ny = (uintptr_t)(tokens - 1) * y_stride * 2 + row;
+    if (x0 + nx <= y0 || y0 + ny <= x0) return true;
+    if (x_stride != y_stride) return false;
+    const uintptr_t stride = (uintptr_t)x_stride * 2, next = (x0 > y0 ? x0 - y0 : y0 - x0) % stride;  // from a row to the other's next
+    return next >= row && next + row <= stride;
 }
 
 // What dkv_page_tables and dkv_page_release share.
@@ -400,7 +405,8 @@ dkv_status dkv_rope(const dkv_rotary* rotary, int32_t dtype, int32_t num_tokens,
     if (!x || !out || !aligned(x, 16) || !aligned(out, 16)) return refuse("x/out is NULL or not 16-byte aligned");
     if (!aligned(status, 4)) return refuse("status must be 4-byte aligned");
     if (!stride_ok("x_stride", x_stride, heads) || !stride_ok("out_stride", out_stride, heads)) return DKV_ERR_INVALID_ARG;
-    if (!apart(x, x_stride, out, out_stride, num_tokens, heads)) return refuse("out overlaps x: it is x, with its stride, or apart from it");
+    if (!apart(x, x_stride, out, out_stride, num_tokens, heads))
+        return refuse("out overlaps x: it is x, with its stride, or its rows (with another stride, its span) are apart from x's");
     a.q = static_cast<const uint16_t*>(x);
     a.q_stride = x_stride;
     a.q_out = static_cast<uint16_t*>(out);
@@ -437,7 +443,7 @@ dkv_status dkv_rope_append(const dkv_pages* g, int32_t layer, const dkv_rotary* 
     if (q) {
         if (!stride_ok("q_stride", q_stride, g->H) || !stride_ok("q_out_stride", q_out_stride, g->H)) return DKV_ERR_INVALID_ARG;
         if (!apart(q, q_stride, q_out, q_out_stride, num_tokens, g->H))
-            return refuse("q_out overlaps q: it is q, with its stride, or apart from it");
+            return refuse("q_out overlaps q: it is q, with its stride, or its rows (with another stride, its span) are apart from q's");
     }
     if (k_new) {
         if (!Kp || !Vp) return refuse("NULL Kp/Vp");
