@@ -94,9 +94,20 @@ def _build_locked(verbose, extra_flags, lib, objdir):
     return lib
 
 
+TORCH_CALLS = os.path.join(CSRC, "dkv_torch.cpp")
+
+
 def torch_calls(version):
-    """The Python module of csrc/dkv_torch.cpp for this version of torch (its tensors are that version's)."""
-    return os.path.join(PKG, f"dkv_torch-{version}.so")
+    """The Python module of csrc/dkv_torch.cpp for this version of torch (its tensors are that version's), this Python and these
+    sources: a module that was built from another include/dkv.h, whose structs and arguments may differ, has another
+    name, and so is not loaded, whoever builds the library alone."""
+    import hashlib
+    import sysconfig
+    text = hashlib.sha256()
+    for path in (os.path.join(INCLUDE, "dkv.h"), TORCH_CALLS):
+        with open(path, "rb") as f:
+            text.update(f.read() + b"\0")
+    return os.path.join(PKG, f"dkv_torch-{version}-{sysconfig.get_config_var('SOABI')}-{text.hexdigest()[:16]}.so")
 
 
 def build_torch_calls(force=False):
@@ -107,7 +118,7 @@ def build_torch_calls(force=False):
         import torch as installed
     except ImportError:
         return None
-    src, lib = os.path.join(CSRC, "dkv_torch.cpp"), torch_calls(installed.__version__)
+    lib = torch_calls(installed.__version__)
     python, torch = sysconfig.get_paths()["include"], os.path.dirname(installed.__file__)
     cuda = os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")
     headers = [os.path.join(python, "Python.h"), os.path.join(torch, "include", "torch", "csrc", "autograd", "python_variable.h")]
@@ -116,16 +127,16 @@ def build_torch_calls(force=False):
     os.makedirs(OBJDIR, exist_ok=True)
     with open(os.path.join(OBJDIR, ".lock_torch"), "w") as lock:
         fcntl.flock(lock, fcntl.LOCK_EX)
-        deps = [src, os.path.join(INCLUDE, "dkv.h"), __file__, *headers]
+        deps = [__file__, *headers]  # (the sources are in its name)
         if not force and os.path.exists(lib) and all(os.path.getmtime(p) <= os.path.getmtime(lib) for p in deps):
             return lib
         tmp = lib + ".tmp"
-        cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", src, "-o", tmp, "-I" + INCLUDE, "-I" + python, "-I" + cuda,
+        cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", TORCH_CALLS, "-o", tmp, "-I" + INCLUDE, "-I" + python, "-I" + cuda,
                "-I" + os.path.join(torch, "include"), "-I" + os.path.join(torch, "include", "torch", "csrc", "api", "include"),
                "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
-            raise RuntimeError(f"g++ failed on {src}:\n{r.stdout}\n{r.stderr}")
+            raise RuntimeError(f"g++ failed on {TORCH_CALLS}:\n{r.stdout}\n{r.stderr}")
         os.replace(tmp, lib)
     return lib
 

@@ -290,10 +290,13 @@ class _Torch:
 
 
 def _torch_calls(version):
-    """The module of csrc/dkv_torch.cpp, which looks at a call's tensors and makes it (None where it was not built: the
-    functions below do the same themselves)."""
+    """The module of csrc/dkv_torch.cpp, which looks at a call's tensors and makes it (None where it was not built of these
+    sources: the functions below do the same themselves)."""
     from .build import torch_calls
-    path = torch_calls(version)
+    try:
+        path = torch_calls(version)
+    except OSError:  # (no sources here)
+        return None
     if not os.path.exists(path):
         return None
     from importlib.machinery import ExtensionFileLoader
