@@ -111,9 +111,11 @@ def torch_calls(version):
 
 
 def build_torch_calls(force=False):
-    """Compile csrc/dkv_torch.cpp against the installed torch. Returns its path, or None where the headers of Python or torch
-    are not installed (dkv.py then looks at tensors in Python)."""
+    """Compile csrc/dkv_torch.cpp against the installed torch. Returns its path, or None where it cannot be built: the
+    headers of Python or torch are not installed, or g++ is not there or fails (a warning says how). dkv.py then looks at
+    tensors in Python."""
     import sysconfig
+    import warnings
     try:
         import torch as installed
     except ImportError:
@@ -134,9 +136,14 @@ def build_torch_calls(force=False):
         cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", TORCH_CALLS, "-o", tmp, "-I" + INCLUDE, "-I" + python, "-I" + cuda,
                "-I" + os.path.join(torch, "include"), "-I" + os.path.join(torch, "include", "torch", "csrc", "api", "include"),
                "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
-        r = subprocess.run(cmd, capture_output=True, text=True)
+        try:
+            r = subprocess.run(cmd, capture_output=True, text=True)
+        except OSError as e:
+            warnings.warn(f"the compiled calls of dkv.py are not built, its own take longer: g++: {e}")
+            return None
         if r.returncode != 0:
-            raise RuntimeError(f"g++ failed on {TORCH_CALLS}:\n{r.stdout}\n{r.stderr}")
+            warnings.warn(f"the compiled calls of dkv.py are not built, its own take longer: g++ failed on {TORCH_CALLS}:\n{r.stdout}\n{r.stderr}")
+            return None
         os.replace(tmp, lib)
     return lib
 

@@ -290,8 +290,8 @@ class _Torch:
 
 
 def _torch_calls(version):
-    """The module of csrc/dkv_torch.cpp, which looks at a call's tensors and makes it (None where it was not built of these
-    sources: the functions below do the same themselves)."""
+    """The module of csrc/dkv_torch.cpp, which looks at a call's tensors and makes it. None where it was not built of these
+    sources, or does not load: the functions below do the same themselves."""
     from .build import torch_calls
     try:
         path = torch_calls(version)
@@ -302,8 +302,13 @@ def _torch_calls(version):
     from importlib.machinery import ExtensionFileLoader
     from importlib.util import module_from_spec, spec_from_file_location
     spec = spec_from_file_location("dkv_torch", path, loader=ExtensionFileLoader("dkv_torch", path))
-    module = module_from_spec(spec)
-    spec.loader.exec_module(module)
+    try:
+        module = module_from_spec(spec)
+        spec.loader.exec_module(module)
+    except (ImportError, OSError) as e:
+        import warnings
+        warnings.warn(f"{path} does not load, so that calls take longer on the host: {e}")
+        return None
     return module
 
 
