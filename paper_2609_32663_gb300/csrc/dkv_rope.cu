@@ -147,7 +147,8 @@ __global__ void __launch_bounds__(kRopeThreads, 1) rope_kernel(const __grid_cons
             const uint32_t bar = smem_u32(full + stage), dst = smem_u32(ring) + stage * stage_bytes;
             mbar_arrive_expect_tx(bar, (h1 - h0) * kRowBytes);
             const int q1 = min(h1, qheads);
-            if (q1 > h0) bulk_g2s(dst, a.q + t * a.q_stride + h0 * kHeadDim, (q1 - h0) * kRowBytes, bar, pol);
+            // (dkv_rope's heads may be more than 2^24: their elements pass 32 bits. Those of a geometry do not.)
+            if (q1 > h0) bulk_g2s(dst, a.q + t * a.q_stride + (int64_t)h0 * kHeadDim, (q1 - h0) * kRowBytes, bar, pol);
             if (POOL) {
                 const int k0 = max(h0, qheads), k1 = min(h1, qheads + a.Hkv), v0 = max(h0, qheads + a.Hkv);
                 const int64_t row = t * a.kv_stride;

@@ -1,4 +1,5 @@
-"""Where dkv_rope and dkv_rope_append may write: other heads of the tokens that are read, as their rows do not overlap."""
+"""Where dkv_rope and dkv_rope_append may read and write: other heads of the tokens that are read, as their rows do not overlap, and
+heads whose elements pass 32 bits."""
 import numpy as np
 import pytest
 import torch
@@ -58,3 +59,19 @@ def test_rows_that_overlap_are_refused(cuda):
                    (d[:20, :2], d[::2, :2]), (d[::2, :4], d[:20, 4:])):
         with pytest.raises(dkv.DkvError, match="overlap"):
             dkv.dkv_rope(x, dev(np.arange(x.shape[0])), r, out)
+
+
+def test_heads_whose_elements_pass_32_bits(cuda):
+    """One token of 2^24 + 57 heads, in place: as 2^24 + 57 tokens of one head at the same position."""
+    heads = 2 ** 24 + 57
+    x = torch.randn((64, 128), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(torch.bfloat16)
+    d = x.repeat(heads // 64 + 1, 1)[:heads].unsqueeze(0)
+    d[0, -50:] *= 3
+    want = torch.empty((64 + 50, 1, 128), dtype=d.dtype, device="cuda")
+    r = dkv.dkv_rotary_make()
+    dkv.dkv_rope(torch.cat([x, d[0, -50:]]).unsqueeze(1), dev(np.full(114, 1234567)), r, want)
+    dkv.dkv_rope(d, dev([1234567]), r, d)
+    torch.cuda.synchronize()
+    n = (heads - 50) // 64
+    assert (d[0, :64 * n].view(n, 64, 128) == want[:64, 0]).all()
+    assert torch.equal(d[0, 64 * n:-50], want[:heads - 50 - 64 * n, 0]) and torch.equal(d[0, -50:], want[64:, 0])
