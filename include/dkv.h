@@ -686,7 +686,11 @@ dkv_status dkv_quant_compact(const dkv_pages* pages, const dkv_plan* plan, const
  *             times their rows' V scales, are rounded to fp16, whose least step is at most 2^-31 of the largest
  *             weight times the largest V scale (of the rows that the token sees). Others: each row of K and V enters the products in dtype, which holds a
  *             bf16 one exactly, an fp16 one to 2^-24 (scale bytes up to 135, 2^8, as rows of fp16
- *             values have them; larger elements than 2^17 are infinite); weights are rounded to dtype.
+ *             values have them); weights are rounded to dtype. So a sequence's roundings go by
+ *             its call: by max_tokens, for 9 to 16 columns.
+ *             fp16, others, where a row of K or V has a scale byte above 135: what sees it is computed in fp32 without
+ *             the tensor cores, about 7 us a row and 256 / (H / H_kv) tokens (over some 250,000
+ *             rows the other waits run out: DKV_DEV_TMA_TIMEOUT).
  * workspace   dkv_quant_workspace_bytes(pages) bytes (-1: a bad geometry), about 46 MB.
  * Other arguments, what is promised and errors are those of dkv_chunk_attn.
  */

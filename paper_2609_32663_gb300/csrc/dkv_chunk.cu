@@ -23,7 +23,8 @@
 //     warp 10         walks the CTA's share and describes its units to the others (11 is idle).
 //   Over 8-bit pools (Q8; sequences of more columns than quant_attn_kernel takes, dkv_quant_attn.cu) the rows land in a ring
 //   of their own, and warps 12-15 turn them into the 16-bit tiles, a row a thread, with its scale: exactly in
-//   bf16, at half their value in fp16. Counters are cleared, and rows were appended, by kernels before.
+//   bf16, at half their value in fp16 (units with rows that this does not hold: redo_rows). Counters are cleared, and rows were
+//   appended, by kernels before.
 //
 // What bounds it. Next tokens stream the cache: 16 sequences of 3K-24K rows, 847 MB, in 131 us, 6.5
 // TB/s of the 6.8 of a plain copy. Turns and queries: a pair unit's tile (four products, 2,048 cycles
@@ -94,7 +95,7 @@ struct Lay {
     static constexpr int kOffScales = kOffRaw + kRaw * kHalf;
     static constexpr int kOffBars = kOffScales + kRaw * kTile;
     static constexpr int kNumBars = 2 * kStages + 2 * kRaw + 3 * kAhead + 11;  // full[], empty[], raw_full[], raw_empty[], said[], q_full[], late[], q_empty[2], s_full[2], p_half[2], p_full[2], o_done[2], fin
-    static constexpr int kOffMisc = kOffBars + (kNumBars + 1) / 2 * 16;       // int[4]: TMEM address, abort, last
+    static constexpr int kOffMisc = kOffBars + (kNumBars + 1) / 2 * 16;       // int[4]: TMEM address, abort, last, units with large rows (Q8 in fp16; bit: unit % 32)
     static constexpr int kOffPieces = kOffMisc + 16;                           // Piece[kAhead]
     static constexpr int kOffMl = kOffPieces + kAhead * kPieceBytes;           // float2[128]: group 1's (m, l), then group 0's
     static constexpr int kSmemBytes = kOffMl + 2 * kTile * 8;
@@ -567,8 +568,12 @@ __device__ __forceinline__ void widen_chunks(uint32_t src, uint32_t dst, int swz
     }
 }
 
+// The largest scale byte of a row that fp16 holds at half its value: 448 2^8 / 2 = 57,344 (rows of fp16 values have no larger one).
+// Units that have a larger one are computed again (redo_rows).
+constexpr uint32_t kMostByte = 135;
+
 // Row r of an 8-bit tile as a row of a 16-bit one, both as the copies' swizzle lays them out: value times 2^(u - 127) (half of
-// that in fp16, see kHalved). Every such value is one of the type, but for fp16 below 2^-23. bf16: the
+// that in fp16, see kHalved). Every such value is one of the type, but for fp16 below 2^-23 (and above kMostByte's). bf16: the
 // exponent and fraction of a code, moved to their places, are the value times 2^-120, subnormal ones too; NaN codes are
 // looked for and written apart.
 template <bool F16>
@@ -617,6 +622,10 @@ __device__ __forceinline__ void convert(unsigned char* sm, uint64_t* full, uint6
         if (!wait(&said[unit % kAhead], (unit / kAhead) & 1)) break;
         k = read_piece(sm + Y::kOffPieces + unit % kAhead * sizeof(Piece));
         ++unit;
+        if constexpr (F16) {
+            // (The softmax groups are a few units behind at most: a bit is looked at long before it is cleared.)
+            if (r == 0) atomicAnd(reinterpret_cast<unsigned*>(sm + Y::kOffMisc) + 3, ~(1u << ((unit + 15) & 31)));
+        }
         const int steps = k.steps();
 #pragma unroll 1
         for (int x = -2; x < 2 * steps && wait.ok; ++x) {
@@ -629,6 +638,10 @@ __device__ __forceinline__ void convert(unsigned char* sm, uint64_t* full, uint6
             ++pos;
             // Rows past the unit's last are zero in V's tiles: 0 NaN is NaN.
             const bool none = value && r >= k.kv - k.tile(s) * kTile;
+            if constexpr (F16) {
+                if (sm[Y::kOffScales + from * kTile + r] > kMostByte && r < k.kv - k.tile(s) * kTile)
+                    atomicOr(reinterpret_cast<unsigned*>(sm + Y::kOffMisc) + 3, 1u << ((unit - 1) & 31));
+            }
             widen_row<F16>(sm + Y::kOffRaw + from * kHalf, sm[Y::kOffScales + from * kTile + r], none, sm + Y::kOffRing + to * kOperand, r);
             fence_proxy_async_smem();
             __syncwarp();
@@ -850,7 +863,7 @@ __device__ __forceinline__ void pool_values(const uint16_t* pool, const uint8_t*
     }
 }
 
-// A value of V that is not finite (as it enters the products), in a later token's row, spoils the rows of the same tile
+// A value of V that is not finite, in a later token's row, spoils the rows of the same tile
 // that do not see it (0 NaN is NaN). Rows whose result is not finite (`odd`) and that have
 // such a value in a masked place, rows [lim, end), are computed again without the tensor cores:
 // o = sum over rows [first, lim) of 2^(s - mc) v, dims [d0, d0 + nd). Slow and rare: 4 rows at
@@ -881,7 +894,7 @@ __device__ __forceinline__ void mend_rows(const ChunkArgs& a, int h, bool odd, i
             float v[16];
             pool_values<F16, Q8>(a.Vp, a.Vs, row, dim, v);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) spoilt += 0.f * (F16 && Q8 ? __half2float(__float2half_rn(v[e] * kHalved<F16, Q8>)) : v[e]);
+            for (int e = 0; e < 16; ++e) spoilt += 0.f * v[e];
         }
         if (!__any_sync(kFull, spoilt != spoilt)) continue;
         float o[16];
@@ -926,6 +939,105 @@ __device__ __forceinline__ void mend_rows(const ChunkArgs& a, int h, bool odd, i
                     reinterpret_cast<uint32_t*>(out1 + dim)[e] = pack16<F16>(o[2 * e] * z1, o[2 * e + 1] * z1);
             }
         }
+        __syncwarp();
+    }
+}
+
+// fp16 over 8-bit rows that have elements which fp16 does not hold (scale bytes above kMostByte): a unit's piece without the tensor
+// cores, in fp32, for all live rows of the warp: max and sum (m, l, as softmax_step has them), and O of dims [d0, d0 + nd) over cache rows
+// [first, min(lim, end)) to `piece`, or divided by the sum to `out`. 32 cache rows at once, 8 lanes and 16 dims a lane each, twice: for
+// the max, then for the rest. Slow (a turn of 4K tokens over 45K rows: 1.16 s for 1.54 ms, 7.5 us a cache row and unit; past 250K rows of a unit
+// the other roles' waits of 2 s run out) and rare: rows of fp16 values have none such, turned ones only where the positions'
+// magnitude passes 1.4.
+__device__ __forceinline__ void redo_rows(const ChunkArgs& a, int h, bool live, int first, int lim, int end, const uint16_t* q, uint16_t* out,
+                                          float4* piece, int d0, int nd, float& m, float& l)
+{
+    constexpr int kRows = 8;  // of 8 lanes, on the way at once
+    constexpr float kHalf16 = kHalved<true, true>;
+    const int lane = threadIdx.x & 31, sub = lane & 7, dim = 16 * sub;
+    const bool mine = dim >= d0 && dim < d0 + nd;
+    unsigned todo = __ballot_sync(kFull, live);
+#pragma unroll 1
+    while (todo) {
+        const int src = __ffs(todo) - 1;
+        todo &= todo - 1;
+        const int last = min(__shfl_sync(kFull, lim, src), end);
+        const uint16_t* q1 = reinterpret_cast<const uint16_t*>(__shfl_sync(kFull, reinterpret_cast<unsigned long long>(q), src));
+        uint16_t* out1 = reinterpret_cast<uint16_t*>(__shfl_sync(kFull, reinterpret_cast<unsigned long long>(out), src));
+        float4* piece1 = reinterpret_cast<float4*>(__shfl_sync(kFull, reinterpret_cast<unsigned long long>(piece), src));
+        float x[16], o[16], top = -INFINITY, sum = 0.f, mc = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float2 y = widen<true>(reinterpret_cast<const uint32_t*>(q1 + dim)[e]);
+            x[2 * e] = y.x;
+            x[2 * e + 1] = y.y;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[e] = 0.f;
+#pragma unroll 1
+        for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll 1
+            for (int r0 = first; r0 < last; r0 += 4 * kRows) {
+                int64_t row[kRows];  // (-1: none, or a bad page's, which is zeros)
+                float s[kRows];
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) {
+                    const int r = r0 + 4 * i + (lane >> 3);
+                    row[i] = r < last ? pool_row(a, h, r) : -1;
+                    s[i] = 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) {
+                    if (row[i] < 0) continue;
+                    float k[16];
+                    pool_values<true, true>(a.Kp, a.Ks, row[i], dim, k);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[i] = fmaf(x[e], k[e], s[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) {
+#pragma unroll
+                    for (int y = 4; y >= 1; y >>= 1) s[i] += __shfl_xor_sync(kFull, s[i], y);
+                    s[i] = r0 + 4 * i + (lane >> 3) < last ? s[i] * kHalf16 : -INFINITY;
+                }
+                if (pass == 0) {
+#pragma unroll
+                    for (int i = 0; i < kRows; ++i) top = fmaxf(top, s[i]);
+                    continue;
+                }
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) {
+                    const float p = r0 + 4 * i + (lane >> 3) < last ? ex2(fmaf(s[i], a.qscale, -mc)) : 0.f;
+                    sum += p;
+                    if (row[i] < 0) continue;
+                    float v[16];
+                    pool_values<true, true>(a.Vp, a.Vs, row[i], dim, v);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] = fmaf(p * kHalf16, v[e], o[e]);
+                }
+            }
+            top = fmaxf(top, __shfl_xor_sync(kFull, top, 8));
+            top = fmaxf(top, __shfl_xor_sync(kFull, top, 16));
+            mc = origin<true>(top, a.qscale);
+        }
+        sum += __shfl_xor_sync(kFull, sum, 8);
+        sum += __shfl_xor_sync(kFull, sum, 16);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            o[e] += __shfl_xor_sync(kFull, o[e], 8);
+            o[e] += __shfl_xor_sync(kFull, o[e], 16);
+        }
+        const float z = inverse<true, true>(sum);
+        if (lane < 8 && mine) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (piece1)
+                    __stcg(reinterpret_cast<float2*>(piece1 + (dim / 4 + e / 2) * kPieceRows) + (e & 1), make_float2(o[2 * e], o[2 * e + 1]));
+                else
+                    reinterpret_cast<uint32_t*>(out1 + dim)[e] = pack16<true>(o[2 * e] * z, o[2 * e + 1] * z);
+            }
+        }
+        if (lane == src) m = top, l = sum;
         __syncwarp();
     }
 }
@@ -1156,6 +1268,7 @@ __global__ void __launch_bounds__(Lay<Q8>::kThreads, 1)
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     if (tid == 0) misc[1] = 0;
+    if (F16 && Q8 && tid == 0) misc[3] = 0;
     if (tid < Y::kNumBars) {
         const uint64_t* bar = full + tid;
         const bool by_warps = (bar >= p_half && bar < p_full + 2) || (Q8 && (bar < empty || (bar >= raw_empty && bar < said)));
@@ -1433,6 +1546,9 @@ __global__ void __launch_bounds__(Lay<Q8>::kThreads, 1)
             if (steps > p && !wait(&o_done[p], no++ & 1)) break;
             tc_fence_after();
             uint16_t* out = a.out + ((int64_t)(k.t0 + tok) * a.H + k.g * a.G + j) * kHeadDim;
+            // A unit with rows that its type does not hold is computed again. (A pair unit's groups have the same tiles, all converted
+            // now; a split unit's other group may still wait for some of its own.)
+            bool large = F16 && Q8 && pair && (misc[3] >> (unit & 31) & 1);
             // Of a pair unit with few pieces, all others may be done: then this one is not stored. (Not if some of
             // its rows may have to be mended.)
             int c0 = c, pieces = 1;
@@ -1443,7 +1559,7 @@ __global__ void __launch_bounds__(Lay<Q8>::kThreads, 1)
                 c0 = d->c0;
                 pieces = d->pieces;
                 if (!in_bounds(c0 >= 0 && c0 <= c && pieces > c - c0 && c0 + pieces <= nctas, a.status)) c0 = c, pieces = 1;
-                few = pair && pieces <= kFew && min(k.kv, k.j1 * kTile) <= k.row0;
+                few = pair && pieces <= kFew && min(k.kv, k.j1 * kTile) <= k.row0 && !large;
                 if (few) {
                     if (tid == 0) {
                         pdl_wait();  // the counters are cleared
@@ -1463,7 +1579,10 @@ __global__ void __launch_bounds__(Lay<Q8>::kThreads, 1)
             float4* o_piece = whole ? nullptr : w.o + slot * (kHeadDim / 4) * kPieceRows + prow;
             float odd = 0.f;  // NaN if a result is not finite
             if (pair) {
-                if (any && !last) {
+                if (large && any) {
+                    if constexpr (F16 && Q8) redo_rows(a, k.h, live, first, lim, end, q, out, o_piece, 0, kHeadDim, m, l);
+                    if (live && !whole) __stcg(w.ml + slot * kPieceRows + prow, make_float2(m, l));
+                } else if (any && !last) {
                     const float z = inverse<F16, Q8>(l);
 #pragma unroll 1
                     for (int e = 0; e < 4; ++e) {
@@ -1484,12 +1603,16 @@ __global__ void __launch_bounds__(Lay<Q8>::kThreads, 1)
                 tc_fence_before();
                 if (!wait.meet()) break;
                 tc_fence_after();
+                large = F16 && Q8 && (misc[3] >> (unit & 31) & 1);
                 const float2 x = sh_ml[r], y = sh_ml[kTile + r];
                 const float M = fmaxf(x.x, y.x);
                 const float fx = x.x == -INFINITY ? 0.f : ex2((x.x - M) * cs), fy = y.x == -INFINITY ? 0.f : ex2((y.x - M) * cs);
                 const float L = x.y * fx + y.y * fy, z = inverse<F16, Q8>(L);
                 const bool two = steps > 1;
-                if (any) {
+                if (large && any) {
+                    if constexpr (F16 && Q8) redo_rows(a, k.h, live, first, lim, end, q, out, o_piece, 64 * p, 64, m, l);
+                    if (live && !whole && p == 0) __stcg(w.ml + slot * kPieceRows + prow, make_float2(m, l));
+                } else if (any) {
 #pragma unroll 1
                     for (int e = 2 * p; e < 2 * p + 2; ++e) {
                         float v[32], v1[32];
