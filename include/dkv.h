@@ -583,8 +583,9 @@ dkv_status dkv_chunk_attn(const dkv_pages* pages, int32_t layer, int32_t dtype, 
  *   What a scaling does not name is not read.
  * dkv_rotary_custom takes the frequencies (host double [rot_dim / 2], |f| < 2^20) and the
  * magnitude (finite) themselves.
- * A frequency is held in 2^-64 of a turn, so that an angle is the low half of an integer product,
- * exact for every position; cos and sin are fp32, and a turned element is rounded once.
+ * A frequency, f_i / 2 pi rounded to a double, is held in 2^-64 of a turn, so that an angle is the
+ * low half of an integer product, exact for every position; cos and sin are fp32, and a turned
+ * element is rounded once.
  * Errors: DKV_ERR_INVALID_ARG.
  */
 typedef struct {

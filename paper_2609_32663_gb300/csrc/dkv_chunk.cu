@@ -41,7 +41,7 @@
 // Over 8-bit pools the turn takes 1,720 us (bf16): a tile's two conversions are 1,300 cycles each of its 3,500, beside the softmax
 // warps on the same schedulers. A row's loads three ahead of their use: 2,012 us to 1,849; the registers split 208, 24 (one-warp
 // roles), 72 (conversion) instead of 208, 48, 48: to 1,720 (208, 40, 56: 1,807; 216, 40, 40: 1,905; 200, 56, 56: 1,970).
-// Drafts of four sequences, 63 MB, take 37 us: 7 to the first tile, 13 tiles a CTA at 1.24 (the conversion), 4 for the pieces' stores, and
+// Drafts of four sequences, 63 MB (fp16), take 38 us: 7 to the first tile, 13 tiles a CTA at 1.24 (the conversion), 4 for the pieces' stores, and
 // the join of up to 17 of them a unit, which the kernel behind this one does on all SMs (by the last CTA of a unit: 50 us).
 //
 // Scores, their max and sum and O are fp32. The weights P are rounded to the inputs' type, as both operands of

@@ -942,7 +942,7 @@ def dkv_quant_workspace_bytes(pages: Pages) -> int:
 def dkv_quant_attn(pages: Pages, layer: int, q, cu_tokens, table, len, Kp, Vp, Ks, Vs, out, workspace, causal: bool = True,
                    scale: float = 0.0, max_tokens: int = 0, status=None, stream=None):
     """One layer's attention of q [T][H][128] over 8-bit pages -> out [T][H][128], both bfloat16 or float16. max_tokens: the
-    most tokens that one sequence brings (0: not known)."""
+    most tokens that one sequence brings (0: not known; a step of next tokens then takes three launches for two)."""
     at, queue = _where(stream)
     if _T.calls is not None:
         done = _T.calls.quant_attn(_entry.get("dkv_quant_attn") or _address("dkv_quant_attn"), at, queue, pages.at, layer, q, cu_tokens, table,
